@@ -348,6 +348,141 @@ int pruner_verify_score(const float* feat, const int32_t* n_stmt, int64_t n_d, c
 int pruner_topk_static(const float* score, const int64_t* seg_off, int32_t n_sg, int32_t k,
                        int32_t* idx_out, float* val_out, void* stream);
 
+/* ---- operators of a trainable Transformer block --------------------------------------------------------------------------
+   The learned model's dataflow branch as pruner_pacm_score runs it is fixed: eight blocks, one head, no positional term.
+   The entry points below are what a block of a model that is trained, and whose sequences grow, is made of. */
+
+#define PRUNER_BF16 0   /* types of activations and of their gradients */
+#define PRUNER_F16 1
+#define PRUNER_F32 2
+
+/*
+ * Checkpoints: a matrix of activations held in 8 bits until the backward pass needs it.
+ * PRUNER_CHECKPOINT_GROUP neighbouring values of a row (the last group of a row may be shorter) share a power of two:
+ *     e = the smallest integer >= -126 with max |x| <= 127 x 2^e,   code = x / 2^e to the nearest integer (ties to even),
+ *     exponent byte = e + 127;  restored value = code x 2^e.
+ * A group that holds an infinity or a NaN has byte 255 and restores as NaN.  A restored value is exact in bfloat16 (a code has
+ * seven bits), so matrix products take it as it is; in binary16 it is exact within that type's range.
+ */
+#define PRUNER_CHECKPOINT_GROUP 32
+typedef struct pruner_checkpoint {
+    int8_t* codes;   /* device [rows][dim]                                     */
+    uint8_t* exps;   /* device [rows][(dim + 31) / 32], the exponent bytes      */
+} pruner_checkpoint;
+
+/*
+ * pruner_checkpoint_pack puts x away, pruner_checkpoint_restore brings it back (both in any of the three types).
+ *   x     device [rows][pitch] of dtype, the first dim of a row count; pitch >= dim
+ *   rows >= 0, 1 <= dim; rows x pitch below 2^40
+ * No workspace.  Errors: PRUNER_EINVAL (null or misaligned pointers: x at its type's size, codes 8 bytes; sizes, type).
+ */
+int pruner_checkpoint_pack(const void* x, int32_t dtype, int64_t rows, int32_t dim, int64_t pitch, const pruner_checkpoint* kept, void* stream);
+int pruner_checkpoint_restore(const pruner_checkpoint* kept, int32_t dtype, int64_t rows, int32_t dim, void* x, int64_t pitch, void* stream);
+
+/*
+ * The weight gradient of a linear layer y = W x from its input's checkpoint:  dW[n][k] (+)= sum_r dy[r][n] x^[r][k].
+ * The restored x^ enters the matrix cores in dy's type, products accumulate in binary32, and rows are summed in an order that
+ * depends on the sizes alone.
+ *   dy          device [rows][dy_pitch], PRUNER_BF16 or PRUNER_F16; dy_pitch >= n_out
+ *   kept        the input's checkpoint, [rows][dim]
+ *   dw          device float [n_out][dim]
+ *   accumulate  0: dw is overwritten; 1: added to
+ * rows >= 0 (0: dw is cleared, or left alone), n_out and dim 1..2^20.
+ * workspace: pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim).
+ * Errors: PRUNER_EINVAL (null or misaligned pointers: dy 2 bytes, codes 8, dw 4; sizes, type), PRUNER_EWORKSPACE.
+ */
+size_t pruner_checkpoint_wgrad_workspace_bytes(int64_t rows, int32_t n_out, int32_t dim);
+int pruner_checkpoint_wgrad(const void* dy, int32_t dtype, int64_t dy_pitch, const pruner_checkpoint* kept, int64_t rows, int32_t n_out, int32_t dim,
+                            float* dw, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The norm behind one block and the norm before the next, with the gate and the residual scale between them.  For every row
+ * (f: the block's output, x: the residual stream, norm(v) = (v - m) / sqrt(mean((v - m)^2) + eps), m = mean(v) if center, else 0):
+ *     u = norm(f) w_post;   h = alpha x + sigmoid(gate) u;   y = norm(h) w_pre
+ * All of it in binary32 on the unrounded h; h and y are rounded once, to the type.
+ *   x, f, h, y     device, dtype; x and f with pitches, outputs contiguous.  f NULL: u = 0 (the first norm of a model).
+ *                  h or y NULL: not wanted.
+ *   w_post, w_pre  device float [dim]; w_post may be NULL with f
+ *   gate           NULL (sigmoid(gate) is then 1), or with gate_pitch > 0 device [rows][gate_pitch] of dtype, or with gate_pitch = 0 device
+ *                  float [dim], one for all rows
+ *   kept_y         NULL, or room for the checkpoint of y as it is stored (y in its type)
+ * rows >= 0, 1 <= dim <= PRUNER_MAX_NORM_DIM.  No workspace.
+ *
+ * pruner_gated_norm_grad: dh and dy are the gradients of the two outputs (dh NULL: zero), f or kept_f (exactly one, or neither if the forward
+ * pass had no f) the block's output or its checkpoint; the statistics are formed again from x, f and the gate.
+ *   dx, df, dgate           device, contiguous, of dtype; dgate float [dim] for one gate of all rows, NULL without gate; df NULL without f
+ *   dw_post, dw_pre         device float [dim] (dw_post NULL without f); sums over rows in binary32, in an order that depends on
+ *                           the sizes and the device alone
+ * workspace: pruner_gated_norm_grad_workspace_bytes(rows, dim).
+ * Errors: PRUNER_EINVAL (null or misaligned pointers: matrices at their type's size, vectors 4 bytes, codes 8; sizes, type, a pitch below
+ * dim, alpha or eps not finite, eps < 0), PRUNER_EWORKSPACE.
+ */
+#define PRUNER_MAX_NORM_DIM 8192
+typedef struct pruner_norm {
+    int64_t rows;
+    int32_t dim, dtype, center;
+    float alpha, eps;
+    const float *w_post, *w_pre;
+    const void* gate;
+    int64_t gate_pitch;
+} pruner_norm;
+int pruner_gated_norm(const pruner_norm* p, const void* x, int64_t x_pitch, const void* f, int64_t f_pitch, void* h, void* y,
+                      const pruner_checkpoint* kept_y, void* stream);
+size_t pruner_gated_norm_grad_workspace_bytes(int64_t rows, int32_t dim);
+int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitch, const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch,
+                           const void* f, int64_t f_pitch, const pruner_checkpoint* kept_f, void* dx, void* df, void* dgate, float* dw_post, float* dw_pre,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention with a learned relative position bias by buckets.  For sequence b with ql = q_len[b] queries and kl = k_len[b] keys, query i
+ * stands at position p_i = kl - ql + i (the queries are the last ones of the sequence), key j at j, and
+ *     s_ij = scale q_i . k_j + table[bucket(j - p_i)][head],   a_ij = softmax over the keys that query i sees,   o_i = sum_j a_ij v_j
+ * It sees keys j < kl; with PRUNER_ATTENTION_CAUSAL only j <= p_i.  lse_i = log sum_j exp(s_ij).  A query that sees no key (and a row at or
+ * beyond ql) has o = 0, lse = -infinity, and passes no gradient.  What rows beyond the lengths hold does not matter.
+ * Query head h reads key/value head h / (q_heads / kv_heads).
+ *   bucket(r) = the number of edges <= |r|, plus n_edges + 1 if r > 0 (two-sided: table [2 (n_edges + 1)][q_heads]); one-sided: the number of
+ *   edges <= max(-r, 0) (table [n_edges + 1][q_heads]); edges ascend strictly, 1 <= edge <= PRUNER_MAX_BIAS_DISTANCE.
+ * Products accumulate in binary32, softmax statistics are binary32; the weights a_ij (and in the backward pass their gradients) are rounded to
+ * the type before the second product.
+ *
+ *   q, o, dout, dq   pruner_heads: token t of sequence b, head h at p + (b batch + t token + h head) elements, head_dim of them contiguous;
+ *   k, v, dk, dv     head_dim a multiple of 8, 8..128; pointers 16-byte aligned, strides multiples of 8; token strides up to 2^22
+ *   q_len, k_len     device int32 [batch], or NULL: q_tokens, k_tokens for all; values outside 0..q_tokens (k_tokens) are clamped
+ *   table            device, of dtype, or NULL: no bias; edges: host int32 [n_edges], n_edges 0..PRUNER_MAX_BIAS_EDGES
+ *   scale            finite, > 0
+ *   lse              device float [batch][q_heads][q_tokens]: out (NULL: not wanted); in, for the gradients
+ *   dtable           device, of dtype, the table's shape, or NULL without table; sums over pairs in binary32 in an order that depends on the
+ *                    sizes and the device alone, rounded once
+ * Outputs are written for every row of q_tokens and k_tokens.  dk and dv are the sums over the query heads that share a key head.
+ * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, batch x q_heads x q_tokens below 2^31.
+ * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes only.
+ * Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
+ */
+#define PRUNER_MAX_BIAS_EDGES 64
+#define PRUNER_MAX_BIAS_DISTANCE 1024
+#define PRUNER_ATTENTION_CAUSAL 1
+#define PRUNER_ATTENTION_TWO_SIDED 2
+typedef struct pruner_heads {
+    void* p;
+    int64_t batch, token, head;
+} pruner_heads;
+typedef struct pruner_attention {
+    int32_t dtype;                     /* PRUNER_BF16 or PRUNER_F16 */
+    int32_t batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, flags;
+    float scale;
+    const int32_t *q_len, *k_len;
+    const void* table;
+    const int32_t* edges;
+    int32_t n_edges;
+} pruner_attention;
+size_t pruner_rel_attention_workspace_bytes(const pruner_attention* a);
+int pruner_rel_attention(const pruner_attention* a, const pruner_heads* q, const pruner_heads* k, const pruner_heads* v, const pruner_heads* o, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
+size_t pruner_rel_attention_grad_workspace_bytes(const pruner_attention* a);
+int pruner_rel_attention_grad(const pruner_attention* a, const pruner_heads* dout, const pruner_heads* q, const pruner_heads* k, const pruner_heads* v,
+                              const pruner_heads* o, const float* lse, const pruner_heads* dq, const pruner_heads* dk, const pruner_heads* dv, void* dtable,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 #define PRUNER_WS_DRAFT 0
 #define PRUNER_WS_TOPK 1
 #define PRUNER_WS_VERIFY 2

@@ -5,7 +5,9 @@ streams, nothing else); descriptors are the dataclasses of the `workloads` packa
 same attribute names.
 """
 import ctypes as C
+import math
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -57,6 +59,31 @@ class CMlp(C.Structure):
                 ("b3", C.c_float)]
 
 
+class CCheckpoint(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p)]
+
+
+class CNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("dtype", C.c_int32), ("center", C.c_int32), ("alpha", C.c_float), ("eps", C.c_float),
+                ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("gate", C.c_void_p), ("gate_pitch", C.c_int64)]
+
+
+class CHeads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class CAttention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("q_tokens", C.c_int32), ("k_tokens", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("flags", C.c_int32), ("scale", C.c_float), ("q_len", C.c_void_p), ("k_len", C.c_void_p), ("table", C.c_void_p),
+                ("edges", C.c_void_p), ("n_edges", C.c_int32)]
+
+
+class Checkpoint(NamedTuple):
+    """A matrix of activations in 8 bits: codes int8 [rows, dim], exps uint8 [rows, ceil(dim / 32)]."""
+    codes: object
+    exps: object
+
+
 _lib = None
 
 
@@ -102,6 +129,22 @@ def load_library():
         lib.pruner_verify_score.restype = C.c_int
         lib.pruner_verify_score.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, P(CMlp), C.c_void_p,
                                             C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_checkpoint_pack.restype = C.c_int
+        lib.pruner_checkpoint_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, P(CCheckpoint), C.c_void_p]
+        lib.pruner_checkpoint_restore.restype = C.c_int
+        lib.pruner_checkpoint_restore.argtypes = [P(CCheckpoint), C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        lib.pruner_checkpoint_wgrad_workspace_bytes.restype = C.c_size_t
+        lib.pruner_checkpoint_wgrad_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+        lib.pruner_checkpoint_wgrad.restype = C.c_int
+        lib.pruner_checkpoint_wgrad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, P(CCheckpoint), C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+                                                C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_gated_norm.restype = C.c_int
+        lib.pruner_gated_norm.argtypes = [P(CNorm), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, P(CCheckpoint), C.c_void_p]
+        lib.pruner_gated_norm_grad_workspace_bytes.restype = C.c_size_t
+        lib.pruner_gated_norm_grad_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+        lib.pruner_gated_norm_grad.restype = C.c_int
+        lib.pruner_gated_norm_grad.argtypes = [P(CNorm), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, P(CCheckpoint),
+                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_workspace_bytes.restype = C.c_size_t
         lib.pruner_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
         lib.pruner_strerror.restype = C.c_char_p
@@ -363,3 +406,152 @@ def verify_score(feat, n_stmt, weights, vscore=None, workspace=None, stream=None
     if rc:
         raise PrunerError(rc, "pruner_verify_score")
     return vscore
+
+
+# ---- operators of a trainable Transformer block
+
+MAX_BIAS_EDGES, MAX_BIAS_DISTANCE, MAX_NORM_DIM, CHECKPOINT_GROUP = 64, 1024, 8192, 32
+_BF16, _F16, _F32 = 0, 1, 2
+_ATTENTION_CAUSAL, _ATTENTION_TWO_SIDED = 1, 2
+
+
+def _dtype(t):
+    import torch
+    return {torch.bfloat16: _BF16, torch.float16: _F16, torch.float32: _F32}.get(t, -1)
+
+
+def _rows_of(t, what):
+    """A matrix [rows, dim] whose rows may lie further apart than dim: (pointer, pitch)."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]), what
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1))
+
+
+def _c_checkpoint(kept, rows, dim):
+    import torch
+    codes, exps = kept
+    assert codes.is_cuda and codes.dtype == torch.int8 and codes.is_contiguous() and codes.shape == (rows, dim), "codes"
+    assert exps.is_cuda and exps.dtype == torch.uint8 and exps.is_contiguous() and exps.shape == (rows, -(-dim // CHECKPOINT_GROUP)), "exps"
+    return CCheckpoint(codes.data_ptr(), exps.data_ptr())
+
+
+def _new_checkpoint(rows, dim, device):
+    import torch
+    return Checkpoint(torch.empty((rows, dim), dtype=torch.int8, device=device), torch.empty((rows, -(-dim // CHECKPOINT_GROUP)), dtype=torch.uint8, device=device))
+
+
+def checkpoint_pack(x, kept=None, stream=None):
+    """pruner_checkpoint_pack.  x: bfloat16, float16 or float32 CUDA [rows, dim] (rows may be further apart).  Returns a Checkpoint."""
+    lib = load_library()
+    p, pitch = _rows_of(x, "x")
+    rows, dim = x.shape
+    if kept is None:
+        kept = _new_checkpoint(rows, dim, x.device)
+    rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, C.byref(_c_checkpoint(kept, rows, dim)), _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_checkpoint_pack")
+    return kept
+
+
+def checkpoint_restore(kept, dtype=None, x=None, stream=None):
+    """pruner_checkpoint_restore.  Returns x (of `dtype`, or a given tensor's)."""
+    import torch
+    lib = load_library()
+    rows, dim = kept[0].shape
+    if x is None:
+        x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
+    assert x.shape == (rows, dim), "x"
+    p, pitch = _rows_of(x, "x")
+    rc = lib.pruner_checkpoint_restore(C.byref(_c_checkpoint(kept, rows, dim)), _dtype(x.dtype), rows, dim, p, pitch, _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_checkpoint_restore")
+    return x
+
+
+def checkpoint_wgrad(dy, kept, dw=None, accumulate=False, workspace=None, stream=None):
+    """pruner_checkpoint_wgrad: the weight gradient [n_out, dim] (float32) of a linear layer whose output's gradient is dy (bfloat16 or float16
+    CUDA [rows, n_out]) and whose input is kept as a Checkpoint.  accumulate: dw is added to."""
+    import torch
+    lib = load_library()
+    p, pitch = _rows_of(dy, "dy")
+    rows, n_out = dy.shape
+    dim = kept[0].shape[1]
+    if dw is None:
+        assert not accumulate, "accumulate needs dw"
+        dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
+    assert dw.is_cuda and dw.dtype == torch.float32 and dw.is_contiguous() and dw.shape == (n_out, dim), "dw"
+    ws = _workspace(workspace, int(lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim)), dy.device)
+    rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, C.byref(_c_checkpoint(kept, rows, dim)), rows, n_out, dim, _ptr(dw), int(accumulate), _ptr(ws), ws.numel(),
+                                     _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_checkpoint_wgrad")
+    return dw
+
+
+def _vector(t, dim, what):
+    import torch
+    assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (dim,), what
+    return t.data_ptr()
+
+
+def _c_norm(x, has_f, w_post, w_pre, gate, alpha, eps, center):
+    rows, dim = x.shape
+    pitch = 0
+    if gate is not None and gate.dim() == 1:
+        _vector(gate, dim, "gate")
+    elif gate is not None:
+        assert gate.dtype == x.dtype and gate.shape == x.shape, "gate"
+        pitch = _rows_of(gate, "gate")[1]
+    return CNorm(rows, dim, _dtype(x.dtype), int(bool(center)), alpha, eps, _vector(w_post, dim, "w_post") if has_f else None,
+                 _vector(w_pre, dim, "w_pre") if w_pre is not None else None, gate.data_ptr() if gate is not None else None, pitch)
+
+
+def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, checkpoint=False, stream=None):
+    """pruner_gated_norm: h = alpha x + sigmoid(gate) norm(f) w_post, y = norm(h) w_pre.  x, f: CUDA [rows, dim] of one type (f None: the first norm
+    of a model; w_post may then be None); w_post, w_pre float32 [dim]; gate None, [rows, dim] of x's type, or float32 [dim]; w_pre None: y is not formed.
+    Returns (h, y), with checkpoint=True (h, y, Checkpoint of y)."""
+    import torch
+    lib = load_library()
+    rows, dim = x.shape
+    px, x_pitch = _rows_of(x, "x")
+    pf, f_pitch = None, 0
+    if f is not None:
+        assert f.dtype == x.dtype and f.shape == x.shape, "f"
+        pf, f_pitch = _rows_of(f, "f")
+    h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+    y = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if w_pre is not None else None
+    kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
+    p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
+    rc = lib.pruner_gated_norm(C.byref(p), px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), C.byref(_c_checkpoint(kept, rows, dim)) if checkpoint else None, _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_gated_norm")
+    return (h, y, kept) if checkpoint else (h, y)
+
+
+def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, workspace=None, stream=None):
+    """pruner_gated_norm_grad.  dh (or None: zero), dy: the gradients of gated_norm's h and y; f: the block's output, its Checkpoint, or None as in the
+    forward pass.  Returns (dx, df, dgate, dw_post, dw_pre); those of what was None are None."""
+    import torch
+    lib = load_library()
+    rows, dim = x.shape
+    kept = f if isinstance(f, tuple) else None
+    px, x_pitch = _rows_of(x, "x")
+    for t, what in ((dh, "dh"), (dy, "dy"), (f if kept is None else None, "f")):
+        assert t is None or (t.dtype == x.dtype and t.shape == x.shape), what
+    pdy, dy_pitch = _rows_of(dy, "dy")
+    pdh, dh_pitch = _rows_of(dh, "dh") if dh is not None else (None, 0)
+    pf, f_pitch = _rows_of(f, "f") if f is not None and kept is None else (None, 0)
+    p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
+    dx = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+    df = dgate = dw_post = None
+    if f is not None:
+        df = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+        dw_post = torch.empty(dim, dtype=torch.float32, device=x.device)
+        if gate is not None:
+            dgate = torch.empty(gate.shape, dtype=gate.dtype, device=x.device)
+    dw_pre = torch.empty(dim, dtype=torch.float32, device=x.device)
+    ws = _workspace(workspace, int(lib.pruner_gated_norm_grad_workspace_bytes(rows, dim)), x.device)
+    rc = lib.pruner_gated_norm_grad(C.byref(p), pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, C.byref(_c_checkpoint(kept, rows, dim)) if kept is not None else None,
+                                    _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(ws), ws.numel(), _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_gated_norm_grad")
+    return dx, df, dgate, dw_post, dw_pre

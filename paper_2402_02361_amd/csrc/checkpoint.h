@@ -1,0 +1,207 @@
+// Activations in 8 bits: 32 neighbouring values of a row share a power of two (see include/pruner.h).  What the kernels that write
+// and read them have in common, and eight neighbouring values of a row in any of the three types.
+#pragma once
+#include "common.h"
+
+namespace pruner {
+namespace ckpt {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kGroup = PRUNER_CHECKPOINT_GROUP;
+constexpr int kEach = 8;                        // values of a row that a thread holds; four threads hold a group
+static_assert(kGroup == 4 * kEach, "a group is four threads' values");
+
+template <typename T> __device__ __forceinline__ float widened(T v) { return (float)v; }
+
+__device__ __forceinline__ uint32_t pair_of(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
+__device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2)); }
+__device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }
+__device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
+
+// Eight neighbouring values as they lie in memory (T), fetched by V at a time: V = 8 needs rows that begin at multiples of 16 bytes,
+// V = 4 of 8 (16 in binary32), V = 1 nothing.  Values at or beyond `left` are not touched; left is a multiple of V.
+template <typename T, int V> struct Eight {
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* __restrict__ p, int left)
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+        if constexpr (V == 8 || (V == 4 && sizeof(T) == 4)) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4)
+                if (i * 4 < left * (int)sizeof(T)) {
+                    const u32x4 q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint32_t*>(p) + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[i + j] = q[j];
+                }
+        } else if constexpr (V == 4) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 2)
+                if (i * 4 < left * (int)sizeof(T)) {
+                    const u32x2 q = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint32_t*>(p) + i);
+                    w[i] = q[0];
+                    w[i + 1] = q[1];
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < left) {
+                    if constexpr (sizeof(T) == 4)
+                        w[j] = __builtin_bit_cast(uint32_t, p[j]);
+                    else
+                        w[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[j]) << (16 * (j % 2));
+                }
+        }
+    }
+    __device__ __forceinline__ void store(T* __restrict__ p, int left) const
+    {
+        if constexpr (V == 8 || (V == 4 && sizeof(T) == 4)) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4)
+                if (i * 4 < left * (int)sizeof(T)) *reinterpret_cast<u32x4*>(reinterpret_cast<uint32_t*>(p) + i) = u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]};
+        } else if constexpr (V == 4) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 2)
+                if (i * 4 < left * (int)sizeof(T)) *reinterpret_cast<u32x2*>(reinterpret_cast<uint32_t*>(p) + i) = u32x2{w[i], w[i + 1]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < left) {
+                    if constexpr (sizeof(T) == 4)
+                        p[j] = __builtin_bit_cast(T, w[j]);
+                    else
+                        p[j] = __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j % 2))));
+                }
+        }
+    }
+    __device__ __forceinline__ void to_floats(float (&v)[kEach]) const
+    {
+#pragma unroll
+        for (int j = 0; j < kEach; j += 2) {
+            if constexpr (sizeof(T) == 4) {
+                v[j] = __uint_as_float(w[j]);
+                v[j + 1] = __uint_as_float(w[j + 1]);
+            } else {
+                const f32x2 q = pair_to(w[j / 2], T{});
+                v[j] = q[0];
+                v[j + 1] = q[1];
+            }
+        }
+    }
+    __device__ __forceinline__ void from_floats(const float (&v)[kEach])   // nearest, ties to even
+    {
+#pragma unroll
+        for (int j = 0; j < kEach; j += 2) {
+            if constexpr (sizeof(T) == 4) {
+                w[j] = __float_as_uint(v[j]);
+                w[j + 1] = __float_as_uint(v[j + 1]);
+            } else {
+                w[j / 2] = pair_of(v[j], v[j + 1], T{});
+            }
+        }
+    }
+};
+
+// Eight codes, by V at a time as above (codes begin at a multiple of 8 bytes and rows are dim long, so V divides their offsets).
+template <int V> struct EightCodes {
+    uint32_t w[2];
+    __device__ __forceinline__ void load(const int8_t* __restrict__ p, int left)
+    {
+        w[0] = w[1] = 0u;
+        if constexpr (V == 8) {
+            if (left > 0) {
+                const u32x2 q = *reinterpret_cast<const u32x2*>(p);
+                w[0] = q[0];
+                w[1] = q[1];
+            }
+        } else if constexpr (V == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (4 * i < left) w[i] = *reinterpret_cast<const uint32_t*>(p + 4 * i);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < left) w[j / 4] |= (uint32_t)(uint8_t)p[j] << (8 * (j % 4));
+        }
+    }
+    __device__ __forceinline__ void store(int8_t* __restrict__ p, int left) const
+    {
+        if constexpr (V == 8) {
+            if (left > 0) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+        } else if constexpr (V == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (4 * i < left) *reinterpret_cast<uint32_t*>(p + 4 * i) = w[i];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < left) p[j] = (int8_t)(uint8_t)(w[j / 4] >> (8 * (j % 4)));
+        }
+    }
+};
+
+// The exponent byte of a group from the largest |x| of it (its bits: a NaN's are above an infinity's, an infinity's above all others).
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t top)
+{
+    const uint32_t field = top >> 23, byte = field - 6u + ((top & 0x7FFFFFu) > 0x7E0000u ? 1u : 0u);   // 127 = 1.984375 x 2^6
+    return field == 255u ? 255u : field < 7u ? 1u : byte;
+}
+
+// What four neighbouring threads hold becomes one group's codes; every one of the four gets the exponent byte.  Values beyond a row's
+// end are 0.  The four threads must be lanes 4 i .. 4 i + 3, all active.
+__device__ __forceinline__ uint32_t pack_group(const float (&v)[kEach], uint32_t (&codes)[2])
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+        top = b > top ? b : top;
+    }
+    uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false);   // quad_perm 1,0,3,2
+    top = other > top ? other : top;
+    other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false);            // quad_perm 2,3,0,1
+    top = other > top ? other : top;
+    const uint32_t byte = exponent_byte(top);
+    const float inverse = __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23);   // 2^-e: the product is exact
+    codes[0] = codes[1] = 0u;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int c = byte == 255u ? 0 : (int)__builtin_rintf(v[j] * inverse);
+        codes[j / 4] |= ((uint32_t)c & 0xFFu) << (8 * (j % 4));
+    }
+    return byte;
+}
+
+__device__ __forceinline__ void restore_eight(const uint32_t (&codes)[2], uint32_t byte, float (&v)[kEach])
+{
+    const float unit = __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);   // NaN x any code, 0 included, is NaN
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) v[j] = (float)(int8_t)(codes[j / 4] >> (8 * (j % 4))) * unit;
+}
+
+// How many values one access may take (8, 4 or 1): pointers and strides of all of a call's matrices come through `fits`.
+struct Access {
+    int v = 8;
+    void fits(const void* p, size_t elem_bytes, int64_t pitch)
+    {
+        if (!p) return;
+        auto ok = [&](int n) {
+            const size_t bytes = n * elem_bytes < 16 ? n * elem_bytes : 16;
+            return aligned(p, bytes) && pitch % n == 0;
+        };
+        while (v > 1 && !ok(v)) v = v == 8 ? 4 : 1;
+    }
+};
+
+inline bool type_known(int32_t dtype) { return dtype == PRUNER_BF16 || dtype == PRUNER_F16 || dtype == PRUNER_F32; }
+inline size_t type_bytes(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
+
+}  // namespace ckpt
+}  // namespace pruner

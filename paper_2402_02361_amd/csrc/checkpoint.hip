@@ -1,0 +1,365 @@
+// Checkpoints of activations in 8 bits (pack, restore) and a linear layer's weight gradient from its input's checkpoint.
+#include "checkpoint.h"
+#include "mfma_tile.h"
+
+namespace pruner {
+namespace {
+
+using namespace ckpt;
+
+// n / d for n below 2^31 and 1 <= d < 2^31, by a multiplication: q = (hi(n m) + n) >> s with m = floor(2^32 (2^s - d) / d) + 1, s = ceil(log2 d).
+struct Divisor {
+    uint32_t d, m, s;
+    explicit Divisor(uint32_t by) : d(by), m(0), s(0)
+    {
+        while ((1ull << s) < d) ++s;
+        m = (uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+
+// A thread takes eight neighbouring values; four threads make a group.  Bound: memory (each value read once, a little over a byte written).
+template <typename T, int V>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int64_t pitch, int dim, uint32_t items, Divisor per_row, int8_t* __restrict__ codes,
+                                                   uint8_t* __restrict__ exps)
+{
+    const uint32_t item = blockIdx.x * 256 + threadIdx.x;   // (items is a multiple of 4: the lanes of a group are active together)
+    if (item >= items) return;
+    const uint32_t row = per_row.of(item), at = item - row * per_row.d;
+    const int col = 8 * (int)at, left = dim - col;
+    Eight<T, V> in;
+    in.load(x + (int64_t)row * pitch + col, left);
+    float v[kEach];
+    in.to_floats(v);
+    EightCodes<V> out;
+    const uint32_t byte = pack_group(v, out.w);
+    out.store(codes + (int64_t)row * dim + col, left);
+    if ((at & 3u) == 0) exps[(int64_t)row * (per_row.d / 4) + at / 4] = (uint8_t)byte;
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, int dim, uint32_t items, Divisor per_row,
+                                                      T* __restrict__ x, int64_t pitch)
+{
+    const uint32_t item = blockIdx.x * 256 + threadIdx.x;
+    if (item >= items) return;
+    const uint32_t row = per_row.of(item), at = item - row * per_row.d;
+    const int col = 8 * (int)at, left = dim - col;
+    EightCodes<V> in;
+    in.load(codes + (int64_t)row * dim + col, left);
+    float v[kEach];
+    restore_eight(in.w, exps[(int64_t)row * (per_row.d / 4) + at / 4], v);
+    Eight<T, V> out;
+    out.from_floats(v);
+    out.store(x + (int64_t)row * pitch + col, left);
+}
+
+// ---- the weight gradient: dW[n][k] = sum_r dy[r][n] x^[r][k] -------------------------------------------------------------
+// A matrix product whose depth is the rows, which is the outer index of both operands: tiles of 64 rows lie in LDS as they lie in memory
+// (x^ restored to dy's type on the way, exactly), and ds_read_b64_tr_b16 hands them to v_mfma_f32_32x32x16 turned over.  That read takes, per 16
+// lanes, four rows of 16 columns (lane t the 8 bytes at row t / 4, column 4 (t % 4)) and gives lane t column t of them.
+// A workgroup of four wavefronts owns 128 x 128 of dW, a wavefront 64 x 64.  Where the tiles of dW are too few for the device, the rows
+// are cut into parts whose sums go to the workspace and are added in their order.
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+using tile::bf16x8;
+using tile::floatx16;
+
+__device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, __bf16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, _Float16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kTileN = 128, kTileK = 128, kTileR = 64;
+constexpr int kTileBytes = kTileR * 256;            // a tile of either operand: rows of 128 values of 16 bits
+constexpr int kChunksEach = kTileR * 16 / 256;      // 16-byte chunks of a tile per thread (4)
+constexpr int kMinPartRows = 512;                   // fewest rows of a part
+constexpr int64_t kEnoughTiles = 512;               // two workgroups for each of the 256 compute units
+
+// Where a row's 16-byte chunk lies: chunks are permuted row by row so that neither the writes (16 lanes, one row) nor the turning reads (four
+// rows of 64 bytes at once) meet in a bank.
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 256 + ((chunk ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4); }
+
+struct WgradPlan {
+    int tiles_n, tiles_k, parts;
+    int64_t rows_each;   // rows of a part, a multiple of kTileR
+};
+WgradPlan wgrad_plan(int64_t rows, int32_t n_out, int32_t dim)
+{
+    WgradPlan p;
+    p.tiles_n = (n_out + kTileN - 1) / kTileN;
+    p.tiles_k = (dim + kTileK - 1) / kTileK;
+    const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
+    int64_t parts = (kEnoughTiles + tiles - 1) / tiles;
+    const int64_t most = (rows + kMinPartRows - 1) / kMinPartRows;
+    parts = parts < most ? parts : most;
+    if (parts < 1) parts = 1;
+    p.rows_each = ((rows + parts - 1) / parts + kTileR - 1) / kTileR * kTileR;
+    if (p.rows_each < kTileR) p.rows_each = kTileR;
+    p.parts = (int)((rows + p.rows_each - 1) / p.rows_each);
+    if (p.parts < 1) p.parts = 1;
+    return p;
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(256, 2) wgrad_kernel(const T* __restrict__ dy, int64_t dy_pitch, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
+                                                       int64_t rows, int n_out, int dim, WgradPlan plan, float* __restrict__ out, int accumulate)
+{
+    __shared__ __attribute__((aligned(16))) char lds[2][2][kTileBytes];   // [turn][dy, x^]
+    // workgroups go to the eight dies in turn: each takes a run of the tiles, part by part, so that a part's rows stay in its cache
+    const uint32_t total = gridDim.x, die = blockIdx.x & 7, in_die = blockIdx.x >> 3, whole = total >> 3, extra = total & 7;
+    const uint32_t id = die * whole + (die < extra ? die : extra) + in_die;
+    const uint32_t tiles = (uint32_t)plan.tiles_n * plan.tiles_k, part = id / tiles, tile_id = id % tiles;
+    const int n0 = (int)(tile_id / plan.tiles_k) * kTileN, k0 = (int)(tile_id % plan.tiles_k) * kTileK;
+    const int64_t r_begin = (int64_t)part * plan.rows_each, r_end = r_begin + plan.rows_each < rows ? r_begin + plan.rows_each : rows;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+    const int groups = (dim + kGroup - 1) / kGroup;
+
+    const int s_row = threadIdx.x >> 4, s_chunk = threadIdx.x & 15;   // this thread's chunks: rows s_row + 16 u
+    const int n_left = n_out - (n0 + 8 * s_chunk), k_left = dim - (k0 + 8 * s_chunk);
+    Eight<T, V> dy_in[kChunksEach];
+    EightCodes<V> x_in[kChunksEach];
+    uint32_t x_exp[kChunksEach];
+    auto fetch = [&](int64_t r0) {
+#pragma unroll
+        for (int u = 0; u < kChunksEach; ++u) {
+            const int64_t r = r0 + s_row + 16 * u;
+            const bool in = r < r_end;
+            dy_in[u].load(dy + r * dy_pitch + n0 + 8 * s_chunk, in ? n_left : 0);
+            x_in[u].load(codes + r * dim + k0 + 8 * s_chunk, in ? k_left : 0);
+            x_exp[u] = in && k_left > 0 ? exps[r * groups + (k0 >> 5) + (s_chunk >> 2)] : 1u;
+        }
+    };
+    auto park = [&](int turn) {
+#pragma unroll
+        for (int u = 0; u < kChunksEach; ++u) {
+            const int at = chunk_at(s_row + 16 * u, s_chunk);
+            *reinterpret_cast<u32x4*>(&lds[turn][0][at]) = u32x4{dy_in[u].w[0], dy_in[u].w[1], dy_in[u].w[2], dy_in[u].w[3]};
+            float v[kEach];
+            restore_eight(x_in[u].w, x_exp[u], v);
+            Eight<T, 8> x;
+            x.from_floats(v);
+            *reinterpret_cast<u32x4*>(&lds[turn][1][at]) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+        }
+    };
+    // this lane's places in a tile: block of 32 columns, four rows q of the eight of its half
+    const int wn = 2 * (wave >> 1), wk = 2 * (wave & 1), t = lane & 15, g = (lane >> 4) & 1;
+    int at_n[2][2], at_k[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int row = 8 * half + 4 * q + (t >> 2), within = 2 * g + ((t >> 1) & 1);
+            at_n[b][q] = chunk_at(row, 4 * (wn + b) + within) + 8 * (t & 1);
+            at_k[b][q] = chunk_at(row, 4 * (wk + b) + within) + 8 * (t & 1);
+        }
+    auto turned = [&](const char* p, const int (&at)[2], int step) {
+        typedef __attribute__((address_space(3))) i16x4* lds_ptr;
+        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[0] + step * 16 * 256));
+        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[1] + step * 16 * 256));
+        const u32x2 lo = __builtin_bit_cast(u32x2, a), hi = __builtin_bit_cast(u32x2, b);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+
+    floatx16 acc[2][2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+    if (r_begin < r_end) {
+        fetch(r_begin);
+        park(0);
+        int turn = 0;
+        for (int64_t r0 = r_begin; r0 < r_end; r0 += kTileR, turn ^= 1) {
+            __syncthreads();
+            const bool more = r0 + kTileR < r_end;
+            if (more) fetch(r0 + kTileR);
+#pragma unroll
+            for (int step = 0; step < kTileR / 16; ++step) {
+                u32x4 fn[2], fk[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    fn[b] = turned(lds[turn][0], at_n[b], step);
+                    fk[b] = turned(lds[turn][1], at_k[b], step);
+                }
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) acc[a][b] = mfma(fn[a], fk[b], acc[a][b], T{});
+            }
+            if (more) park(turn ^ 1);
+        }
+    }
+    float* const to = out + (plan.parts > 1 ? (int64_t)part * n_out * dim : 0);
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int k = k0 + 32 * (wk + b) + l32;
+            if (k >= dim) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = n0 + 32 * (wn + a) + 8 * (i / 4) + 4 * half + i % 4;
+                if (n >= n_out) continue;
+                float* const p = to + (int64_t)n * dim + k;
+                *p = accumulate && plan.parts == 1 ? *p + acc[a][b][i] : acc[a][b][i];
+            }
+        }
+}
+
+// dW (+)= the parts, one after the other; four neighbouring values a thread where all is aligned for it.
+template <int V>
+__global__ void __launch_bounds__(256) wgrad_join_kernel(const float* __restrict__ parts, int n_parts, int64_t n, float* __restrict__ dw, int accumulate)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+    if (i >= n) return;
+    float s[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = accumulate ? dw[i + j] : 0.f;
+    for (int p = 0; p < n_parts; ++p) {
+        const float* const q = parts + p * n + i;
+        if constexpr (V == 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] += v[j];
+        } else {
+            s[0] += q[0];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) dw[i + j] = s[j];
+}
+
+template <typename T, int V>
+int run_wgrad(const void* dy, int64_t dy_pitch, const pruner_checkpoint* kept, int64_t rows, int32_t n_out, int32_t dim, const WgradPlan& plan, float* dw, int32_t accumulate,
+              float* parts, hipStream_t st)
+{
+    const int64_t blocks = (int64_t)plan.tiles_n * plan.tiles_k * plan.parts;
+    hipLaunchKernelGGL((wgrad_kernel<T, V>), dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(dy), dy_pitch, kept->codes, kept->exps, rows, n_out, dim, plan,
+                       plan.parts > 1 ? parts : dw, accumulate);
+    PRUNER_LAUNCH_CHECK();
+    if (plan.parts > 1) {
+        const int64_t n = (int64_t)n_out * dim;
+        if (n % 4 == 0 && aligned(dw, 16))
+            hipLaunchKernelGGL(wgrad_join_kernel<4>, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, parts, plan.parts, n, dw, accumulate);
+        else
+            hipLaunchKernelGGL(wgrad_join_kernel<1>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, parts, plan.parts, n, dw, accumulate);
+        PRUNER_LAUNCH_CHECK();
+    }
+    return PRUNER_OK;
+}
+
+bool wgrad_sizes_ok(int64_t rows, int32_t n_out, int32_t dim)
+{
+    return rows >= 0 && rows < (1ll << 40) && n_out >= 1 && n_out <= (1 << 20) && dim >= 1 && dim <= (1 << 20) && (int64_t)n_out * dim <= (1ll << 36);
+}
+
+bool sizes_ok(int32_t dtype, int64_t rows, int32_t dim, int64_t pitch)
+{
+    return type_known(dtype) && rows >= 0 && dim >= 1 && dim <= (1 << 28) && pitch >= dim && (rows == 0 || pitch < (1ll << 40) / rows);
+}
+bool kept_ok(const pruner_checkpoint* c) { return c && c->codes && c->exps && aligned(c->codes, 8); }
+
+// Rows in launches of below 2^31 threads.
+template <typename Launch> int in_row_chunks(int64_t rows, int32_t dim, Launch&& launch)
+{
+    const Divisor per_row(4u * ((uint32_t)(dim + kGroup - 1) / kGroup));
+    int64_t most = ((1ll << 31) - 512) / per_row.d;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        const uint32_t items = (uint32_t)(n * per_row.d);
+        launch(r, items, dim3((items + 255) / 256), per_row);
+        PRUNER_LAUNCH_CHECK();
+    }
+    return PRUNER_OK;
+}
+
+template <typename T, int V>
+int pack_rows(const void* x, int64_t rows, int32_t dim, int64_t pitch, const pruner_checkpoint* kept, hipStream_t st)
+{
+    return in_row_chunks(rows, dim, [&](int64_t r, uint32_t items, dim3 grid, const Divisor& per_row) {
+        hipLaunchKernelGGL((pack_kernel<T, V>), grid, dim3(256), 0, st, static_cast<const T*>(x) + r * pitch, pitch, dim, items, per_row, kept->codes + r * dim,
+                           kept->exps + r * (per_row.d / 4));
+    });
+}
+template <typename T, int V>
+int restore_rows(const pruner_checkpoint* kept, int64_t rows, int32_t dim, void* x, int64_t pitch, hipStream_t st)
+{
+    return in_row_chunks(rows, dim, [&](int64_t r, uint32_t items, dim3 grid, const Divisor& per_row) {
+        hipLaunchKernelGGL((restore_kernel<T, V>), grid, dim3(256), 0, st, kept->codes + r * dim, kept->exps + r * (per_row.d / 4), dim, items, per_row,
+                           static_cast<T*>(x) + r * pitch, pitch);
+    });
+}
+
+}  // namespace
+}  // namespace pruner
+
+using namespace pruner;
+
+#define BY_TYPE_AND_ACCESS(dtype, v, fn, ...)                                                                                                   \
+    ((dtype) == PRUNER_F32    ? ((v) == 8 ? fn<float, 8>(__VA_ARGS__) : (v) == 4 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))        \
+     : (dtype) == PRUNER_BF16 ? ((v) == 8 ? fn<__bf16, 8>(__VA_ARGS__) : (v) == 4 ? fn<__bf16, 4>(__VA_ARGS__) : fn<__bf16, 1>(__VA_ARGS__))     \
+                              : ((v) == 8 ? fn<_Float16, 8>(__VA_ARGS__) : (v) == 4 ? fn<_Float16, 4>(__VA_ARGS__) : fn<_Float16, 1>(__VA_ARGS__)))
+
+extern "C" int pruner_checkpoint_pack(const void* x, int32_t dtype, int64_t rows, int32_t dim, int64_t pitch, const pruner_checkpoint* kept, void* stream)
+{
+    if (!sizes_ok(dtype, rows, dim, pitch)) return PRUNER_EINVAL;
+    if (rows == 0) return PRUNER_OK;
+    if (!x || !aligned(x, type_bytes(dtype)) || !kept_ok(kept)) return PRUNER_EINVAL;
+    Access a;
+    a.fits(x, type_bytes(dtype), pitch);
+    a.fits(kept->codes, 1, dim);
+    return BY_TYPE_AND_ACCESS(dtype, a.v, pack_rows, x, rows, dim, pitch, kept, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int pruner_checkpoint_restore(const pruner_checkpoint* kept, int32_t dtype, int64_t rows, int32_t dim, void* x, int64_t pitch, void* stream)
+{
+    if (!sizes_ok(dtype, rows, dim, pitch)) return PRUNER_EINVAL;
+    if (rows == 0) return PRUNER_OK;
+    if (!x || !aligned(x, type_bytes(dtype)) || !kept_ok(kept)) return PRUNER_EINVAL;
+    Access a;
+    a.fits(x, type_bytes(dtype), pitch);
+    a.fits(kept->codes, 1, dim);
+    return BY_TYPE_AND_ACCESS(dtype, a.v, restore_rows, kept, rows, dim, x, pitch, static_cast<hipStream_t>(stream));
+}
+
+extern "C" size_t pruner_checkpoint_wgrad_workspace_bytes(int64_t rows, int32_t n_out, int32_t dim)
+{
+    if (!wgrad_sizes_ok(rows, n_out, dim)) return 0;
+    const WgradPlan p = wgrad_plan(rows, n_out, dim);
+    return p.parts > 1 ? round_up((size_t)p.parts * (size_t)n_out * (size_t)dim * 4, 256) : 256;
+}
+
+extern "C" int pruner_checkpoint_wgrad(const void* dy, int32_t dtype, int64_t dy_pitch, const pruner_checkpoint* kept, int64_t rows, int32_t n_out, int32_t dim, float* dw,
+                                       int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if ((dtype != PRUNER_BF16 && dtype != PRUNER_F16) || !wgrad_sizes_ok(rows, n_out, dim) || !dw || !aligned(dw, 4) || (accumulate != 0 && accumulate != 1)) return PRUNER_EINVAL;
+    if (rows > 0 && (!dy || !aligned(dy, 2) || !kept_ok(kept) || dy_pitch < n_out || dy_pitch >= (1ll << 40) / rows)) return PRUNER_EINVAL;
+    if (rows == 0 && accumulate) return PRUNER_OK;
+    const WgradPlan plan = wgrad_plan(rows, n_out, dim);
+    if (plan.parts > 1 && (!workspace || !aligned(workspace, 256) || workspace_bytes < pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim))) return PRUNER_EWORKSPACE;
+    Access a;
+    const pruner_checkpoint none{nullptr, nullptr};
+    if (rows > 0) {
+        a.fits(dy, 2, dy_pitch);
+        a.fits(kept->codes, 1, dim);
+        if (n_out % a.v) a.v = n_out % 4 ? 1 : 4;   // (a row's last access must not pass its end)
+    }
+    const pruner_checkpoint* const c = rows > 0 ? kept : &none;
+    float* const parts = static_cast<float*>(workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == PRUNER_BF16)
+        return a.v == 8   ? run_wgrad<__bf16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+               : a.v == 4 ? run_wgrad<__bf16, 4>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+                          : run_wgrad<__bf16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
+    return a.v == 8   ? run_wgrad<_Float16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+           : a.v == 4 ? run_wgrad<_Float16, 4>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+                      : run_wgrad<_Float16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
+}
