@@ -508,7 +508,7 @@ def _c_norm(x, has_f, w_post, w_pre, gate, alpha, eps, center):
 def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, checkpoint=False, stream=None):
     """pruner_gated_norm: h = alpha x + sigmoid(gate) norm(f) w_post, y = norm(h) w_pre.  x, f: CUDA [rows, dim] of one type (f None: the first norm
     of a model; w_post may then be None); w_post, w_pre float32 [dim]; gate None, [rows, dim] of x's type, or float32 [dim]; w_pre None: y is not formed.
-    Returns (h, y), with checkpoint=True (h, y, Checkpoint of y)."""
+    Returns (h, y, kept): kept is y's Checkpoint with checkpoint=True, else None."""
     import torch
     lib = load_library()
     rows, dim = x.shape
@@ -524,7 +524,7 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
     rc = lib.pruner_gated_norm(C.byref(p), px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), C.byref(_c_checkpoint(kept, rows, dim)) if checkpoint else None, _stream(stream))
     if rc:
         raise PrunerError(rc, "pruner_gated_norm")
-    return (h, y, kept) if checkpoint else (h, y)
+    return h, y, kept
 
 
 def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, workspace=None, stream=None):
