@@ -387,7 +387,7 @@ int pruner_checkpoint_restore(const pruner_checkpoint* kept, int32_t dtype, int6
  *   kept        the input's checkpoint, [rows][dim]
  *   dw          device float [n_out][dim]
  *   accumulate  0: dw is overwritten; 1: added to
- * rows >= 0 (0: dw is cleared, or left alone), n_out and dim 1..2^20.
+ * rows >= 0 (0: dw is cleared, or left alone), n_out and dim 1..2^20, n_out x dim up to 2^31.
  * workspace: pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim).
  * Errors: PRUNER_EINVAL (null or misaligned pointers: dy 2 bytes, codes 8, dw 4; sizes, type), PRUNER_EWORKSPACE.
  */
@@ -454,7 +454,8 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  *   dtable           device, of dtype, the table's shape, or NULL without table; sums over pairs in binary32 in an order that depends on the
  *                    sizes and the device alone, rounded once
  * Outputs are written for every row of q_tokens and k_tokens.  dk and dv are the sums over the query heads that share a key head.
- * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, batch x q_heads x q_tokens below 2^31.
+ * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, batch x q_heads x max(64, q_tokens) below 2^30, and for the
+ * gradients batch x kv_heads x max(64, k_tokens) as well.
  * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes only.
  * Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
  */

@@ -145,6 +145,14 @@ def load_library():
         lib.pruner_gated_norm_grad.restype = C.c_int
         lib.pruner_gated_norm_grad.argtypes = [P(CNorm), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, P(CCheckpoint),
                                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_rel_attention_workspace_bytes.restype = C.c_size_t
+        lib.pruner_rel_attention_workspace_bytes.argtypes = [P(CAttention)]
+        lib.pruner_rel_attention.restype = C.c_int
+        lib.pruner_rel_attention.argtypes = [P(CAttention)] + [P(CHeads)] * 4 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_rel_attention_grad_workspace_bytes.restype = C.c_size_t
+        lib.pruner_rel_attention_grad_workspace_bytes.argtypes = [P(CAttention)]
+        lib.pruner_rel_attention_grad.restype = C.c_int
+        lib.pruner_rel_attention_grad.argtypes = [P(CAttention)] + [P(CHeads)] * 5 + [C.c_void_p] + [P(CHeads)] * 3 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_workspace_bytes.restype = C.c_size_t
         lib.pruner_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
         lib.pruner_strerror.restype = C.c_char_p
@@ -555,3 +563,88 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
     if rc:
         raise PrunerError(rc, "pruner_gated_norm_grad")
     return dx, df, dgate, dw_post, dw_pre
+
+
+def relative_edges(n, max_distance):
+    """Distances at which a new bucket begins, for a table with n of them on a side: 1, 2, .. up to about half of them, the others spread evenly over the
+    logarithm up to max_distance (int32 numpy array, ascending strictly)."""
+    exact = max(1, (n + 1) // 2)
+    assert 1 <= n <= MAX_BIAS_EDGES and n <= max_distance <= MAX_BIAS_DISTANCE, "edges"
+    found = list(range(1, exact + 1))
+    for i in range(1, n - exact + 1):
+        at = int(round(exact * (max_distance / exact) ** (i / (n - exact))))
+        found.append(min(max(at, found[-1] + 1), max_distance - (n - exact - i)))
+    return np.array(found, dtype=np.int32)
+
+
+def _heads(t, what):
+    """A tensor [batch, tokens, heads, head_dim], the last dimension contiguous, as a CHeads (dimensions of one element have no stride of their own)."""
+    assert t.is_cuda and t.dim() == 4 and (t.stride(3) == 1 or t.shape[3] == 1), what
+    n, st = t.shape, t.stride()
+    return CHeads(t.data_ptr(), st[0] if n[0] > 1 else 0, st[1] if n[1] > 1 else 0, st[2] if n[2] > 1 else 0)
+
+
+def _lengths(t, batch, what):
+    import torch
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == batch, what
+    return t.data_ptr()
+
+
+def _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale):
+    batch, q_tokens, q_heads, head_dim = q.shape
+    k_tokens, kv_heads = k.shape[1], k.shape[2]
+    assert k.shape == (batch, k_tokens, kv_heads, head_dim) and v.shape == k.shape and k.dtype == q.dtype and v.dtype == q.dtype, "q, k, v"
+    flags = _ATTENTION_CAUSAL if causal else 0
+    n_edges = 0
+    if table is not None:
+        edges = np.ascontiguousarray(edges if edges is not None else (), dtype=np.int32)
+        n_edges = len(edges)
+        assert table.is_cuda and table.dtype == q.dtype and table.is_contiguous() and table.dim() == 2 and table.shape[1] == q_heads, "table"
+        assert table.shape[0] in (n_edges + 1, 2 * (n_edges + 1)), "table: n_edges + 1 buckets, or twice as many"
+        flags |= _ATTENTION_TWO_SIDED if table.shape[0] == 2 * (n_edges + 1) else 0
+    a = CAttention(_dtype(q.dtype), batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, flags, 1.0 / math.sqrt(head_dim) if scale is None else scale,
+                   _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"), table.data_ptr() if table is not None else None,
+                   edges.ctypes.data if n_edges else None, n_edges)
+    a.keep = edges   # (the host array lives as long as the struct)
+    return a
+
+
+def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causal=False, scale=None, o=None, want_lse=False, workspace=None, stream=None):
+    """pruner_rel_attention: softmax(scale q k^T + bias by relative position) v.  q: bfloat16 or float16 CUDA [batch, q_tokens, q_heads, head_dim], k, v
+    [batch, k_tokens, kv_heads, head_dim], any strides with contiguous heads of at most 128; q_heads a multiple of kv_heads.  table: of the same type,
+    [len(edges) + 1, q_heads] (one-sided) or [2 (len(edges) + 1), q_heads] (two-sided), or None; edges: ascending distances on the host, e.g. from
+    relative_edges.  q_len, k_len: int32 CUDA [batch] or None; query i of a sequence stands at position k_len - q_len + i.  scale None: 1 / sqrt(head_dim).
+    Returns o [batch, q_tokens, q_heads, head_dim], with want_lse=True (o, lse float32 [batch, q_heads, q_tokens])."""
+    import torch
+    lib = load_library()
+    a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert o.shape == q.shape and o.dtype == q.dtype, "o"
+    lse = torch.empty((a.batch, a.q_heads, a.q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
+    ws = _workspace(workspace, int(lib.pruner_rel_attention_workspace_bytes(C.byref(a))), q.device)
+    rc = lib.pruner_rel_attention(C.byref(a), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_rel_attention")
+    return (o, lse) if want_lse else o
+
+
+def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, k_len=None, causal=False, scale=None, workspace=None, stream=None):
+    """pruner_rel_attention_grad.  do: the gradient of rel_attention's o; o, lse: what it returned; the rest as it was called.
+    Returns (dq, dk, dv, dtable), dtable None without table."""
+    import torch
+    lib = load_library()
+    a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    assert do.shape == q.shape and do.dtype == q.dtype and o.shape == q.shape and o.dtype == q.dtype, "do, o"
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (a.batch, a.q_heads, a.q_tokens), "lse"
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dk, dv = torch.empty(k.shape, dtype=q.dtype, device=q.device), torch.empty(v.shape, dtype=q.dtype, device=q.device)
+    dtable = torch.empty(table.shape, dtype=q.dtype, device=q.device) if table is not None else None
+    ws = _workspace(workspace, int(lib.pruner_rel_attention_grad_workspace_bytes(C.byref(a))), q.device)
+    rc = lib.pruner_rel_attention_grad(C.byref(a), _heads(do, "do"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _heads(dq, "dq"),
+                                       _heads(dk, "dk"), _heads(dv, "dv"), _ptr(dtable), _ptr(ws), ws.numel(), _stream(stream))
+    if rc:
+        raise PrunerError(rc, "pruner_rel_attention_grad")
+    return dq, dk, dv, dtable

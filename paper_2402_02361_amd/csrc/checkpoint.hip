@@ -258,7 +258,7 @@ int run_wgrad(const void* dy, int64_t dy_pitch, const pruner_checkpoint* kept, i
 
 bool wgrad_sizes_ok(int64_t rows, int32_t n_out, int32_t dim)
 {
-    return rows >= 0 && rows < (1ll << 40) && n_out >= 1 && n_out <= (1 << 20) && dim >= 1 && dim <= (1 << 20) && (int64_t)n_out * dim <= (1ll << 36);
+    return rows >= 0 && rows < (1ll << 40) && n_out >= 1 && n_out <= (1 << 20) && dim >= 1 && dim <= (1 << 20) && (int64_t)n_out * dim <= (1ll << 31);
 }
 
 bool sizes_ok(int32_t dtype, int64_t rows, int32_t dim, int64_t pitch)

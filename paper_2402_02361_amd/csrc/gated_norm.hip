@@ -18,8 +18,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-g * kLog2e)); }
 
-// Sums over the T threads of a row, N of them at once, the same bits in all of them.  T a power of two in 4..1024; rows of more than 64
-// threads take whole workgroups, whose wavefronts meet in LDS (two places in turn, so one barrier is enough).
+// Sums over the T threads of a row, N of them at once, the same bits in all of them.  T a power of two in 4..1024; the wavefronts of a row
+// of more than 64 threads meet in LDS (two places in turn, so one barrier is enough).
 struct RowSum {
     float (*meet)[16][2];   // [2][16 wavefronts][N <= 2]
     int threads, turn;
@@ -30,7 +30,7 @@ struct RowSum {
 #pragma unroll
             for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], o, kWave);
         if (threads <= kWave) return;
-        const int wave = threadIdx.x >> 6, waves = threads >> 6;
+        const int wave = threadIdx.x >> 6, waves = threads >> 6, first = wave & ~(waves - 1);   // (a workgroup may hold two such rows)
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int n = 0; n < N; ++n) meet[turn][wave][n] = v[n];
@@ -38,7 +38,7 @@ struct RowSum {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             float s = 0.f;
-            for (int w = 0; w < waves; ++w) s += meet[turn][w][n];
+            for (int w = first; w < first + waves; ++w) s += meet[turn][w][n];
             v[n] = s;
         }
         turn ^= 1;

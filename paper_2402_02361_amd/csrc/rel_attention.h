@@ -1,0 +1,236 @@
+// What the kernels of attention with a learned relative position bias have in common (see include/pruner.h for the formulas).
+//
+// Products run on v_mfma_f32_32x32x16 with both operands' outer index in the lanes: of a 32 x 32 result, lane (l32 = lane & 31, half = lane >> 5)
+// holds column l32 and the sixteen rows 8 (i / 4) + 4 half + i % 4.  An operand of depth 16 holds, per lane, the eight depths of its half.  Any
+// numbering of the depth will do as long as both operands use the same one, and with depth (half, j) meaning row 8 (j / 4) + 4 half + j % 4 of a
+// 16-row step, a result's registers 8 s .. 8 s + 7, rounded to 16 bits, are the operand of the next product as they stand: softmax weights and
+// their gradients never leave the registers.  The other operand of that product is a tile turned over, read by ds_read_b64_tr_b16 (16 lanes take
+// four rows of 16 columns; lane t gives the address of row t / 4, columns 4 (t % 4) .., and gets column t of the four rows).
+#pragma once
+#include "common.h"
+
+namespace pruner {
+namespace att {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.693147180559945309417f;
+constexpr float kHuge = 1e30f;   // a bias beyond this is added to a score before anything else is done with either
+#define ATT_INF __builtin_inff()
+
+__device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, __bf16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, _Float16)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pair_of(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
+__device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2)); }
+__device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }
+__device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
+
+__device__ __forceinline__ floatx16 zero16()
+{
+    floatx16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// The other half's value (lane ^ 32).
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+__device__ __forceinline__ int row_of(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+
+// What this wavefront's lanes wrote to LDS is there for its other lanes after.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+struct Heads {
+    char* p;
+    int64_t batch, head;
+    int32_t token;   // elements
+    template <typename T> __device__ __forceinline__ T* at(int b, int h) const { return reinterpret_cast<T*>(p) + b * batch + h * head; }
+};
+
+struct Args {
+    Heads q, k, v;
+    const int32_t *q_len, *k_len;
+    const void* table;
+    int32_t batch, q_tokens, k_tokens, q_heads, kv_heads, group, head_dim, causal, two_sided, n_edges;
+    float scale;
+    int32_t left, right;   // pairs at r <= -left share one bucket, those at r >= right share one (both cut to what the lengths can reach)
+    int32_t edges[PRUNER_MAX_BIAS_EDGES];
+    __device__ __forceinline__ int queries(int b) const { return clamped(q_len, b, q_tokens); }
+    __device__ __forceinline__ int keys(int b) const { return clamped(k_len, b, k_tokens); }
+    __device__ __forceinline__ static int clamped(const int32_t* p, int b, int most)
+    {
+        if (!p) return most;
+        const int n = p[b];
+        return n < 0 ? 0 : n > most ? most : n;
+    }
+    __device__ __forceinline__ int bucket(int r) const
+    {
+        const int d = two_sided ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
+        int n = 0;
+        for (int e = 0; e < n_edges; ++e) n += edges[e] <= d ? 1 : 0;
+        return n + (two_sided && r > 0 ? n_edges + 1 : 0);
+    }
+    template <typename T> __device__ __forceinline__ float bias(int n, int h) const { return (float)static_cast<const T*>(table)[(int64_t)n * q_heads + h]; }
+};
+
+// Biases by r in LDS: those that a tile which is not wholly at one end can ask for, r = first .. first + size - 1.
+constexpr int kWindowPad = 96;   // a tile spans 32 places on one side and at most 64 on the other
+struct Window {
+    int first, size;
+    __host__ __device__ Window(int left, int right) : first(-left - kWindowPad), size(left + right + 2 * kWindowPad) {}
+};
+template <typename T> __device__ __forceinline__ void fill_window(const Args& a, float* lds, int h, int thread, int threads)
+{
+    const Window w(a.left, a.right);
+    for (int i = thread; i < w.size; i += threads) lds[i] = a.bias<T>(a.bucket(w.first + i), h);
+}
+// Where a tile with r = r_lo .. r_hi lies.
+enum { kNear, kLeft, kRight };
+__device__ __forceinline__ int place_of(const Args& a, int r_lo, int r_hi) { return r_hi <= -a.left ? kLeft : r_lo >= a.right ? kRight : kNear; }
+
+// Tiles of DP columns (the head dimension rounded up; columns past it are zero) in LDS: rows of DP values, their 16-byte chunks permuted row by
+// row so that neither 16 rows' reads of one chunk nor a turning read's four rows of 64 bytes meet in a bank.
+template <int DP> struct Tile {
+    static constexpr int kChunks = DP / 8, kRowBytes = DP * 2, kSteps = DP / 16, kBlocks = DP / 32;
+    __device__ __forceinline__ static int turn_of(int row)
+    {
+        if constexpr (DP == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+        if constexpr (DP == 64) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        return (row >> 2) & 3;
+    }
+    __device__ __forceinline__ static int at(int row, int chunk) { return row * kRowBytes + ((chunk ^ turn_of(row)) << 4); }
+};
+
+// The places of a lane's fragments in a tile.
+template <int DP> struct Lane {
+    int row[Tile<DP>::kSteps];          // rows as the outer index: row l32, depths 16 s + 8 half ..
+    int turned[Tile<DP>::kBlocks][2];   // columns as the outer index: columns 32 b + l32, rows 8 q + 4 half .. + 3 of a 16-row step
+    __device__ __forceinline__ void set(int lane)
+    {
+        const int l32 = lane & 31, half = lane >> 5, t = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+        for (int s = 0; s < Tile<DP>::kSteps; ++s) row[s] = Tile<DP>::at(l32, 2 * s + half);
+#pragma unroll
+        for (int b = 0; b < Tile<DP>::kBlocks; ++b)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) turned[b][q] = Tile<DP>::at(8 * q + 4 * half + (t >> 2), 4 * b + 2 * g + ((t >> 1) & 1)) + 8 * (t & 1);
+    }
+    __device__ __forceinline__ u32x4 rows(const char* tile, int block, int s) const
+    {
+        return *reinterpret_cast<const u32x4*>(tile + row[s] + block * 32 * Tile<DP>::kRowBytes);
+    }
+    __device__ __forceinline__ u32x4 columns(const char* tile, int b, int step) const
+    {
+        typedef __attribute__((address_space(3))) i16x4* lds_ptr;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + turned[b][0] + step * 16 * Tile<DP>::kRowBytes));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + turned[b][1] + step * 16 * Tile<DP>::kRowBytes));
+        const u32x2 a = __builtin_bit_cast(u32x2, lo), c = __builtin_bit_cast(u32x2, hi);
+        return u32x4{a[0], a[1], c[0], c[1]};
+    }
+};
+
+// ROWS rows on their way from memory to a tile, by THREADS threads.
+template <typename T, int DP, int ROWS, int THREADS> struct Stage {
+    static constexpr int kEach = ROWS * Tile<DP>::kChunks / THREADS;
+    static_assert(kEach >= 1 && ROWS * Tile<DP>::kChunks % THREADS == 0, "whole chunks per thread");
+    u32x4 w[kEach];
+    __device__ __forceinline__ void fetch(const T* base, int32_t token, int rows, int head_dim, int thread)
+    {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const int id = thread + THREADS * u, row = id / Tile<DP>::kChunks, chunk = id % Tile<DP>::kChunks;
+            const bool in = row < rows && 8 * chunk < head_dim;
+            const uint32_t off = in ? (uint32_t)row * (uint32_t)token + 8u * (uint32_t)chunk : 0u;
+            w[u] = u32x4{0u, 0u, 0u, 0u};
+            if (in) w[u] = *reinterpret_cast<const u32x4*>(base + off);
+        }
+    }
+    __device__ __forceinline__ void park(char* tile, int thread) const
+    {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const int id = thread + THREADS * u;
+            *reinterpret_cast<u32x4*>(tile + Tile<DP>::at(id / Tile<DP>::kChunks, id % Tile<DP>::kChunks)) = w[u];
+        }
+    }
+};
+
+// A row's fragments straight from memory (its owner is lane l32, depths 16 s + 8 half ..); zero where there is no such row or column.
+template <typename T, int DP> __device__ __forceinline__ void load_row(u32x4 (&f)[Tile<DP>::kSteps], const T* p, bool in, int head_dim, int half)
+{
+#pragma unroll
+    for (int s = 0; s < Tile<DP>::kSteps; ++s) {
+        f[s] = u32x4{0u, 0u, 0u, 0u};
+        if (in && 16 * s + 8 * half < head_dim) f[s] = *reinterpret_cast<const u32x4*>(p + 16 * s + 8 * half);
+    }
+}
+// A column of a result to memory: this lane's rows of the 32-row blocks are a row's values 32 b + 8 g + 4 half ..
+template <typename T, int DP> __device__ __forceinline__ void store_row(T* p, const floatx16 (&acc)[Tile<DP>::kBlocks], float factor, int head_dim, int half)
+{
+#pragma unroll
+    for (int b = 0; b < Tile<DP>::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * b + 8 * g + 4 * half;
+            if (d < head_dim)
+                *reinterpret_cast<u32x2*>(p + d) = u32x2{pair_of(acc[b][4 * g] * factor, acc[b][4 * g + 1] * factor, T{}), pair_of(acc[b][4 * g + 2] * factor, acc[b][4 * g + 3] * factor, T{})};
+        }
+}
+template <int DP> __device__ __forceinline__ void store_row32(float* p, const floatx16 (&acc)[Tile<DP>::kBlocks], int half)
+{
+#pragma unroll
+    for (int b = 0; b < Tile<DP>::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(p + 32 * b + 8 * g + 4 * half) = f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
+}
+template <typename T> __device__ __forceinline__ u32x4 weights_of(const floatx16& p, int step)   // a result's registers as the next product's operand
+{
+    return u32x4{pair_of(p[8 * step], p[8 * step + 1], T{}), pair_of(p[8 * step + 2], p[8 * step + 3], T{}), pair_of(p[8 * step + 4], p[8 * step + 5], T{}),
+                 pair_of(p[8 * step + 6], p[8 * step + 7], T{})};
+}
+
+// Workgroups go to the eight dies in turn.  Item i of `heads` x `tiles` items, for a kernel whose workgroups read what their head's others read:
+// a die takes a run of heads, of all of them the last tiles first (under a causal mask these are the longest).
+struct Item {
+    int head, tile;
+};
+__device__ __forceinline__ Item item_of(uint32_t id, uint32_t heads, uint32_t tiles)
+{
+    if (heads % 8 == 0) {
+        const uint32_t own = heads / 8, die = id % 8, j = id / 8;
+        return Item{(int)(die * own + j % own), (int)(tiles - 1 - j / own)};
+    }
+    return Item{(int)(id % heads), (int)(tiles - 1 - id / heads)};
+}
+
+// ---- host
+
+bool heads_ok(const pruner_heads* h);
+// Everything that is refused about sizes and pointers but outputs; fills the kernels' arguments.
+int attention_args(const pruner_attention* a, const pruner_heads* q, const pruner_heads* k, const pruner_heads* v, Args* out);
+bool attention_sizes_ok(const pruner_attention* a);
+Heads heads_of(const pruner_heads* h);
+inline int padded_dim(int head_dim) { return head_dim <= 32 ? 32 : head_dim <= 64 ? 64 : 128; }
+
+}  // namespace att
+}  // namespace pruner

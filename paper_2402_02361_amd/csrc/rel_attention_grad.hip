@@ -1,0 +1,634 @@
+// Attention with a learned relative position bias by buckets, backward.  With P = exp(s - lse), dP = dO V^T, delta_i = sum_d dO o:
+//     dS = P (dP - delta);   dQ = scale dS K;   dK = scale dS^T Q;   dV = P^T dO;   dtable[n][h] = sum of dS over the pairs of bucket n
+//
+//   queries_kernel   a wavefront owns 32 queries, as in the forward pass: S^T and dP^T leave a query's values in its two lanes; dQ^T += K^T dS^T.
+//                    It also leaves delta for the next kernel, and the sums of dS along the diagonals j - p: a tile beyond the largest edge
+//                    adds into one register, the others add into LDS, where a wavefront's half has diagonals of its own (no two lanes of
+//                    one instruction meet, and a wavefront's instructions run in order: the sums do not depend on timing).
+//   keys_kernel      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
+//                    through the query tiles of all heads that share the key head.  Where key tiles are too few for the device, their query
+//                    tiles are cut into parts, whose sums go to the workspace (keys_join_kernel adds them in order).
+//   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, then the diagonals of a bucket.
+// S is formed twice, so nothing is added across workgroups but in a fixed order.
+#include "rel_attention.h"
+
+namespace pruner {
+namespace att {
+namespace {
+
+constexpr int kKeys = 64;
+constexpr int kOwn = 32;   // rows of a wavefront's own tile
+
+// Weights before the second product are at most 1: in binary16, which has fewer bits below 2^-14, they are held times 2^15.
+template <typename T> struct Held;
+template <> struct Held<__bf16> {
+    static constexpr float kShift = 0.f, kUnit = 1.f;
+};
+template <> struct Held<_Float16> {
+    static constexpr float kShift = 15.f, kUnit = 1.f / 32768.f;
+};
+
+struct Grad {
+    Heads dout, o, out0, out1;   // out0, out1: dq, or dk and dv
+    const float* lse;
+    float* delta;                // [batch][q_heads][q_tokens]
+    float* diagonals;            // [part][q_heads][window + 2]
+    float* sums;                 // [part][batch][kv_heads][k_tokens][2][DP]
+    int parts;
+};
+
+template <typename T, int DP, bool SHARED>
+__global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_tiles)
+{
+    constexpr int kN = SHARED ? kKeys : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
+    const uint32_t heads = (uint32_t)a.batch * a.q_heads;
+    int bh, q0, tile_id = 0;
+    if constexpr (SHARED) {
+        const Item it = item_of(blockIdx.x, heads, (uint32_t)q_tiles);
+        bh = it.head;
+        tile_id = it.tile;
+        q0 = it.tile * 128 + 32 * wave;
+    } else {
+        bh = (int)(blockIdx.x * 4 + wave);
+        q0 = 0;
+        if (bh >= (int)heads) return;
+    }
+    const int b = bh / a.q_heads, h = bh % a.q_heads, hk = h / a.group;
+    const int ql = a.queries(b), kl = a.keys(b);
+    const Window window(a.left, a.right);
+    const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
+    // LDS: biases, diagonals of every wavefront's halves, tiles
+    float* const biases = reinterpret_cast<float*>(lds) + (SHARED ? 0 : wave * window_floats);
+    float* const all_diagonals = reinterpret_cast<float*>(lds) + (SHARED ? 1 : 4) * window_floats;
+    float* const diagonals = all_diagonals + (2 * wave + half) * window_floats;
+    char* const tiles = reinterpret_cast<char*>(all_diagonals + 8 * window_floats) + (SHARED ? 0 : wave * 2 * kTileBytes);
+
+    const int first_q = SHARED ? q0 - 32 * wave : 0, rows_here = SHARED ? 128 : 32;
+    const int last_q = first_q + rows_here < ql ? first_q + rows_here - 1 : ql - 1;
+    int end = first_q >= ql ? 0 : a.causal ? kl - ql + last_q + 1 : kl;
+    end = end < kl ? end : kl;
+
+    Lane<DP> at;
+    at.set(lane);
+    const int i = q0 + l32, p = kl - ql + i;
+    const bool mine = i < ql;
+    u32x4 qf[Tile<DP>::kSteps], df[Tile<DP>::kSteps];
+    load_row<T, DP>(qf, a.q.at<T>(b, h) + (int64_t)i * a.q.token, mine, a.head_dim, half);
+    load_row<T, DP>(df, gr.dout.at<T>(b, h) + (int64_t)i * gr.dout.token, mine, a.head_dim, half);
+    float delta = 0.f, lse = ATT_INF;
+    const int64_t row = (int64_t)bh * a.q_tokens + i;
+    if (mine) {
+        lse = gr.lse[row];
+        lse = lse == -ATT_INF ? ATT_INF : lse;   // (no key: every weight is exp(-infinity))
+    }
+    if constexpr (SHARED) {
+        u32x4 of[Tile<DP>::kSteps];
+        load_row<T, DP>(of, gr.o.at<T>(b, h) + (int64_t)i * gr.o.token, mine, a.head_dim, half);
+#pragma unroll
+        for (int s = 0; s < Tile<DP>::kSteps; ++s)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const f32x2 x = pair_to(of[s][w], T{}), y = pair_to(df[s][w], T{});
+                delta = __builtin_fmaf(x[0], y[0], delta);
+                delta = __builtin_fmaf(x[1], y[1], delta);
+            }
+        delta += other_half(delta);
+        if (half == 0 && i < a.q_tokens) gr.delta[row] = delta;
+    }
+    floatx16 dq[Tile<DP>::kBlocks];
+#pragma unroll
+    for (int d = 0; d < Tile<DP>::kBlocks; ++d) dq[d] = zero16();
+    float sum_left = 0.f, sum_right = 0.f;
+    if (a.table)
+        for (int n = l32; n < window_floats; n += 32) diagonals[n] = 0.f;
+    if (end > 0) {
+        const T* const kp = a.k.at<T>(b, hk);
+        const T* const vp = a.v.at<T>(b, hk);
+        Stage<T, DP, kN, kThreads> ks, vs;
+        ks.fetch(kp, a.k.token, kl, a.head_dim, thread);
+        vs.fetch(vp, a.v.token, kl, a.head_dim, thread);
+        float bias_left = 0.f, bias_right = 0.f;
+        if (a.table) {
+            bias_left = a.bias<T>(a.n_edges, h);
+            bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
+            fill_window<T>(a, biases, h, thread, kThreads);
+        }
+        ks.park(tiles, thread);
+        vs.park(tiles + kTileBytes, thread);
+        const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
+        const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
+        const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
+        // P (in s) and dP (in ds) of 32 keys from k0; returns where they lie
+        auto weigh = [&](const char* kt, int n, int k0, floatx16& s, floatx16& ds) {
+            s = ds = zero16();
+#pragma unroll
+            for (int st = 0; st < Tile<DP>::kSteps; ++st) {
+                s = mfma(at.rows(kt, n, st), qf[st], s, T{});
+                ds = mfma(at.rows(kt + kTileBytes, n, st), df[st], ds, T{});
+            }
+            const int r_lo = k0 - (kl - ql + q0 + 31), r_hi = k0 + 31 - (kl - ql + q0);
+            const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
+            const float bias = place == kRight ? bias_right : bias_left;
+            if (place == kNear || !(__builtin_fabsf(bias) < kHuge)) {
+                const float* const w = biases + (k0 - p - window.first + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float t = __builtin_fmaf(s[e], a.scale, place == kNear ? w[8 * (e >> 2) + (e & 3)] : bias);
+                    s[e] = exp2_of((t - lse) * kLog2e);
+                }
+            } else {
+                const float c = a.scale * kLog2e, d = (bias - lse) * kLog2e;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = exp2_of(__builtin_fmaf(s[e], c, d));
+            }
+            if (k0 + 32 > all_see) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = k0 + row_of(e, half) < limit ? s[e] : 0.f;
+            }
+            return place;
+        };
+        if constexpr (!SHARED) {
+            // delta as the sum of P dP: o is rounded, and with a few keys what it lost is as large as the gradient's own rounding
+            for (int key0 = 0; key0 < end; key0 += kN) {
+                wave_fence();
+                if (key0 < seen) {
+                    floatx16 s, dp;
+                    weigh(tiles, 0, key0, s, dp);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) delta = __builtin_fmaf(s[e], dp[e], delta);
+                }
+                wave_fence();
+                const int next = key0 + kN < end ? key0 + kN : 0;
+                if (end > kN) {
+                    ks.fetch(kp + (int64_t)next * a.k.token, a.k.token, kl - next, a.head_dim, thread);
+                    vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, thread);
+                    ks.park(tiles, thread);
+                    vs.park(tiles + kTileBytes, thread);
+                }
+            }
+            delta += other_half(delta);
+        }
+        int turn = 0;
+        for (int key0 = 0; key0 < end; key0 += kN) {
+            if constexpr (SHARED) __syncthreads(); else wave_fence();
+            const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
+            const bool more = key0 + kN < end;
+            if (more) {
+                const int next = key0 + kN;
+                ks.fetch(kp + (int64_t)next * a.k.token, a.k.token, kl - next, a.head_dim, thread);
+                vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, thread);
+            }
+#pragma unroll
+            for (int n = 0; n < kN / 32; ++n) {
+                const int k0 = key0 + 32 * n;
+                if (k0 >= seen) continue;
+                floatx16 s, ds;
+                const int place = weigh(kt, n, k0, s, ds);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ds[e] = s[e] * (ds[e] - delta);
+                if (a.table) {
+                    if (place == kNear) {
+                        float* const w = diagonals + (k0 - p - window.first + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) __hip_atomic_fetch_add(w + 8 * (e >> 2) + (e & 3), ds[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    } else {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sum += ds[e];
+                        if (place == kRight)
+                            sum_right += sum;
+                        else
+                            sum_left += sum;
+                    }
+                }
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const u32x4 w = weights_of<T>(ds, st);
+#pragma unroll
+                    for (int d = 0; d < Tile<DP>::kBlocks; ++d) dq[d] = mfma(at.columns(kt, d, 2 * n + st), w, dq[d], T{});
+                }
+            }
+            if constexpr (SHARED) {
+                turn ^= 1;
+            } else {
+                wave_fence();
+            }
+            if (more) {
+                char* const to = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
+                ks.park(to, thread);
+                vs.park(to + kTileBytes, thread);
+            }
+        }
+    }
+    if (!SHARED && half == 0 && i < a.q_tokens) gr.delta[row] = delta;
+    if (i < a.q_tokens) store_row<T, DP>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token, dq, a.scale, a.head_dim, half);
+    if (!a.table) return;
+    // what this workgroup (wavefront) saw of every diagonal
+    const int width = window.size + 2;
+    float* const to = gr.diagonals + ((int64_t)(SHARED ? b * q_tiles + tile_id : b) * a.q_heads + h) * width;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        sum_left += __shfl_xor(sum_left, o, kWave);
+        sum_right += __shfl_xor(sum_right, o, kWave);
+    }
+    if constexpr (SHARED) {
+        __syncthreads();   // (the tiles are no longer needed)
+        float* const ends = reinterpret_cast<float*>(tiles);
+        if (lane == 0) {
+            ends[2 * wave] = sum_left;
+            ends[2 * wave + 1] = sum_right;
+        }
+        __syncthreads();
+        for (int n = threadIdx.x; n < width; n += 256) {
+            float s = 0.f;
+            if (n < window.size)
+                for (int w = 0; w < 8; ++w) s += all_diagonals[w * window_floats + n];
+            else
+                for (int w = 0; w < 4; ++w) s += ends[2 * w + (n - window.size)];
+            to[n] = s;
+        }
+    } else {
+        wave_fence();
+        const float* const own = all_diagonals + 2 * wave * window_floats;
+        for (int n = lane; n < width; n += kWave) to[n] = n < window.size ? own[n] + own[window_floats + n] : n == window.size ? sum_left : sum_right;
+    }
+}
+
+template <typename T, int DP, bool SHARED>
+__global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_tiles)
+{
+    constexpr int kQ = SHARED && DP < 128 ? 64 : 32, kThreads = SHARED ? 256 : 64, kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kQ * 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
+    const uint32_t heads = (uint32_t)a.batch * a.kv_heads;
+    int part = 0, bh, k0;
+    if constexpr (SHARED) {
+        const Item it = item_of(blockIdx.x, heads, (uint32_t)k_tiles * gr.parts);
+        bh = it.head;
+        part = it.tile % gr.parts;
+        k0 = (k_tiles - 1 - it.tile / gr.parts) * 128 + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
+    } else {
+        bh = (int)(blockIdx.x * 4 + wave);
+        k0 = 0;
+        if (bh >= (int)heads) return;
+    }
+    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int ql = a.queries(b), kl = a.keys(b);
+    const Window window(a.left, a.right);
+    const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
+    float* const biases = reinterpret_cast<float*>(lds) + (SHARED ? 0 : wave * window_floats);
+    char* const turns = lds + (SHARED ? 1 : 4) * window_floats * 4 + (SHARED ? 0 : wave * kTurnBytes);
+
+    // query tiles that see any of this workgroup's keys
+    const int first_key = SHARED ? k0 - 32 * wave : 0, shift = kl - ql;
+    int first_tile = 0;
+    if (a.causal && first_key > shift) first_tile = (first_key - shift) / kQ;
+    int each = (ql + kQ - 1) / kQ - first_tile;
+    if (each < 0 || first_key >= kl) each = 0;
+    const int64_t total = (int64_t)each * a.group;
+    const int from = (int)(total * part / gr.parts), to = (int)(total * (part + 1) / gr.parts);
+
+    Lane<DP> at;
+    at.set(lane);
+    const int j = k0 + l32;
+    u32x4 kf[Tile<DP>::kSteps], vf[Tile<DP>::kSteps];
+    load_row<T, DP>(kf, a.k.at<T>(b, hk) + (int64_t)j * a.k.token, j < kl, a.head_dim, half);
+    load_row<T, DP>(vf, a.v.at<T>(b, hk) + (int64_t)j * a.v.token, j < kl, a.head_dim, half);
+    floatx16 dk[Tile<DP>::kBlocks], dv[Tile<DP>::kBlocks];
+#pragma unroll
+    for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
+
+    if (from < to) {
+        Stage<T, DP, kQ, kThreads> qs, ds_;
+        float stat_lse = 0.f, stat_delta = 0.f;
+        auto fetch = [&](int n) {
+            const int h = hk * a.group + n / each, i0 = (first_tile + n % each) * kQ;
+            qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, a.q.token, ql - i0, a.head_dim, thread);
+            ds_.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, gr.dout.token, ql - i0, a.head_dim, thread);
+            if (thread < kQ) {
+                const bool in = i0 + thread < ql;
+                const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tokens + i0 + thread;
+                stat_lse = in ? gr.lse[row] : -ATT_INF;
+                stat_delta = in ? gr.delta[row] : 0.f;
+            }
+        };
+        auto park = [&](char* turn) {
+            qs.park(turn, thread);
+            ds_.park(turn + kTileBytes, thread);
+            if (thread < kQ) {
+                float* const st = reinterpret_cast<float*>(turn + 2 * kTileBytes);
+                const float lse = stat_lse == -ATT_INF ? ATT_INF : stat_lse;
+                st[thread] = lse;
+                st[kQ + thread] = Held<T>::kShift - lse * kLog2e;
+                st[2 * kQ + thread] = -stat_delta * Held<T>::kUnit;
+            }
+        };
+        fetch(from);
+        park(turns);
+        int turn = 0, head_filled = -1;
+        float bias_left = 0.f, bias_right = 0.f;
+        for (int n = from; n < to; ++n) {
+            const int g = n / each, h = hk * a.group + g, i0 = (first_tile + n % each) * kQ;
+            if (a.table && g != head_filled) {
+                if constexpr (SHARED) __syncthreads(); else wave_fence();   // (the head before is done with its biases)
+                bias_left = a.bias<T>(a.n_edges, h);
+                bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
+                fill_window<T>(a, biases, h, thread, kThreads);
+                head_filled = g;
+            }
+            if constexpr (SHARED) __syncthreads(); else wave_fence();
+            const char* const qt = turns + (SHARED ? turn * kTurnBytes : 0);
+            const float* const st = reinterpret_cast<const float*>(qt + 2 * kTileBytes);
+            const bool more = n + 1 < to;
+            if (more) fetch(n + 1);
+#pragma unroll
+            for (int m = 0; m < kQ / 32; ++m) {
+                const int p0 = shift + i0 + 32 * m;   // position of the block's first query
+                const int r_lo = k0 - (p0 + 31), r_hi = k0 + 31 - p0;
+                if (k0 >= kl || i0 + 32 * m >= ql || (a.causal && r_lo > 0)) continue;   // (no pair here that counts)
+                floatx16 s = zero16(), dp = zero16();
+#pragma unroll
+                for (int step = 0; step < Tile<DP>::kSteps; ++step) {
+                    s = mfma(at.rows(qt, m, step), kf[step], s, T{});
+                    dp = mfma(at.rows(qt + kTileBytes, m, step), vf[step], dp, T{});
+                }
+                const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
+                const float bias = place == kRight ? bias_right : bias_left;
+                if (place == kNear || !(__builtin_fabsf(bias) < kHuge)) {
+                    const float* const w = biases + (j - p0 - window.first - 4 * half);
+#pragma unroll
+                    for (int g4 = 0; g4 < 4; ++g4) {
+                        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * m + 8 * g4 + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float t = __builtin_fmaf(s[4 * g4 + e], a.scale, place == kNear ? w[-(8 * g4 + e)] : bias);
+                            s[4 * g4 + e] = exp2_of(__builtin_fmaf(t - lse[e], kLog2e, Held<T>::kShift));
+                        }
+                    }
+                } else {
+                    const float c = a.scale * kLog2e, d = bias * kLog2e;
+#pragma unroll
+                    for (int g4 = 0; g4 < 4; ++g4) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(st + kQ + 32 * m + 8 * g4 + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[4 * g4 + e] = exp2_of(__builtin_fmaf(s[4 * g4 + e], c, x[e] + d));
+                    }
+                }
+                if (a.causal && r_hi > 0) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = j <= p0 + row_of(e, half) ? s[e] : 0.f;
+                }
+#pragma unroll
+                for (int g4 = 0; g4 < 4; ++g4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(st + 2 * kQ + 32 * m + 8 * g4 + 4 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[4 * g4 + e] = s[4 * g4 + e] * __builtin_fmaf(dp[4 * g4 + e], Held<T>::kUnit, x[e]);
+                }
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+                    const u32x4 wp = weights_of<T>(s, step), wd = weights_of<T>(dp, step);
+#pragma unroll
+                    for (int d = 0; d < Tile<DP>::kBlocks; ++d) {
+                        dv[d] = mfma(at.columns(qt + kTileBytes, d, 2 * m + step), wp, dv[d], T{});
+                        dk[d] = mfma(at.columns(qt, d, 2 * m + step), wd, dk[d], T{});
+                    }
+                }
+            }
+            if constexpr (SHARED) {
+                turn ^= 1;
+            } else {
+                wave_fence();
+            }
+            if (more) park(turns + (SHARED ? turn * kTurnBytes : 0));
+        }
+    }
+    if (j >= a.k_tokens) return;
+    if (j >= kl)   // (what was formed for a key that is not there)
+#pragma unroll
+        for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
+    if (gr.parts > 1) {
+        float* const sum = gr.sums + (((int64_t)part * heads + bh) * a.k_tokens + j) * 2 * DP;
+        store_row32<DP>(sum, dk, half);
+        store_row32<DP>(sum + DP, dv, half);
+    } else {
+        store_row<T, DP>(gr.out0.at<T>(b, hk) + (int64_t)j * gr.out0.token, dk, a.scale, a.head_dim, half);
+        store_row<T, DP>(gr.out1.at<T>(b, hk) + (int64_t)j * gr.out1.token, dv, Held<T>::kUnit, a.head_dim, half);
+    }
+}
+
+template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_kernel(Args a, Grad gr)
+{
+    const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = item / (DP / 2);
+    const int at = 4 * (int)(item % (DP / 2)), d = at % DP;
+    if (row >= rows || d >= a.head_dim) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < gr.parts; ++n) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(gr.sums + (n * rows + row) * 2 * DP + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += x[e];
+    }
+    const int j = (int)(row % a.k_tokens), bh = (int)(row / a.k_tokens), b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const bool is_k = at < DP;
+    const Heads& out = is_k ? gr.out0 : gr.out1;
+    const float f = is_k ? a.scale : Held<T>::kUnit;
+    *reinterpret_cast<u32x2*>(out.at<T>(b, hk) + (int64_t)j * out.token + d) = u32x2{pair_of(s[0] * f, s[1] * f, T{}), pair_of(s[2] * f, s[3] * f, T{})};
+}
+
+// 64 diagonals of a head and 16 runs of workgroups.
+__global__ void __launch_bounds__(1024) diagonals_kernel(const float* __restrict__ diagonals, int parts, int heads, int width, float* __restrict__ sums)
+{
+    __shared__ float runs[16][64];
+    const int n = blockIdx.x * 64 + (threadIdx.x & 63), run = threadIdx.x >> 6, h = blockIdx.y;
+    const int each = (parts + 15) / 16, lo = run * each, hi = lo + each < parts ? lo + each : parts;
+    float s = 0.f;
+    if (n < width) {
+#pragma unroll 8
+        for (int p = lo; p < hi; ++p) s += diagonals[((int64_t)p * heads + h) * width + n];
+    }
+    runs[run][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (run == 0 && n < width) {
+#pragma unroll
+        for (int r = 1; r < 16; ++r) s += runs[r][threadIdx.x & 63];
+        sums[(int64_t)h * width + n] = s;
+    }
+}
+
+// A wavefront per bucket: its distances' diagonals on either side, and what lay beyond the window.
+template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args a, const float* __restrict__ sums, T* __restrict__ dtable)
+{
+    const Window window(a.left, a.right);
+    const int lane = threadIdx.x & 63, buckets = (a.n_edges + 1) * (a.two_sided ? 2 : 1), h = blockIdx.y;
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (n >= buckets) return;
+    const float* const of = sums + (int64_t)h * (window.size + 2);
+    const bool right = a.two_sided && n > a.n_edges;
+    const int e = right ? n - a.n_edges - 1 : n;
+    const int near = e == 0 ? 0 : a.edges[e - 1];                         // distances near .. far - 1
+    const int far = e == a.n_edges ? (1 << 30) : a.edges[e];
+    // r = lo .. hi - 1; the first bucket of a one-sided table also has every r > 0, that of the right side begins at 1
+    int lo = right ? (near > 1 ? near : 1) : 1 - far, hi = right ? far : e == 0 && !a.two_sided ? (1 << 30) : 1 - near;
+    const int last = window.first + window.size;
+    lo = lo > window.first ? lo : window.first;
+    hi = hi < last ? hi : last;
+    float s = 0.f;
+    for (int r = lo + lane; r < hi; r += kWave) s += of[r - window.first];
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) s += __shfl_xor(s, o, kWave);
+    if (lane == 0) {
+        // tiles wholly at one end
+        if (!right && e == a.n_edges) s += of[window.size];
+        if (a.two_sided ? right && e == a.n_edges : e == 0) s += of[window.size + 1];
+        dtable[(int64_t)n * a.q_heads + h] = (T)s;
+    }
+}
+
+struct Plan {
+    bool own_queries, own_keys;
+    int q_tiles, k_tiles, parts, diagonal_parts, width;
+    size_t delta, diagonals, sums, tables, total;   // bytes
+};
+constexpr int64_t kEnough = 1024;
+Plan plan_of(const pruner_attention* a)
+{
+    Plan p{};
+    p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;
+    p.own_keys = a->k_tokens <= 32 && (int64_t)a->q_tokens * (a->q_heads / a->kv_heads) <= 256;
+    p.q_tiles = (a->q_tokens + 127) / 128;
+    p.k_tiles = (a->k_tokens + 127) / 128;
+    p.parts = 1;
+    const int64_t groups = (int64_t)a->batch * a->kv_heads * p.k_tiles, tiles = (int64_t)(a->q_heads / a->kv_heads) * ((a->q_tokens + 31) / 32);
+    if (!p.own_keys && groups > 0) {
+        int64_t parts = (kEnough + groups - 1) / groups;
+        const int64_t most = tiles / 8;   // eight query tiles of 32 at least
+        parts = parts < most ? parts : most;
+        p.parts = parts < 1 ? 1 : (int)parts;
+    }
+    // (the window for the largest edge that there can be: sizes alone decide)
+    const int64_t reach = (int64_t)a->q_tokens + a->k_tokens;
+    const int most = (int)(reach < PRUNER_MAX_BIAS_DISTANCE ? reach : PRUNER_MAX_BIAS_DISTANCE);
+    const int widest = Window(most, a->flags & PRUNER_ATTENTION_TWO_SIDED ? (most > 1 ? most : 1) : 0).size + 2;
+    p.diagonal_parts = p.own_queries ? a->batch : a->batch * p.q_tiles;
+    p.delta = round_up((size_t)a->batch * a->q_heads * a->q_tokens * 4, 256);
+    p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
+    p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
+    p.sums = p.parts > 1 ? round_up((size_t)p.parts * a->batch * a->kv_heads * a->k_tokens * 2 * padded_dim(a->head_dim) * 4, 256) : 0;
+    p.total = p.delta + p.diagonals + p.tables + p.sums + 256;
+    return p;
+}
+
+struct Call {
+    Args args;
+    Grad queries, keys;
+    Plan plan;
+    float* table_sums;
+    void* dtable;
+    hipStream_t st;
+};
+template <typename T, int DP> int run(const Call& c)
+{
+    static PerDeviceFlag ready;
+    const int dev = current_device(nullptr);
+    if (dev < 0) return PRUNER_EHIP;
+    if (!ready.get(dev)) {
+        for (const void* fn : {reinterpret_cast<const void*>(&queries_kernel<T, DP, true>), reinterpret_cast<const void*>(&queries_kernel<T, DP, false>),
+                               reinterpret_cast<const void*>(&keys_kernel<T, DP, true>), reinterpret_cast<const void*>(&keys_kernel<T, DP, false>)})
+            if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+        ready.mark(dev);
+    }
+    const Args& a = c.args;
+    const Window w(a.left, a.right);
+    const size_t window = a.table ? round_up((size_t)w.size, 4) * 4 : 0;
+    const int64_t q_heads = (int64_t)a.batch * a.q_heads, k_heads = (int64_t)a.batch * a.kv_heads;
+    if (a.q_tokens > 0) {
+        if (c.plan.own_queries)
+            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 12 * window + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
+        else
+            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 9 * window + 4 * kKeys * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
+        PRUNER_LAUNCH_CHECK();
+    }
+    if (a.k_tokens > 0) {
+        if (c.plan.own_keys) {
+            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads + 3) / 4)), dim3(256), 4 * (window + 2 * 32 * DP * 2 + 3 * 32 * 4), c.st, a, c.keys, 1);
+        } else {
+            const size_t q = DP < 128 ? 64 : 32;
+            hipLaunchKernelGGL((keys_kernel<T, DP, true>), dim3((unsigned)(k_heads * c.plan.k_tiles * c.plan.parts)), dim3(256), window + 2 * (2 * q * DP * 2 + 3 * q * 4), c.st, a, c.keys,
+                               c.plan.k_tiles);
+        }
+        PRUNER_LAUNCH_CHECK();
+        if (c.plan.parts > 1) {
+            const int64_t items = k_heads * a.k_tokens * (DP / 2);
+            hipLaunchKernelGGL((keys_join_kernel<T, DP>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, c.st, a, c.keys);
+            PRUNER_LAUNCH_CHECK();
+        }
+    }
+    if (a.table) {
+        const int width = w.size + 2, buckets = (a.n_edges + 1) * (a.two_sided ? 2 : 1);
+        hipLaunchKernelGGL(diagonals_kernel, dim3((width + 63) / 64, a.q_heads), dim3(1024), 0, c.st, c.queries.diagonals, a.q_tokens > 0 ? c.plan.diagonal_parts : 0, a.q_heads, width,
+                           c.table_sums);
+        PRUNER_LAUNCH_CHECK();
+        hipLaunchKernelGGL(buckets_kernel<T>, dim3((buckets + 3) / 4, a.q_heads), dim3(256), 0, c.st, a, c.table_sums, static_cast<T*>(c.dtable));
+        PRUNER_LAUNCH_CHECK();
+    }
+    return PRUNER_OK;
+}
+
+bool grad_sizes_ok(const pruner_attention* a)
+{
+    if (!attention_sizes_ok(a)) return false;
+    const int64_t heads = (int64_t)a->batch * a->kv_heads;
+    return heads * (a->k_tokens / 64 + 1) < (1 << 24) && a->q_heads <= 65535;
+}
+
+}  // namespace
+}  // namespace att
+}  // namespace pruner
+
+using namespace pruner;
+
+extern "C" size_t pruner_rel_attention_grad_workspace_bytes(const pruner_attention* a) { return att::grad_sizes_ok(a) ? att::plan_of(a).total : 0; }
+
+extern "C" int pruner_rel_attention_grad(const pruner_attention* a, const pruner_heads* dout, const pruner_heads* q, const pruner_heads* k, const pruner_heads* v,
+                                         const pruner_heads* o, const float* lse, const pruner_heads* dq, const pruner_heads* dk, const pruner_heads* dv, void* dtable,
+                                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!att::grad_sizes_ok(a)) return PRUNER_EINVAL;
+    if ((a->table != nullptr) != (dtable != nullptr) || (dtable && !aligned(dtable, 2))) return PRUNER_EINVAL;
+    const pruner_heads none{nullptr, 0, 0, 0};
+    const bool queries = a->batch > 0 && a->q_tokens > 0, keys = a->batch > 0 && a->k_tokens > 0;
+    if (!queries) q = dout = o = dq = &none;
+    if (!keys) k = v = dk = dv = &none;
+    att::Call c{};
+    const int rc = att::attention_args(a, q, k, v, &c.args);
+    if (rc) return rc;
+    if (queries && (!att::heads_ok(dout) || !att::heads_ok(o) || !att::heads_ok(dq) || !lse || !aligned(lse, 4))) return PRUNER_EINVAL;
+    if (keys && (!att::heads_ok(dk) || !att::heads_ok(dv))) return PRUNER_EINVAL;
+    c.plan = att::plan_of(a);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < c.plan.total) return PRUNER_EWORKSPACE;
+    char* const ws = static_cast<char*>(workspace);
+    att::Grad g{};
+    g.dout = att::heads_of(dout);
+    g.o = att::heads_of(o);
+    g.lse = lse;
+    g.delta = reinterpret_cast<float*>(ws);
+    g.diagonals = reinterpret_cast<float*>(ws + c.plan.delta);
+    c.table_sums = reinterpret_cast<float*>(ws + c.plan.delta + c.plan.diagonals);
+    g.sums = reinterpret_cast<float*>(ws + c.plan.delta + c.plan.diagonals + c.plan.tables);
+    g.parts = c.plan.parts;
+    c.queries = c.keys = g;
+    c.queries.out0 = att::heads_of(dq);
+    c.keys.out0 = att::heads_of(dk);
+    c.keys.out1 = att::heads_of(dv);
+    c.dtable = dtable;
+    c.st = static_cast<hipStream_t>(stream);
+    if (a->batch == 0) {   // (no pair: a table's gradient is zero)
+        c.args.batch = 0;
+        c.args.q_tokens = c.args.k_tokens = 0;
+    }
+    const int dp = att::padded_dim(a->head_dim);
+    if (a->dtype == PRUNER_BF16) return dp == 32 ? att::run<__bf16, 32>(c) : dp == 64 ? att::run<__bf16, 64>(c) : att::run<__bf16, 128>(c);
+    return dp == 32 ? att::run<_Float16, 32>(c) : dp == 64 ? att::run<_Float16, 64>(c) : att::run<_Float16, 128>(c);
+}
