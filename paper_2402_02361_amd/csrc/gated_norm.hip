@@ -391,7 +391,7 @@ extern "C" int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int6
                                       size_t workspace_bytes, void* stream)
 {
     if (!norm_ok(p) || (f && kept_f)) return PRUNER_EINVAL;
-    const bool has_f = f || kept_f;
+    const bool has_f = f || kept_f || (p->rows == 0 && dw_post);   // (a matrix without rows may have no address: its sums are zero)
     if (!vector_ok(dw_pre) || !vector_ok(p->w_pre) || (has_f && (!vector_ok(dw_post) || !vector_ok(p->w_post)))) return PRUNER_EINVAL;
     const size_t bytes = type_bytes(p->dtype);
     const bool gate_rows = has_f && p->gate && p->gate_pitch, gate_vector = has_f && p->gate && !p->gate_pitch;
