@@ -423,9 +423,35 @@ _BF16, _F16, _F32 = 0, 1, 2
 _ATTENTION_CAUSAL, _ATTENTION_TWO_SIDED = 1, 2
 
 
+_dtypes, _raw_stream = {}, None
+
+
 def _dtype(t):
-    import torch
-    return {torch.bfloat16: _BF16, torch.float16: _F16, torch.float32: _F32}.get(t, -1)
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.bfloat16: _BF16, torch.float16: _F16, torch.float32: _F32})
+    return _dtypes.get(t, -1)
+
+
+def _stream_on(stream, t):
+    """The given stream, or the current one of t's device (a call of a few microseconds notices the 2.7 that torch.cuda.current_stream takes)."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(t.get_device())
+
+
+def _scratch(workspace, need, device):
+    """(pointer, bytes) of the given workspace, or of a new one that is held until the call has been made; none where none is needed."""
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def _rows_of(t, what):
@@ -454,7 +480,7 @@ def checkpoint_pack(x, kept=None, stream=None):
     rows, dim = x.shape
     if kept is None:
         kept = _new_checkpoint(rows, dim, x.device)
-    rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, C.byref(_c_checkpoint(kept, rows, dim)), _stream(stream))
+    rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, C.byref(_c_checkpoint(kept, rows, dim)), _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_pack")
     return kept
@@ -469,7 +495,7 @@ def checkpoint_restore(kept, dtype=None, x=None, stream=None):
         x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
     assert x.shape == (rows, dim), "x"
     p, pitch = _rows_of(x, "x")
-    rc = lib.pruner_checkpoint_restore(C.byref(_c_checkpoint(kept, rows, dim)), _dtype(x.dtype), rows, dim, p, pitch, _stream(stream))
+    rc = lib.pruner_checkpoint_restore(C.byref(_c_checkpoint(kept, rows, dim)), _dtype(x.dtype), rows, dim, p, pitch, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_restore")
     return x
@@ -487,9 +513,9 @@ def checkpoint_wgrad(dy, kept, dw=None, accumulate=False, workspace=None, stream
         assert not accumulate, "accumulate needs dw"
         dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
     assert dw.is_cuda and dw.dtype == torch.float32 and dw.is_contiguous() and dw.shape == (n_out, dim), "dw"
-    ws = _workspace(workspace, int(lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim)), dy.device)
-    rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, C.byref(_c_checkpoint(kept, rows, dim)), rows, n_out, dim, _ptr(dw), int(accumulate), _ptr(ws), ws.numel(),
-                                     _stream(stream))
+    held, ws, size = _scratch(workspace, lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim), dy.device)
+    rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, C.byref(_c_checkpoint(kept, rows, dim)), rows, n_out, dim, dw.data_ptr(), int(accumulate), ws, size,
+                                     _stream_on(stream, dy))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_wgrad")
     return dw
@@ -525,11 +551,11 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
     if f is not None:
         assert f.dtype == x.dtype and f.shape == x.shape, "f"
         pf, f_pitch = _rows_of(f, "f")
-    h = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-    y = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if w_pre is not None else None
+    h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    y = torch.empty_like(h) if w_pre is not None else None
     kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
-    rc = lib.pruner_gated_norm(C.byref(p), px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), C.byref(_c_checkpoint(kept, rows, dim)) if checkpoint else None, _stream(stream))
+    rc = lib.pruner_gated_norm(C.byref(p), px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), C.byref(_c_checkpoint(kept, rows, dim)) if checkpoint else None, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_gated_norm")
     return h, y, kept
@@ -549,17 +575,17 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
     pdh, dh_pitch = _rows_of(dh, "dh") if dh is not None else (None, 0)
     pf, f_pitch = _rows_of(f, "f") if f is not None and kept is None else (None, 0)
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
-    dx = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
     df = dgate = dw_post = None
     if f is not None:
-        df = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-        dw_post = torch.empty(dim, dtype=torch.float32, device=x.device)
+        df = torch.empty_like(dx)
+        dw_post = torch.empty_like(w_post)
         if gate is not None:
-            dgate = torch.empty(gate.shape, dtype=gate.dtype, device=x.device)
-    dw_pre = torch.empty(dim, dtype=torch.float32, device=x.device)
-    ws = _workspace(workspace, int(lib.pruner_gated_norm_grad_workspace_bytes(rows, dim)), x.device)
+            dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
+    dw_pre = torch.empty_like(w_pre)
+    held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device)
     rc = lib.pruner_gated_norm_grad(C.byref(p), pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, C.byref(_c_checkpoint(kept, rows, dim)) if kept is not None else None,
-                                    _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), _ptr(ws), ws.numel(), _stream(stream))
+                                    _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), ws, size, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_gated_norm_grad")
     return dx, df, dgate, dw_post, dw_pre
@@ -599,14 +625,15 @@ def _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale):
     flags = _ATTENTION_CAUSAL if causal else 0
     n_edges = 0
     if table is not None:
-        edges = np.ascontiguousarray(edges if edges is not None else (), dtype=np.int32)
+        if not (isinstance(edges, np.ndarray) and edges.dtype == np.int32 and edges.flags.c_contiguous):
+            edges = np.ascontiguousarray(edges if edges is not None else (), dtype=np.int32)
         n_edges = len(edges)
         assert table.is_cuda and table.dtype == q.dtype and table.is_contiguous() and table.dim() == 2 and table.shape[1] == q_heads, "table"
         assert table.shape[0] in (n_edges + 1, 2 * (n_edges + 1)), "table: n_edges + 1 buckets, or twice as many"
         flags |= _ATTENTION_TWO_SIDED if table.shape[0] == 2 * (n_edges + 1) else 0
     a = CAttention(_dtype(q.dtype), batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, flags, 1.0 / math.sqrt(head_dim) if scale is None else scale,
                    _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"), table.data_ptr() if table is not None else None,
-                   edges.ctypes.data if n_edges else None, n_edges)
+                   edges.__array_interface__["data"][0] if n_edges else None, n_edges)
     a.keep = edges   # (the host array lives as long as the struct)
     return a
 
@@ -621,11 +648,11 @@ def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causa
     lib = load_library()
     a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
     assert o.shape == q.shape and o.dtype == q.dtype, "o"
     lse = torch.empty((a.batch, a.q_heads, a.q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
-    ws = _workspace(workspace, int(lib.pruner_rel_attention_workspace_bytes(C.byref(a))), q.device)
-    rc = lib.pruner_rel_attention(C.byref(a), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream))
+    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_workspace_bytes(a), q.device)
+    rc = lib.pruner_rel_attention(a, _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
     if rc:
         raise PrunerError(rc, "pruner_rel_attention")
     return (o, lse) if want_lse else o
@@ -639,12 +666,12 @@ def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, 
     a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
     assert do.shape == q.shape and do.dtype == q.dtype and o.shape == q.shape and o.dtype == q.dtype, "do, o"
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (a.batch, a.q_heads, a.q_tokens), "lse"
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    dk, dv = torch.empty(k.shape, dtype=q.dtype, device=q.device), torch.empty(v.shape, dtype=q.dtype, device=q.device)
-    dtable = torch.empty(table.shape, dtype=q.dtype, device=q.device) if table is not None else None
-    ws = _workspace(workspace, int(lib.pruner_rel_attention_grad_workspace_bytes(C.byref(a))), q.device)
-    rc = lib.pruner_rel_attention_grad(C.byref(a), _heads(do, "do"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _heads(dq, "dq"),
-                                       _heads(dk, "dk"), _heads(dv, "dv"), _ptr(dtable), _ptr(ws), ws.numel(), _stream(stream))
+    dense = torch.contiguous_format
+    dq, dk, dv = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense), torch.empty_like(v, memory_format=dense)
+    dtable = torch.empty_like(table) if table is not None else None
+    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_grad_workspace_bytes(a), q.device)
+    rc = lib.pruner_rel_attention_grad(a, _heads(do, "do"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _heads(dq, "dq"),
+                                       _heads(dk, "dk"), _heads(dv, "dv"), _ptr(dtable), ws, size, _stream_on(stream, q))
     if rc:
         raise PrunerError(rc, "pruner_rel_attention_grad")
     return dq, dk, dv, dtable

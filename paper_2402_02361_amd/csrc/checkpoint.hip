@@ -334,7 +334,7 @@ extern "C" size_t pruner_checkpoint_wgrad_workspace_bytes(int64_t rows, int32_t 
 {
     if (!wgrad_sizes_ok(rows, n_out, dim)) return 0;
     const WgradPlan p = wgrad_plan(rows, n_out, dim);
-    return p.parts > 1 ? round_up((size_t)p.parts * (size_t)n_out * (size_t)dim * 4, 256) : 256;
+    return p.parts > 1 ? round_up((size_t)p.parts * (size_t)n_out * (size_t)dim * 4, 256) : 0;
 }
 
 extern "C" int pruner_checkpoint_wgrad(const void* dy, int32_t dtype, int64_t dy_pitch, const pruner_checkpoint* kept, int64_t rows, int32_t n_out, int32_t dim, float* dw,

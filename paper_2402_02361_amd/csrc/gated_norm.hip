@@ -382,7 +382,7 @@ extern "C" int pruner_gated_norm(const pruner_norm* p, const void* x, int64_t x_
 
 extern "C" size_t pruner_gated_norm_grad_workspace_bytes(int64_t rows, int32_t dim)
 {
-    if (rows <= 0 || dim < 1 || dim > PRUNER_MAX_NORM_DIM) return 256;
+    if (rows <= 0 || dim < 1 || dim > PRUNER_MAX_NORM_DIM) return 0;
     return round_up((size_t)shape_of(rows, dim, kMaxParts).blocks * 3 * (size_t)dim * 4, 256);
 }
 

@@ -426,7 +426,7 @@ Plan plan_of(const pruner_attention* a)
         p.parts = (int)((a->k_tokens + (int64_t)p.part_keys - 1) / p.part_keys);
         if (p.parts < 1) p.parts = 1;
     }
-    p.workspace = p.parts > 1 ? round_up((size_t)p.parts * p.rows * 8, 256) + round_up((size_t)p.parts * p.rows * padded_dim(a->head_dim) * 4, 256) : 256;
+    p.workspace = p.parts > 1 ? round_up((size_t)p.parts * p.rows * 8, 256) + round_up((size_t)p.parts * p.rows * padded_dim(a->head_dim) * 4, 256) : 0;
     return p;
 }
 

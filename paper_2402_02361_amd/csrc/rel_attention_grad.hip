@@ -3,8 +3,7 @@
 //
 //   queries_kernel   a wavefront owns 32 queries, as in the forward pass: S^T and dP^T leave a query's values in its two lanes; dQ^T += K^T dS^T.
 //                    It also leaves delta for the next kernel, and the sums of dS along the diagonals j - p: a tile beyond the largest edge
-//                    adds into one register, the others add into LDS, where a wavefront's half has diagonals of its own (no two lanes of
-//                    one instruction meet, and a wavefront's instructions run in order: the sums do not depend on timing).
+//                    adds into one register, the others add into LDS, where every wavefront has diagonals of its own.
 //   keys_kernel      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
 //                    through the query tiles of all heads that share the key head.  Where key tiles are too few for the device, their query
 //                    tiles are cut into parts, whose sums go to the workspace (keys_join_kernel adds them in order).
@@ -16,7 +15,6 @@ namespace pruner {
 namespace att {
 namespace {
 
-constexpr int kKeys = 64;
 constexpr int kOwn = 32;   // rows of a wavefront's own tile
 
 // Weights before the second product are at most 1: in binary16, which has fewer bits below 2^-14, they are held times 2^15.
@@ -37,10 +35,35 @@ struct Grad {
     int parts;
 };
 
+// Sums of a 32 x 32 result along its diagonals, sixteen rows at a time: element (row, column) goes to place row of line row - column + 31, so a
+// line is a diagonal; lane d adds line d's sixteen places (those that no element reaches stay zero) and adds that to its diagonal's sum.  Lines are 18
+// floats apart: 32 columns' writes meet two to a bank, the lanes' 8-byte reads none.  (Adding element by element into the sums, by LDS additions,
+// took 157 us where this takes SKEWED us: 16 sequences of up to 500 tokens, 12 heads of 64, edges up to 128.)
+constexpr int kLine = 18, kLines = 47, kSkewFloats = kLines * kLine + 2;
+__device__ __forceinline__ void add_diagonals(float* skew, float* sums, const floatx16& x, int lane, int half, int l32)
+{
+    float* const to = skew + (4 * half - l32 + 31) * kLine + 4 * half;
+    const float* const from = skew + (lane < kLines ? lane : 0) * kLine;
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[(8 * (e >> 2) + (e & 3)) * (kLine + 1)] = x[8 * hb + e];
+        wave_fence();
+        float s = 0.f;
+#pragma unroll
+        for (int t = 0; t < 16; t += 2) {
+            const f32x2 v = *reinterpret_cast<const f32x2*>(from + t);
+            s += v[0] + v[1];
+        }
+        if (lane < kLines) sums[16 * hb + lane] += s;
+        wave_fence();
+    }
+}
+
 template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_tiles)
 {
-    constexpr int kN = SHARED ? kKeys : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;
+    constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;   // (128: registers for 32 rows on their way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
@@ -59,11 +82,13 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     const int ql = a.queries(b), kl = a.keys(b);
     const Window window(a.left, a.right);
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
-    // LDS: biases, diagonals of every wavefront's halves, tiles
-    float* const biases = reinterpret_cast<float*>(lds) + (SHARED ? 0 : wave * window_floats);
-    float* const all_diagonals = reinterpret_cast<float*>(lds) + (SHARED ? 1 : 4) * window_floats;
-    float* const diagonals = all_diagonals + (2 * wave + half) * window_floats;
-    char* const tiles = reinterpret_cast<char*>(all_diagonals + 8 * window_floats) + (SHARED ? 0 : wave * 2 * kTileBytes);
+    // LDS: tiles, biases, every wavefront's diagonals and its skewed square
+    char* const tiles = lds + (SHARED ? 0 : wave * 2 * kTileBytes);
+    float* const floats = reinterpret_cast<float*>(lds + (SHARED ? 4 : 8) * kTileBytes);
+    float* const biases = floats + (SHARED ? 0 : wave * window_floats);
+    float* const all_diagonals = floats + (SHARED ? 1 : 4) * window_floats;
+    float* const diagonals = all_diagonals + wave * window_floats;
+    float* const skew = all_diagonals + 4 * window_floats + wave * kSkewFloats;
 
     const int first_q = SHARED ? q0 - 32 * wave : 0, rows_here = SHARED ? 128 : 32;
     const int last_q = first_q + rows_here < ql ? first_q + rows_here - 1 : ql - 1;
@@ -101,8 +126,10 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
 #pragma unroll
     for (int d = 0; d < Tile<DP>::kBlocks; ++d) dq[d] = zero16();
     float sum_left = 0.f, sum_right = 0.f;
-    if (a.table)
-        for (int n = l32; n < window_floats; n += 32) diagonals[n] = 0.f;
+    if (a.table) {
+        for (int n = lane; n < window_floats; n += kWave) diagonals[n] = 0.f;
+        for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
+    }
     if (end > 0) {
         const T* const kp = a.k.at<T>(b, hk);
         const T* const vp = a.v.at<T>(b, hk);
@@ -190,9 +217,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 for (int e = 0; e < 16; ++e) ds[e] = s[e] * (ds[e] - delta);
                 if (a.table) {
                     if (place == kNear) {
-                        float* const w = diagonals + (k0 - p - window.first + 4 * half);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) __hip_atomic_fetch_add(w + 8 * (e >> 2) + (e & 3), ds[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        add_diagonals(skew, diagonals + (k0 - (kl - ql + q0) - 31 - window.first), ds, lane, half, l32);
                     } else {
                         float sum = 0.f;
 #pragma unroll
@@ -244,15 +269,14 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         for (int n = threadIdx.x; n < width; n += 256) {
             float s = 0.f;
             if (n < window.size)
-                for (int w = 0; w < 8; ++w) s += all_diagonals[w * window_floats + n];
+                for (int w = 0; w < 4; ++w) s += all_diagonals[w * window_floats + n];
             else
                 for (int w = 0; w < 4; ++w) s += ends[2 * w + (n - window.size)];
             to[n] = s;
         }
     } else {
         wave_fence();
-        const float* const own = all_diagonals + 2 * wave * window_floats;
-        for (int n = lane; n < width; n += kWave) to[n] = n < window.size ? own[n] + own[window_floats + n] : n == window.size ? sum_left : sum_right;
+        for (int n = lane; n < width; n += kWave) to[n] = n < window.size ? diagonals[n] : n == window.size ? sum_left : sum_right;
     }
 }
 
@@ -516,7 +540,7 @@ Plan plan_of(const pruner_attention* a)
     p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
     p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
     p.sums = p.parts > 1 ? round_up((size_t)p.parts * a->batch * a->kv_heads * a->k_tokens * 2 * padded_dim(a->head_dim) * 4, 256) : 0;
-    p.total = p.delta + p.diagonals + p.tables + p.sums + 256;
+    p.total = p.delta + p.diagonals + p.tables + p.sums;
     return p;
 }
 
@@ -541,13 +565,13 @@ template <typename T, int DP> int run(const Call& c)
     }
     const Args& a = c.args;
     const Window w(a.left, a.right);
-    const size_t window = a.table ? round_up((size_t)w.size, 4) * 4 : 0;
+    const size_t window = a.table ? round_up((size_t)w.size, 4) * 4 : 0, skew = a.table ? kSkewFloats * 4 : 0;
     const int64_t q_heads = (int64_t)a.batch * a.q_heads, k_heads = (int64_t)a.batch * a.kv_heads;
     if (a.q_tokens > 0) {
         if (c.plan.own_queries)
-            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 12 * window + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
+            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + 4 * skew + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
         else
-            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 9 * window + 4 * kKeys * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
+            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 5 * window + 4 * skew + 4 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
         PRUNER_LAUNCH_CHECK();
     }
     if (a.k_tokens > 0) {
@@ -607,7 +631,7 @@ extern "C" int pruner_rel_attention_grad(const pruner_attention* a, const pruner
     if (queries && (!att::heads_ok(dout) || !att::heads_ok(o) || !att::heads_ok(dq) || !lse || !aligned(lse, 4))) return PRUNER_EINVAL;
     if (keys && (!att::heads_ok(dk) || !att::heads_ok(dv))) return PRUNER_EINVAL;
     c.plan = att::plan_of(a);
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < c.plan.total) return PRUNER_EWORKSPACE;
+    if (c.plan.total > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < c.plan.total)) return PRUNER_EWORKSPACE;
     char* const ws = static_cast<char*>(workspace);
     att::Grad g{};
     g.dout = att::heads_of(dout);
