@@ -121,49 +121,57 @@ template <int DP> struct Tile {
     __device__ __forceinline__ static int at(int row, int chunk) { return row * kRowBytes + ((chunk ^ turn_of(row)) << 4); }
 };
 
-// The places of a lane's fragments in a tile.
+// The places of a lane's fragments in a tile.  A step or a block further is one bit pattern further in the chunk's number, so all of them come from three
+// places by an exclusive or.
 template <int DP> struct Lane {
-    int row[Tile<DP>::kSteps];          // rows as the outer index: row l32, depths 16 s + 8 half ..
-    int turned[Tile<DP>::kBlocks][2];   // columns as the outer index: columns 32 b + l32, rows 8 q + 4 half .. + 3 of a 16-row step
+    int row;         // rows as the outer index: row l32, depths 16 s + 8 half .. at row ^ (s << 5)
+    int turned[2];   // columns as the outer index: columns 32 b + l32, rows 8 q + 4 half .. + 3 of a 16-row step at turned[q] ^ (b << 6)
     __device__ __forceinline__ void set(int lane)
     {
         const int l32 = lane & 31, half = lane >> 5, t = lane & 15, g = (lane >> 4) & 1;
+        row = Tile<DP>::at(l32, half);
 #pragma unroll
-        for (int s = 0; s < Tile<DP>::kSteps; ++s) row[s] = Tile<DP>::at(l32, 2 * s + half);
-#pragma unroll
-        for (int b = 0; b < Tile<DP>::kBlocks; ++b)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) turned[b][q] = Tile<DP>::at(8 * q + 4 * half + (t >> 2), 4 * b + 2 * g + ((t >> 1) & 1)) + 8 * (t & 1);
+        for (int q = 0; q < 2; ++q) turned[q] = Tile<DP>::at(8 * q + 4 * half + (t >> 2), 2 * g + ((t >> 1) & 1)) + 8 * (t & 1);
     }
+    // Inside a loop whose registers are all taken: the places are formed again from the three, not kept.
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(row), "+v"(turned[0]), "+v"(turned[1])); }
     __device__ __forceinline__ u32x4 rows(const char* tile, int block, int s) const
     {
-        return *reinterpret_cast<const u32x4*>(tile + row[s] + block * 32 * Tile<DP>::kRowBytes);
+        return *reinterpret_cast<const u32x4*>(tile + (row ^ (s << 5)) + block * 32 * Tile<DP>::kRowBytes);
     }
     __device__ __forceinline__ u32x4 columns(const char* tile, int b, int step) const
     {
         typedef __attribute__((address_space(3))) i16x4* lds_ptr;
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + turned[b][0] + step * 16 * Tile<DP>::kRowBytes));
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + turned[b][1] + step * 16 * Tile<DP>::kRowBytes));
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (turned[0] ^ (b << 6)) + step * 16 * Tile<DP>::kRowBytes));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (turned[1] ^ (b << 6)) + step * 16 * Tile<DP>::kRowBytes));
         const u32x2 a = __builtin_bit_cast(u32x2, lo), c = __builtin_bit_cast(u32x2, hi);
         return u32x4{a[0], a[1], c[0], c[1]};
     }
 };
 
-// ROWS rows on their way from memory to a tile, by THREADS threads.
+// ROWS rows on their way from memory to a tile, by THREADS threads.  Reads are bounds-checked buffer loads: rows at or beyond `rows` and columns at or beyond
+// the head dimension arrive as zeros.  (Where tokens lie closer than a head is wide, rows overlap and a row that is not there may arrive as one that
+// is; nothing depends on it, its pairs are masked.)
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
-    static constexpr int kEach = ROWS * Tile<DP>::kChunks / THREADS;
-    static_assert(kEach >= 1 && ROWS * Tile<DP>::kChunks % THREADS == 0, "whole chunks per thread");
+    static constexpr int kEach = ROWS * Tile<DP>::kChunks / THREADS, kRowStep = THREADS / Tile<DP>::kChunks;
+    static_assert(kEach >= 1 && ROWS * Tile<DP>::kChunks % THREADS == 0 && THREADS % Tile<DP>::kChunks == 0, "whole chunks per thread, of one column");
     u32x4 w[kEach];
-    __device__ __forceinline__ void fetch(const T* base, int32_t token, int rows, int head_dim, int thread)
+    uint32_t at;
+    int32_t row_bytes, width;
+    __device__ __forceinline__ void set(int32_t token, int head_dim, int thread)
     {
+        row_bytes = token * 2;
+        width = head_dim * 2;
+        const int chunk = thread % Tile<DP>::kChunks;
+        at = 16 * chunk < width ? (uint32_t)(thread / Tile<DP>::kChunks) * (uint32_t)row_bytes + 16u * (uint32_t)chunk : 0x80000000u;
+    }
+    __device__ __forceinline__ void fetch(const T* base, int rows)   // base and rows: the same in all lanes
+    {
+        rows = rows < ROWS ? rows : ROWS;
+        const int bytes = rows > 0 ? (rows - 1) * row_bytes + width : 0;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00027000);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            const int id = thread + THREADS * u, row = id / Tile<DP>::kChunks, chunk = id % Tile<DP>::kChunks;
-            const bool in = row < rows && 8 * chunk < head_dim;
-            const uint32_t off = in ? (uint32_t)row * (uint32_t)token + 8u * (uint32_t)chunk : 0u;
-            w[u] = u32x4{0u, 0u, 0u, 0u};
-            if (in) w[u] = *reinterpret_cast<const u32x4*>(base + off);
-        }
+        for (int u = 0; u < kEach; ++u) w[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, u * kRowStep * row_bytes, 0));
     }
     __device__ __forceinline__ void park(char* tile, int thread) const
     {

@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
 {
     constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
     int part = 0, bh, q0;
     if constexpr (SHARED) {
@@ -159,8 +159,10 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         const T* const kp = a.k.at<T>(b, hk);
         const T* const vp = a.v.at<T>(b, hk);
         Stage<T, DP, kN, kThreads> ks, vs;
-        ks.fetch(kp + (int64_t)begin * a.k.token, a.k.token, kl - begin, a.head_dim, thread);
-        vs.fetch(vp + (int64_t)begin * a.v.token, a.v.token, kl - begin, a.head_dim, thread);
+        ks.set(a.k.token, a.head_dim, thread);
+        vs.set(a.v.token, a.head_dim, thread);
+        ks.fetch(kp + (int64_t)begin * a.k.token, kl - begin);
+        vs.fetch(vp + (int64_t)begin * a.v.token, kl - begin);
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
@@ -180,8 +182,8 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
             const bool more = key0 + kN < end;
             if (more) {
                 const int next = key0 + kN;
-                ks.fetch(kp + (int64_t)next * a.k.token, a.k.token, kl - next, a.head_dim, thread);
-                vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, thread);
+                ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
+                vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
             }
             if (key0 < seen) {
                 floatx16 s[kN / 32];
@@ -249,7 +251,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
 {
     constexpr int kTileBytes = kOwnKeys * Tile<DP>::kRowBytes, kStride = DP + 4;   // (sums: rows of DP + 4 floats, so that neighbouring rows lie in other banks)
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int columns = a.q_tokens * a.group;
     const int part = blockIdx.x % parts.count, bh = blockIdx.x / parts.count, b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int ql = a.queries(b), kl = a.keys(b);
@@ -277,10 +279,11 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
         const T* const kp = a.k.at<T>(b, hk);
         const T* const vp = a.v.at<T>(b, hk);
         Stage<T, DP, kOwnKeys, 64> vs;
+        vs.set(a.v.token, a.head_dim, lane);
         int key0 = begin + kOwnKeys * wave;
         if (key0 < end) {
             load_row<T, DP>(kf, kp + (int64_t)(key0 + l32) * a.k.token, key0 + l32 < kl, a.head_dim, half);
-            vs.fetch(vp + (int64_t)key0 * a.v.token, a.v.token, kl - key0, a.head_dim, lane);
+            vs.fetch(vp + (int64_t)key0 * a.v.token, kl - key0);
         }
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
@@ -300,7 +303,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
             const int next = key0 + 4 * kOwnKeys;
             if (next < end) load_row<T, DP>(kf, kp + (int64_t)(next + l32) * a.k.token, next + l32 < kl, a.head_dim, half);
             vs.park(tile, lane);
-            if (next < end) vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, lane);
+            if (next < end) vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
             const int r_lo = key0 - (kl - ql + a.q_tokens - 1), r_hi = key0 + kOwnKeys - 1 - (kl - ql);
             const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
             const float bias = place == kRight ? bias_right : bias_left;

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
 {
     constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;   // (128: registers for 32 rows on their way)
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
     int bh, q0, tile_id = 0;
     if constexpr (SHARED) {
@@ -134,8 +134,10 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         const T* const kp = a.k.at<T>(b, hk);
         const T* const vp = a.v.at<T>(b, hk);
         Stage<T, DP, kN, kThreads> ks, vs;
-        ks.fetch(kp, a.k.token, kl, a.head_dim, thread);
-        vs.fetch(vp, a.v.token, kl, a.head_dim, thread);
+        ks.set(a.k.token, a.head_dim, thread);
+        vs.set(a.v.token, a.head_dim, thread);
+        ks.fetch(kp, kl);
+        vs.fetch(vp, kl);
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
@@ -189,8 +191,8 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 wave_fence();
                 const int next = key0 + kN < end ? key0 + kN : 0;
                 if (end > kN) {
-                    ks.fetch(kp + (int64_t)next * a.k.token, a.k.token, kl - next, a.head_dim, thread);
-                    vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, thread);
+                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
+                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
                     ks.park(tiles, thread);
                     vs.park(tiles + kTileBytes, thread);
                 }
@@ -204,8 +206,8 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
             const bool more = key0 + kN < end;
             if (more) {
                 const int next = key0 + kN;
-                ks.fetch(kp + (int64_t)next * a.k.token, a.k.token, kl - next, a.head_dim, thread);
-                vs.fetch(vp + (int64_t)next * a.v.token, a.v.token, kl - next, a.head_dim, thread);
+                ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
+                vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
             }
 #pragma unroll
             for (int n = 0; n < kN / 32; ++n) {
@@ -280,19 +282,32 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     }
 }
 
+// A wavefront's keys and values as operands: in registers, or, where these are needed for other things (KEPT of K, V: 0, 1 or 2 in LDS), each lane's own
+// sixteen bytes of every step side by side in LDS.
+template <typename T, int DP, bool SHARED> struct KeysShape {
+    static constexpr bool kWide = SHARED && DP == 128;
+    static constexpr int kWaves = kWide ? 8 : 4;              // of a workgroup
+    static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
+    static constexpr int kTurns = SHARED ? 2 : 1;
+    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kQ * 4;
+    static constexpr int kHeldBytes = kWide ? Tile<DP>::kSteps * 1024 : 0;   // of a wavefront
+    static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
+};
 template <typename T, int DP, bool SHARED>
-__global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_tiles)
+__global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) keys_kernel(Args a, Grad gr, int k_tiles)
 {
-    constexpr int kQ = SHARED && DP < 128 ? 64 : 32, kThreads = SHARED ? 256 : 64, kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kQ * 4;
+    typedef KeysShape<T, DP, SHARED> Shape;
+    constexpr int kQ = Shape::kQ, kThreads = SHARED ? 64 * Shape::kWaves : 64, kTileBytes = Shape::kTileBytes, kTurnBytes = Shape::kTurnBytes;
+    constexpr bool kWide = Shape::kWide;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.kv_heads;
     int part = 0, bh, k0;
     if constexpr (SHARED) {
         const Item it = item_of(blockIdx.x, heads, (uint32_t)k_tiles * gr.parts);
         bh = it.head;
         part = it.tile % gr.parts;
-        k0 = (k_tiles - 1 - it.tile / gr.parts) * 128 + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
+        k0 = (k_tiles - 1 - it.tile / gr.parts) * Shape::kKeys + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
     } else {
         bh = (int)(blockIdx.x * 4 + wave);
         k0 = 0;
@@ -302,8 +317,9 @@ __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_til
     const int ql = a.queries(b), kl = a.keys(b);
     const Window window(a.left, a.right);
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
-    float* const biases = reinterpret_cast<float*>(lds) + (SHARED ? 0 : wave * window_floats);
-    char* const turns = lds + (SHARED ? 1 : 4) * window_floats * 4 + (SHARED ? 0 : wave * kTurnBytes);
+    char* const turns = lds + (SHARED ? 0 : wave * kTurnBytes);
+    char* const held = lds + 2 * kTurnBytes + wave * Shape::kHeldBytes + 16 * lane;
+    float* const biases = reinterpret_cast<float*>(lds + (SHARED ? Shape::kTurns * kTurnBytes + Shape::kWaves * Shape::kHeldBytes : 4 * kTurnBytes)) + (SHARED ? 0 : wave * window_floats);
 
     // query tiles that see any of this workgroup's keys
     const int first_key = SHARED ? k0 - 32 * wave : 0, shift = kl - ql;
@@ -320,17 +336,29 @@ __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_til
     u32x4 kf[Tile<DP>::kSteps], vf[Tile<DP>::kSteps];
     load_row<T, DP>(kf, a.k.at<T>(b, hk) + (int64_t)j * a.k.token, j < kl, a.head_dim, half);
     load_row<T, DP>(vf, a.v.at<T>(b, hk) + (int64_t)j * a.v.token, j < kl, a.head_dim, half);
+    if constexpr (kWide) {
+#pragma unroll
+        for (int st = 0; st < Tile<DP>::kSteps; ++st) *reinterpret_cast<u32x4*>(held + 1024 * st) = vf[st];
+    }
+    auto value = [&](int st) -> u32x4 {
+        if constexpr (kWide)
+            return *reinterpret_cast<const u32x4*>(held + 1024 * st);
+        else
+            return vf[st];
+    };
     floatx16 dk[Tile<DP>::kBlocks], dv[Tile<DP>::kBlocks];
 #pragma unroll
     for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
 
     if (from < to) {
         Stage<T, DP, kQ, kThreads> qs, ds_;
+        qs.set(a.q.token, a.head_dim, thread);
+        ds_.set(gr.dout.token, a.head_dim, thread);
         float stat_lse = 0.f, stat_delta = 0.f;
         auto fetch = [&](int n) {
             const int h = hk * a.group + n / each, i0 = (first_tile + n % each) * kQ;
-            qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, a.q.token, ql - i0, a.head_dim, thread);
-            ds_.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, gr.dout.token, ql - i0, a.head_dim, thread);
+            qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, ql - i0);
+            ds_.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, ql - i0);
             if (thread < kQ) {
                 const bool in = i0 + thread < ql;
                 const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tokens + i0 + thread;
@@ -363,6 +391,7 @@ __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_til
                 head_filled = g;
             }
             if constexpr (SHARED) __syncthreads(); else wave_fence();
+            if constexpr (kWide) at.forget();
             const char* const qt = turns + (SHARED ? turn * kTurnBytes : 0);
             const float* const st = reinterpret_cast<const float*>(qt + 2 * kTileBytes);
             const bool more = n + 1 < to;
@@ -376,7 +405,7 @@ __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, Grad gr, int k_til
 #pragma unroll
                 for (int step = 0; step < Tile<DP>::kSteps; ++step) {
                     s = mfma(at.rows(qt, m, step), kf[step], s, T{});
-                    dp = mfma(at.rows(qt + kTileBytes, m, step), vf[step], dp, T{});
+                    dp = mfma(at.rows(qt + kTileBytes, m, step), value(step), dp, T{});
                 }
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
@@ -522,11 +551,13 @@ Plan plan_of(const pruner_attention* a)
     p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;
     p.own_keys = a->k_tokens <= 32 && (int64_t)a->q_tokens * (a->q_heads / a->kv_heads) <= 256;
     p.q_tiles = (a->q_tokens + 127) / 128;
-    p.k_tiles = (a->k_tokens + 127) / 128;
+    const int tile_keys = padded_dim(a->head_dim) == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
+    p.k_tiles = (a->k_tokens + tile_keys - 1) / tile_keys;
     p.parts = 1;
     const int64_t groups = (int64_t)a->batch * a->kv_heads * p.k_tiles, tiles = (int64_t)(a->q_heads / a->kv_heads) * ((a->q_tokens + 31) / 32);
     if (!p.own_keys && groups > 0) {
-        int64_t parts = (kEnough + groups - 1) / groups;
+        const int64_t enough = padded_dim(a->head_dim) == 128 ? kEnough / 2 : kEnough;   // (workgroups of eight wavefronts)
+        int64_t parts = (enough + groups - 1) / groups;
         const int64_t most = tiles / 8;   // eight query tiles of 32 at least
         parts = parts < most ? parts : most;
         p.parts = parts < 1 ? 1 : (int)parts;
@@ -576,11 +607,11 @@ template <typename T, int DP> int run(const Call& c)
     }
     if (a.k_tokens > 0) {
         if (c.plan.own_keys) {
-            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads + 3) / 4)), dim3(256), 4 * (window + 2 * 32 * DP * 2 + 3 * 32 * 4), c.st, a, c.keys, 1);
+            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, 1);
         } else {
-            const size_t q = DP < 128 ? 64 : 32;
-            hipLaunchKernelGGL((keys_kernel<T, DP, true>), dim3((unsigned)(k_heads * c.plan.k_tiles * c.plan.parts)), dim3(256), window + 2 * (2 * q * DP * 2 + 3 * q * 4), c.st, a, c.keys,
-                               c.plan.k_tiles);
+            typedef KeysShape<T, DP, true> Shape;
+            hipLaunchKernelGGL((keys_kernel<T, DP, true>), dim3((unsigned)(k_heads * c.plan.k_tiles * c.plan.parts)), dim3(64 * Shape::kWaves),
+                               window + Shape::kTurns * Shape::kTurnBytes + Shape::kWaves * Shape::kHeldBytes, c.st, a, c.keys, c.plan.k_tiles);
         }
         PRUNER_LAUNCH_CHECK();
         if (c.plan.parts > 1) {
