@@ -7,7 +7,9 @@
 //                 a sequence and head of its own.  The bias is a function of j - p: tiles beyond the largest edge add one number, the others read a
 //                 window of it in LDS.
 //   rows_kernel   few queries: the queries of all heads that share a key head, at most 32 together, are the 32 columns; the four wavefronts take
-//                 32 keys each in turn, keys straight from memory into operand registers, and meet at the end.
+//                 32 keys each in turn, through LDS of their own (keys straight from memory into operand registers, 32 bytes of a row at a time:
+//                 476 us where this takes 400), and meet at the end.  Neighbouring workgroups take the heads of one sequence, whose
+//                 rows lie side by side (parts of one head instead: 584 us).
 //   join_kernel   the parts of a key axis that was split over workgroups.
 #include "rel_attention.h"
 
@@ -253,7 +255,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int columns = a.q_tokens * a.group;
-    const int part = blockIdx.x % parts.count, bh = blockIdx.x / parts.count, b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int hk = blockIdx.x % a.kv_heads, part = blockIdx.x / a.kv_heads % parts.count, b = blockIdx.x / a.kv_heads / parts.count;
     const int ql = a.queries(b), kl = a.keys(b);
     const int t = l32 / a.group, g = l32 % a.group, h = hk * a.group + (l32 < columns ? g : 0);
     const bool mine = l32 < columns && t < ql;
@@ -262,7 +264,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
     float* const biases = reinterpret_cast<float*>(lds);   // [bucket][group]
     const RowsLds places(a);
     uint8_t* const buckets = reinterpret_cast<uint8_t*>(lds + places.biases);   // by r
-    char* const tile = lds + places.biases + places.buckets + wave * kTileBytes;
+    char* const tile = lds + places.biases + places.buckets + wave * 2 * kTileBytes;
 
     int end = ql == 0 ? 0 : kl;   // (the last query sees all keys under the causal mask too)
     const int begin = part * parts.keys;
@@ -271,18 +273,19 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
 
     Lane<DP> at;
     at.set(lane);
-    u32x4 qf[Tile<DP>::kSteps], kf[Tile<DP>::kSteps];
+    u32x4 qf[Tile<DP>::kSteps];
     load_row<T, DP>(qf, a.q.at<T>(b, h) + (int64_t)t * a.q.token, mine, a.head_dim, half);
     Running<T, DP> run;
     run.clear();
     if (begin < end) {
         const T* const kp = a.k.at<T>(b, hk);
         const T* const vp = a.v.at<T>(b, hk);
-        Stage<T, DP, kOwnKeys, 64> vs;
+        Stage<T, DP, kOwnKeys, 64> ks, vs;
+        ks.set(a.k.token, a.head_dim, lane);
         vs.set(a.v.token, a.head_dim, lane);
         int key0 = begin + kOwnKeys * wave;
         if (key0 < end) {
-            load_row<T, DP>(kf, kp + (int64_t)(key0 + l32) * a.k.token, key0 + l32 < kl, a.head_dim, half);
+            ks.fetch(kp + (int64_t)key0 * a.k.token, kl - key0);
             vs.fetch(vp + (int64_t)key0 * a.v.token, kl - key0);
         }
         float bias_left = 0.f, bias_right = 0.f;
@@ -297,11 +300,13 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
         }
         __syncthreads();
         for (; key0 < end; key0 += 4 * kOwnKeys) {
+            ks.park(tile + kTileBytes, lane);
+            wave_fence();
             floatx16 s[1] = {zero16()};
 #pragma unroll
-            for (int st = 0; st < Tile<DP>::kSteps; ++st) s[0] = mfma(kf[st], qf[st], s[0], T{});
+            for (int st = 0; st < Tile<DP>::kSteps; ++st) s[0] = mfma(at.rows(tile + kTileBytes, 0, st), qf[st], s[0], T{});
             const int next = key0 + 4 * kOwnKeys;
-            if (next < end) load_row<T, DP>(kf, kp + (int64_t)(next + l32) * a.k.token, next + l32 < kl, a.head_dim, half);
+            if (next < end) ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
             vs.park(tile, lane);
             if (next < end) vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
             const int r_lo = key0 - (kl - ql + a.q_tokens - 1), r_hi = key0 + kOwnKeys - 1 - (kl - ql);
@@ -379,19 +384,21 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) join_kernel
     const int d = 4 * (int)(item % (DP / 4));
     if (row >= rows) return;
     float m = -ATT_INF, total = 0.f;
+#pragma unroll 8
     for (int n = 0; n < parts.count; ++n) {
         const float2 st = parts.stats[n * rows + row];
-        if (st.y != 0.f) m = __builtin_fmaxf(m, st.x);
+        m = __builtin_fmaxf(m, st.y != 0.f ? st.x : -ATT_INF);
     }
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int n = 0; n < parts.count; ++n) {
         const float2 st = parts.stats[n * rows + row];
-        if (st.y == 0.f) continue;
-        const float f = exp2_of((st.x - m) * kLog2e);
-        total = __builtin_fmaf(f, st.y, total);
         const f32x4 x = *reinterpret_cast<const f32x4*>(parts.sums + (n * rows + row) * DP + d);
+        const bool any = st.y != 0.f;   // (a part that no key reached counts for nothing, whatever it left)
+        const float f = any ? exp2_of((st.x - m) * kLog2e) : 0.f;
+        total = __builtin_fmaf(f, st.y, total);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, any ? x[e] : 0.f, o[e]);
     }
     const float f = total != 0.f ? 1.f / total : 0.f;
     const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads;
@@ -408,7 +415,9 @@ struct Plan {
     int64_t rows;
     size_t workspace;
 };
-constexpr int64_t kEnough = 1024;   // workgroups that fill the device: four for each of 256 compute units
+constexpr int64_t kEnough = 1024;       // workgroups that fill the device: four for each of 256 compute units
+constexpr int64_t kEnoughRows = 4096;   // ... where all they do is read, and their sequences' lengths differ (32 caches of up to 32768 tokens, 8 heads of 128:
+                                        // 536 us with 2048, 476 with 4096, 468 and more to join with 8192)
 Plan plan_of(const pruner_attention* a)
 {
     Plan p{};
@@ -420,7 +429,7 @@ Plan plan_of(const pruner_attention* a)
     int64_t groups = p.route == Route::kRows ? (int64_t)a->batch * a->kv_heads : (int64_t)a->batch * a->q_heads * p.q_tiles;
     if (p.route != Route::kOwn && groups > 0) {
         const int fewest = 512;   // keys of a part at least
-        int64_t parts = (kEnough + groups - 1) / groups;
+        int64_t parts = ((p.route == Route::kRows ? kEnoughRows : kEnough) + groups - 1) / groups;
         const int64_t most = ((int64_t)a->k_tokens + fewest - 1) / fewest;
         parts = parts < most ? parts : most;
         if (parts < 1) parts = 1;
@@ -457,7 +466,7 @@ template <typename T, int DP> int run(const Args& args, const Plan& plan, const 
     } else if (plan.route == Route::kRows) {
         const size_t columns = (size_t)args.q_tokens * args.group, last = 4 * 32 * 8 + 4 * columns * (DP + 4) * 4;
         const RowsLds places(args);
-        const size_t tiles = (size_t)places.biases + places.buckets + 4 * kOwnKeys * DP * 2;
+        const size_t tiles = (size_t)places.biases + places.buckets + 8 * kOwnKeys * DP * 2;
         hipLaunchKernelGGL((rows_kernel<T, DP>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > tiles ? last : tiles, st, args, out, lse, parts);
     } else {
         hipLaunchKernelGGL((tile_kernel<T, DP, true>), dim3((unsigned)(heads * plan.q_tiles * plan.parts)), dim3(256), window + 4 * kKeys * DP * 2, st, args, out, lse, parts,
