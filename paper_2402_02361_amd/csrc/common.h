@@ -45,6 +45,21 @@ __device__ __forceinline__ uint32_t row_inclusive_max(uint32_t v)
 __device__ __forceinline__ uint32_t rows_inclusive_max(uint32_t v) { return max_with<0x143, 0xc>(max_with<0x142, 0xa>(v)); }
 __device__ __forceinline__ uint32_t wave_inclusive_max(uint32_t v) { return rows_inclusive_max(row_inclusive_max(v)); }
 
+// v and the value of the lane 32 (16) away, in either order: half a wavefront's registers change places with the other half's.
+struct TwoFloats {
+    float a, b;
+};
+__device__ __forceinline__ TwoFloats across_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return TwoFloats{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ TwoFloats across_rows(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return TwoFloats{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
 // After a launch: PRUNER_EHIP if the runtime reports an error.  hipGetLastError returns (and clears) the last error
 // of the calling thread, so an error left by an earlier, unrelated runtime call is reported here as well; launches that
 // came before in the same call stay enqueued.

@@ -20,15 +20,31 @@ __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf
 
 // Sums over the T threads of a row, N of them at once, the same bits in all of them.  T a power of two in 4..1024; the wavefronts of a row
 // of more than 64 threads meet in LDS (two places in turn, so one barrier is enough).
+template <int CTRL> __device__ __forceinline__ float moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
 struct RowSum {
     float (*meet)[16][2];   // [2][16 wavefronts][N <= 2]
     int threads, turn;
     template <int N> __device__ __forceinline__ void of(float (&v)[N])
     {
-        const int inside = threads < kWave ? threads : kWave;
-        for (int o = 1; o < inside; o <<= 1)
+        // by moves inside the vector unit: pairs, fours, eights and sixteens of a row of 16 lanes, rows, halves
 #pragma unroll
-            for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], o, kWave);
+        for (int n = 0; n < N; ++n) {
+            v[n] += moved<0xB1>(v[n]);                        // quad_perm 1,0,3,2
+            v[n] += moved<0x4E>(v[n]);                        // quad_perm 2,3,0,1
+            if (threads >= 8) v[n] += moved<0x141>(v[n]);     // row_half_mirror: the other four of eight
+            if (threads >= 16) v[n] += moved<0x140>(v[n]);    // row_mirror: the other eight of sixteen
+            if (threads >= 32) {
+                const TwoFloats t = across_rows(v[n]);
+                v[n] = t.a + t.b;
+            }
+            if (threads >= 64) {
+                const TwoFloats t = across_halves(v[n]);
+                v[n] = t.a + t.b;
+            }
+        }
         if (threads <= kWave) return;
         const int wave = threadIdx.x >> 6, waves = threads >> 6, first = wave & ~(waves - 1);   // (a workgroup may hold two such rows)
         if ((threadIdx.x & 63) == 0)
@@ -98,8 +114,8 @@ struct Norm {
 };
 enum { kNoGate, kGateRows, kGateVector };
 
-template <typename T, int V>
-__global__ void __launch_bounds__(1024) norm_kernel(Norm p, const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch, T* __restrict__ h,
+template <typename T, int V, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch, T* __restrict__ h,
                                                     T* __restrict__ y, int8_t* __restrict__ codes, uint8_t* __restrict__ exps)
 {
     __shared__ float meet[2][16][2];
@@ -113,14 +129,23 @@ __global__ void __launch_bounds__(1024) norm_kernel(Norm p, const T* __restrict_
     load_vector(gate == kGateVector ? static_cast<const float*>(p.gate) : nullptr, col, left, s_all);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) s_all[j] = gate == kGateVector ? sigmoid(s_all[j]) : 1.f;
-    for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += (int64_t)gridDim.x * in_block) {
+    const int64_t stride = (int64_t)gridDim.x * in_block;
+    Eight<T, V> xin, fin, gin, x_next, f_next, g_next;   // the next row's values are on their way while a row is worked on
+    auto fetch = [&](int64_t row) {
+        const int some = row < p.rows ? left : 0;
+        x_next.load(x + row * x_pitch + col, some);
+        if (f) f_next.load(f + row * f_pitch + col, some);
+        if (gate == kGateRows) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
+    };
+    fetch((int64_t)blockIdx.x * in_block + slot);
+    for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
         // (threads past the last row go through the same steps on zeros: the wavefront's exchanges and the barriers need them)
         const int64_t row = first + slot;
         const int mine = row < p.rows ? left : 0;
-        Eight<T, V> xin, fin, gin;
-        xin.load(x + row * x_pitch + col, mine);
-        if (f) fin.load(f + row * f_pitch + col, mine);
-        if (gate == kGateRows) gin.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, mine);
+        xin = x_next;
+        fin = f_next;
+        gin = g_next;
+        fetch(row + stride);
         float v[kEach], z[kEach];
         xin.to_floats(v);
 #pragma unroll
@@ -155,8 +180,8 @@ __global__ void __launch_bounds__(1024) norm_kernel(Norm p, const T* __restrict_
 }
 
 // sums: [3][dim] of every workgroup (dw_post, dw_pre, dgate of one gate for all rows)
-template <typename T, int V>
-__global__ void __launch_bounds__(1024) norm_grad_kernel(Norm p, const T* __restrict__ dh, int64_t dh_pitch, const T* __restrict__ dy, int64_t dy_pitch,
+template <typename T, int V, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __restrict__ dh, int64_t dh_pitch, const T* __restrict__ dy, int64_t dy_pitch,
                                                          const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch,
                                                          const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, T* __restrict__ dx, T* __restrict__ df,
                                                          T* __restrict__ dgate, float* __restrict__ sums)
@@ -178,33 +203,42 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(Norm p, const T* __rest
         s_all[j] = gate == kGateVector ? sigmoid(s_all[j]) : 1.f;
         sum_post[j] = sum_pre[j] = sum_gate[j] = 0.f;
     }
-    for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += (int64_t)gridDim.x * in_block) {
+    const int64_t stride = (int64_t)gridDim.x * in_block;
+    struct Row {
+        Eight<T, V> x, f, g, dh, dy;
+        EightCodes<V> c;
+        uint32_t byte;
+    } now, next;
+    auto fetch = [&](int64_t row) {
+        const int some = row < p.rows ? left : 0;
+        next.x.load(x + row * x_pitch + col, some);
+        next.dy.load(dy + row * dy_pitch + col, some);
+        if (f) next.f.load(f + row * f_pitch + col, some);
+        if (codes) {
+            next.c.load(codes + row * p.dim + col, some);
+            next.byte = some > 0 ? exps[row * groups + t / 4] : 1u;
+        }
+        if (gate == kGateRows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
+        if (dh) next.dh.load(dh + row * dh_pitch + col, some);
+    };
+    fetch((int64_t)blockIdx.x * in_block + slot);
+    for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
         const int64_t row = first + slot;
         const int mine = row < p.rows ? left : 0;
-        Eight<T, V> xin, fin, gin, dhin, dyin;
-        EightCodes<V> cin;
-        uint32_t byte = 0;
-        xin.load(x + row * x_pitch + col, mine);
-        dyin.load(dy + row * dy_pitch + col, mine);
-        if (f) fin.load(f + row * f_pitch + col, mine);
-        if (codes) {
-            cin.load(codes + row * p.dim + col, mine);
-            byte = mine > 0 ? exps[row * groups + t / 4] : 1u;
-        }
-        if (gate == kGateRows) gin.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, mine);
-        if (dh) dhin.load(dh + row * dh_pitch + col, mine);
+        now = next;
+        fetch(row + stride);
         float v[kEach], z1[kEach], z2[kEach], s[kEach], d[kEach], w[kEach];
         float r1 = 0.f;
-        xin.to_floats(v);
+        now.x.to_floats(v);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) v[j] *= p.alpha;
         if (has_f) {
             if (codes)
-                restore_eight(cin.w, byte, w);
+                restore_eight(now.c.w, now.byte, w);
             else
-                fin.to_floats(w);
+                now.f.to_floats(w);
             r1 = normalise(sum, w, z1, mine, p.per_dim, p.center, p.eps);
-            if (gate == kGateRows) gin.to_floats(s);
+            if (gate == kGateRows) now.g.to_floats(s);
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 s[j] = gate == kGateRows ? sigmoid(s[j]) : s_all[j];
@@ -212,7 +246,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(Norm p, const T* __rest
             }
         }
         const float r2 = normalise(sum, v, z2, mine, p.per_dim, p.center, p.eps);
-        dyin.to_floats(d);
+        now.dy.to_floats(d);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             sum_pre[j] = __builtin_fmaf(d[j], z2[j], sum_pre[j]);
@@ -220,7 +254,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(Norm p, const T* __rest
         }
         back(sum, d, z2, r2, mine, p.per_dim, p.center);
         if (dh) {
-            dhin.to_floats(w);
+            now.dh.to_floats(w);
 #pragma unroll
             for (int j = 0; j < kEach; ++j) d[j] += w[j];
         }
@@ -271,23 +305,25 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(Norm p, const T* __rest
     }
 }
 
-// The workgroups' sums, added in their order: 32 columns and 8 runs of workgroups per workgroup.
-__global__ void __launch_bounds__(256) norm_sums_kernel(const float* __restrict__ sums, int parts, int dim, float* __restrict__ dw_post, float* __restrict__ dw_pre,
-                                                        float* __restrict__ dgate)
+// The workgroups' sums, added in their order: 32 columns and 32 runs of workgroups per workgroup.
+__global__ void __launch_bounds__(1024) norm_sums_kernel(const float* __restrict__ sums, int parts, int dim, float* __restrict__ dw_post, float* __restrict__ dw_pre,
+                                                         float* __restrict__ dgate)
 {
-    __shared__ float runs[8][33];
+    __shared__ float runs[32][33];
     const int which = blockIdx.y, col = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
     float* const out = which == 0 ? dw_post : which == 1 ? dw_pre : dgate;
     if (!out) return;
-    const int each = (parts + 7) / 8, lo = run * each, hi = lo + each < parts ? lo + each : parts;
+    const int each = (parts + 31) / 32, lo = run * each, hi = lo + each < parts ? lo + each : parts;
     float s = 0.f;
-    if (col < dim)
+    if (col < dim) {
+#pragma unroll 8
         for (int i = lo; i < hi; ++i) s += sums[((int64_t)i * 3 + which) * dim + col];
+    }
     runs[run][threadIdx.x & 31] = s;
     __syncthreads();
     if (run == 0 && col < dim) {
 #pragma unroll
-        for (int r = 1; r < 8; ++r) s += runs[r][threadIdx.x & 31];
+        for (int r = 1; r < 32; ++r) s += runs[r][threadIdx.x & 31];
         out[col] = s;
     }
 }
@@ -331,7 +367,7 @@ Norm norm_of(const pruner_norm* p, int threads)
 template <typename T, int V>
 int run_norm(const pruner_norm* p, const Shape& s, const void* x, int64_t x_pitch, const void* f, int64_t f_pitch, void* h, void* y, const pruner_checkpoint* kept, hipStream_t st)
 {
-    hipLaunchKernelGGL((norm_kernel<T, V>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch,
+    hipLaunchKernelGGL((s.block > 256 ? &norm_kernel<T, V, 1024> : &norm_kernel<T, V, 256>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch,
                        static_cast<T*>(h), static_cast<T*>(y), kept ? kept->codes : nullptr, kept ? kept->exps : nullptr);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
@@ -341,7 +377,7 @@ template <typename T, int V>
 int run_norm_grad(const pruner_norm* p, const Shape& s, const void* dh, int64_t dh_pitch, const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, const void* f,
                   int64_t f_pitch, const pruner_checkpoint* kept, void* dx, void* df, void* dgate, float* sums, hipStream_t st)
 {
-    hipLaunchKernelGGL((norm_grad_kernel<T, V>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(dh), dh_pitch, static_cast<const T*>(dy),
+    hipLaunchKernelGGL((s.block > 512 ? &norm_grad_kernel<T, V, 1024> : s.block > 256 ? &norm_grad_kernel<T, V, 512> : &norm_grad_kernel<T, V, 256>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(dh), dh_pitch, static_cast<const T*>(dy),
                        dy_pitch, static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch, kept ? kept->codes : nullptr, kept ? kept->exps : nullptr,
                        static_cast<T*>(dx), static_cast<T*>(df), static_cast<T*>(dgate), sums);
     PRUNER_LAUNCH_CHECK();
@@ -428,7 +464,7 @@ extern "C" int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int6
         const int rc = BY_TYPE_AND_ACCESS(p->dtype, a.v, run_norm_grad, &q, s, dh, dh_pitch, dy, dy_pitch, x, x_pitch, f, f_pitch, kept_f, dx, df, gate_rows ? dgate : nullptr, sums, st);
         if (rc) return rc;
     }
-    hipLaunchKernelGGL(norm_sums_kernel, dim3((p->dim + 31) / 32, 3), dim3(256), 0, st, sums, parts, p->dim, has_f ? dw_post : nullptr, dw_pre,
+    hipLaunchKernelGGL(norm_sums_kernel, dim3((p->dim + 31) / 32, 3), dim3(1024), 0, st, sums, parts, p->dim, has_f ? dw_post : nullptr, dw_pre,
                        gate_vector ? static_cast<float*>(dgate) : nullptr);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;

@@ -49,8 +49,17 @@ __device__ __forceinline__ floatx16 zero16()
     return z;
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-// The other half's value (lane ^ 32).
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// Of a lane and the one of the same column in the other half.
+__device__ __forceinline__ float sum_of_halves(float v)
+{
+    const TwoFloats t = across_halves(v);
+    return t.a + t.b;
+}
+__device__ __forceinline__ float max_of_halves(float v)
+{
+    const TwoFloats t = across_halves(v);
+    return __builtin_fmaxf(t.a, t.b);
+}
 __device__ __forceinline__ int row_of(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
 // What this wavefront's lanes wrote to LDS is there for its other lanes after.

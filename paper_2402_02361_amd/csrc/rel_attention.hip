@@ -47,7 +47,7 @@ template <typename T, int DP> struct Running {
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, s[n][i]);
-        top = __builtin_fmaxf(top, other_half(top));
+        top = max_of_halves(top);
         if (fused) top = __builtin_fmaf(top, scale, bias);
         if (__any(top > m + kSlack)) {   // (from minus infinity: any score)
             const float now = __builtin_fmaxf(m, top), factor = now == -ATT_INF ? 1.f : exp2_of((m - now) * kLog2e);
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         }
     }
     if (i >= a.q_tokens) return;
-    const float l = run.l + other_half(run.l);
+    const float l = sum_of_halves(run.l);
     const int64_t row = (int64_t)bh * a.q_tokens + i;
     if (parts.count > 1) {
         const int64_t slot = (int64_t)part * heads * a.q_tokens + row;
@@ -340,7 +340,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
     __syncthreads();
     float2* const stats = reinterpret_cast<float2*>(lds);           // [4][32]
     float* const sums = reinterpret_cast<float*>(lds + 4 * 32 * 8); // [4][columns][kStride]
-    const float l = run.l + other_half(run.l);
+    const float l = sum_of_halves(run.l);
     if (half == 0) stats[wave * 32 + l32] = make_float2(run.m, mine ? l : 0.f);
     if (l32 < columns) store_row32<DP>(sums + (wave * columns + l32) * kStride, run.o, half);
     __syncthreads();

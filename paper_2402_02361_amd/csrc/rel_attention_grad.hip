@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 delta = __builtin_fmaf(x[0], y[0], delta);
                 delta = __builtin_fmaf(x[1], y[1], delta);
             }
-        delta += other_half(delta);
+        delta = sum_of_halves(delta);
         if (half == 0 && i < a.q_tokens) gr.delta[row] = delta;
     }
     floatx16 dq[Tile<DP>::kBlocks];
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                     vs.park(tiles + kTileBytes, thread);
                 }
             }
-            delta += other_half(delta);
+            delta = sum_of_halves(delta);
         }
         int turn = 0;
         for (int key0 = 0; key0 < end; key0 += kN) {
