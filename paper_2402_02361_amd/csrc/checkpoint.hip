@@ -58,8 +58,10 @@ __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__
 // A matrix product whose depth is the rows, which is the outer index of both operands: tiles of 64 rows lie in LDS as they lie in memory
 // (x^ restored to dy's type on the way, exactly), and ds_read_b64_tr_b16 hands them to v_mfma_f32_32x32x16 turned over.  That read takes, per 16
 // lanes, four rows of 16 columns (lane t the 8 bytes at row t / 4, column 4 (t % 4)) and gives lane t column t of them.
-// A workgroup of four wavefronts owns 128 x 128 of dW, a wavefront 64 x 64.  Where the tiles of dW are too few for the device, the rows
-// are cut into parts whose sums go to the workspace and are added in their order.
+// A workgroup of four wavefronts owns 128 x 128 of dW, a wavefront 64 x 64; or, where there are enough of these for the device, one of eight owns 256 x 256, a
+// wavefront 64 x 128.  What bounds it is LDS: a wavefront's 16 rows take 4 KB of reads for four products of 32 x 32 (128 cycles, in which
+// LDS hands out 16 KB to four wavefronts), or 6 KB for eight.  Where the tiles of dW are too few for the device, the rows are cut into
+// parts whose sums go to the workspace and are added in their order.
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -75,28 +77,36 @@ __device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, _Float16)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-constexpr int kTileN = 128, kTileK = 128, kTileR = 64;
-constexpr int kTileBytes = kTileR * 256;            // a tile of either operand: rows of 128 values of 16 bits
-constexpr int kChunksEach = kTileR * 16 / 256;      // 16-byte chunks of a tile per thread (4)
+constexpr int kTileR = 64;
 constexpr int kMinPartRows = 512;                   // fewest rows of a part
-constexpr int64_t kEnoughTiles = 512;               // two workgroups for each of the 256 compute units
-
-// Where a row's 16-byte chunk lies: chunks are permuted row by row so that neither the writes (16 lanes, one row) nor the turning reads (four
-// rows of 64 bytes at once) meet in a bank.
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 256 + ((chunk ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4); }
+template <bool BIG> struct WgradShape {
+    static constexpr int kSide = BIG ? 256 : 128, kThreads = 2 * kSide;
+    static constexpr int kChunks = kSide / 8, kRowBytes = 2 * kSide, kTileBytes = kTileR * kRowBytes;   // a tile of either operand: rows of kSide values of 16 bits
+    static constexpr int kRowStep = kThreads / kChunks, kEach = kTileR / kRowStep;                      // 16-byte chunks of a tile per thread
+    static constexpr int kN = 2, kK = BIG ? 4 : 2;                                                      // blocks of 32 of a wavefront
+    // Where a row's 16-byte chunk lies: chunks are permuted row by row so that neither the writes (16 lanes, one row) nor the turning reads (four
+    // rows of 64 bytes at once) meet in a bank.
+    __device__ __forceinline__ static int chunk_at(int row, int chunk) { return row * kRowBytes + ((chunk ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4); }
+};
 
 struct WgradPlan {
+    bool big;
     int tiles_n, tiles_k, parts;
     int64_t rows_each;   // rows of a part, a multiple of kTileR
 };
 WgradPlan wgrad_plan(int64_t rows, int32_t n_out, int32_t dim)
 {
     WgradPlan p;
-    p.tiles_n = (n_out + kTileN - 1) / kTileN;
-    p.tiles_k = (dim + kTileK - 1) / kTileK;
-    const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-    int64_t parts = (kEnoughTiles + tiles - 1) / tiles;
     const int64_t most = (rows + kMinPartRows - 1) / kMinPartRows;
+    auto tiles_of = [&](int side) { return (int64_t)((n_out + side - 1) / side) * ((dim + side - 1) / side); };
+    // the large tiles where, cut into parts, they give each of the 256 compute units one, and where the last of either side is not mostly beyond the matrix
+    const int64_t padded = tiles_of(256) * 65536, small = tiles_of(128) * 16384;
+    p.big = tiles_of(256) * (most > 1 ? most : 1) >= 256 && padded <= small + small / 4;
+    const int side = p.big ? 256 : 128;
+    p.tiles_n = (n_out + side - 1) / side;
+    p.tiles_k = (dim + side - 1) / side;
+    const int64_t tiles = tiles_of(side), enough = p.big ? 256 : 512;   // workgroups that fill the device
+    int64_t parts = (enough + tiles - 1) / tiles;
     parts = parts < most ? parts : most;
     if (parts < 1) parts = 1;
     p.rows_each = ((rows + parts - 1) / parts + kTileR - 1) / kTileR * kTileR;
@@ -106,29 +116,31 @@ WgradPlan wgrad_plan(int64_t rows, int32_t n_out, int32_t dim)
     return p;
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(256, 2) wgrad_kernel(const T* __restrict__ dy, int64_t dy_pitch, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
+template <typename T, int V, bool BIG>
+__global__ void __launch_bounds__(WgradShape<BIG>::kThreads, 2) wgrad_kernel(const T* __restrict__ dy, int64_t dy_pitch, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps,
                                                        int64_t rows, int n_out, int dim, WgradPlan plan, float* __restrict__ out, int accumulate)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2][2][kTileBytes];   // [turn][dy, x^]
+    typedef WgradShape<BIG> S;
+    constexpr int kSide = S::kSide, kEach_ = S::kEach;
+    extern __shared__ __attribute__((aligned(16))) char lds[];   // [turn][dy, x^] tiles
     // workgroups go to the eight dies in turn: each takes a run of the tiles, part by part, so that a part's rows stay in its cache
     const uint32_t total = gridDim.x, die = blockIdx.x & 7, in_die = blockIdx.x >> 3, whole = total >> 3, extra = total & 7;
     const uint32_t id = die * whole + (die < extra ? die : extra) + in_die;
     const uint32_t tiles = (uint32_t)plan.tiles_n * plan.tiles_k, part = id / tiles, tile_id = id % tiles;
-    const int n0 = (int)(tile_id / plan.tiles_k) * kTileN, k0 = (int)(tile_id % plan.tiles_k) * kTileK;
+    const int n0 = (int)(tile_id / plan.tiles_k) * kSide, k0 = (int)(tile_id % plan.tiles_k) * kSide;
     const int64_t r_begin = (int64_t)part * plan.rows_each, r_end = r_begin + plan.rows_each < rows ? r_begin + plan.rows_each : rows;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
     const int groups = (dim + kGroup - 1) / kGroup;
 
-    const int s_row = threadIdx.x >> 4, s_chunk = threadIdx.x & 15;   // this thread's chunks: rows s_row + 16 u
+    const int s_row = threadIdx.x / S::kChunks, s_chunk = threadIdx.x % S::kChunks;   // this thread's chunks: rows s_row + kRowStep u
     const int n_left = n_out - (n0 + 8 * s_chunk), k_left = dim - (k0 + 8 * s_chunk);
-    Eight<T, V> dy_in[kChunksEach];
-    EightCodes<V> x_in[kChunksEach];
-    uint32_t x_exp[kChunksEach];
+    Eight<T, V> dy_in[kEach_];
+    EightCodes<V> x_in[kEach_];
+    uint32_t x_exp[kEach_];
     auto fetch = [&](int64_t r0) {
 #pragma unroll
-        for (int u = 0; u < kChunksEach; ++u) {
-            const int64_t r = r0 + s_row + 16 * u;
+        for (int u = 0; u < kEach_; ++u) {
+            const int64_t r = r0 + s_row + S::kRowStep * u;
             const bool in = r < r_end;
             dy_in[u].load(dy + r * dy_pitch + n0 + 8 * s_chunk, in ? n_left : 0);
             x_in[u].load(codes + r * dim + k0 + 8 * s_chunk, in ? k_left : 0);
@@ -137,40 +149,40 @@ __global__ void __launch_bounds__(256, 2) wgrad_kernel(const T* __restrict__ dy,
     };
     auto park = [&](int turn) {
 #pragma unroll
-        for (int u = 0; u < kChunksEach; ++u) {
-            const int at = chunk_at(s_row + 16 * u, s_chunk);
-            *reinterpret_cast<u32x4*>(&lds[turn][0][at]) = u32x4{dy_in[u].w[0], dy_in[u].w[1], dy_in[u].w[2], dy_in[u].w[3]};
+        for (int u = 0; u < kEach_; ++u) {
+            const int at = S::chunk_at(s_row + S::kRowStep * u, s_chunk);
+            *reinterpret_cast<u32x4*>(lds + 2 * turn * S::kTileBytes + at) = u32x4{dy_in[u].w[0], dy_in[u].w[1], dy_in[u].w[2], dy_in[u].w[3]};
             float v[kEach];
             restore_eight(x_in[u].w, x_exp[u], v);
             Eight<T, 8> x;
             x.from_floats(v);
-            *reinterpret_cast<u32x4*>(&lds[turn][1][at]) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
+            *reinterpret_cast<u32x4*>(lds + (2 * turn + 1) * S::kTileBytes + at) = u32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
         }
     };
     // this lane's places in a tile: block of 32 columns, four rows q of the eight of its half
-    const int wn = 2 * (wave >> 1), wk = 2 * (wave & 1), t = lane & 15, g = (lane >> 4) & 1;
-    int at_n[2][2], at_k[2][2];
+    const int wn = S::kN * (wave >> 1), wk = S::kK * (wave & 1), t = lane & 15, g = (lane >> 4) & 1;
+    int at_n[S::kN][2], at_k[S::kK][2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int q = 0; q < 2; ++q) {
+        const int row = 8 * half + 4 * q + (t >> 2), within = 2 * g + ((t >> 1) & 1);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int row = 8 * half + 4 * q + (t >> 2), within = 2 * g + ((t >> 1) & 1);
-            at_n[b][q] = chunk_at(row, 4 * (wn + b) + within) + 8 * (t & 1);
-            at_k[b][q] = chunk_at(row, 4 * (wk + b) + within) + 8 * (t & 1);
-        }
+        for (int b = 0; b < S::kN; ++b) at_n[b][q] = S::chunk_at(row, 4 * (wn + b) + within) + 8 * (t & 1);
+#pragma unroll
+        for (int b = 0; b < S::kK; ++b) at_k[b][q] = S::chunk_at(row, 4 * (wk + b) + within) + 8 * (t & 1);
+    }
     auto turned = [&](const char* p, const int (&at)[2], int step) {
         typedef __attribute__((address_space(3))) i16x4* lds_ptr;
-        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[0] + step * 16 * 256));
-        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[1] + step * 16 * 256));
+        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[0] + step * 16 * S::kRowBytes));
+        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + at[1] + step * 16 * S::kRowBytes));
         const u32x2 lo = __builtin_bit_cast(u32x2, a), hi = __builtin_bit_cast(u32x2, b);
         return u32x4{lo[0], lo[1], hi[0], hi[1]};
     };
 
-    floatx16 acc[2][2];
+    floatx16 acc[S::kN][S::kK];
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < S::kN; ++a)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < S::kK; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
     if (r_begin < r_end) {
@@ -183,25 +195,24 @@ __global__ void __launch_bounds__(256, 2) wgrad_kernel(const T* __restrict__ dy,
             if (more) fetch(r0 + kTileR);
 #pragma unroll
             for (int step = 0; step < kTileR / 16; ++step) {
-                u32x4 fn[2], fk[2];
+                u32x4 fn[S::kN], fk[S::kK];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    fn[b] = turned(lds[turn][0], at_n[b], step);
-                    fk[b] = turned(lds[turn][1], at_k[b], step);
-                }
+                for (int b = 0; b < S::kN; ++b) fn[b] = turned(lds + 2 * turn * S::kTileBytes, at_n[b], step);
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
+                for (int b = 0; b < S::kK; ++b) fk[b] = turned(lds + (2 * turn + 1) * S::kTileBytes, at_k[b], step);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) acc[a][b] = mfma(fn[a], fk[b], acc[a][b], T{});
+                for (int a = 0; a < S::kN; ++a)
+#pragma unroll
+                    for (int b = 0; b < S::kK; ++b) acc[a][b] = mfma(fn[a], fk[b], acc[a][b], T{});
             }
             if (more) park(turn ^ 1);
         }
     }
     float* const to = out + (plan.parts > 1 ? (int64_t)part * n_out * dim : 0);
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < S::kN; ++a)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < S::kK; ++b) {
             const int k = k0 + 32 * (wk + b) + l32;
             if (k >= dim) continue;
 #pragma unroll
@@ -242,7 +253,17 @@ int run_wgrad(const void* dy, int64_t dy_pitch, const pruner_checkpoint* kept, i
               float* parts, hipStream_t st)
 {
     const int64_t blocks = (int64_t)plan.tiles_n * plan.tiles_k * plan.parts;
-    hipLaunchKernelGGL((wgrad_kernel<T, V>), dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(dy), dy_pitch, kept->codes, kept->exps, rows, n_out, dim, plan,
+    static PerDeviceFlag ready;
+    const int dev = current_device(nullptr);
+    if (dev < 0) return PRUNER_EHIP;
+    if (!ready.get(dev)) {
+        for (const void* fn : {reinterpret_cast<const void*>(&wgrad_kernel<T, V, false>), reinterpret_cast<const void*>(&wgrad_kernel<T, V, true>)})
+            if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 4 * WgradShape<true>::kTileBytes) != hipSuccess) return PRUNER_EHIP;
+        ready.mark(dev);
+    }
+    auto* const kernel = plan.big ? &wgrad_kernel<T, V, true> : &wgrad_kernel<T, V, false>;
+    const int threads = plan.big ? WgradShape<true>::kThreads : WgradShape<false>::kThreads, bytes = 4 * (plan.big ? WgradShape<true>::kTileBytes : WgradShape<false>::kTileBytes);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), bytes, st, static_cast<const T*>(dy), dy_pitch, kept->codes, kept->exps, rows, n_out, dim, plan,
                        plan.parts > 1 ? parts : dw, accumulate);
     PRUNER_LAUNCH_CHECK();
     if (plan.parts > 1) {

@@ -4,7 +4,7 @@
 // Backward, with <.> the mean over a row and N(d, z, r) = r (d - [<d>] - z <d z>) (the middle term with the mean only):
 //     dH = dh + N(dy w_pre, z2, r2);   dx = alpha dH;   dgate = dH u s (1 - s);   df = N(dH s w_post, z1, r1)
 //     dw_pre = sum over rows of dy z2;   dw_post = sum over rows of dH s z1
-// A row lives in the registers of T threads, eight neighbouring values each, T the power of two that covers it: every matrix is
+// A row lives in the registers of T threads, eight neighbouring values each, T the power of two that covers it, or beyond 64 the whole wavefronts that do: every matrix is
 // read once and written once, and the statistics are formed again in the backward pass, where they cost no bytes.
 // All in binary32.  Bound: memory.
 #include "checkpoint.h"
@@ -18,15 +18,15 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-g * kLog2e)); }
 
-// Sums over the T threads of a row, N of them at once, the same bits in all of them.  T a power of two in 4..1024; the wavefronts of a row
-// of more than 64 threads meet in LDS (two places in turn, so one barrier is enough).
+// Sums over the T threads of a row, N of them at once, the same bits in all of them.  T a power of two in 4..64, or whole wavefronts; the wavefronts of a
+// row of more than 64 threads meet in LDS (two places in turn, so one barrier is enough).
 template <int CTRL> __device__ __forceinline__ float moved(float v)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
 }
 struct RowSum {
     float (*meet)[16][2];   // [2][16 wavefronts][N <= 2]
-    int threads, turn;
+    int threads, slot, turn;   // slot: which of the workgroup's rows
     template <int N> __device__ __forceinline__ void of(float (&v)[N])
     {
         // by moves inside the vector unit: pairs, fours, eights and sixteens of a row of 16 lanes, rows, halves
@@ -46,7 +46,7 @@ struct RowSum {
             }
         }
         if (threads <= kWave) return;
-        const int wave = threadIdx.x >> 6, waves = threads >> 6, first = wave & ~(waves - 1);   // (a workgroup may hold two such rows)
+        const int wave = threadIdx.x >> 6, waves = threads >> 6, first = slot * waves;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int n = 0; n < N; ++n) meet[turn][wave][n] = v[n];
@@ -61,29 +61,32 @@ struct RowSum {
     }
 };
 
-// z <- norm(v) over a row, of which `left` values begin here (those past its end are 0 and stay 0); returns r.
+// z <- norm(v) over a row, of which `left` values begin here (those past its end are 0 and stay 0); returns r.  Where accesses take all eight values (V = 8)
+// a thread has all of them or none.
+template <int V>
 __device__ __forceinline__ float normalise(RowSum& sum, const float (&v)[kEach], float (&z)[kEach], int left, float per_dim, bool center, float eps)
 {
     float m = 0.f;
     if (center) {
         float s[1] = {((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]))};
         sum.of(s);
-        m = s[0] * per_dim;
+        m = left > 0 ? s[0] * per_dim : 0.f;
     }
     float q[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        z[j] = j < left ? v[j] - m : 0.f;
+        z[j] = V == 8 || j < left ? v[j] - m : 0.f;
         q[0] = __builtin_fmaf(z[j], z[j], q[0]);
     }
     sum.of(q);
-    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(q[0], per_dim, eps));
+    const float r = left > 0 ? __builtin_amdgcn_rsqf(__builtin_fmaf(q[0], per_dim, eps)) : 0.f;   // (it may be infinite where eps is 0)
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) z[j] = j < left ? z[j] * r : 0.f;   // (r may be infinite where eps is 0)
+    for (int j = 0; j < kEach; ++j) z[j] = V == 8 || j < left ? z[j] * r : 0.f;
     return r;
 }
 
 // d <- r (d - [<d>] - z <d z>)
+template <int V>
 __device__ __forceinline__ void back(RowSum& sum, float (&d)[kEach], const float (&z)[kEach], float r, int left, float per_dim, bool center)
 {
     float s[2] = {0.f, 0.f};
@@ -95,7 +98,7 @@ __device__ __forceinline__ void back(RowSum& sum, float (&d)[kEach], const float
     sum.of(s);
     const float a = s[0] * per_dim, b = center ? s[1] * per_dim : 0.f;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) d[j] = j < left ? r * (d[j] - b - z[j] * a) : 0.f;
+    for (int j = 0; j < kEach; ++j) d[j] = V == 8 || j < left ? r * __builtin_fmaf(-z[j], a, d[j] - b) : 0.f;   // (r is 0 where nothing is left)
 }
 
 __device__ __forceinline__ void load_vector(const float* __restrict__ p, int col, int left, float (&v)[kEach])
@@ -119,8 +122,8 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
                                                     T* __restrict__ y, int8_t* __restrict__ codes, uint8_t* __restrict__ exps)
 {
     __shared__ float meet[2][16][2];
-    RowSum sum{meet, p.threads, 0};
-    const int in_block = (int)blockDim.x / p.threads, slot = (int)threadIdx.x / p.threads, t = (int)threadIdx.x & (p.threads - 1);
+    const int in_block = (int)blockDim.x / p.threads, slot = (int)threadIdx.x / p.threads, t = (int)threadIdx.x - slot * p.threads;
+    RowSum sum{meet, p.threads, slot, 0};
     const int col = 8 * t, left = p.dim - col;
     const int gate = !p.gate ? kNoGate : p.gate_pitch ? kGateRows : kGateVector;
     float w_post[kEach], w_pre[kEach], s_all[kEach];
@@ -153,10 +156,15 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
         if (f) {
             float u[kEach], g[kEach];
             fin.to_floats(u);
-            normalise(sum, u, z, mine, p.per_dim, p.center, p.eps);
-            if (gate == kGateRows) gin.to_floats(g);
+            normalise<V>(sum, u, z, mine, p.per_dim, p.center, p.eps);
+            if (gate == kGateRows) {
+                gin.to_floats(g);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(gate == kGateRows ? sigmoid(g[j]) : s_all[j], z[j] * w_post[j], v[j]);
+                for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(sigmoid(g[j]), z[j] * w_post[j], v[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(s_all[j], z[j] * w_post[j], v[j]);
+            }
         }
         Eight<T, V> out;
         if (h) {
@@ -164,7 +172,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
             out.store(h + row * p.dim + col, mine);
         }
         if (!y && !codes) continue;
-        normalise(sum, v, z, mine, p.per_dim, p.center, p.eps);
+        normalise<V>(sum, v, z, mine, p.per_dim, p.center, p.eps);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) z[j] *= w_pre[j];
         out.from_floats(z);
@@ -180,7 +188,8 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
 }
 
 // sums: [3][dim] of every workgroup (dw_post, dw_pre, dgate of one gate for all rows)
-template <typename T, int V, int BLOCK>
+// VECTOR: the gate is one for all rows
+template <typename T, int V, int BLOCK, bool VECTOR>
 __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __restrict__ dh, int64_t dh_pitch, const T* __restrict__ dy, int64_t dy_pitch,
                                                          const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch,
                                                          const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, T* __restrict__ dx, T* __restrict__ df,
@@ -188,19 +197,19 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
 {
     __shared__ float meet[2][16][2];
     __shared__ float fold[256 * kEach];
-    RowSum sum{meet, p.threads, 0};
-    const int in_block = (int)blockDim.x / p.threads, slot = (int)threadIdx.x / p.threads, t = (int)threadIdx.x & (p.threads - 1);
+    const int in_block = (int)blockDim.x / p.threads, slot = (int)threadIdx.x / p.threads, t = (int)threadIdx.x - slot * p.threads;
+    RowSum sum{meet, p.threads, slot, 0};
     const int col = 8 * t, left = p.dim - col;
-    const int gate = !p.gate ? kNoGate : p.gate_pitch ? kGateRows : kGateVector;
+    const bool gate_rows = !VECTOR && p.gate;
     const bool has_f = f || codes;
     const int groups = (p.dim + kGroup - 1) / kGroup;
     float w_post[kEach], w_pre[kEach], s_all[kEach], sum_post[kEach], sum_pre[kEach], sum_gate[kEach];
     load_vector(p.w_post, col, left, w_post);
     load_vector(p.w_pre, col, left, w_pre);
-    load_vector(gate == kGateVector ? static_cast<const float*>(p.gate) : nullptr, col, left, s_all);
+    if constexpr (VECTOR) load_vector(static_cast<const float*>(p.gate), col, left, s_all);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        s_all[j] = gate == kGateVector ? sigmoid(s_all[j]) : 1.f;
+        s_all[j] = VECTOR ? sigmoid(s_all[j]) : 1.f;
         sum_post[j] = sum_pre[j] = sum_gate[j] = 0.f;
     }
     const int64_t stride = (int64_t)gridDim.x * in_block;
@@ -218,7 +227,7 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
             next.c.load(codes + row * p.dim + col, some);
             next.byte = some > 0 ? exps[row * groups + t / 4] : 1u;
         }
-        if (gate == kGateRows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
+        if (gate_rows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
         if (dh) next.dh.load(dh + row * dh_pitch + col, some);
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
@@ -237,22 +246,26 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
                 restore_eight(now.c.w, now.byte, w);
             else
                 now.f.to_floats(w);
-            r1 = normalise(sum, w, z1, mine, p.per_dim, p.center, p.eps);
-            if (gate == kGateRows) now.g.to_floats(s);
+            r1 = normalise<V>(sum, w, z1, mine, p.per_dim, p.center, p.eps);
+            if (gate_rows) {
+                now.g.to_floats(s);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                s[j] = gate == kGateRows ? sigmoid(s[j]) : s_all[j];
-                v[j] = __builtin_fmaf(s[j], z1[j] * w_post[j], v[j]);
+                for (int j = 0; j < kEach; ++j) s[j] = sigmoid(s[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) s[j] = s_all[j];
             }
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(s[j], z1[j] * w_post[j], v[j]);
         }
-        const float r2 = normalise(sum, v, z2, mine, p.per_dim, p.center, p.eps);
+        const float r2 = normalise<V>(sum, v, z2, mine, p.per_dim, p.center, p.eps);
         now.dy.to_floats(d);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             sum_pre[j] = __builtin_fmaf(d[j], z2[j], sum_pre[j]);
             d[j] *= w_pre[j];
         }
-        back(sum, d, z2, r2, mine, p.per_dim, p.center);
+        back<V>(sum, d, z2, r2, mine, p.per_dim, p.center);
         if (dh) {
             now.dh.to_floats(w);
 #pragma unroll
@@ -266,17 +279,23 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
         if (!has_f) continue;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            w[j] = d[j] * (z1[j] * w_post[j]) * s[j] * (1.f - s[j]);
             d[j] *= s[j];
-            sum_post[j] = __builtin_fmaf(d[j], z1[j], sum_post[j]);
-            sum_gate[j] += w[j];
+            w[j] = d[j] * z1[j];
+            sum_post[j] += w[j];
             d[j] *= w_post[j];
         }
-        if (gate == kGateRows) {
-            out.from_floats(w);
-            out.store(dgate + row * p.dim + col, mine);
+        if (VECTOR || gate_rows) {   // dgate = dH u s (1 - s)
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) w[j] *= w_post[j] * (1.f - s[j]);
+            if constexpr (VECTOR) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) sum_gate[j] += w[j];
+            } else {
+                out.from_floats(w);
+                out.store(dgate + row * p.dim + col, mine);
+            }
         }
-        back(sum, d, z1, r1, mine, p.per_dim, p.center);
+        back<V>(sum, d, z1, r1, mine, p.per_dim, p.center);
         out.from_floats(d);
         out.store(df + row * p.dim + col, mine);
     }
@@ -301,7 +320,7 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
     leave(sum_pre, to + p.dim);
     if (has_f) {
         leave(sum_post, to);
-        if (gate == kGateVector) leave(sum_gate, to + 2 * p.dim);
+        if constexpr (VECTOR) leave(sum_gate, to + 2 * p.dim);
     }
 }
 
@@ -331,8 +350,8 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const float* __restrict
 int row_threads(int32_t dim)   // threads per row
 {
     int t = 4;
-    while (8 * t < dim) t *= 2;
-    return t;
+    while (8 * t < dim && t < kWave) t *= 2;
+    return 8 * t < dim ? (dim + 8 * kWave - 1) / (8 * kWave) * kWave : t;
 }
 struct Shape {
     int threads, block, blocks;
@@ -340,7 +359,7 @@ struct Shape {
 constexpr int64_t kMaxParts = 2048;   // workgroups of the backward pass (their sums are read again)
 Shape shape_of(int64_t rows, int32_t dim, int64_t most_blocks)
 {
-    const int t = row_threads(dim), block = t < 256 ? 256 : t;
+    const int t = row_threads(dim), block = t <= 128 ? 256 : t;
     const int64_t need = (rows + block / t - 1) / (block / t);
     return Shape{t, block, (int)(need < most_blocks ? need : most_blocks)};
 }
@@ -364,10 +383,30 @@ Norm norm_of(const pruner_norm* p, int threads)
     return Norm{p->rows, p->dim, threads, p->center != 0, p->alpha, p->eps, 1.f / (float)p->dim, p->w_post, p->w_pre, p->gate, p->gate_pitch};
 }
 
+// Workgroups of a kernel that the current device holds at once: as many are started, each takes its rows in turn (1024 where 768 fit: the last quarter ran alone,
+// 531 us over 65536 x 2048 rows where this takes 427).
+struct Held {
+    int of[kMaxDevices] = {};
+    int64_t get(const void* kernel, int block, int64_t most)
+    {
+        int cus = 0, each = 0;
+        const int dev = current_device(&cus);
+        if (dev < 0) return -1;
+        if (dev < kMaxDevices && of[dev]) return of[dev] < most ? of[dev] : most;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, block, 0) != hipSuccess || each < 1) return -1;
+        if (dev < kMaxDevices) of[dev] = each * cus;
+        return (int64_t)each * cus < most ? (int64_t)each * cus : most;
+    }
+};
+
 template <typename T, int V>
 int run_norm(const pruner_norm* p, const Shape& s, const void* x, int64_t x_pitch, const void* f, int64_t f_pitch, void* h, void* y, const pruner_checkpoint* kept, hipStream_t st)
 {
-    hipLaunchKernelGGL((s.block > 256 ? &norm_kernel<T, V, 1024> : &norm_kernel<T, V, 256>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch,
+    static Held held[17];   // by wavefronts of a workgroup
+    auto* const kernel = s.block > 256 ? &norm_kernel<T, V, 1024> : &norm_kernel<T, V, 256>;
+    const int64_t blocks = held[s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
+    if (blocks < 0) return PRUNER_EHIP;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch,
                        static_cast<T*>(h), static_cast<T*>(y), kept ? kept->codes : nullptr, kept ? kept->exps : nullptr);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
@@ -375,9 +414,17 @@ int run_norm(const pruner_norm* p, const Shape& s, const void* x, int64_t x_pitc
 
 template <typename T, int V>
 int run_norm_grad(const pruner_norm* p, const Shape& s, const void* dh, int64_t dh_pitch, const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, const void* f,
-                  int64_t f_pitch, const pruner_checkpoint* kept, void* dx, void* df, void* dgate, float* sums, hipStream_t st)
+                  int64_t f_pitch, const pruner_checkpoint* kept, void* dx, void* df, void* dgate, float* sums, int* parts, hipStream_t st)
 {
-    hipLaunchKernelGGL((s.block > 512 ? &norm_grad_kernel<T, V, 1024> : s.block > 256 ? &norm_grad_kernel<T, V, 512> : &norm_grad_kernel<T, V, 256>), dim3(s.blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(dh), dh_pitch, static_cast<const T*>(dy),
+    const bool vector = p->gate && !p->gate_pitch;
+    auto* const kernel = s.block > 512   ? (vector ? &norm_grad_kernel<T, V, 1024, true> : &norm_grad_kernel<T, V, 1024, false>)
+                         : s.block > 256 ? (vector ? &norm_grad_kernel<T, V, 512, true> : &norm_grad_kernel<T, V, 512, false>)
+                                         : (vector ? &norm_grad_kernel<T, V, 256, true> : &norm_grad_kernel<T, V, 256, false>);
+    static Held held[2][17];
+    const int64_t blocks = held[vector][s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
+    if (blocks < 0) return PRUNER_EHIP;
+    *parts = (int)blocks;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(dh), dh_pitch, static_cast<const T*>(dy),
                        dy_pitch, static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch, kept ? kept->codes : nullptr, kept ? kept->exps : nullptr,
                        static_cast<T*>(dx), static_cast<T*>(df), static_cast<T*>(dgate), sums);
     PRUNER_LAUNCH_CHECK();
@@ -403,8 +450,6 @@ extern "C" int pruner_gated_norm(const pruner_norm* p, const void* x, int64_t x_
     if (!matrix_ok(x, x_pitch, p) || (f && !matrix_ok(f, f_pitch, p)) || (f && !vector_ok(p->w_post)) || !gate_ok(p)) return PRUNER_EINVAL;
     if ((h && !aligned(h, bytes)) || (y && !aligned(y, bytes)) || (kept_y && !kept_ok(kept_y)) || ((y || kept_y) && !vector_ok(p->w_pre))) return PRUNER_EINVAL;
     if (!h && !y && !kept_y) return PRUNER_EINVAL;
-    int cus = 0;
-    if (current_device(&cus) < 0) return PRUNER_EHIP;
     Access a;
     a.fits(x, bytes, x_pitch);
     a.fits(f, bytes, f_pitch);
@@ -412,7 +457,7 @@ extern "C" int pruner_gated_norm(const pruner_norm* p, const void* x, int64_t x_
     a.fits(h, bytes, p->dim);
     a.fits(y, bytes, p->dim);
     if (kept_y) a.fits(kept_y->codes, 1, p->dim);
-    const Shape s = shape_of(p->rows, p->dim, 8ll * cus);
+    const Shape s = shape_of(p->rows, p->dim, 1 << 22);
     return BY_TYPE_AND_ACCESS(p->dtype, a.v, run_norm, p, s, x, x_pitch, f, f_pitch, h, y, kept_y, static_cast<hipStream_t>(stream));
 }
 
@@ -439,8 +484,6 @@ extern "C" int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int6
         if (!dx || !aligned(dx, bytes) || (has_f && (!df || !aligned(df, bytes)))) return PRUNER_EINVAL;
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < pruner_gated_norm_grad_workspace_bytes(p->rows, p->dim)) return PRUNER_EWORKSPACE;
     }
-    int cus = 0;
-    if (current_device(&cus) < 0) return PRUNER_EHIP;
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* const sums = static_cast<float*>(workspace);
     int parts = 0;
@@ -457,11 +500,9 @@ extern "C" int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int6
         a.fits(df, bytes, p->dim);
         Norm n = norm_of(p, 0);
         if (!has_f) n.gate = nullptr;
-        const int64_t most = 4ll * cus < kMaxParts ? 4ll * cus : kMaxParts;
-        const Shape s = shape_of(p->rows, p->dim, most);
-        parts = s.blocks;
+        const Shape s = shape_of(p->rows, p->dim, kMaxParts);
         const pruner_norm q{p->rows, p->dim, p->dtype, p->center, p->alpha, p->eps, p->w_post, p->w_pre, n.gate, p->gate_pitch};
-        const int rc = BY_TYPE_AND_ACCESS(p->dtype, a.v, run_norm_grad, &q, s, dh, dh_pitch, dy, dy_pitch, x, x_pitch, f, f_pitch, kept_f, dx, df, gate_rows ? dgate : nullptr, sums, st);
+        const int rc = BY_TYPE_AND_ACCESS(p->dtype, a.v, run_norm_grad, &q, s, dh, dh_pitch, dy, dy_pitch, x, x_pitch, f, f_pitch, kept_f, dx, df, gate_rows ? dgate : nullptr, sums, &parts, st);
         if (rc) return rc;
     }
     hipLaunchKernelGGL(norm_sums_kernel, dim3((p->dim + 31) / 32, 3), dim3(1024), 0, st, sums, parts, p->dim, has_f ? dw_post : nullptr, dw_pre,
