@@ -383,7 +383,7 @@ int pruner_checkpoint_restore(const pruner_checkpoint* kept, int32_t dtype, int6
  * The weight gradient of a linear layer y = W x from its input's checkpoint:  dW[n][k] (+)= sum_r dy[r][n] x^[r][k].
  * The restored x^ enters the matrix cores in dy's type, products accumulate in binary32, and rows are summed in an order that
  * depends on the sizes alone.
- *   dy          device [rows][dy_pitch], PRUNER_BF16 or PRUNER_F16; dy_pitch >= n_out
+ *   dy          device [rows][dy_pitch], PRUNER_BF16 or PRUNER_F16; n_out <= dy_pitch < 2^24
  *   kept        the input's checkpoint, [rows][dim]
  *   dw          device float [n_out][dim]
  *   accumulate  0: dw is overwritten; 1: added to

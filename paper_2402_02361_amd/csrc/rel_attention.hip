@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
     int part = 0, bh, q0;
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, heads, (uint32_t)q_tiles * parts.count);
+        const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles * parts.count);
         bh = it.head;
         part = it.tile % parts.count;
         q0 = it.tile / parts.count * 128 + 32 * wave;

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
     int bh, q0, tile_id = 0;
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, heads, (uint32_t)q_tiles);
+        const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles);
         bh = it.head;
         tile_id = it.tile;
         q0 = it.tile * 128 + 32 * wave;
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     const uint32_t heads = (uint32_t)a.batch * a.kv_heads;
     int part = 0, bh, k0;
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, heads, (uint32_t)k_tiles * gr.parts);
+        const Item it = item_of(blockIdx.x, heads, 1, (uint32_t)k_tiles * gr.parts);
         bh = it.head;
         part = it.tile % gr.parts;
         k0 = (k_tiles - 1 - it.tile / gr.parts) * Shape::kKeys + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
