@@ -83,7 +83,7 @@ struct Args {
     int32_t batch, q_tokens, k_tokens, q_heads, kv_heads, group, head_dim, causal, two_sided, n_edges;
     float scale;
     int32_t left, right;   // pairs at r <= -left share one bucket, those at r >= right share one (both cut to what the lengths can reach)
-    int32_t edges[PRUNER_MAX_BIAS_EDGES];
+    int32_t edges[PRUNER_MAX_BIAS_EDGES];   // INT32_MAX from n_edges on
     __device__ __forceinline__ int queries(int b) const { return clamped(q_len, b, q_tokens); }
     __device__ __forceinline__ int keys(int b) const { return clamped(k_len, b, k_tokens); }
     __device__ __forceinline__ static int clamped(const int32_t* p, int b, int most)
@@ -96,7 +96,9 @@ struct Args {
     {
         const int d = two_sided ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
         int n = 0;
-        for (int e = 0; e < n_edges; ++e) n += edges[e] <= d ? 1 : 0;
+        for (int e = 0; e < n_edges; e += 16)   // (sixteen by one scalar load; those past the last are beyond every distance)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) n += edges[e + k] <= d ? 1 : 0;
         return n + (two_sided && r > 0 ? n_edges + 1 : 0);
     }
     template <typename T> __device__ __forceinline__ float bias(int n, int h) const { return (float)static_cast<const T*>(table)[(int64_t)n * q_heads + h]; }
@@ -228,7 +230,7 @@ template <typename T> __device__ __forceinline__ u32x4 weights_of(const floatx16
 
 // Workgroups go to the eight dies in turn.  Item i of (sequences x key heads) x (query heads that share one) x tiles, for a kernel whose workgroups read what
 // the others of their key head read: a die takes every eighth key head, so that sequences of different lengths spread over the dies (a run of heads per
-// die instead: 16 sequences of up to 777 tokens, 12 heads of 64, 43 us where this takes SPREAD), of all of them the last tiles first (under a causal
+// die instead: 16 sequences of up to 777 tokens, 12 heads of 64, 43 us where this takes 37), of all of them the last tiles first (under a causal
 // mask these are the longest).
 struct Item {
     int head, tile;

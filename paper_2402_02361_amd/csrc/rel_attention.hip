@@ -528,6 +528,7 @@ int attention_args(const pruner_attention* a, const pruner_heads* q, const prune
     r.causal = (a->flags & PRUNER_ATTENTION_CAUSAL) != 0;
     r.two_sided = (a->flags & PRUNER_ATTENTION_TWO_SIDED) != 0;
     r.scale = a->scale;
+    for (int e = 0; e < PRUNER_MAX_BIAS_EDGES; ++e) r.edges[e] = INT32_MAX;
     if (a->table) {
         int last = 0;
         for (int e = 0; e < a->n_edges; ++e) {
