@@ -117,10 +117,13 @@ __device__ __forceinline__ bool finish_scores(floatx16 (&s)[N], const Args& a, c
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -ATT_INF : __builtin_fmaf(__builtin_amdgcn_logf(l), kLn2, m); }   // (logf: base 2)
 
+// Turns of a shared tile in LDS: the one that is worked on and those on their way.
+constexpr int turns_of(int dp, bool shared) { return !shared ? 1 : dp == 128 ? 2 : 3; }
+
 template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
 {
-    constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;
+    constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED);
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
@@ -139,8 +142,8 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     const int ql = a.queries(b), kl = a.keys(b);
     const Window window(a.left, a.right);
     const int window_bytes = a.table ? (window.size * 4 + 15) & ~15 : 0;
-    char* const tiles = lds + (SHARED ? window_bytes : 4 * window_bytes + wave * 2 * kTileBytes);
-    float* const biases = reinterpret_cast<float*>(lds + (SHARED ? 0 : wave * window_bytes));
+    char* const tiles = lds + (SHARED ? 0 : wave * 2 * kTileBytes);
+    float* const biases = reinterpret_cast<float*>(lds + (SHARED ? kTurns : 4) * 2 * kTileBytes + (SHARED ? 0 : wave * window_bytes));
 
     // the keys that this workgroup's queries see, and of them this part's
     const int first_q = SHARED ? q0 - 32 * wave : 0, rows_here = SHARED ? 128 : 32;
@@ -150,6 +153,28 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     const int begin = part * parts.keys;
     if (parts.count > 1) end = end < begin + parts.keys ? end : begin + parts.keys;
 
+    const T* const kp = a.k.at<T>(b, hk);
+    const T* const vp = a.v.at<T>(b, hk);
+    Stage<T, DP, kN, kThreads> ks, vs;       // a wavefront's own tiles
+    Flow<T, DP, kKeys, 256> kf, vf;          // shared ones
+    if constexpr (SHARED) {
+        kf.set(a.k.token, a.head_dim, thread, wave);
+        vf.set(a.v.token, a.head_dim, thread, wave);
+    } else {
+        ks.set(a.k.token, a.head_dim, thread);
+        vs.set(a.v.token, a.head_dim, thread);
+    }
+    auto request = [&](int key0, int turn) {
+        const uint32_t to = (uint32_t)(turn * 2 * kTileBytes);
+        const int left = key0 < end ? kl - key0 : 0;
+        kf.request(kp + (int64_t)key0 * a.k.token, left, to);
+        vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
+    };
+    if constexpr (SHARED) {
+        if (begin < end)
+#pragma unroll
+            for (int t = 0; t < kTurns - 1; ++t) request(begin + t * kN, t);
+    }
     Lane<DP> at;
     at.set(lane);
     const int i = q0 + l32, p = kl - ql + i;
@@ -158,35 +183,40 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     Running<T, DP> run;
     run.clear();
     if (begin < end) {
-        const T* const kp = a.k.at<T>(b, hk);
-        const T* const vp = a.v.at<T>(b, hk);
-        Stage<T, DP, kN, kThreads> ks, vs;
-        ks.set(a.k.token, a.head_dim, thread);
-        vs.set(a.v.token, a.head_dim, thread);
-        ks.fetch(kp + (int64_t)begin * a.k.token, kl - begin);
-        vs.fetch(vp + (int64_t)begin * a.v.token, kl - begin);
+        if constexpr (!SHARED) {
+            ks.fetch(kp + (int64_t)begin * a.k.token, kl - begin);
+            vs.fetch(vp + (int64_t)begin * a.v.token, kl - begin);
+        }
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
             bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
             fill_window<T>(a, biases, h, thread, kThreads);
         }
-        ks.park(tiles, thread);
-        vs.park(tiles + kTileBytes, thread);
+        if constexpr (!SHARED) {
+            ks.park(tiles, thread);
+            vs.park(tiles + kTileBytes, thread);
+        }
         // of this wavefront's queries
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
         const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
         int turn = 0;
         for (int key0 = begin; key0 < end; key0 += kN) {
-            if constexpr (SHARED) __syncthreads(); else wave_fence();
-            const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
             const bool more = key0 + kN < end;
-            if (more) {
-                const int next = key0 + kN;
-                ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
-                vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
+            if constexpr (SHARED) {
+                wait_for<(kTurns - 2) * 2 * Flow<T, DP, kKeys, 256>::kEach>();
+                __syncthreads();   // (and the tile before is done with)
+                request(key0 + (kTurns - 1) * kN, turn == 0 ? kTurns - 1 : turn - 1);
+            } else {
+                wave_fence();
+                if (more) {
+                    const int next = key0 + kN;
+                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
+                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
+                }
             }
+            const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
             if (key0 < seen) {
                 floatx16 s[kN / 32];
 #pragma unroll
@@ -210,16 +240,16 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
                     }
             }
             if constexpr (SHARED) {
-                turn ^= 1;
+                turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
                 wave_fence();
-            }
-            if (more) {
-                char* const to = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
-                ks.park(to, thread);
-                vs.park(to + kTileBytes, thread);
+                if (more) {
+                    ks.park(tiles, thread);
+                    vs.park(tiles + kTileBytes, thread);
+                }
             }
         }
+        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
     }
     if (i >= a.q_tokens) return;
     const float l = sum_of_halves(run.l);
@@ -469,7 +499,7 @@ template <typename T, int DP> int run(const Args& args, const Plan& plan, const 
         const size_t tiles = (size_t)places.biases + places.buckets + 8 * kOwnKeys * DP * 2;
         hipLaunchKernelGGL((rows_kernel<T, DP>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > tiles ? last : tiles, st, args, out, lse, parts);
     } else {
-        hipLaunchKernelGGL((tile_kernel<T, DP, true>), dim3((unsigned)(heads * plan.q_tiles * plan.parts)), dim3(256), window + 4 * kKeys * DP * 2, st, args, out, lse, parts,
+        hipLaunchKernelGGL((tile_kernel<T, DP, true>), dim3((unsigned)(heads * plan.q_tiles * plan.parts)), dim3(256), window + turns_of(DP, true) * 2 * kKeys * DP * 2, st, args, out, lse, parts,
                            plan.q_tiles);
     }
     PRUNER_LAUNCH_CHECK();
