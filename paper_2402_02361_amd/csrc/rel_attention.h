@@ -287,6 +287,9 @@ __device__ __forceinline__ Item item_of(uint32_t id, uint32_t key_heads, uint32_
     return Item{(int)(id % heads), (int)(tiles - 1 - id / heads)};
 }
 
+// Turns of a shared tile in LDS: the one that is worked on and those on their way.
+constexpr int turns_of(int dp, bool shared, int rows) { return !shared ? 1 : dp * rows >= 8192 ? 2 : 3; }
+
 // ---- host
 
 bool heads_ok(const pruner_heads* h);

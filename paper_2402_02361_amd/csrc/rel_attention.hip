@@ -117,13 +117,10 @@ __device__ __forceinline__ bool finish_scores(floatx16 (&s)[N], const Args& a, c
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -ATT_INF : __builtin_fmaf(__builtin_amdgcn_logf(l), kLn2, m); }   // (logf: base 2)
 
-// Turns of a shared tile in LDS: the one that is worked on and those on their way.
-constexpr int turns_of(int dp, bool shared) { return !shared ? 1 : dp == 128 ? 2 : 3; }
-
 template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
 {
-    constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED);
+    constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
@@ -459,7 +456,8 @@ Plan plan_of(const pruner_attention* a)
     int64_t groups = p.route == Route::kRows ? (int64_t)a->batch * a->kv_heads : (int64_t)a->batch * a->q_heads * p.q_tiles;
     if (p.route != Route::kOwn && groups > 0) {
         const int fewest = 512;   // keys of a part at least
-        int64_t parts = ((p.route == Route::kRows ? kEnoughRows : kEnough) + groups - 1) / groups;
+        const int64_t enough = p.route == Route::kRows ? kEnoughRows : groups >= kEnough / 2 ? groups : kEnough;   // (cut only what leaves the device half empty)
+        int64_t parts = (enough + groups - 1) / groups;
         const int64_t most = ((int64_t)a->k_tokens + fewest - 1) / fewest;
         parts = parts < most ? parts : most;
         if (parts < 1) parts = 1;
@@ -499,7 +497,7 @@ template <typename T, int DP> int run(const Args& args, const Plan& plan, const 
         const size_t tiles = (size_t)places.biases + places.buckets + 8 * kOwnKeys * DP * 2;
         hipLaunchKernelGGL((rows_kernel<T, DP>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > tiles ? last : tiles, st, args, out, lse, parts);
     } else {
-        hipLaunchKernelGGL((tile_kernel<T, DP, true>), dim3((unsigned)(heads * plan.q_tiles * plan.parts)), dim3(256), window + turns_of(DP, true) * 2 * kKeys * DP * 2, st, args, out, lse, parts,
+        hipLaunchKernelGGL((tile_kernel<T, DP, true>), dim3((unsigned)(heads * plan.q_tiles * plan.parts)), dim3(256), window + turns_of(DP, true, kKeys) * 2 * kKeys * DP * 2, st, args, out, lse, parts,
                            plan.q_tiles);
     }
     PRUNER_LAUNCH_CHECK();

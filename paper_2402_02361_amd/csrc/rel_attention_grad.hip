@@ -29,11 +29,23 @@ template <> struct Held<_Float16> {
 struct Grad {
     Heads dout, o, out0, out1;   // out0, out1: dq, or dk and dv
     const float* lse;
-    float* delta;                // [batch][q_heads][q_tokens]
+    float* stats;                // [3][batch][q_heads][stat_rows]: see leave_stats
+    int stat_rows;               // q_tokens rounded up to 32
     float* diagonals;            // [part][q_heads][window + 2]
     float* sums;                 // [part][batch][kv_heads][k_tokens][2][DP]
     int parts;
 };
+
+// What the keys' kernel needs of a query: lse (plus infinity without a key, or where there is no query: every weight is then exp(-infinity)), what is added to the exponent of 2, and
+// -delta, both as they go with the form in which the weights are held.
+template <typename T> __device__ __forceinline__ void leave_stats(const Grad& gr, int64_t heads, int bh, int i, float lse, float delta)
+{
+    if (i >= gr.stat_rows) return;
+    const int64_t all = heads * gr.stat_rows, row = (int64_t)bh * gr.stat_rows + i;
+    gr.stats[row] = lse;
+    gr.stats[all + row] = Held<T>::kShift - lse * kLog2e;
+    gr.stats[2 * all + row] = -delta * Held<T>::kUnit;
+}
 
 // Sums of a 32 x 32 result along its diagonals, sixteen rows at a time: element (row, column) goes to place row of line row - column + 31, so a
 // line is a diagonal; lane d adds line d's sixteen places (those that no element reaches stay zero) and adds that to its diagonal's sum.  Lines are 18
@@ -63,7 +75,7 @@ __device__ __forceinline__ void add_diagonals(float* skew, float* sums, const fl
 template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_tiles)
 {
-    constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes;   // (128: registers for 32 rows on their way)
+    constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);   // (64 keys of 128 would leave no room for a second workgroup)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
@@ -84,7 +96,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
     // LDS: tiles, biases, every wavefront's diagonals and its skewed square
     char* const tiles = lds + (SHARED ? 0 : wave * 2 * kTileBytes);
-    float* const floats = reinterpret_cast<float*>(lds + (SHARED ? 4 : 8) * kTileBytes);
+    float* const floats = reinterpret_cast<float*>(lds + (SHARED ? 2 * kTurns : 8) * kTileBytes);
     float* const biases = floats + (SHARED ? 0 : wave * window_floats);
     float* const all_diagonals = floats + (SHARED ? 1 : 4) * window_floats;
     float* const diagonals = all_diagonals + wave * window_floats;
@@ -95,6 +107,28 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     int end = first_q >= ql ? 0 : a.causal ? kl - ql + last_q + 1 : kl;
     end = end < kl ? end : kl;
 
+    const T* const kp = a.k.at<T>(b, hk);
+    const T* const vp = a.v.at<T>(b, hk);
+    Stage<T, DP, kN, kThreads> ks, vs;                    // a wavefront's own tiles
+    Flow<T, DP, SHARED ? kN : 64, 256> kf, vf;            // shared ones
+    if constexpr (SHARED) {
+        kf.set(a.k.token, a.head_dim, thread, wave);
+        vf.set(a.v.token, a.head_dim, thread, wave);
+    } else {
+        ks.set(a.k.token, a.head_dim, thread);
+        vs.set(a.v.token, a.head_dim, thread);
+    }
+    auto request = [&](int key0, int turn) {
+        const uint32_t to = (uint32_t)(turn * 2 * kTileBytes);
+        const int left = key0 < end ? kl - key0 : 0;
+        kf.request(kp + (int64_t)key0 * a.k.token, left, to);
+        vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
+    };
+    if constexpr (SHARED) {
+        if (end > 0)
+#pragma unroll
+            for (int t = 0; t < kTurns - 1; ++t) request(t * kN, t);
+    }
     Lane<DP> at;
     at.set(lane);
     const int i = q0 + l32, p = kl - ql + i;
@@ -120,7 +154,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 delta = __builtin_fmaf(x[1], y[1], delta);
             }
         delta = sum_of_halves(delta);
-        if (half == 0 && i < a.q_tokens) gr.delta[row] = delta;
+        if (half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
     }
     floatx16 dq[Tile<DP>::kBlocks];
 #pragma unroll
@@ -131,21 +165,20 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
     }
     if (end > 0) {
-        const T* const kp = a.k.at<T>(b, hk);
-        const T* const vp = a.v.at<T>(b, hk);
-        Stage<T, DP, kN, kThreads> ks, vs;
-        ks.set(a.k.token, a.head_dim, thread);
-        vs.set(a.v.token, a.head_dim, thread);
-        ks.fetch(kp, kl);
-        vs.fetch(vp, kl);
+        if constexpr (!SHARED) {
+            ks.fetch(kp, kl);
+            vs.fetch(vp, kl);
+        }
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
             bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
             fill_window<T>(a, biases, h, thread, kThreads);
         }
-        ks.park(tiles, thread);
-        vs.park(tiles + kTileBytes, thread);
+        if constexpr (!SHARED) {
+            ks.park(tiles, thread);
+            vs.park(tiles + kTileBytes, thread);
+        }
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
         const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
@@ -201,14 +234,20 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         }
         int turn = 0;
         for (int key0 = 0; key0 < end; key0 += kN) {
-            if constexpr (SHARED) __syncthreads(); else wave_fence();
-            const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
             const bool more = key0 + kN < end;
-            if (more) {
-                const int next = key0 + kN;
-                ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
-                vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
+            if constexpr (SHARED) {
+                wait_for<(kTurns - 2) * 2 * Flow<T, DP, SHARED ? kN : 64, 256>::kEach>();
+                __syncthreads();   // (and the tile before is done with)
+                request(key0 + (kTurns - 1) * kN, turn == 0 ? kTurns - 1 : turn - 1);
+            } else {
+                wave_fence();
+                if (more) {
+                    const int next = key0 + kN;
+                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
+                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
+                }
             }
+            const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
 #pragma unroll
             for (int n = 0; n < kN / 32; ++n) {
                 const int k0 = key0 + 32 * n;
@@ -238,18 +277,18 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 }
             }
             if constexpr (SHARED) {
-                turn ^= 1;
+                turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
                 wave_fence();
-            }
-            if (more) {
-                char* const to = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
-                ks.park(to, thread);
-                vs.park(to + kTileBytes, thread);
+                if (more) {
+                    ks.park(tiles, thread);
+                    vs.park(tiles + kTileBytes, thread);
+                }
             }
         }
+        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is used for other things, or no longer this workgroup's)
     }
-    if (!SHARED && half == 0 && i < a.q_tokens) gr.delta[row] = delta;
+    if (!SHARED && half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
     if (i < a.q_tokens) store_row<T, DP>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token, dq, a.scale, a.head_dim, half);
     if (!a.table) return;
     // what this workgroup (wavefront) saw of every diagonal
@@ -288,8 +327,9 @@ template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr bool kWide = SHARED && DP == 128;
     static constexpr int kWaves = kWide ? 8 : 4;              // of a workgroup
     static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
-    static constexpr int kTurns = SHARED ? 2 : 1;
-    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kQ * 4;
+    static constexpr int kTurns = SHARED ? (kWide ? 2 : 3) : 1;
+    static constexpr int kStat = 64;                          // floats of a tile's stats, three of them
+    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kStat * 4;
     static constexpr int kHeldBytes = kWide ? Tile<DP>::kSteps * 1024 : 0;   // of a wavefront
     static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
 };
@@ -299,6 +339,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     typedef KeysShape<T, DP, SHARED> Shape;
     constexpr int kQ = Shape::kQ, kThreads = SHARED ? 64 * Shape::kWaves : 64, kTileBytes = Shape::kTileBytes, kTurnBytes = Shape::kTurnBytes;
     constexpr bool kWide = Shape::kWide;
+    constexpr int kTurns = Shape::kTurns, kStat = Shape::kStat;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.kv_heads;
@@ -318,7 +359,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     const Window window(a.left, a.right);
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
     char* const turns = lds + (SHARED ? 0 : wave * kTurnBytes);
-    char* const held = lds + 2 * kTurnBytes + wave * Shape::kHeldBytes + 16 * lane;
+    char* const held = lds + Shape::kTurns * kTurnBytes + wave * Shape::kHeldBytes + 16 * lane;
     float* const biases = reinterpret_cast<float*>(lds + (SHARED ? Shape::kTurns * kTurnBytes + Shape::kWaves * Shape::kHeldBytes : 4 * kTurnBytes)) + (SHARED ? 0 : wave * window_floats);
 
     // query tiles that see any of this workgroup's keys
@@ -330,6 +371,48 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     const int64_t total = (int64_t)each * a.group;
     const int from = (int)(total * part / gr.parts), to = (int)(total * (part + 1) / gr.parts);
 
+    Stage<T, DP, kQ, kThreads> qs, os;       // a wavefront's own tiles
+    Flow<T, DP, SHARED ? kQ : 64, SHARED ? kThreads : 256> qf, of;   // shared ones
+    if constexpr (SHARED) {
+        qf.set(a.q.token, a.head_dim, thread, wave);
+        of.set(gr.dout.token, a.head_dim, thread, wave);
+    } else {
+        qs.set(a.q.token, a.head_dim, thread);
+        os.set(gr.dout.token, a.head_dim, thread);
+    }
+    const int64_t all = (int64_t)a.batch * a.q_heads * gr.stat_rows;
+    float stat[3] = {0.f, 0.f, 0.f};
+    auto fetch = [&](int n) {
+        const int h = hk * a.group + n / each, i0 = (first_tile + n % each) * kQ;
+        qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, ql - i0);
+        os.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, ql - i0);
+        const int64_t row = ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0 + thread;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) stat[w] = thread < kQ && i0 + thread < ql ? gr.stats[w * all + row] : w == 0 ? ATT_INF : w == 1 ? -ATT_INF : 0.f;
+    };
+    auto park = [&](char* turn) {
+        qs.park(turn, thread);
+        os.park(turn + kTileBytes, thread);
+        if (thread < kQ)
+#pragma unroll
+            for (int w = 0; w < 3; ++w) reinterpret_cast<float*>(turn + 2 * kTileBytes)[kStat * w + thread] = stat[w];
+    };
+    // Wavefronts 0 to 2 ask for a stat each.
+    auto request = [&](int n, int turn) {
+        const bool some = n < to;
+        const int h = some ? hk * a.group + n / each : 0, i0 = some ? (first_tile + n % each) * kQ : 0, left = some ? ql - i0 : 0;
+        const uint32_t place = (uint32_t)(turn * kTurnBytes);
+        qf.request(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, left, place);
+        of.request(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, left, place + kTileBytes);
+        if (wave < 3)
+            request_4(place + 2 * kTileBytes + 4 * kStat * wave, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
+                      buffer_of(gr.stats + wave * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
+    };
+    if constexpr (SHARED) {
+        if (from < to)
+#pragma unroll
+            for (int t = 0; t < kTurns - 1; ++t) request(from + t, t);
+    }
     Lane<DP> at;
     at.set(lane);
     const int j = k0 + l32;
@@ -351,34 +434,10 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
 
     if (from < to) {
-        Stage<T, DP, kQ, kThreads> qs, ds_;
-        qs.set(a.q.token, a.head_dim, thread);
-        ds_.set(gr.dout.token, a.head_dim, thread);
-        float stat_lse = 0.f, stat_delta = 0.f;
-        auto fetch = [&](int n) {
-            const int h = hk * a.group + n / each, i0 = (first_tile + n % each) * kQ;
-            qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, ql - i0);
-            ds_.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, ql - i0);
-            if (thread < kQ) {
-                const bool in = i0 + thread < ql;
-                const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tokens + i0 + thread;
-                stat_lse = in ? gr.lse[row] : -ATT_INF;
-                stat_delta = in ? gr.delta[row] : 0.f;
-            }
-        };
-        auto park = [&](char* turn) {
-            qs.park(turn, thread);
-            ds_.park(turn + kTileBytes, thread);
-            if (thread < kQ) {
-                float* const st = reinterpret_cast<float*>(turn + 2 * kTileBytes);
-                const float lse = stat_lse == -ATT_INF ? ATT_INF : stat_lse;
-                st[thread] = lse;
-                st[kQ + thread] = Held<T>::kShift - lse * kLog2e;
-                st[2 * kQ + thread] = -stat_delta * Held<T>::kUnit;
-            }
-        };
-        fetch(from);
-        park(turns);
+        if constexpr (!SHARED) {
+            fetch(from);
+            park(turns);
+        }
         int turn = 0, head_filled = -1;
         float bias_left = 0.f, bias_right = 0.f;
         for (int n = from; n < to; ++n) {
@@ -390,12 +449,22 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                 fill_window<T>(a, biases, h, thread, kThreads);
                 head_filled = g;
             }
-            if constexpr (SHARED) __syncthreads(); else wave_fence();
+            const bool more = n + 1 < to;
+            if constexpr (SHARED) {
+                constexpr int kLater = (kTurns - 2) * 2 * Flow<T, DP, SHARED ? kQ : 64, SHARED ? kThreads : 256>::kEach;
+                if (kLater > 0 && wave < 3)
+                    wait_for<kLater + (kTurns - 2)>();
+                else
+                    wait_for<kLater>();
+                __syncthreads();   // (and the tile before is done with)
+                request(n + kTurns - 1, turn == 0 ? kTurns - 1 : turn - 1);
+            } else {
+                wave_fence();
+                if (more) fetch(n + 1);
+            }
             if constexpr (kWide) at.forget();
             const char* const qt = turns + (SHARED ? turn * kTurnBytes : 0);
             const float* const st = reinterpret_cast<const float*>(qt + 2 * kTileBytes);
-            const bool more = n + 1 < to;
-            if (more) fetch(n + 1);
 #pragma unroll
             for (int m = 0; m < kQ / 32; ++m) {
                 const int p0 = shift + i0 + 32 * m;   // position of the block's first query
@@ -424,7 +493,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                     const float c = a.scale * kLog2e, d = bias * kLog2e;
 #pragma unroll
                     for (int g4 = 0; g4 < 4; ++g4) {
-                        const f32x4 x = *reinterpret_cast<const f32x4*>(st + kQ + 32 * m + 8 * g4 + 4 * half);
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(st + kStat + 32 * m + 8 * g4 + 4 * half);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[4 * g4 + e] = exp2_of(__builtin_fmaf(s[4 * g4 + e], c, x[e] + d));
                     }
@@ -435,7 +504,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                 }
 #pragma unroll
                 for (int g4 = 0; g4 < 4; ++g4) {
-                    const f32x4 x = *reinterpret_cast<const f32x4*>(st + 2 * kQ + 32 * m + 8 * g4 + 4 * half);
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(st + 2 * kStat + 32 * m + 8 * g4 + 4 * half);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) dp[4 * g4 + e] = s[4 * g4 + e] * __builtin_fmaf(dp[4 * g4 + e], Held<T>::kUnit, x[e]);
                 }
@@ -450,12 +519,13 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                 }
             }
             if constexpr (SHARED) {
-                turn ^= 1;
+                turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
                 wave_fence();
+                if (more) park(turns);
             }
-            if (more) park(turns + (SHARED ? turn * kTurnBytes : 0));
         }
+        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
     }
     if (j >= a.k_tokens) return;
     if (j >= kl)   // (what was formed for a key that is not there)
@@ -542,9 +612,9 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
 struct Plan {
     bool own_queries, own_keys;
     int q_tiles, k_tiles, parts, diagonal_parts, width;
-    size_t delta, diagonals, sums, tables, total;   // bytes
+    size_t stats, diagonals, sums, tables, total;   // bytes
 };
-constexpr int64_t kEnough = 1024;
+constexpr int64_t kHeld = 512;   // workgroups that the device holds at once; fewer are cut into parts, for twice as many
 Plan plan_of(const pruner_attention* a)
 {
     Plan p{};
@@ -556,8 +626,8 @@ Plan plan_of(const pruner_attention* a)
     p.parts = 1;
     const int64_t groups = (int64_t)a->batch * a->kv_heads * p.k_tiles, tiles = (int64_t)(a->q_heads / a->kv_heads) * ((a->q_tokens + 31) / 32);
     if (!p.own_keys && groups > 0) {
-        const int64_t enough = padded_dim(a->head_dim) == 128 ? kEnough / 2 : kEnough;   // (workgroups of eight wavefronts)
-        int64_t parts = (enough + groups - 1) / groups;
+        const int64_t held = padded_dim(a->head_dim) == 128 ? kHeld / 2 : kHeld;   // (workgroups of eight wavefronts)
+        int64_t parts = groups >= held ? 1 : (2 * held + groups - 1) / groups;
         const int64_t most = tiles / 8;   // eight query tiles of 32 at least
         parts = parts < most ? parts : most;
         p.parts = parts < 1 ? 1 : (int)parts;
@@ -567,11 +637,11 @@ Plan plan_of(const pruner_attention* a)
     const int most = (int)(reach < PRUNER_MAX_BIAS_DISTANCE ? reach : PRUNER_MAX_BIAS_DISTANCE);
     const int widest = Window(most, a->flags & PRUNER_ATTENTION_TWO_SIDED ? (most > 1 ? most : 1) : 0).size + 2;
     p.diagonal_parts = p.own_queries ? a->batch : a->batch * p.q_tiles;
-    p.delta = round_up((size_t)a->batch * a->q_heads * a->q_tokens * 4, 256);
+    p.stats = round_up((size_t)a->batch * a->q_heads * round_up((size_t)a->q_tokens, 32) * 3 * 4, 256);
     p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
     p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
     p.sums = p.parts > 1 ? round_up((size_t)p.parts * a->batch * a->kv_heads * a->k_tokens * 2 * padded_dim(a->head_dim) * 4, 256) : 0;
-    p.total = p.delta + p.diagonals + p.tables + p.sums;
+    p.total = p.stats + p.diagonals + p.tables + p.sums;
     return p;
 }
 
@@ -602,7 +672,7 @@ template <typename T, int DP> int run(const Call& c)
         if (c.plan.own_queries)
             hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + 4 * skew + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
         else
-            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 5 * window + 4 * skew + 4 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
+            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 5 * window + 4 * skew + turns_of(DP, true, DP < 128 ? 64 : 32) * 2 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
         PRUNER_LAUNCH_CHECK();
     }
     if (a.k_tokens > 0) {
@@ -668,11 +738,12 @@ extern "C" int pruner_rel_attention_grad(const pruner_attention* a, const pruner
     g.dout = att::heads_of(dout);
     g.o = att::heads_of(o);
     g.lse = lse;
-    g.delta = reinterpret_cast<float*>(ws);
-    g.diagonals = reinterpret_cast<float*>(ws + c.plan.delta);
-    c.table_sums = reinterpret_cast<float*>(ws + c.plan.delta + c.plan.diagonals);
-    g.sums = reinterpret_cast<float*>(ws + c.plan.delta + c.plan.diagonals + c.plan.tables);
+    g.stats = reinterpret_cast<float*>(ws);
+    g.diagonals = reinterpret_cast<float*>(ws + c.plan.stats);
+    c.table_sums = reinterpret_cast<float*>(ws + c.plan.stats + c.plan.diagonals);
+    g.sums = reinterpret_cast<float*>(ws + c.plan.stats + c.plan.diagonals + c.plan.tables);
     g.parts = c.plan.parts;
+    g.stat_rows = (int)round_up((size_t)a->q_tokens, 32);
     c.queries = c.keys = g;
     c.queries.out0 = att::heads_of(dq);
     c.keys.out0 = att::heads_of(dk);
