@@ -195,7 +195,7 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
 };
 
 // The same without registers on the way: bounds-checked buffer loads whose data go to LDS (64 lanes' 16 bytes side by side from M0 on), for a tile that all
-// wavefronts of a workgroup share.  What was requested has arrived after wait_for<n>(), n the number of this wavefront's later requests, and is
+// wavefronts of a workgroup share, or one's own.  What was requested has arrived after wait_for<n>(), n the number of this wavefront's later requests, and is
 // there for the others after a barrier.  Tiles that these fill lie in the first 64 KB of LDS.  (A row's chunks are permuted on the way: a
 // lane asks for the chunk whose place it fills.)  The requests are written out because the compiler, seeing them, would wait for all
 // of them before any read of LDS; they return nothing in registers.
@@ -208,6 +208,8 @@ __device__ __forceinline__ void request_4(uint32_t lds, uint32_t at, u32x4 from)
     asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(from) : "memory");
 }
 template <int N> __device__ __forceinline__ void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// Before a wavefront asks for a tile of its own again: what it read of the last one has come.
+__device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ u32x4 buffer_of(const void* base, int bytes)   // base and bytes: the same in all lanes
 {
     const uint64_t p = reinterpret_cast<uint64_t>(base);
@@ -216,23 +218,28 @@ __device__ __forceinline__ u32x4 buffer_of(const void* base, int bytes)   // bas
 }
 template <typename T, int DP, int ROWS, int THREADS> struct Flow {
     static constexpr int kEach = ROWS * Tile<DP>::kChunks / THREADS, kRowStep = THREADS / Tile<DP>::kChunks;
-    static_assert(kEach >= 1 && ROWS * Tile<DP>::kChunks % THREADS == 0 && kRowStep % 16 == 0, "a thread's chunks are of one column, permuted alike");
-    uint32_t at, place;
+    static constexpr int kWays = kRowStep >= 16 ? 1 : 16 / kRowStep;   // permutations that a thread's rows go through in turn
+    static_assert(kEach >= 1 && ROWS * Tile<DP>::kChunks % THREADS == 0 && THREADS % Tile<DP>::kChunks == 0, "a thread's chunks are of whole rows");
+    uint32_t at[kWays], place;
     int32_t row_bytes, width;
-    __device__ __forceinline__ void set(int32_t token, int head_dim, int thread, int wave)
+    __device__ __forceinline__ void set(int32_t token, int head_dim, int thread, int wave)   // wave: of those that share the tile
     {
         row_bytes = token * 2;
         width = head_dim * 2;
-        const int row = thread / Tile<DP>::kChunks, chunk = (thread % Tile<DP>::kChunks) ^ Tile<DP>::turn_of(row);
-        at = 16 * chunk < width ? (uint32_t)row * (uint32_t)row_bytes + 16u * (uint32_t)chunk : 0x80000000u;
         place = 1024u * (uint32_t)wave;
+        const int row = thread / Tile<DP>::kChunks;
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) {
+            const int chunk = (thread % Tile<DP>::kChunks) ^ Tile<DP>::turn_of(row + w * kRowStep);
+            at[w] = 16 * chunk < width ? (uint32_t)row * (uint32_t)row_bytes + 16u * (uint32_t)chunk : 0x80000000u;
+        }
     }
     __device__ __forceinline__ void request(const T* base, int rows, uint32_t tile) const   // tile: its place in LDS
     {
         rows = rows < ROWS ? rows : ROWS;
         const u32x4 from = buffer_of(base, rows > 0 ? (rows - 1) * row_bytes + width : 0);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) request_16(tile + place + u * THREADS * 16u, at, from, (uint32_t)(u * kRowStep * row_bytes));
+        for (int u = 0; u < kEach; ++u) request_16(tile + place + u * THREADS * 16u, at[u % kWays], from, (uint32_t)(u * kRowStep * row_bytes));
     }
 };
 

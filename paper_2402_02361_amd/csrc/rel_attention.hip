@@ -152,26 +152,19 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
 
     const T* const kp = a.k.at<T>(b, hk);
     const T* const vp = a.v.at<T>(b, hk);
-    Stage<T, DP, kN, kThreads> ks, vs;       // a wavefront's own tiles
-    Flow<T, DP, kKeys, 256> kf, vf;          // shared ones
-    if constexpr (SHARED) {
-        kf.set(a.k.token, a.head_dim, thread, wave);
-        vf.set(a.v.token, a.head_dim, thread, wave);
-    } else {
-        ks.set(a.k.token, a.head_dim, thread);
-        vs.set(a.v.token, a.head_dim, thread);
-    }
+    Flow<T, DP, kN, kThreads> kf, vf;
+    kf.set(a.k.token, a.head_dim, thread, SHARED ? wave : 0);
+    vf.set(a.v.token, a.head_dim, thread, SHARED ? wave : 0);
     auto request = [&](int key0, int turn) {
-        const uint32_t to = (uint32_t)(turn * 2 * kTileBytes);
+        const uint32_t to = (uint32_t)((SHARED ? turn : wave) * 2 * kTileBytes);
         const int left = key0 < end ? kl - key0 : 0;
         kf.request(kp + (int64_t)key0 * a.k.token, left, to);
         vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
     };
-    if constexpr (SHARED) {
-        if (begin < end)
+    constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
+    if (begin < end)
 #pragma unroll
-            for (int t = 0; t < kTurns - 1; ++t) request(begin + t * kN, t);
-    }
+        for (int t = 0; t < kAhead; ++t) request(begin + t * kN, t);
     Lane<DP> at;
     at.set(lane);
     const int i = q0 + l32, p = kl - ql + i;
@@ -180,19 +173,11 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     Running<T, DP> run;
     run.clear();
     if (begin < end) {
-        if constexpr (!SHARED) {
-            ks.fetch(kp + (int64_t)begin * a.k.token, kl - begin);
-            vs.fetch(vp + (int64_t)begin * a.v.token, kl - begin);
-        }
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
             bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
             fill_window<T>(a, biases, h, thread, kThreads);
-        }
-        if constexpr (!SHARED) {
-            ks.park(tiles, thread);
-            vs.park(tiles + kTileBytes, thread);
         }
         // of this wavefront's queries
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
@@ -200,18 +185,13 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
         int turn = 0;
         for (int key0 = begin; key0 < end; key0 += kN) {
-            const bool more = key0 + kN < end;
             if constexpr (SHARED) {
-                wait_for<(kTurns - 2) * 2 * Flow<T, DP, kKeys, 256>::kEach>();
+                wait_for<(kTurns - 2) * 2 * Flow<T, DP, kN, kThreads>::kEach>();
                 __syncthreads();   // (and the tile before is done with)
                 request(key0 + (kTurns - 1) * kN, turn == 0 ? kTurns - 1 : turn - 1);
             } else {
+                wait_for<0>();
                 wave_fence();
-                if (more) {
-                    const int next = key0 + kN;
-                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
-                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
-                }
             }
             const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
             if (key0 < seen) {
@@ -239,14 +219,12 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
+                wait_for_reads();
                 wave_fence();
-                if (more) {
-                    ks.park(tiles, thread);
-                    vs.park(tiles + kTileBytes, thread);
-                }
+                if (key0 + kN < end) request(key0 + kN, 0);
             }
         }
-        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
+        wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
     }
     if (i >= a.q_tokens) return;
     const float l = sum_of_halves(run.l);

@@ -109,26 +109,19 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
 
     const T* const kp = a.k.at<T>(b, hk);
     const T* const vp = a.v.at<T>(b, hk);
-    Stage<T, DP, kN, kThreads> ks, vs;                    // a wavefront's own tiles
-    Flow<T, DP, SHARED ? kN : 64, 256> kf, vf;            // shared ones
-    if constexpr (SHARED) {
-        kf.set(a.k.token, a.head_dim, thread, wave);
-        vf.set(a.v.token, a.head_dim, thread, wave);
-    } else {
-        ks.set(a.k.token, a.head_dim, thread);
-        vs.set(a.v.token, a.head_dim, thread);
-    }
+    Flow<T, DP, kN, kThreads> kf, vf;
+    kf.set(a.k.token, a.head_dim, thread, SHARED ? wave : 0);
+    vf.set(a.v.token, a.head_dim, thread, SHARED ? wave : 0);
     auto request = [&](int key0, int turn) {
-        const uint32_t to = (uint32_t)(turn * 2 * kTileBytes);
+        const uint32_t to = (uint32_t)((SHARED ? turn : wave) * 2 * kTileBytes);
         const int left = key0 < end ? kl - key0 : 0;
         kf.request(kp + (int64_t)key0 * a.k.token, left, to);
         vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
     };
-    if constexpr (SHARED) {
-        if (end > 0)
+    constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
+    if (end > 0)
 #pragma unroll
-            for (int t = 0; t < kTurns - 1; ++t) request(t * kN, t);
-    }
+        for (int t = 0; t < kAhead; ++t) request(t * kN, t);
     Lane<DP> at;
     at.set(lane);
     const int i = q0 + l32, p = kl - ql + i;
@@ -165,19 +158,11 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
     }
     if (end > 0) {
-        if constexpr (!SHARED) {
-            ks.fetch(kp, kl);
-            vs.fetch(vp, kl);
-        }
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
             bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
             fill_window<T>(a, biases, h, thread, kThreads);
-        }
-        if constexpr (!SHARED) {
-            ks.park(tiles, thread);
-            vs.park(tiles + kTileBytes, thread);
         }
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
@@ -214,6 +199,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         if constexpr (!SHARED) {
             // delta as the sum of P dP: o is rounded, and with a few keys what it lost is as large as the gradient's own rounding
             for (int key0 = 0; key0 < end; key0 += kN) {
+                wait_for<0>();
                 wave_fence();
                 if (key0 < seen) {
                     floatx16 s, dp;
@@ -221,31 +207,21 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
 #pragma unroll
                     for (int e = 0; e < 16; ++e) delta = __builtin_fmaf(s[e], dp[e], delta);
                 }
+                wait_for_reads();
                 wave_fence();
-                const int next = key0 + kN < end ? key0 + kN : 0;
-                if (end > kN) {
-                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
-                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
-                    ks.park(tiles, thread);
-                    vs.park(tiles + kTileBytes, thread);
-                }
+                if (end > kN) request(key0 + kN < end ? key0 + kN : 0, 0);
             }
             delta = sum_of_halves(delta);
         }
         int turn = 0;
         for (int key0 = 0; key0 < end; key0 += kN) {
-            const bool more = key0 + kN < end;
             if constexpr (SHARED) {
-                wait_for<(kTurns - 2) * 2 * Flow<T, DP, SHARED ? kN : 64, 256>::kEach>();
+                wait_for<(kTurns - 2) * 2 * Flow<T, DP, kN, kThreads>::kEach>();
                 __syncthreads();   // (and the tile before is done with)
                 request(key0 + (kTurns - 1) * kN, turn == 0 ? kTurns - 1 : turn - 1);
             } else {
+                wait_for<0>();
                 wave_fence();
-                if (more) {
-                    const int next = key0 + kN;
-                    ks.fetch(kp + (int64_t)next * a.k.token, kl - next);
-                    vs.fetch(vp + (int64_t)next * a.v.token, kl - next);
-                }
             }
             const char* const kt = tiles + (SHARED ? turn * 2 * kTileBytes : 0);
 #pragma unroll
@@ -279,14 +255,12 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
+                wait_for_reads();
                 wave_fence();
-                if (more) {
-                    ks.park(tiles, thread);
-                    vs.park(tiles + kTileBytes, thread);
-                }
+                if (key0 + kN < end) request(key0 + kN, 0);
             }
         }
-        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is used for other things, or no longer this workgroup's)
+        wait_for<0>();   // (nothing may arrive in LDS that is used for other things, or no longer this workgroup's)
     }
     if (!SHARED && half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
     if (i < a.q_tokens) store_row<T, DP>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token, dq, a.scale, a.head_dim, half);
@@ -334,7 +308,7 @@ template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
 };
 template <typename T, int DP, bool SHARED>
-__global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) keys_kernel(Args a, Grad gr, int k_tiles)
+__global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHARED || DP < 128 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles)
 {
     typedef KeysShape<T, DP, SHARED> Shape;
     constexpr int kQ = Shape::kQ, kThreads = SHARED ? 64 * Shape::kWaves : 64, kTileBytes = Shape::kTileBytes, kTurnBytes = Shape::kTurnBytes;
@@ -371,48 +345,27 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     const int64_t total = (int64_t)each * a.group;
     const int from = (int)(total * part / gr.parts), to = (int)(total * (part + 1) / gr.parts);
 
-    Stage<T, DP, kQ, kThreads> qs, os;       // a wavefront's own tiles
-    Flow<T, DP, SHARED ? kQ : 64, SHARED ? kThreads : 256> qf, of;   // shared ones
-    if constexpr (SHARED) {
-        qf.set(a.q.token, a.head_dim, thread, wave);
-        of.set(gr.dout.token, a.head_dim, thread, wave);
-    } else {
-        qs.set(a.q.token, a.head_dim, thread);
-        os.set(gr.dout.token, a.head_dim, thread);
-    }
+    Flow<T, DP, kQ, kThreads> qf, of;
+    qf.set(a.q.token, a.head_dim, thread, SHARED ? wave : 0);
+    of.set(gr.dout.token, a.head_dim, thread, SHARED ? wave : 0);
     const int64_t all = (int64_t)a.batch * a.q_heads * gr.stat_rows;
-    float stat[3] = {0.f, 0.f, 0.f};
-    auto fetch = [&](int n) {
-        const int h = hk * a.group + n / each, i0 = (first_tile + n % each) * kQ;
-        qs.fetch(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, ql - i0);
-        os.fetch(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, ql - i0);
-        const int64_t row = ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0 + thread;
-#pragma unroll
-        for (int w = 0; w < 3; ++w) stat[w] = thread < kQ && i0 + thread < ql ? gr.stats[w * all + row] : w == 0 ? ATT_INF : w == 1 ? -ATT_INF : 0.f;
-    };
-    auto park = [&](char* turn) {
-        qs.park(turn, thread);
-        os.park(turn + kTileBytes, thread);
-        if (thread < kQ)
-#pragma unroll
-            for (int w = 0; w < 3; ++w) reinterpret_cast<float*>(turn + 2 * kTileBytes)[kStat * w + thread] = stat[w];
-    };
-    // Wavefronts 0 to 2 ask for a stat each.
+    // Of those that share a tile, wavefronts 0 to 2 ask for a stat each.
     auto request = [&](int n, int turn) {
         const bool some = n < to;
         const int h = some ? hk * a.group + n / each : 0, i0 = some ? (first_tile + n % each) * kQ : 0, left = some ? ql - i0 : 0;
-        const uint32_t place = (uint32_t)(turn * kTurnBytes);
+        const uint32_t place = (uint32_t)((SHARED ? turn : wave) * kTurnBytes);
         qf.request(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, left, place);
         of.request(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, left, place + kTileBytes);
-        if (wave < 3)
-            request_4(place + 2 * kTileBytes + 4 * kStat * wave, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
-                      buffer_of(gr.stats + wave * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
-    };
-    if constexpr (SHARED) {
-        if (from < to)
 #pragma unroll
-            for (int t = 0; t < kTurns - 1; ++t) request(from + t, t);
-    }
+        for (int w = 0; w < 3; ++w)
+            if (!SHARED || wave == w)
+                request_4(place + 2 * kTileBytes + 4 * kStat * w, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
+                          buffer_of(gr.stats + w * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
+    };
+    constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
+    if (from < to)
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) request(from + t, t);
     Lane<DP> at;
     at.set(lane);
     const int j = k0 + l32;
@@ -434,10 +387,6 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
     for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
 
     if (from < to) {
-        if constexpr (!SHARED) {
-            fetch(from);
-            park(turns);
-        }
         int turn = 0, head_filled = -1;
         float bias_left = 0.f, bias_right = 0.f;
         for (int n = from; n < to; ++n) {
@@ -449,9 +398,8 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                 fill_window<T>(a, biases, h, thread, kThreads);
                 head_filled = g;
             }
-            const bool more = n + 1 < to;
             if constexpr (SHARED) {
-                constexpr int kLater = (kTurns - 2) * 2 * Flow<T, DP, SHARED ? kQ : 64, SHARED ? kThreads : 256>::kEach;
+                constexpr int kLater = (kTurns - 2) * 2 * Flow<T, DP, kQ, kThreads>::kEach;
                 if (kLater > 0 && wave < 3)
                     wait_for<kLater + (kTurns - 2)>();
                 else
@@ -459,8 +407,8 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
                 __syncthreads();   // (and the tile before is done with)
                 request(n + kTurns - 1, turn == 0 ? kTurns - 1 : turn - 1);
             } else {
+                wait_for<0>();
                 wave_fence();
-                if (more) fetch(n + 1);
             }
             if constexpr (kWide) at.forget();
             const char* const qt = turns + (SHARED ? turn * kTurnBytes : 0);
@@ -521,11 +469,12 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), 2) ke
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;
             } else {
+                wait_for_reads();
                 wave_fence();
-                if (more) park(turns);
+                if (n + 1 < to) request(n + 1, 0);
             }
         }
-        if constexpr (SHARED) wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
+        wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
     }
     if (j >= a.k_tokens) return;
     if (j >= kl)   // (what was formed for a key that is not there)
