@@ -420,8 +420,7 @@ struct Plan {
     int64_t rows;
     size_t workspace;
 };
-constexpr int64_t kEnough = 1024;       // workgroups that fill the device: four for each of 256 compute units
-constexpr int64_t kEnoughRows = 4096;   // ... where all they do is read, and their sequences' lengths differ (32 caches of up to 32768 tokens, 8 heads of 128:
+constexpr int64_t kEnoughRows = 4096;   // workgroups that fill the device where all they do is read, and their sequences' lengths differ (32 caches of up to 32768 tokens, 8 heads of 128:
                                         // 536 us with 2048, 476 with 4096, 468 and more to join with 8192)
 Plan plan_of(const pruner_attention* a)
 {
@@ -431,13 +430,19 @@ Plan plan_of(const pruner_attention* a)
     p.q_tiles = (a->q_tokens + 127) / 128;
     p.parts = 1;
     p.route = a->q_tokens <= 32 && a->k_tokens <= 2 * kOwnKeys ? Route::kOwn : (int64_t)a->q_tokens * group <= 32 ? Route::kRows : Route::kTiles;
-    int64_t groups = p.route == Route::kRows ? (int64_t)a->batch * a->kv_heads : (int64_t)a->batch * a->q_heads * p.q_tiles;
+    const int64_t groups = p.route == Route::kRows ? (int64_t)a->batch * a->kv_heads : (int64_t)a->batch * a->q_heads * p.q_tiles;
     if (p.route != Route::kOwn && groups > 0) {
-        const int fewest = 512;   // keys of a part at least
-        const int64_t enough = p.route == Route::kRows ? kEnoughRows : groups >= kEnough / 2 ? groups : kEnough;   // (cut only what leaves the device half empty)
-        int64_t parts = (enough + groups - 1) / groups;
-        const int64_t most = ((int64_t)a->k_tokens + fewest - 1) / fewest;
-        parts = parts < most ? parts : most;
+        const int dp = padded_dim(a->head_dim);
+        int64_t parts;
+        if (p.route == Route::kRows) {
+            const int fewest = 512;   // keys of a part at least
+            parts = (kEnoughRows + groups - 1) / groups;
+            const int64_t most = ((int64_t)a->k_tokens + fewest - 1) / fewest;
+            parts = parts < most ? parts : most;
+        } else {   // (steps as measured: 8192 causal tokens, 16 heads of 128; 5417, 4 of 64)
+            parts = parts_of((double)groups, (a->k_tokens + kKeys - 1) / kKeys, a->flags & PRUNER_ATTENTION_CAUSAL, dp == 128 ? 512 : 768, dp == 128 ? 1.5 : dp == 64 ? 1.1 : 0.8,
+                             dp == 32 ? 1.6 : 2.2, (double)p.rows * dp * 4);
+        }
         if (parts < 1) parts = 1;
         const int64_t keys = ((a->k_tokens + parts - 1) / parts + kKeys - 1) / kKeys * kKeys;
         p.part_keys = (int)(keys > 0 ? keys : kKeys);

@@ -32,8 +32,8 @@ struct Grad {
     float* stats;                // [3][batch][q_heads][stat_rows]: see leave_stats
     int stat_rows;               // q_tokens rounded up to 32
     float* diagonals;            // [part][q_heads][window + 2]
-    float* sums;                 // [part][batch][kv_heads][k_tokens][2][DP]
-    int parts;
+    float* sums;                 // of the parts: [part][batch][q_heads][q_tokens][DP], or [part][batch][kv_heads][k_tokens][2][DP]
+    int parts, part_keys;        // part_keys: of the queries' kernel, a multiple of 64
 };
 
 // What the keys' kernel needs of a query: lse (plus infinity without a key, or where there is no query: every weight is then exp(-infinity)), what is added to the exponent of 2, and
@@ -52,6 +52,7 @@ template <typename T> __device__ __forceinline__ void leave_stats(const Grad& gr
 // floats apart: 32 columns' writes meet two to a bank, the lanes' 8-byte reads none.  (Adding element by element into the sums, by LDS additions,
 // took 157 us where this takes SKEWED us: 16 sequences of up to 500 tokens, 12 heads of 64, edges up to 128.)
 constexpr int kLine = 18, kLines = 47, kSkewFloats = kLines * kLine + 2;
+constexpr bool skew_in_values(int dp, bool shared) { return !shared && dp >= 64; }
 __device__ __forceinline__ void add_diagonals(float* skew, float* sums, const floatx16& x, int lane, int half, int l32)
 {
     float* const to = skew + (4 * half - l32 + 31) * kLine + 4 * half;
@@ -79,12 +80,13 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
-    int bh, q0, tile_id = 0;
+    int bh, q0, tile_id = 0, part = 0;   // (tile_id: of the tiles and their parts)
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles);
+        const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles * gr.parts);
         bh = it.head;
         tile_id = it.tile;
-        q0 = it.tile * 128 + 32 * wave;
+        part = it.tile % gr.parts;
+        q0 = it.tile / gr.parts * 128 + 32 * wave;
     } else {
         bh = (int)(blockIdx.x * 4 + wave);
         q0 = 0;
@@ -100,12 +102,17 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     float* const biases = floats + (SHARED ? 0 : wave * window_floats);
     float* const all_diagonals = floats + (SHARED ? 1 : 4) * window_floats;
     float* const diagonals = all_diagonals + wave * window_floats;
-    float* const skew = all_diagonals + 4 * window_floats + wave * kSkewFloats;
+    // (a wavefront's own, where it fits: where its values lie, once they have been used)
+    constexpr bool kInValues = skew_in_values(DP, SHARED);
+    static_assert(!kInValues || kSkewFloats * 4 <= kTileBytes, "the square fits the values' tile");
+    float* const skew = kInValues ? reinterpret_cast<float*>(tiles + kTileBytes) : all_diagonals + 4 * window_floats + wave * kSkewFloats;
 
     const int first_q = SHARED ? q0 - 32 * wave : 0, rows_here = SHARED ? 128 : 32;
     const int last_q = first_q + rows_here < ql ? first_q + rows_here - 1 : ql - 1;
     int end = first_q >= ql ? 0 : a.causal ? kl - ql + last_q + 1 : kl;
     end = end < kl ? end : kl;
+    const int begin = SHARED ? part * gr.part_keys : 0;
+    if (SHARED && gr.parts > 1) end = end < begin + gr.part_keys ? end : begin + gr.part_keys;
 
     const T* const kp = a.k.at<T>(b, hk);
     const T* const vp = a.v.at<T>(b, hk);
@@ -119,9 +126,9 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
     };
     constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
-    if (end > 0)
+    if (begin < end)
 #pragma unroll
-        for (int t = 0; t < kAhead; ++t) request(t * kN, t);
+        for (int t = 0; t < kAhead; ++t) request(begin + t * kN, t);
     Lane<DP> at;
     at.set(lane);
     const int i = q0 + l32, p = kl - ql + i;
@@ -147,7 +154,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 delta = __builtin_fmaf(x[1], y[1], delta);
             }
         delta = sum_of_halves(delta);
-        if (half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
+        if (half == 0 && part == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
     }
     floatx16 dq[Tile<DP>::kBlocks];
 #pragma unroll
@@ -155,9 +162,10 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     float sum_left = 0.f, sum_right = 0.f;
     if (a.table) {
         for (int n = lane; n < window_floats; n += kWave) diagonals[n] = 0.f;
-        for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
+        if constexpr (!kInValues)
+            for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
     }
-    if (end > 0) {
+    if (begin < end) {
         float bias_left = 0.f, bias_right = 0.f;
         if (a.table) {
             bias_left = a.bias<T>(a.n_edges, h);
@@ -214,7 +222,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
             delta = sum_of_halves(delta);
         }
         int turn = 0;
-        for (int key0 = 0; key0 < end; key0 += kN) {
+        for (int key0 = begin; key0 < end; key0 += kN) {
             if constexpr (SHARED) {
                 wait_for<(kTurns - 2) * 2 * Flow<T, DP, kN, kThreads>::kEach>();
                 __syncthreads();   // (and the tile before is done with)
@@ -234,6 +242,12 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 for (int e = 0; e < 16; ++e) ds[e] = s[e] * (ds[e] - delta);
                 if (a.table) {
                     if (place == kNear) {
+                        if constexpr (kInValues) {
+                            wait_for_reads();
+                            wave_fence();
+                            for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
+                            wave_fence();
+                        }
                         add_diagonals(skew, diagonals + (k0 - (kl - ql + q0) - 31 - window.first), ds, lane, half, l32);
                     } else {
                         float sum = 0.f;
@@ -263,11 +277,16 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         wait_for<0>();   // (nothing may arrive in LDS that is used for other things, or no longer this workgroup's)
     }
     if (!SHARED && half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
-    if (i < a.q_tokens) store_row<T, DP>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token, dq, a.scale, a.head_dim, half);
+    if (i < a.q_tokens) {
+        if (SHARED && gr.parts > 1)
+            store_row32<DP>(gr.sums + ((int64_t)part * heads * a.q_tokens + row) * DP, dq, half);
+        else
+            store_row<T, DP>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token, dq, a.scale, a.head_dim, half);
+    }
     if (!a.table) return;
     // what this workgroup (wavefront) saw of every diagonal
     const int width = window.size + 2;
-    float* const to = gr.diagonals + ((int64_t)(SHARED ? b * q_tiles + tile_id : b) * a.q_heads + h) * width;
+    float* const to = gr.diagonals + ((int64_t)(SHARED ? b * q_tiles * gr.parts + tile_id : b) * a.q_heads + h) * width;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
         sum_left += __shfl_xor(sum_left, o, kWave);
@@ -324,9 +343,10 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
         part = it.tile % gr.parts;
         k0 = (k_tiles - 1 - it.tile / gr.parts) * Shape::kKeys + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
     } else {
-        bh = (int)(blockIdx.x * 4 + wave);
-        k0 = 0;
-        if (bh >= (int)heads) return;
+        const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+        if (unit >= (int64_t)heads * k_tiles) return;
+        bh = (int)(unit / k_tiles);
+        k0 = (int)(unit % k_tiles) * 32;
     }
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const int ql = a.queries(b), kl = a.keys(b);
@@ -337,7 +357,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     float* const biases = reinterpret_cast<float*>(lds + (SHARED ? Shape::kTurns * kTurnBytes + Shape::kWaves * Shape::kHeldBytes : 4 * kTurnBytes)) + (SHARED ? 0 : wave * window_floats);
 
     // query tiles that see any of this workgroup's keys
-    const int first_key = SHARED ? k0 - 32 * wave : 0, shift = kl - ql;
+    const int first_key = SHARED ? k0 - 32 * wave : k0, shift = kl - ql;
     int first_tile = 0;
     if (a.causal && first_key > shift) first_tile = (first_key - shift) / kQ;
     int each = (ql + kQ - 1) / kQ - first_tile;
@@ -497,6 +517,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_k
     const int at = 4 * (int)(item % (DP / 2)), d = at % DP;
     if (row >= rows || d >= a.head_dim) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int n = 0; n < gr.parts; ++n) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(gr.sums + (n * rows + row) * 2 * DP + at);
 #pragma unroll
@@ -507,6 +528,24 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_k
     const Heads& out = is_k ? gr.out0 : gr.out1;
     const float f = is_k ? a.scale : Held<T>::kUnit;
     *reinterpret_cast<u32x2*>(out.at<T>(b, hk) + (int64_t)j * out.token + d) = u32x2{pair_of(s[0] * f, s[1] * f, T{}), pair_of(s[2] * f, s[3] * f, T{})};
+}
+
+template <typename T, int DP> __global__ void __launch_bounds__(256) queries_join_kernel(Args a, Grad gr)
+{
+    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = item / (DP / 4);
+    const int d = 4 * (int)(item % (DP / 4));
+    if (row >= rows || d >= a.head_dim) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int n = 0; n < gr.parts; ++n) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(gr.sums + (n * rows + row) * DP + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += x[e];
+    }
+    const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads;
+    *reinterpret_cast<u32x2*>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token + d) =
+        u32x2{pair_of(s[0] * a.scale, s[1] * a.scale, T{}), pair_of(s[2] * a.scale, s[3] * a.scale, T{})};
 }
 
 // 64 diagonals of a head and 16 runs of workgroups.
@@ -560,36 +599,46 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
 
 struct Plan {
     bool own_queries, own_keys;
-    int q_tiles, k_tiles, parts, diagonal_parts, width;
-    size_t stats, diagonals, sums, tables, total;   // bytes
+    int q_tiles, q_parts, q_part_keys, k_tiles, parts, diagonal_parts;
+    size_t stats, diagonals, sums, tables, total;   // bytes (sums: of either kernel's parts, one after the other)
 };
-constexpr int64_t kHeld = 512;   // workgroups that the device holds at once; fewer are cut into parts, for twice as many
 Plan plan_of(const pruner_attention* a)
 {
     Plan p{};
+    const int dp = padded_dim(a->head_dim), group = a->q_heads / a->kv_heads;
+    const bool causal = a->flags & PRUNER_ATTENTION_CAUSAL;
     p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;
-    p.own_keys = a->k_tokens <= 32 && (int64_t)a->q_tokens * (a->q_heads / a->kv_heads) <= 256;
+    // (a wavefront's 32 keys need all of few queries: little is gained by sharing them, unless heads are so wide that one wavefront per SIMD is left:
+    // 171 sequences of 6 queries and 542 keys, 7 heads of 128 sharing one, 118 us by wavefronts of their own and 80 shared; 783 of 6 and 55, 16 sharing 8, 194 and 244)
+    p.own_keys = a->q_tokens <= 32 && (dp < 128 || a->k_tokens <= 64);
     p.q_tiles = (a->q_tokens + 127) / 128;
-    const int tile_keys = padded_dim(a->head_dim) == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
+    const int tile_keys = p.own_keys ? 32 : dp == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
     p.k_tiles = (a->k_tokens + tile_keys - 1) / tile_keys;
-    p.parts = 1;
-    const int64_t groups = (int64_t)a->batch * a->kv_heads * p.k_tiles, tiles = (int64_t)(a->q_heads / a->kv_heads) * ((a->q_tokens + 31) / 32);
-    if (!p.own_keys && groups > 0) {
-        const int64_t held = padded_dim(a->head_dim) == 128 ? kHeld / 2 : kHeld;   // (workgroups of eight wavefronts)
-        int64_t parts = groups >= held ? 1 : (2 * held + groups - 1) / groups;
-        const int64_t most = tiles / 8;   // eight query tiles of 32 at least
-        parts = parts < most ? parts : most;
-        p.parts = parts < 1 ? 1 : (int)parts;
+    p.q_parts = p.parts = 1;
+    p.q_part_keys = a->k_tokens;
+    const double rows = (double)a->batch * a->q_heads * a->q_tokens, keys = (double)a->batch * a->kv_heads * a->k_tokens;
+    // (steps as measured: 5001 causal tokens, 16 heads of 128 sharing 4; 16 sequences of up to 500, 12 of 64)
+    if (!p.own_queries && rows > 0 && keys > 0) {
+        const int step = dp < 128 ? 64 : 32, parts = parts_of((double)a->batch * a->q_heads * p.q_tiles, (a->k_tokens + step - 1) / step, causal, 512,
+                                                              dp == 128 ? 1.2 : dp == 64 ? 1.4 : 1.0, dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, rows * dp * 4);
+        p.q_part_keys = ((a->k_tokens + parts - 1) / parts + 63) / 64 * 64;
+        p.q_parts = (a->k_tokens + p.q_part_keys - 1) / p.q_part_keys;
+    }
+    if (!p.own_keys && rows > 0 && keys > 0) {
+        const int step = dp < 128 ? 64 : 32;
+        p.parts = parts_of((double)a->batch * a->kv_heads * p.k_tiles, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, dp < 128 ? 512 : 256, dp == 128 ? 2.2 : dp == 64 ? 1.5 : 1.0,
+                           dp == 128 ? 2.8 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
     }
     // (the window for the largest edge that there can be: sizes alone decide)
     const int64_t reach = (int64_t)a->q_tokens + a->k_tokens;
     const int most = (int)(reach < PRUNER_MAX_BIAS_DISTANCE ? reach : PRUNER_MAX_BIAS_DISTANCE);
     const int widest = Window(most, a->flags & PRUNER_ATTENTION_TWO_SIDED ? (most > 1 ? most : 1) : 0).size + 2;
-    p.diagonal_parts = p.own_queries ? a->batch : a->batch * p.q_tiles;
+    p.diagonal_parts = p.own_queries ? a->batch : a->batch * p.q_tiles * p.q_parts;
     p.stats = round_up((size_t)a->batch * a->q_heads * round_up((size_t)a->q_tokens, 32) * 3 * 4, 256);
     p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
     p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
-    p.sums = p.parts > 1 ? round_up((size_t)p.parts * a->batch * a->kv_heads * a->k_tokens * 2 * padded_dim(a->head_dim) * 4, 256) : 0;
+    const size_t of_queries = p.q_parts > 1 ? (size_t)p.q_parts * (size_t)rows * dp * 4 : 0, of_keys = p.parts > 1 ? (size_t)p.parts * (size_t)keys * 2 * dp * 4 : 0;
+    p.sums = round_up(of_queries > of_keys ? of_queries : of_keys, 256);
     p.total = p.stats + p.diagonals + p.tables + p.sums;
     return p;
 }
@@ -619,14 +668,19 @@ template <typename T, int DP> int run(const Call& c)
     const int64_t q_heads = (int64_t)a.batch * a.q_heads, k_heads = (int64_t)a.batch * a.kv_heads;
     if (a.q_tokens > 0) {
         if (c.plan.own_queries)
-            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + 4 * skew + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
+            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + (skew_in_values(DP, false) ? 0 : 4 * skew) + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
         else
-            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles)), dim3(256), 5 * window + 4 * skew + turns_of(DP, true, DP < 128 ? 64 : 32) * 2 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
+            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles * c.plan.q_parts)), dim3(256), 5 * window + 4 * skew + turns_of(DP, true, DP < 128 ? 64 : 32) * 2 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
         PRUNER_LAUNCH_CHECK();
+        if (c.plan.q_parts > 1) {   // (before the keys' kernel, which may use the same sums)
+            const int64_t items = q_heads * a.q_tokens * (DP / 4);
+            hipLaunchKernelGGL((queries_join_kernel<T, DP>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, c.st, a, c.queries);
+            PRUNER_LAUNCH_CHECK();
+        }
     }
     if (a.k_tokens > 0) {
         if (c.plan.own_keys) {
-            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, 1);
+            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads * c.plan.k_tiles + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, c.plan.k_tiles);
         } else {
             typedef KeysShape<T, DP, true> Shape;
             hipLaunchKernelGGL((keys_kernel<T, DP, true>), dim3((unsigned)(k_heads * c.plan.k_tiles * c.plan.parts)), dim3(64 * Shape::kWaves),
@@ -691,9 +745,11 @@ extern "C" int pruner_rel_attention_grad(const pruner_attention* a, const pruner
     g.diagonals = reinterpret_cast<float*>(ws + c.plan.stats);
     c.table_sums = reinterpret_cast<float*>(ws + c.plan.stats + c.plan.diagonals);
     g.sums = reinterpret_cast<float*>(ws + c.plan.stats + c.plan.diagonals + c.plan.tables);
-    g.parts = c.plan.parts;
+    g.part_keys = c.plan.q_part_keys;
     g.stat_rows = (int)round_up((size_t)a->q_tokens, 32);
     c.queries = c.keys = g;
+    c.queries.parts = c.plan.q_parts;
+    c.keys.parts = c.plan.parts;
     c.queries.out0 = att::heads_of(dq);
     c.keys.out0 = att::heads_of(dk);
     c.keys.out1 = att::heads_of(dv);
