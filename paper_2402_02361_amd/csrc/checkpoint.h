@@ -24,61 +24,60 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
 
-// Eight neighbouring values as they lie in memory (T), fetched by V at a time: V = 8 needs rows that begin at multiples of 16 bytes,
-// V = 4 of 8 (16 in binary32), V = 1 nothing.  Values at or beyond `left` are not touched; left is a multiple of V.
+// Eight neighbouring values as they lie in memory (T).  V = 8: rows begin at multiples of 16 bytes and hold whole eights.  V = 1: they begin anywhere; a
+// whole eight moves by accesses that need no alignment, what is left of a row one by one.  Values at or beyond `left` are not touched and are 0.
 template <typename T, int V> struct Eight {
     static constexpr int kWords = 2 * (int)sizeof(T);
+    typedef u32x4 Loose __attribute__((aligned(2)));
     uint32_t w[kWords];
     __device__ __forceinline__ void load(const T* __restrict__ p, int left)
     {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = 0u;
-        if constexpr (V == 8 || (V == 4 && sizeof(T) == 4)) {
+        if (left >= kEach) {
 #pragma unroll
-            for (int i = 0; i < kWords; i += 4)
-                if (i * 4 < left * (int)sizeof(T)) {
-                    const u32x4 q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint32_t*>(p) + i);
+            for (int i = 0; i < kWords; i += 4) {
+                u32x4 q;
+                if constexpr (V == 8)
+                    q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint32_t*>(p) + i);
+                else
+                    q = *reinterpret_cast<const Loose*>(p + i * 4 / (int)sizeof(T));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[i + j] = q[j];
-                }
-        } else if constexpr (V == 4) {
+                for (int j = 0; j < 4; ++j) w[i + j] = q[j];
+            }
+        } else if constexpr (V == 1) {
+            if (left > 0)
 #pragma unroll
-            for (int i = 0; i < kWords; i += 2)
-                if (i * 4 < left * (int)sizeof(T)) {
-                    const u32x2 q = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint32_t*>(p) + i);
-                    w[i] = q[0];
-                    w[i + 1] = q[1];
-                }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < left) {
-                    if constexpr (sizeof(T) == 4)
-                        w[j] = __builtin_bit_cast(uint32_t, p[j]);
-                    else
-                        w[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[j]) << (16 * (j % 2));
-                }
+                for (int j = 0; j < kEach; ++j)
+                    if (j < left) {
+                        if constexpr (sizeof(T) == 4)
+                            w[j] = __builtin_bit_cast(uint32_t, p[j]);
+                        else
+                            w[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[j]) << (16 * (j % 2));
+                    }
         }
     }
     __device__ __forceinline__ void store(T* __restrict__ p, int left) const
     {
-        if constexpr (V == 8 || (V == 4 && sizeof(T) == 4)) {
+        if (left >= kEach) {
 #pragma unroll
-            for (int i = 0; i < kWords; i += 4)
-                if (i * 4 < left * (int)sizeof(T)) *reinterpret_cast<u32x4*>(reinterpret_cast<uint32_t*>(p) + i) = u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]};
-        } else if constexpr (V == 4) {
+            for (int i = 0; i < kWords; i += 4) {
+                const u32x4 q = {w[i], w[i + 1], w[i + 2], w[i + 3]};
+                if constexpr (V == 8)
+                    *reinterpret_cast<u32x4*>(reinterpret_cast<uint32_t*>(p) + i) = q;
+                else
+                    *reinterpret_cast<Loose*>(p + i * 4 / (int)sizeof(T)) = q;
+            }
+        } else if constexpr (V == 1) {
+            if (left > 0)
 #pragma unroll
-            for (int i = 0; i < kWords; i += 2)
-                if (i * 4 < left * (int)sizeof(T)) *reinterpret_cast<u32x2*>(reinterpret_cast<uint32_t*>(p) + i) = u32x2{w[i], w[i + 1]};
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < left) {
-                    if constexpr (sizeof(T) == 4)
-                        p[j] = __builtin_bit_cast(T, w[j]);
-                    else
-                        p[j] = __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j % 2))));
-                }
+                for (int j = 0; j < kEach; ++j)
+                    if (j < left) {
+                        if constexpr (sizeof(T) == 4)
+                            p[j] = __builtin_bit_cast(T, w[j]);
+                        else
+                            p[j] = __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j % 2))));
+                    }
         }
     }
     __device__ __forceinline__ void to_floats(float (&v)[kEach]) const
@@ -109,40 +108,40 @@ template <typename T, int V> struct Eight {
     }
 };
 
-// Eight codes, by V at a time as above (codes begin at a multiple of 8 bytes and rows are dim long, so V divides their offsets).
+// Eight codes, as above.
 template <int V> struct EightCodes {
+    typedef u32x2 Loose __attribute__((aligned(1)));
     uint32_t w[2];
     __device__ __forceinline__ void load(const int8_t* __restrict__ p, int left)
     {
         w[0] = w[1] = 0u;
-        if constexpr (V == 8) {
-            if (left > 0) {
-                const u32x2 q = *reinterpret_cast<const u32x2*>(p);
-                w[0] = q[0];
-                w[1] = q[1];
-            }
-        } else if constexpr (V == 4) {
+        if (left >= kEach) {
+            u32x2 q;
+            if constexpr (V == 8)
+                q = *reinterpret_cast<const u32x2*>(p);
+            else
+                q = *reinterpret_cast<const Loose*>(p);
+            w[0] = q[0];
+            w[1] = q[1];
+        } else if constexpr (V == 1) {
+            if (left > 0)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (4 * i < left) w[i] = *reinterpret_cast<const uint32_t*>(p + 4 * i);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < left) w[j / 4] |= (uint32_t)(uint8_t)p[j] << (8 * (j % 4));
+                for (int j = 0; j < kEach; ++j)
+                    if (j < left) w[j / 4] |= (uint32_t)(uint8_t)p[j] << (8 * (j % 4));
         }
     }
     __device__ __forceinline__ void store(int8_t* __restrict__ p, int left) const
     {
-        if constexpr (V == 8) {
-            if (left > 0) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
-        } else if constexpr (V == 4) {
+        if (left >= kEach) {
+            if constexpr (V == 8)
+                *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+            else
+                *reinterpret_cast<Loose*>(p) = u32x2{w[0], w[1]};
+        } else if constexpr (V == 1) {
+            if (left > 0)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (4 * i < left) *reinterpret_cast<uint32_t*>(p + 4 * i) = w[i];
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < left) p[j] = (int8_t)(uint8_t)(w[j / 4] >> (8 * (j % 4)));
+                for (int j = 0; j < kEach; ++j)
+                    if (j < left) p[j] = (int8_t)(uint8_t)(w[j / 4] >> (8 * (j % 4)));
         }
     }
 };
@@ -186,22 +185,23 @@ __device__ __forceinline__ void restore_eight(const uint32_t (&codes)[2], uint32
     for (int j = 0; j < kEach; ++j) v[j] = (float)(int8_t)(codes[j / 4] >> (8 * (j % 4))) * unit;
 }
 
-// How many values one access may take (8, 4 or 1): pointers and strides of all of a call's matrices come through `fits`.
+// Whether all of a call's matrices lie so that accesses of eight values are aligned and rows hold whole eights (8), or not (1).
 struct Access {
     int v = 8;
     void fits(const void* p, size_t elem_bytes, int64_t pitch)
     {
-        if (!p) return;
-        auto ok = [&](int n) {
-            const size_t bytes = n * elem_bytes < 16 ? n * elem_bytes : 16;
-            return aligned(p, bytes) && pitch % n == 0;
-        };
-        while (v > 1 && !ok(v)) v = v == 8 ? 4 : 1;
+        const size_t bytes = 8 * elem_bytes < 16 ? 8 * elem_bytes : 16;
+        if (p && !(aligned(p, bytes) && pitch % 8 == 0)) v = 1;
     }
 };
 
 inline bool type_known(int32_t dtype) { return dtype == PRUNER_BF16 || dtype == PRUNER_F16 || dtype == PRUNER_F32; }
 inline size_t type_bytes(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
+
+#define BY_TYPE_AND_ACCESS(dtype, v, fn, ...)                                                   \
+    ((dtype) == PRUNER_F32    ? ((v) == 8 ? fn<float, 8>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))   \
+     : (dtype) == PRUNER_BF16 ? ((v) == 8 ? fn<__bf16, 8>(__VA_ARGS__) : fn<__bf16, 1>(__VA_ARGS__)) \
+                              : ((v) == 8 ? fn<_Float16, 8>(__VA_ARGS__) : fn<_Float16, 1>(__VA_ARGS__)))
 
 }  // namespace ckpt
 }  // namespace pruner

@@ -346,11 +346,6 @@ int restore_rows(const pruner_checkpoint* kept, int64_t rows, int32_t dim, void*
 
 using namespace pruner;
 
-#define BY_TYPE_AND_ACCESS(dtype, v, fn, ...)                                                                                                   \
-    ((dtype) == PRUNER_F32    ? ((v) == 8 ? fn<float, 8>(__VA_ARGS__) : (v) == 4 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))        \
-     : (dtype) == PRUNER_BF16 ? ((v) == 8 ? fn<__bf16, 8>(__VA_ARGS__) : (v) == 4 ? fn<__bf16, 4>(__VA_ARGS__) : fn<__bf16, 1>(__VA_ARGS__))     \
-                              : ((v) == 8 ? fn<_Float16, 8>(__VA_ARGS__) : (v) == 4 ? fn<_Float16, 4>(__VA_ARGS__) : fn<_Float16, 1>(__VA_ARGS__)))
-
 extern "C" int pruner_checkpoint_pack(const void* x, int32_t dtype, int64_t rows, int32_t dim, int64_t pitch, const pruner_checkpoint* kept, void* stream)
 {
     if (!sizes_ok(dtype, rows, dim, pitch)) return PRUNER_EINVAL;
@@ -393,16 +388,14 @@ extern "C" int pruner_checkpoint_wgrad(const void* dy, int32_t dtype, int64_t dy
     if (rows > 0) {
         a.fits(dy, 2, dy_pitch);
         a.fits(kept->codes, 1, dim);
-        if (n_out % a.v) a.v = n_out % 4 ? 1 : 4;   // (a row's last access must not pass its end)
+        if (n_out % 8) a.v = 1;   // (a row's last access must not pass its end)
     }
     const pruner_checkpoint* const c = rows > 0 ? kept : &none;
     float* const parts = static_cast<float*>(workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == PRUNER_BF16)
-        return a.v == 8   ? run_wgrad<__bf16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
-               : a.v == 4 ? run_wgrad<__bf16, 4>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
-                          : run_wgrad<__bf16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
-    return a.v == 8   ? run_wgrad<_Float16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
-           : a.v == 4 ? run_wgrad<_Float16, 4>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
-                      : run_wgrad<_Float16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
+        return a.v == 8 ? run_wgrad<__bf16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+                        : run_wgrad<__bf16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
+    return a.v == 8 ? run_wgrad<_Float16, 8>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st)
+                    : run_wgrad<_Float16, 1>(dy, dy_pitch, c, rows, n_out, dim, plan, dw, accumulate, parts, st);
 }

@@ -436,11 +436,6 @@ int run_norm_grad(const pruner_norm* p, const Shape& s, const void* dh, int64_t 
 
 using namespace pruner;
 
-#define BY_TYPE_AND_ACCESS(dtype, v, fn, ...)                                                                                                   \
-    ((dtype) == PRUNER_F32    ? ((v) == 8 ? fn<float, 8>(__VA_ARGS__) : (v) == 4 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))        \
-     : (dtype) == PRUNER_BF16 ? ((v) == 8 ? fn<__bf16, 8>(__VA_ARGS__) : (v) == 4 ? fn<__bf16, 4>(__VA_ARGS__) : fn<__bf16, 1>(__VA_ARGS__))     \
-                              : ((v) == 8 ? fn<_Float16, 8>(__VA_ARGS__) : (v) == 4 ? fn<_Float16, 4>(__VA_ARGS__) : fn<_Float16, 1>(__VA_ARGS__)))
-
 extern "C" int pruner_gated_norm(const pruner_norm* p, const void* x, int64_t x_pitch, const void* f, int64_t f_pitch, void* h, void* y, const pruner_checkpoint* kept_y,
                                  void* stream)
 {

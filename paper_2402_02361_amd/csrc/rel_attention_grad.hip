@@ -376,11 +376,16 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
         const uint32_t place = (uint32_t)((SHARED ? turn : wave) * kTurnBytes);
         qf.request(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, left, place);
         of.request(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, left, place + kTileBytes);
+        auto stat = [&](int w) {
+            request_4(place + 2 * kTileBytes + 4 * kStat * w, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
+                      buffer_of(gr.stats + w * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
+        };
+        if constexpr (SHARED) {
+            if (wave < 3) stat(wave);
+        } else {
 #pragma unroll
-        for (int w = 0; w < 3; ++w)
-            if (!SHARED || wave == w)
-                request_4(place + 2 * kTileBytes + 4 * kStat * w, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
-                          buffer_of(gr.stats + w * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
+            for (int w = 0; w < 3; ++w) stat(w);
+        }
     };
     constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
     if (from < to)
