@@ -24,17 +24,27 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
 
-// Eight neighbouring values as they lie in memory (T).  V = 8: rows begin at multiples of 16 bytes and hold whole eights.  V = 1: they begin anywhere; a
-// whole eight moves by accesses that need no alignment, what is left of a row one by one.  Values at or beyond `left` are not touched and are 0.
+// How many of eight values from a place in a row, where `left` of the row's values remain and `after` rows follow, lie within the matrix.
+__device__ __forceinline__ int room_of(int64_t after, int64_t pitch, int left)
+{
+    if (after >= 8) return 8;
+    const int64_t n = after * pitch + left;
+    return n < 8 ? (int)n : 8;
+}
+
+// Eight neighbouring values as they lie in memory (T).  V = 8: rows begin at multiples of 16 bytes and hold whole eights.  V = 1: they begin anywhere; an
+// eight moves by accesses that need no alignment.  Of a row's last values the read takes the next row's along, where the matrix has that much room
+// (one by one a row's tail is what such rows then cost: the weight gradient 1601 x 903 over 30000 rows took 522 us).  Values at or beyond `left` are 0
+// after a read and are not written.
 template <typename T, int V> struct Eight {
     static constexpr int kWords = 2 * (int)sizeof(T);
     typedef u32x4 Loose __attribute__((aligned(2)));
     uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* __restrict__ p, int left)
+    __device__ __forceinline__ void load(const T* __restrict__ p, int left, int room)
     {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = 0u;
-        if (left >= kEach) {
+        if (V == 8 ? left >= kEach : left > 0 && room >= kEach) {
 #pragma unroll
             for (int i = 0; i < kWords; i += 4) {
                 u32x4 q;
@@ -45,16 +55,28 @@ template <typename T, int V> struct Eight {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[i + j] = q[j];
             }
-        } else if constexpr (V == 1) {
-            if (left > 0)
+            if constexpr (V == 1) {
 #pragma unroll
-                for (int j = 0; j < kEach; ++j)
-                    if (j < left) {
-                        if constexpr (sizeof(T) == 4)
-                            w[j] = __builtin_bit_cast(uint32_t, p[j]);
-                        else
-                            w[j / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[j]) << (16 * (j % 2));
-                    }
+                for (int i = 0; i < kWords; ++i) {
+                    if constexpr (sizeof(T) == 4)
+                        w[i] = i < left ? w[i] : 0u;
+                    else
+                        w[i] = 2 * i + 1 < left ? w[i] : 2 * i < left ? w[i] & 0xFFFFu : 0u;
+                }
+            }
+        } else if constexpr (V == 1) {
+            if (left > 0) {   // (the matrix's last values)
+#pragma unroll 1
+                for (int j = 0; j < left; ++j) {
+                    uint32_t v;
+                    if constexpr (sizeof(T) == 4)
+                        v = __builtin_bit_cast(uint32_t, p[j]);
+                    else
+                        v = (uint32_t)__builtin_bit_cast(uint16_t, p[j]) << (16 * (j % 2));
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) w[i] |= i == j * (int)sizeof(T) / 4 ? v : 0u;
+                }
+            }
         }
     }
     __device__ __forceinline__ void store(T* __restrict__ p, int left) const
@@ -69,15 +91,28 @@ template <typename T, int V> struct Eight {
                     *reinterpret_cast<Loose*>(p + i * 4 / (int)sizeof(T)) = q;
             }
         } else if constexpr (V == 1) {
-            if (left > 0)
-#pragma unroll
-                for (int j = 0; j < kEach; ++j)
-                    if (j < left) {
-                        if constexpr (sizeof(T) == 4)
-                            p[j] = __builtin_bit_cast(T, w[j]);
-                        else
-                            p[j] = __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j % 2))));
+            if (left > 0) {   // a row's tail: four, two and one of its values
+                typedef uint32_t Word __attribute__((aligned(2)));
+                typedef u32x2 Pair __attribute__((aligned(2)));
+                const bool four = left & 4;
+                if constexpr (sizeof(T) == 4) {
+                    if (four) {
+                        *reinterpret_cast<Loose*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+                        if (left > 4) p[4] = __builtin_bit_cast(T, w[4]);
+                        if (left > 5) p[5] = __builtin_bit_cast(T, w[5]);
+                        if (left > 6) p[6] = __builtin_bit_cast(T, w[6]);
+                    } else {
+                        p[0] = __builtin_bit_cast(T, w[0]);
+                        if (left > 1) p[1] = __builtin_bit_cast(T, w[1]);
+                        if (left > 2) p[2] = __builtin_bit_cast(T, w[2]);
                     }
+                } else {
+                    if (four) *reinterpret_cast<Pair*>(p) = u32x2{w[0], w[1]};
+                    const uint32_t two = four ? +w[2] : +w[0], one = left & 2 ? (four ? +w[3] : +w[1]) : two;
+                    if (left & 2) *reinterpret_cast<Word*>(p + (left & 4)) = two;
+                    if (left & 1) p[left & 6] = __builtin_bit_cast(T, (uint16_t)one);
+                }
+            }
         }
     }
     __device__ __forceinline__ void to_floats(float (&v)[kEach]) const
@@ -112,10 +147,10 @@ template <typename T, int V> struct Eight {
 template <int V> struct EightCodes {
     typedef u32x2 Loose __attribute__((aligned(1)));
     uint32_t w[2];
-    __device__ __forceinline__ void load(const int8_t* __restrict__ p, int left)
+    __device__ __forceinline__ void load(const int8_t* __restrict__ p, int left, int room)   // (what is beyond `left` may be anything)
     {
         w[0] = w[1] = 0u;
-        if (left >= kEach) {
+        if (V == 8 ? left >= kEach : left > 0 && room >= kEach) {
             u32x2 q;
             if constexpr (V == 8)
                 q = *reinterpret_cast<const u32x2*>(p);
@@ -178,11 +213,11 @@ __device__ __forceinline__ uint32_t pack_group(const float (&v)[kEach], uint32_t
     return byte;
 }
 
-__device__ __forceinline__ void restore_eight(const uint32_t (&codes)[2], uint32_t byte, float (&v)[kEach])
+__device__ __forceinline__ void restore_eight(const uint32_t (&codes)[2], uint32_t byte, float (&v)[kEach], int left = kEach)   // (0 from `left` on)
 {
     const float unit = __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);   // NaN x any code, 0 included, is NaN
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) v[j] = (float)(int8_t)(codes[j / 4] >> (8 * (j % 4))) * unit;
+    for (int j = 0; j < kEach; ++j) v[j] = j < left ? (float)(int8_t)(codes[j / 4] >> (8 * (j % 4))) * unit : 0.f;
 }
 
 // Whether all of a call's matrices lie so that accesses of eight values are aligned and rows hold whole eights (8), or not (1).

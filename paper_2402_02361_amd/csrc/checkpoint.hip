@@ -20,7 +20,7 @@ struct Divisor {
 
 // A thread takes eight neighbouring values; four threads make a group.  Bound: memory (each value read once, a little over a byte written).
 template <typename T, int V>
-__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int64_t pitch, int dim, uint32_t items, Divisor per_row, int8_t* __restrict__ codes,
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int64_t pitch, int64_t rows, int dim, uint32_t items, Divisor per_row, int8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ exps)
 {
     const uint32_t item = blockIdx.x * 256 + threadIdx.x;   // (items is a multiple of 4: the lanes of a group are active together)
@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int6
     const uint32_t row = per_row.of(item), at = item - row * per_row.d;
     const int col = 8 * (int)at, left = dim - col;
     Eight<T, V> in;
-    in.load(x + (int64_t)row * pitch + col, left);
+    in.load(x + (int64_t)row * pitch + col, left, room_of(rows - 1 - row, pitch, left));
     float v[kEach];
     in.to_floats(v);
     EightCodes<V> out;
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int6
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, int dim, uint32_t items, Divisor per_row,
+__global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, int64_t rows, int dim, uint32_t items, Divisor per_row,
                                                       T* __restrict__ x, int64_t pitch)
 {
     const uint32_t item = blockIdx.x * 256 + threadIdx.x;
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__
     const uint32_t row = per_row.of(item), at = item - row * per_row.d;
     const int col = 8 * (int)at, left = dim - col;
     EightCodes<V> in;
-    in.load(codes + (int64_t)row * dim + col, left);
+    in.load(codes + (int64_t)row * dim + col, left, room_of(rows - 1 - row, dim, left));
     float v[kEach];
     restore_eight(in.w, exps[(int64_t)row * (per_row.d / 4) + at / 4], v);
     Eight<T, V> out;
@@ -159,8 +159,10 @@ __global__ void __launch_bounds__(WgradShape<BIG>::kThreads, 2) wgrad_kernel(con
         } else {
             const int64_t r = r0 + s_row + S::kRowStep * u;
             const bool in = r < r_end;
-            dy_in[u].load(dy + r * dy_pitch + n0 + 8 * s_chunk, in ? n_left : 0);
-            x_in[u].load(codes + r * dim + k0 + 8 * s_chunk, in ? k_left : 0);
+            // (columns past the matrix's may hold anything: their results are not kept)
+            const int n_room = room_of(rows - 1 - r, dy_pitch, n_left), k_room = room_of(rows - 1 - r, dim, k_left);
+            dy_in[u].load(dy + r * dy_pitch + n0 + 8 * s_chunk, in && n_left > 0 ? (n_room >= 8 ? 8 : n_left) : 0, n_room);
+            x_in[u].load(codes + r * dim + k0 + 8 * s_chunk, in && k_left > 0 ? (k_room >= 8 ? 8 : k_left) : 0, k_room);
             x_exp[u] = in && k_left > 0 ? exps[r * groups + (k0 >> 5) + (s_chunk >> 2)] : 0u;
         }
     };
@@ -256,6 +258,7 @@ __global__ void __launch_bounds__(256) wgrad_join_kernel(const float* __restrict
     float s[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = accumulate ? dw[i + j] : 0.f;
+#pragma unroll 8
     for (int p = 0; p < n_parts; ++p) {
         const float* const q = parts + p * n + i;
         if constexpr (V == 4) {
@@ -328,7 +331,7 @@ template <typename T, int V>
 int pack_rows(const void* x, int64_t rows, int32_t dim, int64_t pitch, const pruner_checkpoint* kept, hipStream_t st)
 {
     return in_row_chunks(rows, dim, [&](int64_t r, uint32_t items, dim3 grid, const Divisor& per_row) {
-        hipLaunchKernelGGL((pack_kernel<T, V>), grid, dim3(256), 0, st, static_cast<const T*>(x) + r * pitch, pitch, dim, items, per_row, kept->codes + r * dim,
+        hipLaunchKernelGGL((pack_kernel<T, V>), grid, dim3(256), 0, st, static_cast<const T*>(x) + r * pitch, pitch, rows - r, dim, items, per_row, kept->codes + r * dim,
                            kept->exps + r * (per_row.d / 4));
     });
 }
@@ -336,7 +339,7 @@ template <typename T, int V>
 int restore_rows(const pruner_checkpoint* kept, int64_t rows, int32_t dim, void* x, int64_t pitch, hipStream_t st)
 {
     return in_row_chunks(rows, dim, [&](int64_t r, uint32_t items, dim3 grid, const Divisor& per_row) {
-        hipLaunchKernelGGL((restore_kernel<T, V>), grid, dim3(256), 0, st, kept->codes + r * dim, kept->exps + r * (per_row.d / 4), dim, items, per_row,
+        hipLaunchKernelGGL((restore_kernel<T, V>), grid, dim3(256), 0, st, kept->codes + r * dim, kept->exps + r * (per_row.d / 4), rows - r, dim, items, per_row,
                            static_cast<T*>(x) + r * pitch, pitch);
     });
 }

@@ -136,9 +136,10 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
     Eight<T, V> xin, fin, gin, x_next, f_next, g_next;   // the next row's values are on their way while a row is worked on
     auto fetch = [&](int64_t row) {
         const int some = row < p.rows ? left : 0;
-        x_next.load(x + row * x_pitch + col, some);
-        if (f) f_next.load(f + row * f_pitch + col, some);
-        if (gate == kGateRows) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
+        const int64_t after = p.rows - 1 - row;
+        x_next.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left));
+        if (f) f_next.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left));
+        if (gate == kGateRows) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
     for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
@@ -220,15 +221,16 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
     } now, next;
     auto fetch = [&](int64_t row) {
         const int some = row < p.rows ? left : 0;
-        next.x.load(x + row * x_pitch + col, some);
-        next.dy.load(dy + row * dy_pitch + col, some);
-        if (f) next.f.load(f + row * f_pitch + col, some);
+        const int64_t after = p.rows - 1 - row;
+        next.x.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left));
+        next.dy.load(dy + row * dy_pitch + col, some, room_of(after, dy_pitch, left));
+        if (f) next.f.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left));
         if (codes) {
-            next.c.load(codes + row * p.dim + col, some);
+            next.c.load(codes + row * p.dim + col, some, room_of(after, p.dim, left));
             next.byte = some > 0 ? exps[row * groups + t / 4] : 1u;
         }
-        if (gate_rows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some);
-        if (dh) next.dh.load(dh + row * dh_pitch + col, some);
+        if (gate_rows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
+        if (dh) next.dh.load(dh + row * dh_pitch + col, some, room_of(after, dh_pitch, left));
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
     for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
@@ -243,7 +245,7 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
         for (int j = 0; j < kEach; ++j) v[j] *= p.alpha;
         if (has_f) {
             if (codes)
-                restore_eight(now.c.w, now.byte, w);
+                restore_eight(now.c.w, now.byte, w, mine);
             else
                 now.f.to_floats(w);
             r1 = normalise<V>(sum, w, z1, mine, p.per_dim, p.center, p.eps);
