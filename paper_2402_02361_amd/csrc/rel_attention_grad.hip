@@ -7,7 +7,8 @@
 //   keys_kernel      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
 //                    through the query tiles of all heads that share the key head.  Where key tiles are too few for the device, their query
 //                    tiles are cut into parts, whose sums go to the workspace (keys_join_kernel adds them in order).
-//   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, then the diagonals of a bucket.
+//   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, and the diagonals of a bucket (where the workgroups are few, by the
+//                    latter alone).
 // S is formed twice, so nothing is added across workgroups but in a fixed order.
 #include "rel_attention.h"
 
@@ -553,7 +554,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) queries_joi
         u32x2{pair_of(s[0] * a.scale, s[1] * a.scale, T{}), pair_of(s[2] * a.scale, s[3] * a.scale, T{})};
 }
 
-// 64 diagonals of a head and 16 runs of workgroups.
+// Diagonals of a head: 64 of them and 16 runs of workgroups.
 __global__ void __launch_bounds__(1024) diagonals_kernel(const float* __restrict__ diagonals, int parts, int heads, int width, float* __restrict__ sums)
 {
     __shared__ float runs[16][64];
@@ -573,14 +574,13 @@ __global__ void __launch_bounds__(1024) diagonals_kernel(const float* __restrict
     }
 }
 
-// A wavefront per bucket: its distances' diagonals on either side, and what lay beyond the window.
-template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args a, const float* __restrict__ sums, T* __restrict__ dtable)
+// A workgroup per bucket and head: its distances' diagonals on either side and what lay beyond the window, over `parts` workgroups' sums (each wavefront
+// a run of them).
+template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args a, const float* __restrict__ diagonals, int parts, T* __restrict__ dtable)
 {
+    __shared__ float runs[4];
     const Window window(a.left, a.right);
-    const int lane = threadIdx.x & 63, buckets = (a.n_edges + 1) * (a.two_sided ? 2 : 1), h = blockIdx.y;
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (n >= buckets) return;
-    const float* const of = sums + (int64_t)h * (window.size + 2);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, n = blockIdx.x, width = window.size + 2;
     const bool right = a.two_sided && n > a.n_edges;
     const int e = right ? n - a.n_edges - 1 : n;
     const int near = e == 0 ? 0 : a.edges[e - 1];                         // distances near .. far - 1
@@ -588,20 +588,28 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
     // r = lo .. hi - 1; the first bucket of a one-sided table also has every r > 0, that of the right side begins at 1
     int lo = right ? (near > 1 ? near : 1) : 1 - far, hi = right ? far : e == 0 && !a.two_sided ? (1 << 30) : 1 - near;
     const int last = window.first + window.size;
-    lo = lo > window.first ? lo : window.first;
-    hi = hi < last ? hi : last;
+    lo = (lo > window.first ? lo : window.first) - window.first;
+    hi = (hi < last ? hi : last) - window.first;
+    // tiles wholly at one end: one place each behind the window
+    const bool left_end = !right && e == a.n_edges, right_end = a.two_sided ? right && e == a.n_edges : e == 0;
+    const int each = (parts + 3) / 4, first = wave * each, end = first + each < parts ? first + each : parts;
     float s = 0.f;
-    for (int r = lo + lane; r < hi; r += kWave) s += of[r - window.first];
+    for (int at = lo + lane; at < hi; at += kWave) {
+#pragma unroll 8
+        for (int p = first; p < end; ++p) s += diagonals[((int64_t)p * a.q_heads + h) * width + at];
+    }
+    if ((lane == 0 && left_end) || (lane == 1 && right_end)) {
+#pragma unroll 8
+        for (int p = first; p < end; ++p) s += diagonals[((int64_t)p * a.q_heads + h) * width + window.size + lane];
+    }
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) s += __shfl_xor(s, o, kWave);
-    if (lane == 0) {
-        // tiles wholly at one end
-        if (!right && e == a.n_edges) s += of[window.size];
-        if (a.two_sided ? right && e == a.n_edges : e == 0) s += of[window.size + 1];
-        dtable[(int64_t)n * a.q_heads + h] = (T)s;
-    }
+    if (lane == 0) runs[wave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) dtable[(int64_t)n * a.q_heads + h] = (T)(((runs[0] + runs[1]) + runs[2]) + runs[3]);
 }
 
+constexpr int kFewParts = 64;   // workgroups whose diagonals the buckets' kernel adds itself (more of them by a launch of their own)
 struct Plan {
     bool own_queries, own_keys;
     int q_tiles, q_parts, q_part_keys, k_tiles, parts, diagonal_parts;
@@ -700,10 +708,15 @@ template <typename T, int DP> int run(const Call& c)
     }
     if (a.table) {
         const int width = w.size + 2, buckets = (a.n_edges + 1) * (a.two_sided ? 2 : 1);
-        hipLaunchKernelGGL(diagonals_kernel, dim3((width + 63) / 64, a.q_heads), dim3(1024), 0, c.st, c.queries.diagonals, a.q_tokens > 0 ? c.plan.diagonal_parts : 0, a.q_heads, width,
-                           c.table_sums);
-        PRUNER_LAUNCH_CHECK();
-        hipLaunchKernelGGL(buckets_kernel<T>, dim3((buckets + 3) / 4, a.q_heads), dim3(256), 0, c.st, a, c.table_sums, static_cast<T*>(c.dtable));
+        const float* from = c.queries.diagonals;
+        int parts = a.q_tokens > 0 ? c.plan.diagonal_parts : 0;
+        if (parts > kFewParts) {
+            hipLaunchKernelGGL(diagonals_kernel, dim3((width + 63) / 64, a.q_heads), dim3(1024), 0, c.st, from, parts, a.q_heads, width, c.table_sums);
+            PRUNER_LAUNCH_CHECK();
+            from = c.table_sums;
+            parts = 1;
+        }
+        hipLaunchKernelGGL(buckets_kernel<T>, dim3(buckets, a.q_heads), dim3(256), 0, c.st, a, from, parts, static_cast<T*>(c.dtable));
         PRUNER_LAUNCH_CHECK();
     }
     return PRUNER_OK;
