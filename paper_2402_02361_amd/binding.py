@@ -7,6 +7,7 @@ same attribute names.
 import ctypes as C
 import math
 import os
+import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -130,29 +131,29 @@ def load_library():
         lib.pruner_verify_score.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, P(CMlp), C.c_void_p,
                                             C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_checkpoint_pack.restype = C.c_int
-        lib.pruner_checkpoint_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, P(CCheckpoint), C.c_void_p]
+        lib.pruner_checkpoint_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p]
         lib.pruner_checkpoint_restore.restype = C.c_int
-        lib.pruner_checkpoint_restore.argtypes = [P(CCheckpoint), C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        lib.pruner_checkpoint_restore.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
         lib.pruner_checkpoint_wgrad_workspace_bytes.restype = C.c_size_t
         lib.pruner_checkpoint_wgrad_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
         lib.pruner_checkpoint_wgrad.restype = C.c_int
-        lib.pruner_checkpoint_wgrad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, P(CCheckpoint), C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+        lib.pruner_checkpoint_wgrad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                                                 C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_gated_norm.restype = C.c_int
-        lib.pruner_gated_norm.argtypes = [P(CNorm), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, P(CCheckpoint), C.c_void_p]
+        lib.pruner_gated_norm.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.pruner_gated_norm_grad_workspace_bytes.restype = C.c_size_t
         lib.pruner_gated_norm_grad_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
         lib.pruner_gated_norm_grad.restype = C.c_int
-        lib.pruner_gated_norm_grad.argtypes = [P(CNorm), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, P(CCheckpoint),
+        lib.pruner_gated_norm_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
                                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_rel_attention_workspace_bytes.restype = C.c_size_t
-        lib.pruner_rel_attention_workspace_bytes.argtypes = [P(CAttention)]
+        lib.pruner_rel_attention_workspace_bytes.argtypes = [C.c_void_p]
         lib.pruner_rel_attention.restype = C.c_int
-        lib.pruner_rel_attention.argtypes = [P(CAttention)] + [P(CHeads)] * 4 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_rel_attention.argtypes = [C.c_void_p] * 5 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_rel_attention_grad_workspace_bytes.restype = C.c_size_t
-        lib.pruner_rel_attention_grad_workspace_bytes.argtypes = [P(CAttention)]
+        lib.pruner_rel_attention_grad_workspace_bytes.argtypes = [C.c_void_p]
         lib.pruner_rel_attention_grad.restype = C.c_int
-        lib.pruner_rel_attention_grad.argtypes = [P(CAttention)] + [P(CHeads)] * 5 + [C.c_void_p] + [P(CHeads)] * 3 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.pruner_rel_attention_grad.argtypes = [C.c_void_p] * 10 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         lib.pruner_workspace_bytes.restype = C.c_size_t
         lib.pruner_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
         lib.pruner_strerror.restype = C.c_char_p
@@ -424,6 +425,9 @@ _ATTENTION_CAUSAL, _ATTENTION_TWO_SIDED = 1, 2
 
 
 _dtypes, _raw_stream = {}, None
+# The structs of include/pruner.h as bytes, which a call takes like a pointer to them (a ctypes structure takes a call of a few microseconds half of one more).
+_PACK_CHECKPOINT, _PACK_HEADS = struct.Struct("@2P"), struct.Struct("@P3q")
+_PACK_NORM, _PACK_ATTENTION = struct.Struct("@q3i2f4x3Pq"), struct.Struct("@8if4x4Pi4x")
 
 
 def _dtype(t):
@@ -465,7 +469,7 @@ def _c_checkpoint(kept, rows, dim):
     codes, exps = kept
     assert codes.is_cuda and codes.dtype == torch.int8 and codes.is_contiguous() and codes.shape == (rows, dim), "codes"
     assert exps.is_cuda and exps.dtype == torch.uint8 and exps.is_contiguous() and exps.shape == (rows, -(-dim // CHECKPOINT_GROUP)), "exps"
-    return CCheckpoint(codes.data_ptr(), exps.data_ptr())
+    return _PACK_CHECKPOINT.pack(codes.data_ptr(), exps.data_ptr())
 
 
 def _new_checkpoint(rows, dim, device):
@@ -480,7 +484,7 @@ def checkpoint_pack(x, kept=None, stream=None):
     rows, dim = x.shape
     if kept is None:
         kept = _new_checkpoint(rows, dim, x.device)
-    rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, C.byref(_c_checkpoint(kept, rows, dim)), _stream_on(stream, x))
+    rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, _c_checkpoint(kept, rows, dim), _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_pack")
     return kept
@@ -495,7 +499,7 @@ def checkpoint_restore(kept, dtype=None, x=None, stream=None):
         x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
     assert x.shape == (rows, dim), "x"
     p, pitch = _rows_of(x, "x")
-    rc = lib.pruner_checkpoint_restore(C.byref(_c_checkpoint(kept, rows, dim)), _dtype(x.dtype), rows, dim, p, pitch, _stream_on(stream, x))
+    rc = lib.pruner_checkpoint_restore(_c_checkpoint(kept, rows, dim), _dtype(x.dtype), rows, dim, p, pitch, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_restore")
     return x
@@ -514,7 +518,7 @@ def checkpoint_wgrad(dy, kept, dw=None, accumulate=False, workspace=None, stream
         dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
     assert dw.is_cuda and dw.dtype == torch.float32 and dw.is_contiguous() and dw.shape == (n_out, dim), "dw"
     held, ws, size = _scratch(workspace, lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim), dy.device)
-    rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, C.byref(_c_checkpoint(kept, rows, dim)), rows, n_out, dim, dw.data_ptr(), int(accumulate), ws, size,
+    rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, _c_checkpoint(kept, rows, dim), rows, n_out, dim, dw.data_ptr(), int(accumulate), ws, size,
                                      _stream_on(stream, dy))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_wgrad")
@@ -535,8 +539,8 @@ def _c_norm(x, has_f, w_post, w_pre, gate, alpha, eps, center):
     elif gate is not None:
         assert gate.dtype == x.dtype and gate.shape == x.shape, "gate"
         pitch = _rows_of(gate, "gate")[1]
-    return CNorm(rows, dim, _dtype(x.dtype), int(bool(center)), alpha, eps, _vector(w_post, dim, "w_post") if has_f else None,
-                 _vector(w_pre, dim, "w_pre") if w_pre is not None else None, gate.data_ptr() if gate is not None else None, pitch)
+    return _PACK_NORM.pack(rows, dim, _dtype(x.dtype), 1 if center else 0, alpha, eps, _vector(w_post, dim, "w_post") if has_f else 0,
+                           _vector(w_pre, dim, "w_pre") if w_pre is not None else 0, gate.data_ptr() if gate is not None else 0, pitch)
 
 
 def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, checkpoint=False, stream=None):
@@ -555,7 +559,7 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
     y = torch.empty_like(h) if w_pre is not None else None
     kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
-    rc = lib.pruner_gated_norm(C.byref(p), px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), C.byref(_c_checkpoint(kept, rows, dim)) if checkpoint else None, _stream_on(stream, x))
+    rc = lib.pruner_gated_norm(p, px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), _c_checkpoint(kept, rows, dim) if checkpoint else None, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_gated_norm")
     return h, y, kept
@@ -584,7 +588,7 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
             dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
     dw_pre = torch.empty_like(w_pre)
     held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device)
-    rc = lib.pruner_gated_norm_grad(C.byref(p), pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, C.byref(_c_checkpoint(kept, rows, dim)) if kept is not None else None,
+    rc = lib.pruner_gated_norm_grad(p, pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, _c_checkpoint(kept, rows, dim) if kept is not None else None,
                                     _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), ws, size, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_gated_norm_grad")
@@ -604,16 +608,16 @@ def relative_edges(n, max_distance):
 
 
 def _heads(t, what):
-    """A tensor [batch, tokens, heads, head_dim], the last dimension contiguous, as a CHeads (dimensions of one element have no stride of their own)."""
-    assert t.is_cuda and t.dim() == 4 and (t.stride(3) == 1 or t.shape[3] == 1), what
-    n, st = t.shape, t.stride()
-    return CHeads(t.data_ptr(), st[0] if n[0] > 1 else 0, st[1] if n[1] > 1 else 0, st[2] if n[2] > 1 else 0)
+    """A tensor [batch, tokens, heads, head_dim], the last dimension contiguous, as a pruner_heads (dimensions of one element have no stride of their own)."""
+    (b, n, h, d), (sb, sn, sh, sd) = t.shape, t.stride()
+    assert t.is_cuda and (sd == 1 or d == 1), what
+    return _PACK_HEADS.pack(t.data_ptr(), sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)
 
 
 def _lengths(t, batch, what):
     import torch
     if t is None:
-        return None
+        return 0
     assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == batch, what
     return t.data_ptr()
 
@@ -631,11 +635,12 @@ def _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale):
         assert table.is_cuda and table.dtype == q.dtype and table.is_contiguous() and table.dim() == 2 and table.shape[1] == q_heads, "table"
         assert table.shape[0] in (n_edges + 1, 2 * (n_edges + 1)), "table: n_edges + 1 buckets, or twice as many"
         flags |= _ATTENTION_TWO_SIDED if table.shape[0] == 2 * (n_edges + 1) else 0
-    a = CAttention(_dtype(q.dtype), batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, flags, 1.0 / math.sqrt(head_dim) if scale is None else scale,
-                   _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"), table.data_ptr() if table is not None else None,
-                   edges.__array_interface__["data"][0] if n_edges else None, n_edges)
-    a.keep = edges   # (the host array lives as long as the struct)
-    return a
+    if scale is None:
+        scale = 1.0 / math.sqrt(head_dim)
+    # (the edges are held until the call has been made)
+    return _PACK_ATTENTION.pack(_dtype(q.dtype), batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, flags, scale, _lengths(q_len, batch, "q_len"),
+                                _lengths(k_len, batch, "k_len"), table.data_ptr() if table is not None else 0, edges.__array_interface__["data"][0] if n_edges else 0,
+                                n_edges), edges
 
 
 def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causal=False, scale=None, o=None, want_lse=False, workspace=None, stream=None):
@@ -646,11 +651,12 @@ def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causa
     Returns o [batch, q_tokens, q_heads, head_dim], with want_lse=True (o, lse float32 [batch, q_heads, q_tokens])."""
     import torch
     lib = load_library()
-    a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    a, held_edges = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    batch, q_tokens, q_heads, _ = q.shape
     if o is None:
         o = torch.empty_like(q, memory_format=torch.contiguous_format)
     assert o.shape == q.shape and o.dtype == q.dtype, "o"
-    lse = torch.empty((a.batch, a.q_heads, a.q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
     held, ws, size = _scratch(workspace, lib.pruner_rel_attention_workspace_bytes(a), q.device)
     rc = lib.pruner_rel_attention(a, _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
     if rc:
@@ -663,9 +669,10 @@ def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, 
     Returns (dq, dk, dv, dtable), dtable None without table."""
     import torch
     lib = load_library()
-    a = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    a, held_edges = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    batch, q_tokens, q_heads, _ = q.shape
     assert do.shape == q.shape and do.dtype == q.dtype and o.shape == q.shape and o.dtype == q.dtype, "do, o"
-    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (a.batch, a.q_heads, a.q_tokens), "lse"
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, q_heads, q_tokens), "lse"
     dense = torch.contiguous_format
     dq, dk, dv = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense), torch.empty_like(v, memory_format=dense)
     dtable = torch.empty_like(table) if table is not None else None
