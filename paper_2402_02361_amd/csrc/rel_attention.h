@@ -160,6 +160,27 @@ template <int DP> struct Lane {
     }
 };
 
+// N products, each with an operand from LDS that is read AHEAD products before it is needed: left to itself the compiler reads each right before its
+// product and waits for it, MEASURED.
+template <int N, int AHEAD> struct Operands {
+    u32x4 w[AHEAD];
+    template <typename Read> __device__ __forceinline__ void start(const Read& read)
+    {
+#pragma unroll
+        for (int i = 0; i < AHEAD && i < N; ++i) w[i] = read(i);
+        __builtin_amdgcn_sched_barrier(6);
+    }
+    template <typename Read, typename Use> __device__ __forceinline__ void products(const Read& read, const Use& use)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            use(i, w[i % AHEAD]);
+            if (i + AHEAD < N) w[i % AHEAD] = read(i + AHEAD);
+            __builtin_amdgcn_sched_barrier(6);   // (vector and scalar arithmetic may cross, reads and products stay as written)
+        }
+    }
+};
+
 // ROWS rows on their way from memory to a tile, by THREADS threads.  Reads are bounds-checked buffer loads: rows at or beyond `rows` and columns at or beyond
 // the head dimension arrive as zeros.  (Where tokens lie closer than a head is wide, rows overlap and a row that is not there may arrive as one that
 // is; nothing depends on it, its pairs are masked.)
@@ -208,6 +229,9 @@ __device__ __forceinline__ void request_4(uint32_t lds, uint32_t at, u32x4 from)
     asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(from) : "memory");
 }
 template <int N> __device__ __forceinline__ void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// Before a loop: all that was loaded into registers has come.  (Where the compiler finds a first use inside the loop, it waits there each time, and with
+// that for the requests, of which it does not know.)
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
 // Before a wavefront asks for a tile of its own again: what it read of the last one has come.
 __device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ u32x4 buffer_of(const void* base, int bytes)   // base and bytes: the same in all lanes

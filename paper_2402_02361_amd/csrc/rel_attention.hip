@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         kf.request(kp + (int64_t)key0 * a.k.token, left, to);
         vf.request(vp + (int64_t)key0 * a.v.token, left, to + kTileBytes);
     };
+    constexpr int kAheadK = 4, kAheadV = 4;
     constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
     if (begin < end)
 #pragma unroll
@@ -183,6 +184,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
         const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
+        settle();
         int turn = 0;
         for (int key0 = begin; key0 < end; key0 += kN) {
             if constexpr (SHARED) {
@@ -197,24 +199,25 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
             if (key0 < seen) {
                 floatx16 s[kN / 32];
 #pragma unroll
-                for (int n = 0; n < kN / 32; ++n) {
-                    s[n] = zero16();
-#pragma unroll
-                    for (int st = 0; st < Tile<DP>::kSteps; ++st) s[n] = mfma(at.rows(kt, n, st), qf[st], s[n], T{});
-                }
+                for (int n = 0; n < kN / 32; ++n) s[n] = zero16();
+                auto key = [&](int x) { return at.rows(kt, x % (kN / 32), x / (kN / 32)); };
+                Operands<kN / 32 * Tile<DP>::kSteps, kAheadK> keys;
+                keys.start(key);
+                keys.products(key, [&](int x, u32x4 w) { s[x % (kN / 32)] = mfma(w, qf[x / (kN / 32)], s[x % (kN / 32)], T{}); });
+                auto value = [&](int x) { return at.columns(kt + kTileBytes, x % Tile<DP>::kBlocks, x / Tile<DP>::kBlocks); };
+                Operands<kN / 16 * Tile<DP>::kBlocks, kAheadV> values;
+                values.start(value);
                 const int r_lo = key0 - (kl - ql + q0 + 31), r_hi = key0 + kN - 1 - (kl - ql + q0);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
                 const bool fused = finish_scores(s, a, biases, window.first, place, bias, key0, p, limit, key0 + kN > all_see, half);
                 run.weigh(s, fused, a.scale, bias);
-#pragma unroll
-                for (int n = 0; n < kN / 32; ++n)
-#pragma unroll
-                    for (int st = 0; st < 2; ++st) {
-                        const u32x4 w = weights_of<T>(s[n], st);
-#pragma unroll
-                        for (int d = 0; d < Tile<DP>::kBlocks; ++d) run.o[d] = mfma(at.columns(kt + kTileBytes, d, 2 * n + st), w, run.o[d], T{});
-                    }
+                u32x4 weights{};
+                values.products(value, [&](int x, u32x4 w) {
+                    const int step = x / Tile<DP>::kBlocks, d = x % Tile<DP>::kBlocks;
+                    if (d == 0) weights = weights_of<T>(s[step / 2], step % 2);
+                    run.o[d] = mfma(w, weights, run.o[d], T{});
+                });
             }
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;

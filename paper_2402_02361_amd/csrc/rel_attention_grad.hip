@@ -179,11 +179,15 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         // P (in s) and dP (in ds) of 32 keys from k0; returns where they lie
         auto weigh = [&](const char* kt, int n, int k0, floatx16& s, floatx16& ds) {
             s = ds = zero16();
-#pragma unroll
-            for (int st = 0; st < Tile<DP>::kSteps; ++st) {
-                s = mfma(at.rows(kt, n, st), qf[st], s, T{});
-                ds = mfma(at.rows(kt + kTileBytes, n, st), df[st], ds, T{});
-            }
+            auto key_or_value = [&](int x) { return at.rows(kt + x % 2 * kTileBytes, n, x / 2); };
+            Operands<2 * Tile<DP>::kSteps, 6> rows;
+            rows.start(key_or_value);
+            rows.products(key_or_value, [&](int x, u32x4 w) {
+                if (x % 2 == 0)
+                    s = mfma(w, qf[x / 2], s, T{});
+                else
+                    ds = mfma(w, df[x / 2], ds, T{});
+            });
             const int r_lo = k0 - (kl - ql + q0 + 31), r_hi = k0 + 31 - (kl - ql + q0);
             const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
             const float bias = place == kRight ? bias_right : bias_left;
@@ -205,6 +209,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
             }
             return place;
         };
+        settle();
         if constexpr (!SHARED) {
             // delta as the sum of P dP: o is rounded, and with a few keys what it lost is as large as the gradient's own rounding
             for (int key0 = 0; key0 < end; key0 += kN) {
@@ -239,6 +244,9 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                 if (k0 >= seen) continue;
                 floatx16 s, ds;
                 const int place = weigh(kt, n, k0, s, ds);
+                auto key = [&](int x) { return at.columns(kt, x % Tile<DP>::kBlocks, 2 * n + x / Tile<DP>::kBlocks); };
+                Operands<2 * Tile<DP>::kBlocks, 4> columns;
+                columns.start(key);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) ds[e] = s[e] * (ds[e] - delta);
                 if (a.table) {
@@ -260,12 +268,11 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
                             sum_left += sum;
                     }
                 }
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const u32x4 w = weights_of<T>(ds, st);
-#pragma unroll
-                    for (int d = 0; d < Tile<DP>::kBlocks; ++d) dq[d] = mfma(at.columns(kt, d, 2 * n + st), w, dq[d], T{});
-                }
+                u32x4 weights{};
+                columns.products(key, [&](int x, u32x4 w) {
+                    if (x % Tile<DP>::kBlocks == 0) weights = weights_of<T>(ds, x / Tile<DP>::kBlocks);
+                    dq[x % Tile<DP>::kBlocks] = mfma(w, weights, dq[x % Tile<DP>::kBlocks], T{});
+                });
             }
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;
@@ -408,11 +415,13 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
         else
             return vf[st];
     };
+    constexpr int kAheadR = kWide ? 4 : 6, kAheadC = 4;
     floatx16 dk[Tile<DP>::kBlocks], dv[Tile<DP>::kBlocks];
 #pragma unroll
     for (int d = 0; d < Tile<DP>::kBlocks; ++d) dk[d] = dv[d] = zero16();
 
     if (from < to) {
+        settle();
         int turn = 0, head_filled = -1;
         float bias_left = 0.f, bias_right = 0.f;
         for (int n = from; n < to; ++n) {
@@ -445,11 +454,28 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
                 const int r_lo = k0 - (p0 + 31), r_hi = k0 + 31 - p0;
                 if (k0 >= kl || i0 + 32 * m >= ql || (a.causal && r_lo > 0)) continue;   // (no pair here that counts)
                 floatx16 s = zero16(), dp = zero16();
-#pragma unroll
-                for (int step = 0; step < Tile<DP>::kSteps; ++step) {
-                    s = mfma(at.rows(qt, m, step), kf[step], s, T{});
-                    dp = mfma(at.rows(qt + kTileBytes, m, step), value(step), dp, T{});
+                auto query_or_gradient = [&](int x) { return at.rows(qt + x % 2 * kTileBytes, m, x / 2); };
+                Operands<2 * Tile<DP>::kSteps, kAheadR> rows;
+                u32x4 of_value[2];   // (wide: values two steps ahead as well)
+                if constexpr (kWide) {
+                    of_value[0] = value(0);
+                    of_value[1] = value(1);
                 }
+                rows.start(query_or_gradient);
+                rows.products(query_or_gradient, [&](int x, u32x4 w) {
+                    const int step = x / 2;
+                    if (x % 2 == 0) {
+                        s = mfma(w, kf[step], s, T{});
+                    } else if constexpr (kWide) {
+                        dp = mfma(w, of_value[step % 2], dp, T{});
+                        if (step + 2 < Tile<DP>::kSteps) of_value[step % 2] = value(step + 2);
+                    } else {
+                        dp = mfma(w, vf[step], dp, T{});
+                    }
+                });
+                auto turned = [&](int x) { return at.columns(qt + (x % 2 == 0 ? kTileBytes : 0), x / 2 % Tile<DP>::kBlocks, 2 * m + x / (2 * Tile<DP>::kBlocks)); };
+                Operands<4 * Tile<DP>::kBlocks, kAheadC> columns;
+                if constexpr (!kWide) columns.start(turned);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
                 if (place == kNear || !(__builtin_fabsf(bias) < kHuge)) {
@@ -482,15 +508,19 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
 #pragma unroll
                     for (int e = 0; e < 4; ++e) dp[4 * g4 + e] = s[4 * g4 + e] * __builtin_fmaf(dp[4 * g4 + e], Held<T>::kUnit, x[e]);
                 }
-#pragma unroll
-                for (int step = 0; step < 2; ++step) {
-                    const u32x4 wp = weights_of<T>(s, step), wd = weights_of<T>(dp, step);
-#pragma unroll
-                    for (int d = 0; d < Tile<DP>::kBlocks; ++d) {
-                        dv[d] = mfma(at.columns(qt + kTileBytes, d, 2 * m + step), wp, dv[d], T{});
-                        dk[d] = mfma(at.columns(qt, d, 2 * m + step), wd, dk[d], T{});
+                if constexpr (kWide) columns.start(turned);
+                u32x4 wp{}, wd{};
+                columns.products(turned, [&](int x, u32x4 w) {
+                    const int step = x / (2 * Tile<DP>::kBlocks), d = x / 2 % Tile<DP>::kBlocks;
+                    if (x % (2 * Tile<DP>::kBlocks) == 0) {
+                        wp = weights_of<T>(s, step);
+                        wd = weights_of<T>(dp, step);
                     }
-                }
+                    if (x % 2 == 0)
+                        dv[d] = mfma(w, wp, dv[d], T{});
+                    else
+                        dk[d] = mfma(w, wd, dk[d], T{});
+                });
             }
             if constexpr (SHARED) {
                 turn = turn == kTurns - 1 ? 0 : turn + 1;
