@@ -202,16 +202,19 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
                 for (int n = 0; n < kN / 32; ++n) s[n] = zero16();
                 auto key = [&](int x) { return at.rows(kt, x % (kN / 32), x / (kN / 32)); };
                 Operands<kN / 32 * Tile<DP>::kSteps, kAheadK> keys;
+                __builtin_amdgcn_s_setprio(0);
                 keys.start(key);
                 keys.products(key, [&](int x, u32x4 w) { s[x % (kN / 32)] = mfma(w, qf[x / (kN / 32)], s[x % (kN / 32)], T{}); });
                 auto value = [&](int x) { return at.columns(kt + kTileBytes, x % Tile<DP>::kBlocks, x / Tile<DP>::kBlocks); };
                 Operands<kN / 16 * Tile<DP>::kBlocks, kAheadV> values;
                 values.start(value);
+                __builtin_amdgcn_s_setprio(1);
                 const int r_lo = key0 - (kl - ql + q0 + 31), r_hi = key0 + kN - 1 - (kl - ql + q0);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
                 const bool fused = finish_scores(s, a, biases, window.first, place, bias, key0, p, limit, key0 + kN > all_see, half);
                 run.weigh(s, fused, a.scale, bias);
+                __builtin_amdgcn_s_setprio(0);
                 u32x4 weights{};
                 values.products(value, [&](int x, u32x4 w) {
                     const int step = x / Tile<DP>::kBlocks, d = x % Tile<DP>::kBlocks;
