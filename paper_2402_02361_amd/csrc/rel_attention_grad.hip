@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
 // sixteen bytes of every step side by side in LDS.
 template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr bool kWide = SHARED && DP == 128;
-    static constexpr int kWaves = kWide ? 8 : 4;              // of a workgroup
+    static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this takes 228)
     static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
     static constexpr int kTurns = SHARED ? (kWide ? 2 : 3) : 1;
     static constexpr int kStat = 64;                          // floats of a tile's stats, three of them
@@ -669,8 +669,8 @@ Plan plan_of(const pruner_attention* a)
     }
     if (!p.own_keys && rows > 0 && keys > 0) {
         const int step = dp < 128 ? 64 : 32;
-        p.parts = parts_of((double)a->batch * a->kv_heads * p.k_tiles, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, dp < 128 ? 512 : 256, dp == 128 ? 2.2 : dp == 64 ? 1.5 : 1.0,
-                           dp == 128 ? 2.8 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
+        p.parts = parts_of((double)a->batch * a->kv_heads * p.k_tiles, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, 512, dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0,
+                           dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
     }
     // (the window for the largest edge that there can be: sizes alone decide)
     const int64_t reach = (int64_t)a->q_tokens + a->k_tokens;
