@@ -110,11 +110,44 @@ struct Window {
     int first, size;
     __host__ __device__ Window(int left, int right) : first(-left - kWindowPad), size(left + right + 2 * kWindowPad) {}
 };
-template <typename T> __device__ __forceinline__ void fill_window(const Args& a, float* lds, int h, int thread, int threads)
-{
-    const Window w(a.left, a.right);
-    for (int i = thread; i < w.size; i += threads) lds[i] = a.bias<T>(a.bucket(w.first + i), h);
-}
+// Filled by THREADS threads in two calls, so that the table's first values come while other things are asked for: a thread's first kAtOnce places are loaded
+// by load(), the rest by store().
+template <typename T, int THREADS> struct WindowFill {
+    static constexpr int kAtOnce = THREADS >= 256 ? 2 : 4;
+    T x[kAtOnce];
+    __device__ __forceinline__ void load_from(const Args& a, const Window& w, int h, int first)
+    {
+        int d[kAtOnce], n[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int r = w.first + first + THREADS * u;
+            d[u] = r < 0 ? -r : a.two_sided ? r : 0;
+            n[u] = a.two_sided && r > 0 ? a.n_edges + 1 : 0;
+        }
+        for (int e = 0; e < a.n_edges; e += 16)   // (sixteen edges by one scalar load; those past the last are beyond every distance)
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) n[u] += a.edges[e + k] <= d[u] ? 1 : 0;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) x[u] = static_cast<const T*>(a.table)[(int64_t)n[u] * a.q_heads + h];   // (a bucket for every r)
+    }
+    __device__ __forceinline__ void store_to(float* lds, const Window& w, int first) const
+    {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (first + THREADS * u < w.size) lds[first + THREADS * u] = (float)x[u];
+    }
+    __device__ __forceinline__ void load(const Args& a, const Window& w, int h, int thread) { load_from(a, w, h, thread); }
+    __device__ __forceinline__ void store(const Args& a, const Window& w, float* lds, int h, int thread)
+    {
+        store_to(lds, w, thread);
+        for (int i = thread + THREADS * kAtOnce; i < w.size; i += THREADS * kAtOnce) {
+            load_from(a, w, h, i);
+            store_to(lds, w, i);
+        }
+    }
+};
 // Where a tile with r = r_lo .. r_hi lies.
 enum { kNear, kLeft, kRight };
 __device__ __forceinline__ int place_of(const Args& a, int r_lo, int r_hi) { return r_hi <= -a.left ? kLeft : r_lo >= a.right ? kRight : kNear; }

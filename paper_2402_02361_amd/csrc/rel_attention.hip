@@ -85,10 +85,11 @@ template <typename T, int DP> struct Running {
 // Keys at or beyond `limit` leave the softmax.
 template <int N> __device__ __forceinline__ void mask_scores(floatx16 (&s)[N], int key0, int limit, int half)
 {
+    const int left = limit - key0 - 4 * half;
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = key0 + 32 * n + row_of(i, half) < limit ? s[n][i] : -ATT_INF;
+        for (int i = 0; i < 16; ++i) s[n][i] = 32 * n + row_of(i, 0) < left ? s[n][i] : -ATT_INF;
 }
 
 // Scores with their bias and mask for one query (position p) against keys key0 + 32 n + row.  bias_end: the bias of tiles at either end.
@@ -118,7 +119,7 @@ __device__ __forceinline__ bool finish_scores(floatx16 (&s)[N], const Args& a, c
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -ATT_INF : __builtin_fmaf(__builtin_amdgcn_logf(l), kLn2, m); }   // (logf: base 2)
 
 template <typename T, int DP, bool SHARED>
-__global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
+__global__ void __launch_bounds__(256, (DP == 128 ? 2 : 3)) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
 {
     constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -136,8 +137,15 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
         if (bh >= (int)heads) return;   // (wavefronts have nothing in common)
     }
     const int b = bh / a.q_heads, h = bh % a.q_heads, hk = h / a.group;
-    const int ql = a.queries(b), kl = a.keys(b);
     const Window window(a.left, a.right);
+    WindowFill<T, kThreads> fill;
+    float bias_left = 0.f, bias_right = 0.f;
+    if (a.table) {
+        fill.load(a, window, h, thread);
+        bias_left = a.bias<T>(a.n_edges, h);
+        bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
+    }
+    const int ql = a.queries(b), kl = a.keys(b);
     const int window_bytes = a.table ? (window.size * 4 + 15) & ~15 : 0;
     char* const tiles = lds + (SHARED ? 0 : wave * 2 * kTileBytes);
     float* const biases = reinterpret_cast<float*>(lds + (SHARED ? kTurns : 4) * 2 * kTileBytes + (SHARED ? 0 : wave * window_bytes));
@@ -174,12 +182,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(Args a, Heads out, float* 
     Running<T, DP> run;
     run.clear();
     if (begin < end) {
-        float bias_left = 0.f, bias_right = 0.f;
-        if (a.table) {
-            bias_left = a.bias<T>(a.n_edges, h);
-            bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
-            fill_window<T>(a, biases, h, thread, kThreads);
-        }
+        if (a.table) fill.store(a, window, biases, h, thread);
         // of this wavefront's queries
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;

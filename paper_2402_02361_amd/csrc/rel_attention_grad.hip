@@ -94,8 +94,15 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
         if (bh >= (int)heads) return;
     }
     const int b = bh / a.q_heads, h = bh % a.q_heads, hk = h / a.group;
-    const int ql = a.queries(b), kl = a.keys(b);
     const Window window(a.left, a.right);
+    WindowFill<T, kThreads> fill;
+    float bias_left = 0.f, bias_right = 0.f;
+    if (a.table) {
+        fill.load(a, window, h, thread);
+        bias_left = a.bias<T>(a.n_edges, h);
+        bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
+    }
+    const int ql = a.queries(b), kl = a.keys(b);
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
     // LDS: tiles, biases, every wavefront's diagonals and its skewed square
     char* const tiles = lds + (SHARED ? 0 : wave * 2 * kTileBytes);
@@ -167,12 +174,7 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
             for (int n = lane; n < kSkewFloats; n += kWave) skew[n] = 0.f;
     }
     if (begin < end) {
-        float bias_left = 0.f, bias_right = 0.f;
-        if (a.table) {
-            bias_left = a.bias<T>(a.n_edges, h);
-            bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
-            fill_window<T>(a, biases, h, thread, kThreads);
-        }
+        if (a.table) fill.store(a, window, biases, h, thread);
         const int wave_last = q0 + 31 < ql ? q0 + 31 : ql - 1;
         const int seen = q0 >= ql ? 0 : a.causal ? (kl - ql + wave_last + 1 < kl ? kl - ql + wave_last + 1 : kl) : kl;
         const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, all_see = a.causal ? (kl - ql + q0 + 1 < kl ? kl - ql + q0 + 1 : kl) : kl;
@@ -399,6 +401,17 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     if (from < to)
 #pragma unroll
         for (int t = 0; t < kAhead; ++t) request(from + t, t);
+    WindowFill<T, kThreads> fill;
+    float bias_left = 0.f, bias_right = 0.f;
+    int head_loaded = 0;
+    auto load = [&](int g) {
+        const int h = hk * a.group + g;
+        fill.load(a, window, h, thread);
+        bias_left = a.bias<T>(a.n_edges, h);
+        bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
+        head_loaded = g;
+    };
+    if (from < to && a.table) load(from / each);
     Lane<DP> at;
     at.set(lane);
     const int j = k0 + l32;
@@ -423,14 +436,13 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     if (from < to) {
         settle();
         int turn = 0, head_filled = -1;
-        float bias_left = 0.f, bias_right = 0.f;
         for (int n = from; n < to; ++n) {
             const int g = n / each, h = hk * a.group + g, i0 = (first_tile + n % each) * kQ;
             if (a.table && g != head_filled) {
                 if constexpr (SHARED) __syncthreads(); else wave_fence();   // (the head before is done with its biases)
-                bias_left = a.bias<T>(a.n_edges, h);
-                bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, h);
-                fill_window<T>(a, biases, h, thread, kThreads);
+                if (g != head_loaded) load(g);
+                fill.store(a, window, biases, h, thread);
+                settle();
                 head_filled = g;
             }
             if constexpr (SHARED) {
