@@ -115,9 +115,10 @@ struct Norm {
     const void* gate;
     int64_t gate_pitch;
 };
-enum { kNoGate, kGateRows, kGateVector };
 
-template <typename T, int V, int BLOCK>
+// GATE_ROWS: the gate is a matrix; else one for all rows, or none (known here because a gate's rows take 16 registers in binary32 and with them a workgroup per
+// unit: 16384 x 1100 rows, one gate, 67 us where this takes 64; 5000 x 5000 in binary16 104 and 75).
+template <typename T, int V, int BLOCK, bool GATE_ROWS>
 __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch, T* __restrict__ h,
                                                     T* __restrict__ y, int8_t* __restrict__ codes, uint8_t* __restrict__ exps)
 {
@@ -125,13 +126,15 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
     const int in_block = (int)blockDim.x / p.threads, slot = (int)threadIdx.x / p.threads, t = (int)threadIdx.x - slot * p.threads;
     RowSum sum{meet, p.threads, slot, 0};
     const int col = 8 * t, left = p.dim - col;
-    const int gate = !p.gate ? kNoGate : p.gate_pitch ? kGateRows : kGateVector;
-    float w_post[kEach], w_pre[kEach], s_all[kEach];
+    float w_post[kEach], w_pre[kEach];   // (w_post: with the gate that all rows share)
     load_vector(p.w_post, col, left, w_post);
     load_vector(p.w_pre, col, left, w_pre);
-    load_vector(gate == kGateVector ? static_cast<const float*>(p.gate) : nullptr, col, left, s_all);
+    if (!GATE_ROWS && p.gate) {
+        float g[kEach];
+        load_vector(static_cast<const float*>(p.gate), col, left, g);
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) s_all[j] = gate == kGateVector ? sigmoid(s_all[j]) : 1.f;
+        for (int j = 0; j < kEach; ++j) w_post[j] *= sigmoid(g[j]);
+    }
     const int64_t stride = (int64_t)gridDim.x * in_block;
     Eight<T, V> xin, fin, gin, x_next, f_next, g_next;   // the next row's values are on their way while a row is worked on
     auto fetch = [&](int64_t row) {
@@ -139,7 +142,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
         const int64_t after = p.rows - 1 - row;
         x_next.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left));
         if (f) f_next.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left));
-        if (gate == kGateRows) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
+        if constexpr (GATE_ROWS) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
     for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
@@ -158,13 +161,13 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
             float u[kEach], g[kEach];
             fin.to_floats(u);
             normalise<V>(sum, u, z, mine, p.per_dim, p.center, p.eps);
-            if (gate == kGateRows) {
-                gin.to_floats(g);
+            if constexpr (GATE_ROWS) gin.to_floats(g);
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(sigmoid(g[j]), z[j] * w_post[j], v[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(s_all[j], z[j] * w_post[j], v[j]);
+            for (int j = 0; j < kEach; ++j) {
+                if constexpr (GATE_ROWS)
+                    v[j] = __builtin_fmaf(sigmoid(g[j]), z[j] * w_post[j], v[j]);
+                else
+                    v[j] = __builtin_fmaf(z[j], w_post[j], v[j]);
             }
         }
         Eight<T, V> out;
@@ -404,9 +407,10 @@ struct Held {
 template <typename T, int V>
 int run_norm(const pruner_norm* p, const Shape& s, const void* x, int64_t x_pitch, const void* f, int64_t f_pitch, void* h, void* y, const pruner_checkpoint* kept, hipStream_t st)
 {
-    static Held held[17];   // by wavefronts of a workgroup
-    auto* const kernel = s.block > 256 ? &norm_kernel<T, V, 1024> : &norm_kernel<T, V, 256>;
-    const int64_t blocks = held[s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
+    const bool rows = p->gate && p->gate_pitch;
+    static Held held[2][17];   // by wavefronts of a workgroup
+    auto* const kernel = s.block > 256 ? (rows ? &norm_kernel<T, V, 1024, true> : &norm_kernel<T, V, 1024, false>) : (rows ? &norm_kernel<T, V, 256, true> : &norm_kernel<T, V, 256, false>);
+    const int64_t blocks = held[rows][s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
     if (blocks < 0) return PRUNER_EHIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(x), x_pitch, static_cast<const T*>(f), f_pitch,
                        static_cast<T*>(h), static_cast<T*>(y), kept ? kept->codes : nullptr, kept ? kept->exps : nullptr);
