@@ -388,7 +388,7 @@ int pruner_checkpoint_restore(const pruner_checkpoint* kept, int32_t dtype, int6
  *   dw          device float [n_out][dim]
  *   accumulate  0: dw is overwritten; 1: added to
  * rows >= 0 (0: dw is cleared, or left alone), n_out and dim 1..2^20, n_out x dim up to 2^31.
- * workspace: pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim).
+ * workspace: pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim); 0: none is needed and workspace may be NULL.
  * Errors: PRUNER_EINVAL (null or misaligned pointers: dy 2 bytes, codes 8, dw 4; sizes, type), PRUNER_EWORKSPACE.
  */
 size_t pruner_checkpoint_wgrad_workspace_bytes(int64_t rows, int32_t n_out, int32_t dim);
@@ -438,7 +438,8 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  * stands at position p_i = kl - ql + i (the queries are the last ones of the sequence), key j at j, and
  *     s_ij = scale q_i . k_j + table[bucket(j - p_i)][head],   a_ij = softmax over the keys that query i sees,   o_i = sum_j a_ij v_j
  * It sees keys j < kl; with PRUNER_ATTENTION_CAUSAL only j <= p_i.  lse_i = log sum_j exp(s_ij).  A query that sees no key (and a row at or
- * beyond ql) has o = 0, lse = -infinity, and passes no gradient.  What rows beyond the lengths hold does not matter.
+ * beyond ql) has o = 0, lse = -infinity, and passes no gradient.  What rows beyond the lengths hold does not matter.  (A NaN or an infinity in a value
+ * or a gradient within the lengths may reach every row of its sequence: its weight there is 0, but it is multiplied.)
  * Query head h reads key/value head h / (q_heads / kv_heads).
  *   bucket(r) = the number of edges <= |r|, plus n_edges + 1 if r > 0 (two-sided: table [2 (n_edges + 1)][q_heads]); one-sided: the number of
  *   edges <= max(-r, 0) (table [n_edges + 1][q_heads]); edges ascend strictly, 1 <= edge <= PRUNER_MAX_BIAS_DISTANCE.
@@ -456,7 +457,8 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  * Outputs are written for every row of q_tokens and k_tokens.  dk and dv are the sums over the query heads that share a key head.
  * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, batch x q_heads x max(64, q_tokens) below 2^30, and for the
  * gradients batch x kv_heads x max(64, k_tokens) as well.
- * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes only.
+ * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes only.  0: none is
+ * needed and workspace may be NULL.
  * Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
  */
 #define PRUNER_MAX_BIAS_EDGES 64

