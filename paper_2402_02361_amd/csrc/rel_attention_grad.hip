@@ -1,19 +1,21 @@
 // Attention with a learned relative position bias by buckets, backward.  With P = exp(s - lse), dP = dO V^T, delta_i = sum_d dO o:
 //     dS = P (dP - delta);   dQ = scale dS K;   dK = scale dS^T Q;   dV = P^T dO;   dtable[n][h] = sum of dS over the pairs of bucket n
 //
-//   queries_kernel   a wavefront owns 32 queries, as in the forward pass: S^T and dP^T leave a query's values in its two lanes; dQ^T += K^T dS^T.
-//                    It also leaves delta for the next kernel, and the sums of dS along the diagonals j - p: a tile beyond the largest edge
-//                    adds into one register, the others add into LDS, where every wavefront has diagonals of its own.
-//   keys_kernel      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
-//                    through the query tiles of all heads that share the key head.  Where key tiles are too few for the device, their query
-//                    tiles are cut into parts, whose sums go to the workspace (keys_join_kernel adds them in order).
+//   queries   a wavefront owns 32 queries, as in the forward pass: S^T and dP^T leave a query's values in its two lanes; dQ^T += K^T dS^T.
+//             It also leaves the sums of dS along the diagonals j - p: a tile beyond the largest edge adds into one register, the others add
+//             into LDS, where every wavefront has diagonals of its own.
+//   keys      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
+//             through the query tiles of all heads that share the key head.
+//   Where either has too few tiles for the device, their long axis is cut into parts, whose sums go to the workspace (join_kernel adds them in order).
+//   stats_kernel, both_kernel    lse and delta of every query, then queries and keys in one launch.
+//   queries_kernel, keys_kernel  the same for sequences of few queries and keys, each by a wavefront; delta is the sum of P dP there.
 //   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, and the diagonals of a bucket (where the workgroups are few, by the
-//                    latter alone).
+//             latter alone).
 // S and dP are formed twice (14 products of a pair's depth where 10 would do), so that nothing is added across workgroups but in a fixed order.
 //
-// Bound: the matrix cores with the exponentials and LDS reads between their products.  5001 causal tokens, 16 heads of 128 sharing 4: queries 190 us (820
-// TFLOP/s), keys 240 (860) and 23 for their parts, where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 36 to 45 us either, bound by
-// a workgroup's chain of tiles and its start (5 us).
+// Bound: the matrix cores with the exponentials and LDS reads between their products.  5001 causal tokens, 16 heads of 128 sharing 4: 414 us in all, queries alone on the device
+// 190 (820 TFLOP/s), keys 240 (860), where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 79 us in all, bound by a
+// workgroup's chain of tiles and its start (5 us).
 #include "rel_attention.h"
 
 namespace pruner {
@@ -78,8 +80,7 @@ __device__ __forceinline__ void add_diagonals(float* skew, float* sums, const fl
     }
 }
 
-template <typename T, int DP, bool SHARED>
-__global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_tiles)
+template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queries_of(const Args& a, const Grad& gr, int q_tiles, uint32_t block)
 {
     constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);   // (64 keys of 128 would leave no room for a second workgroup)
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -87,13 +88,13 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
     int bh, q0, tile_id = 0, part = 0;   // (tile_id: of the tiles and their parts)
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles * gr.parts);
+        const Item it = item_of(block, (uint32_t)a.batch * a.kv_heads, a.group, (uint32_t)q_tiles * gr.parts);
         bh = it.head;
         tile_id = it.tile;
         part = it.tile % gr.parts;
         q0 = it.tile / gr.parts * 128 + 32 * wave;
     } else {
-        bh = (int)(blockIdx.x * 4 + wave);
+        bh = (int)(block * 4 + wave);
         q0 = 0;
         if (bh >= (int)heads) return;
     }
@@ -151,22 +152,14 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     float delta = 0.f, lse = ATT_INF;
     const int64_t row = (int64_t)bh * a.q_tokens + i;
     if (mine) {
-        lse = gr.lse[row];
-        lse = lse == -ATT_INF ? ATT_INF : lse;   // (no key: every weight is exp(-infinity))
-    }
-    if constexpr (SHARED) {
-        u32x4 of[Tile<DP>::kSteps];
-        load_row<T, DP>(of, gr.o.at<T>(b, h) + (int64_t)i * gr.o.token, mine, a.head_dim, half);
-#pragma unroll
-        for (int s = 0; s < Tile<DP>::kSteps; ++s)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const f32x2 x = pair_to(of[s][w], T{}), y = pair_to(df[s][w], T{});
-                delta = __builtin_fmaf(x[0], y[0], delta);
-                delta = __builtin_fmaf(x[1], y[1], delta);
-            }
-        delta = sum_of_halves(delta);
-        if (half == 0 && part == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
+        if constexpr (SHARED) {
+            const int64_t stat = (int64_t)bh * gr.stat_rows + i;
+            lse = gr.stats[stat];
+            delta = gr.stats[2 * (int64_t)heads * gr.stat_rows + stat] * (-1.f / Held<T>::kUnit);
+        } else {
+            lse = gr.lse[row];
+            lse = lse == -ATT_INF ? ATT_INF : lse;   // (no key: every weight is exp(-infinity))
+        }
     }
     floatx16 dq[Tile<DP>::kBlocks];
 #pragma unroll
@@ -328,11 +321,13 @@ __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr, int q_
     }
 }
 
+template <typename T, int DP> __global__ void __launch_bounds__(256, 2) queries_kernel(Args a, Grad gr) { queries_of<T, DP, false>(a, gr, 1, blockIdx.x); }
+
 // A wavefront's keys and values are operands in registers; of 128 wide heads the values' lie in LDS, each lane's own sixteen bytes of every step side by side (in
 // registers they left the sums no room: 821 us where this took 295 at 5001 causal tokens).
 template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr bool kWide = SHARED && DP == 128;
-    static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this takes 228)
+    static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this took 228)
     static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
     static constexpr int kTurns = SHARED ? (kWide ? 2 : 3) : 1;
     static constexpr int kStat = 64;                          // floats of a tile's stats, three of them
@@ -340,8 +335,7 @@ template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr int kHeldBytes = kWide ? Tile<DP>::kSteps * 1024 : 0;   // of a wavefront
     static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
 };
-template <typename T, int DP, bool SHARED>
-__global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHARED || DP < 128 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles)
+template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_of(const Args& a, const Grad& gr, int k_tiles, uint32_t block)
 {
     typedef KeysShape<T, DP, SHARED> Shape;
     constexpr int kQ = Shape::kQ, kThreads = SHARED ? 64 * Shape::kWaves : 64, kTileBytes = Shape::kTileBytes, kTurnBytes = Shape::kTurnBytes;
@@ -352,12 +346,12 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     const uint32_t heads = (uint32_t)a.batch * a.kv_heads;
     int part = 0, bh, k0;
     if constexpr (SHARED) {
-        const Item it = item_of(blockIdx.x, heads, 1, (uint32_t)k_tiles * gr.parts);
+        const Item it = item_of(block, heads, 1, (uint32_t)k_tiles * gr.parts);
         bh = it.head;
         part = it.tile % gr.parts;
         k0 = (k_tiles - 1 - it.tile / gr.parts) * Shape::kKeys + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
     } else {
-        const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+        const int64_t unit = (int64_t)block * 4 + wave;
         if (unit >= (int64_t)heads * k_tiles) return;
         bh = (int)(unit / k_tiles);
         k0 = (int)(unit % k_tiles) * 32;
@@ -562,10 +556,53 @@ __global__ void __launch_bounds__((64 * KeysShape<T, DP, SHARED>::kWaves), (SHAR
     }
 }
 
-// The parts of a key's (a query's) sums, four neighbouring values a thread.  Bound: memory (seven parts of 5001 x 4 x 256 floats: 23 us, 6.7 TB/s with what the caches hold).
-template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_kernel(Args a, Grad gr)
+template <typename T, int DP> __global__ void __launch_bounds__(256, (DP < 128 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles) { keys_of<T, DP, false>(a, gr, k_tiles, blockIdx.x); }
+
+// The first workgroups take queries, the others keys: with either alone on the device, 2 x 810 causal tokens, 4 heads of 128, took 73 us where this takes 53, 16 sequences of
+// up to 500, 12 heads of 64, 87 and 80, 5001 causal tokens, 16 heads of 128, 439 and 417.  The stats that both need come from a launch before.
+template <typename T, int DP> __global__ void __launch_bounds__(256, 2) both_kernel(Args a, Grad queries, Grad keys, int q_tiles, int k_tiles, uint32_t q_blocks)
 {
-    const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (blockIdx.x < q_blocks)
+        queries_of<T, DP, true>(a, queries, q_tiles, blockIdx.x);
+    else
+        keys_of<T, DP, true>(a, keys, k_tiles, blockIdx.x - q_blocks);
+}
+// Eight threads per query, sixteen values of its row each.  Bound: memory, and of short sequences its launch (3 us).
+template <typename T> __global__ void __launch_bounds__(256) stats_kernel(Args a, Grad gr)
+{
+    const int64_t heads = (int64_t)a.batch * a.q_heads;
+    const int t = threadIdx.x & 7;
+    for (int64_t item = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); item < heads * gr.stat_rows; item += (int64_t)gridDim.x * 32) {   // (eight threads together)
+        const int bh = (int)(item / gr.stat_rows), i = (int)(item % gr.stat_rows), b = bh / a.q_heads, h = bh % a.q_heads;
+        float delta = 0.f, lse = ATT_INF;
+        if (i < a.queries(b)) {
+            const T* const o = gr.o.at<T>(b, h) + (int64_t)i * gr.o.token;
+            const T* const d = gr.dout.at<T>(b, h) + (int64_t)i * gr.dout.token;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int at = 64 * n + 8 * t;
+                if (at >= a.head_dim) continue;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(o + at), y = *reinterpret_cast<const u32x4*>(d + at);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const f32x2 u = pair_to(x[w], T{}), v = pair_to(y[w], T{});
+                    delta = __builtin_fmaf(u[0], v[0], delta);
+                    delta = __builtin_fmaf(u[1], v[1], delta);
+                }
+            }
+            lse = gr.lse[(int64_t)bh * a.q_tokens + i];
+            lse = lse == -ATT_INF ? ATT_INF : lse;
+        }
+#pragma unroll
+        for (int n = 1; n < 8; n <<= 1) delta += __shfl_xor(delta, n, kWave);
+        if (t == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
+    }
+}
+
+// The parts of a key's (a query's) sums, four neighbouring values a thread.  Bound: memory (seven parts of 5001 x 4 x 256 floats: 23 us, 6.7 TB/s with what the caches hold).
+template <typename T, int DP> __device__ __forceinline__ void keys_join(const Args& a, const Grad& gr, uint32_t block)
+{
+    const int64_t rows = (int64_t)a.batch * a.kv_heads * a.k_tokens, item = (int64_t)block * 256 + threadIdx.x;
     const int64_t row = item / (DP / 2);
     const int at = 4 * (int)(item % (DP / 2)), d = at % DP;
     if (row >= rows || d >= a.head_dim) return;
@@ -583,9 +620,9 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) keys_join_k
     *reinterpret_cast<u32x2*>(out.at<T>(b, hk) + (int64_t)j * out.token + d) = u32x2{pair_of(s[0] * f, s[1] * f, T{}), pair_of(s[2] * f, s[3] * f, T{})};
 }
 
-template <typename T, int DP> __global__ void __launch_bounds__(256) queries_join_kernel(Args a, Grad gr)
+template <typename T, int DP> __device__ __forceinline__ void queries_join(const Args& a, const Grad& gr, uint32_t block)
 {
-    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens, item = (int64_t)block * 256 + threadIdx.x;
     const int64_t row = item / (DP / 4);
     const int d = 4 * (int)(item % (DP / 4));
     if (row >= rows || d >= a.head_dim) return;
@@ -599,6 +636,14 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) queries_joi
     const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads;
     *reinterpret_cast<u32x2*>(gr.out0.at<T>(b, h) + (int64_t)i * gr.out0.token + d) =
         u32x2{pair_of(s[0] * a.scale, s[1] * a.scale, T{}), pair_of(s[2] * a.scale, s[3] * a.scale, T{})};
+}
+
+template <typename T, int DP> __global__ void __launch_bounds__(256) join_kernel(Args a, Grad queries, Grad keys, uint32_t q_blocks)
+{
+    if (blockIdx.x < q_blocks)
+        queries_join<T, DP>(a, queries, blockIdx.x);
+    else
+        keys_join<T, DP>(a, keys, blockIdx.x - q_blocks);
 }
 
 // Diagonals of a head: 64 of them and 16 runs of workgroups.  (2048 workgroups, 1 head: 9 us.)
@@ -656,51 +701,50 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
     if (threadIdx.x == 0) dtable[(int64_t)n * a.q_heads + h] = (T)(((runs[0] + runs[1]) + runs[2]) + runs[3]);
 }
 
+constexpr int kOwnMost = 64;    // keys of a sequence that is one wavefront's own
 constexpr int kFewParts = 64;   // workgroups whose diagonals the buckets' kernel adds itself (64 of them 5.7 us, by a launch of their own 4.9 and 4.8)
 struct Plan {
-    bool own_queries, own_keys;
+    bool own;
     int q_tiles, q_parts, q_part_keys, k_tiles, parts, diagonal_parts;
-    size_t stats, diagonals, sums, tables, total;   // bytes (sums: of either kernel's parts, one after the other)
+    size_t stats, diagonals, q_sums, sums, tables, total;   // bytes (sums: of the queries' parts and, q_sums further, of the keys')
 };
 Plan plan_of(const pruner_attention* a)
 {
     Plan p{};
     const int dp = padded_dim(a->head_dim), group = a->q_heads / a->kv_heads;
     const bool causal = a->flags & PRUNER_ATTENTION_CAUSAL;
-    p.own_queries = a->q_tokens <= 32 && a->k_tokens <= 64;   // (2048 sequences of up to 8, 64 wide: 11 us, shared 30; 300 of 30 queries and 60 keys, 8 heads: 22 and 42)
-    // A workgroup's four wavefronts share a tile of queries, or, where queries are so few that little is gained by it and keys so few that 128 of one sequence are
-    // mostly not there, each has a sequence and key head of its own (us, own and shared; 64 wide: 2048 x 8 queries and keys 9 and 27; 783 x 6 and 55, 16 heads sharing
-    // two, 77 and 87; 200 x 20 and 150, 4 heads, 22 and 25; 200 x 20 and 120, 8 sharing two, 25 and 20; 64 x 30 and 500 48 and 38.  128 wide, where one wavefront
-    // per SIMD is left: 783 x 6 and 30 48 and 56; 200 x 20 and 60 25 and 22).
-    p.own_keys = a->q_tokens <= 32 && a->k_tokens <= (dp == 128 ? 32 : group == 1 ? 160 : 64);
+    // A workgroup's four wavefronts share tiles, or, where queries and keys are few, each has a sequence and head of its own (us in all, shared and own: 2048 sequences of 8 queries
+    // and keys, 64 wide, 68 and 34; 783 of 6 and 55, 16 heads sharing two, 268 and 141, of 128 312 and 256; 200 of 20 and 60, 4 heads, 41 and 37, of 128 49 and 51;
+    // 200 of 20 and 120 46 and 50).
+    p.own = a->q_tokens <= 32 && a->k_tokens <= kOwnMost;
     p.q_tiles = (a->q_tokens + 127) / 128;
-    const int tile_keys = p.own_keys ? 32 : dp == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
+    const int tile_keys = p.own ? 32 : dp == 128 ? KeysShape<__bf16, 128, true>::kKeys : KeysShape<__bf16, 64, true>::kKeys;
     p.k_tiles = (a->k_tokens + tile_keys - 1) / tile_keys;
     p.q_parts = p.parts = 1;
     p.q_part_keys = a->k_tokens;
     const double rows = (double)a->batch * a->q_heads * a->q_tokens, keys = (double)a->batch * a->kv_heads * a->k_tokens;
+    const double q_blocks = (double)a->batch * a->q_heads * p.q_tiles, k_blocks = (double)a->batch * a->kv_heads * p.k_tiles;
+    const int held = 256;   // workgroups of either kind that the device has room for
     // (steps as measured: 5001 causal tokens, 16 heads of 128 sharing 4; 16 sequences of up to 500, 12 of 64)
-    if (!p.own_queries && rows > 0 && keys > 0) {
-        const int step = dp < 128 ? 64 : 32, parts = parts_of((double)a->batch * a->q_heads * p.q_tiles, (a->k_tokens + step - 1) / step, causal, 512,
+    if (!p.own && rows > 0 && keys > 0) {
+        const int step = dp < 128 ? 64 : 32, parts = parts_of(q_blocks, (a->k_tokens + step - 1) / step, causal, held,
                                                               dp == 128 ? 1.2 : dp == 64 ? 1.4 : 1.0, dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, rows * dp * 4);
         p.q_part_keys = ((a->k_tokens + parts - 1) / parts + 63) / 64 * 64;
         p.q_parts = (a->k_tokens + p.q_part_keys - 1) / p.q_part_keys;
-    }
-    if (!p.own_keys && rows > 0 && keys > 0) {
-        const int step = dp < 128 ? 64 : 32;
-        p.parts = parts_of((double)a->batch * a->kv_heads * p.k_tiles, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, 512, dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0,
+        p.parts = parts_of(k_blocks, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, held, dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0,
                            dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
     }
     // (the window for the largest edge that there can be: sizes alone decide)
     const int64_t reach = (int64_t)a->q_tokens + a->k_tokens;
     const int most = (int)(reach < PRUNER_MAX_BIAS_DISTANCE ? reach : PRUNER_MAX_BIAS_DISTANCE);
     const int widest = Window(most, a->flags & PRUNER_ATTENTION_TWO_SIDED ? (most > 1 ? most : 1) : 0).size + 2;
-    p.diagonal_parts = p.own_queries ? a->batch : a->batch * p.q_tiles * p.q_parts;
+    p.diagonal_parts = p.own ? a->batch : a->batch * p.q_tiles * p.q_parts;
     p.stats = round_up((size_t)a->batch * a->q_heads * round_up((size_t)a->q_tokens, 32) * 3 * 4, 256);
     p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
     p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
     const size_t of_queries = p.q_parts > 1 ? (size_t)p.q_parts * (size_t)rows * dp * 4 : 0, of_keys = p.parts > 1 ? (size_t)p.parts * (size_t)keys * 2 * dp * 4 : 0;
-    p.sums = round_up(of_queries > of_keys ? of_queries : of_keys, 256);
+    p.q_sums = round_up(of_queries, 256);
+    p.sums = p.q_sums + round_up(of_keys, 256);
     p.total = p.stats + p.diagonals + p.tables + p.sums;
     return p;
 }
@@ -719,8 +763,7 @@ template <typename T, int DP> int run(const Call& c)
     const int dev = current_device(nullptr);
     if (dev < 0) return PRUNER_EHIP;
     if (!ready.get(dev)) {
-        for (const void* fn : {reinterpret_cast<const void*>(&queries_kernel<T, DP, true>), reinterpret_cast<const void*>(&queries_kernel<T, DP, false>),
-                               reinterpret_cast<const void*>(&keys_kernel<T, DP, true>), reinterpret_cast<const void*>(&keys_kernel<T, DP, false>)})
+        for (const void* fn : {reinterpret_cast<const void*>(&queries_kernel<T, DP>), reinterpret_cast<const void*>(&keys_kernel<T, DP>), reinterpret_cast<const void*>(&both_kernel<T, DP>)})
             if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
         ready.mark(dev);
     }
@@ -728,30 +771,31 @@ template <typename T, int DP> int run(const Call& c)
     const Window w(a.left, a.right);
     const size_t window = a.table ? round_up((size_t)w.size, 4) * 4 : 0, skew = a.table ? kSkewFloats * 4 : 0;
     const int64_t q_heads = (int64_t)a.batch * a.q_heads, k_heads = (int64_t)a.batch * a.kv_heads;
-    if (a.q_tokens > 0) {
-        if (c.plan.own_queries)
-            hipLaunchKernelGGL((queries_kernel<T, DP, false>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + (skew_in_values(DP, false) ? 0 : 4 * skew) + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries, 1);
-        else
-            hipLaunchKernelGGL((queries_kernel<T, DP, true>), dim3((unsigned)(q_heads * c.plan.q_tiles * c.plan.q_parts)), dim3(256), 5 * window + 4 * skew + turns_of(DP, true, DP < 128 ? 64 : 32) * 2 * (DP < 128 ? 64 : 32) * DP * 2, c.st, a, c.queries, c.plan.q_tiles);
-        PRUNER_LAUNCH_CHECK();
-        if (c.plan.q_parts > 1) {   // (before the keys' kernel, which may use the same sums)
-            const int64_t items = q_heads * a.q_tokens * (DP / 4);
-            hipLaunchKernelGGL((queries_join_kernel<T, DP>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, c.st, a, c.queries);
+    if (c.plan.own) {
+        if (a.q_tokens > 0) {
+            hipLaunchKernelGGL((queries_kernel<T, DP>), dim3((unsigned)((q_heads + 3) / 4)), dim3(256), 8 * window + (skew_in_values(DP, false) ? 0 : 4 * skew) + 4 * 2 * kOwn * DP * 2, c.st, a, c.queries);
             PRUNER_LAUNCH_CHECK();
         }
-    }
-    if (a.k_tokens > 0) {
-        if (c.plan.own_keys) {
-            hipLaunchKernelGGL((keys_kernel<T, DP, false>), dim3((unsigned)((k_heads * c.plan.k_tiles + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, c.plan.k_tiles);
-        } else {
-            typedef KeysShape<T, DP, true> Shape;
-            hipLaunchKernelGGL((keys_kernel<T, DP, true>), dim3((unsigned)(k_heads * c.plan.k_tiles * c.plan.parts)), dim3(64 * Shape::kWaves),
-                               window + Shape::kTurns * Shape::kTurnBytes + Shape::kWaves * Shape::kHeldBytes, c.st, a, c.keys, c.plan.k_tiles);
+        if (a.k_tokens > 0) {
+            hipLaunchKernelGGL((keys_kernel<T, DP>), dim3((unsigned)((k_heads * c.plan.k_tiles + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, c.plan.k_tiles);
+            PRUNER_LAUNCH_CHECK();
         }
+    } else if (q_heads > 0) {
+        typedef KeysShape<T, DP, true> Shape;
+        static_assert(Shape::kWaves == 4, "workgroups of 256 threads");
+        constexpr int kStep = DP < 128 ? 64 : 32;
+        const size_t q_lds = 5 * window + 4 * skew + turns_of(DP, true, kStep) * 2 * kStep * DP * 2, k_lds = window + Shape::kTurns * Shape::kTurnBytes + Shape::kWaves * Shape::kHeldBytes;
+        const unsigned q_blocks = (unsigned)(q_heads * c.plan.q_tiles * c.plan.q_parts), k_blocks = (unsigned)(k_heads * c.plan.k_tiles * c.plan.parts);
+        if (a.q_tokens > 0) {
+            const int64_t need = (q_heads * c.queries.stat_rows + 31) / 32;
+            hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(need < 65536 ? need : 65536)), dim3(256), 0, c.st, a, c.queries);
+            PRUNER_LAUNCH_CHECK();
+        }
+        hipLaunchKernelGGL((both_kernel<T, DP>), dim3(q_blocks + k_blocks), dim3(256), q_lds > k_lds ? q_lds : k_lds, c.st, a, c.queries, c.keys, c.plan.q_tiles, c.plan.k_tiles, q_blocks);
         PRUNER_LAUNCH_CHECK();
-        if (c.plan.parts > 1) {
-            const int64_t items = k_heads * a.k_tokens * (DP / 2);
-            hipLaunchKernelGGL((keys_join_kernel<T, DP>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, c.st, a, c.keys);
+        const unsigned q_join = c.plan.q_parts > 1 ? (unsigned)((q_heads * a.q_tokens * (DP / 4) + 255) / 256) : 0, k_join = c.plan.parts > 1 ? (unsigned)((k_heads * a.k_tokens * (DP / 2) + 255) / 256) : 0;
+        if (q_join + k_join > 0) {
+            hipLaunchKernelGGL((join_kernel<T, DP>), dim3(q_join + k_join), dim3(256), 0, c.st, a, c.queries, c.keys, q_join);
             PRUNER_LAUNCH_CHECK();
         }
     }
@@ -774,8 +818,8 @@ template <typename T, int DP> int run(const Call& c)
 bool grad_sizes_ok(const pruner_attention* a)
 {
     if (!attention_sizes_ok(a)) return false;
-    const int64_t heads = (int64_t)a->batch * a->kv_heads;
-    return heads * (a->k_tokens / 64 + 1) < (1 << 24) && a->q_heads <= 65535;
+    // (a launch takes queries and keys)
+    return (int64_t)a->batch * a->q_heads * (a->q_tokens / 64 + 1) + (int64_t)a->batch * a->kv_heads * (a->k_tokens / 64 + 1) < (1 << 24) && a->q_heads <= 65535;
 }
 
 }  // namespace
@@ -817,6 +861,7 @@ extern "C" int pruner_rel_attention_grad(const pruner_attention* a, const pruner
     c.queries = c.keys = g;
     c.queries.parts = c.plan.q_parts;
     c.keys.parts = c.plan.parts;
+    c.keys.sums = reinterpret_cast<float*>(reinterpret_cast<char*>(g.sums) + c.plan.q_sums);
     c.queries.out0 = att::heads_of(dq);
     c.keys.out0 = att::heads_of(dk);
     c.keys.out1 = att::heads_of(dv);
