@@ -79,7 +79,6 @@ __device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, _Float16)
 }
 
 constexpr int kTileR = 64;
-constexpr int kMinPartRows = 512;                   // fewest rows of a part
 template <bool BIG> struct WgradShape {
     static constexpr int kSide = BIG ? 256 : 128, kThreads = 2 * kSide;
     static constexpr int kChunks = kSide / 8, kRowBytes = 2 * kSide, kTileBytes = kTileR * kRowBytes;   // a tile of either operand: rows of kSide values of 16 bits
@@ -95,27 +94,38 @@ struct WgradPlan {
     int tiles_n, tiles_k, parts;
     int64_t rows_each;   // rows of a part, a multiple of kTileR
 };
+// Small or large tiles and how many parts, by what they cost (microseconds): a start, the steps of 64 rows that the busiest unit goes through in turn, and the parts'
+// sums read again (at 4 TB/s, by one more launch).  A step as measured where workgroups are alone on their units and, of the small ones, two share one;
+// rows that begin anywhere take longer.  (Kernel and join, large and small: 2048 x 1024 over 65536 rows 273 and 386; 512 x 512 55 and 64; 4096 x 4096 over 2048 rows
+// 73 and 99; 1024 x 1024 over 8192 rows 42 and 39.  Parts: 1600 x 904 over 30000 rows nine, 252 workgroups, 116, ten, 280 workgroups, 170; 44 x 16 over 1885 rows
+// four 26, fifteen 17.)
 WgradPlan wgrad_plan(int64_t rows, int32_t n_out, int32_t dim)
 {
-    WgradPlan p;
-    const int64_t most = (rows + kMinPartRows - 1) / kMinPartRows;
-    auto tiles_of = [&](int side) { return (int64_t)((n_out + side - 1) / side) * ((dim + side - 1) / side); };
-    // the large tiles where, cut into parts, they give each of the 256 compute units one, and where the last of either side is not mostly beyond the matrix (us with the
-    // join, large and small: 2048 x 1024 over 65536 rows 273 and 386; 512 x 512 55 and 59; 4096 x 4096 over 2048 rows 73 and 99; 1024 x 1024 over 8192 rows 42 and 39)
-    const int64_t padded = tiles_of(256) * 65536, small = tiles_of(128) * 16384;
-    p.big = tiles_of(256) * (most > 1 ? most : 1) >= 256 && padded <= small + small / 4;
-    const int side = p.big ? 256 : 128;
-    p.tiles_n = (n_out + side - 1) / side;
-    p.tiles_k = (dim + side - 1) / side;
-    const int64_t tiles = tiles_of(side), enough = p.big ? 256 : 512;   // workgroups that fill the device
-    int64_t parts = (enough + tiles - 1) / tiles;
-    parts = parts < most ? parts : most;
-    if (parts < 1) parts = 1;
-    p.rows_each = ((rows + parts - 1) / parts + kTileR - 1) / kTileR * kTileR;
-    if (p.rows_each < kTileR) p.rows_each = kTileR;
-    p.parts = (int)((rows + p.rows_each - 1) / p.rows_each);
-    if (p.parts < 1) p.parts = 1;
-    return p;
+    const bool loose = n_out % 8 || dim % 8;
+    const int64_t chain = (rows + kTileR - 1) / kTileR;
+    const double part_us = (double)n_out * dim * 4 / 4e6;
+    WgradPlan best{};
+    double least = 0;
+    for (int big = 0; big < 2; ++big) {
+        WgradPlan p;
+        const int side = big ? 256 : 128;
+        p.big = big;
+        p.tiles_n = (n_out + side - 1) / side;
+        p.tiles_k = (dim + side - 1) / side;
+        const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
+        const double alone = big ? (loose ? 4.2 : 2.1) : loose ? 2.5 : 1.05, full = loose ? 3.3 : 1.5;
+        for (int64_t parts = 1; parts == 1 || (parts <= chain && parts <= 512); parts += parts < 16 ? 1 : parts / 8) {
+            const int64_t steps = (chain + parts - 1) / parts, blocks = tiles * parts, units = big || blocks <= 256 ? 256 : 512;
+            const double us = 7.0 + (double)((blocks + units - 1) / units * steps) * (units == 256 ? alone : full) + (parts > 1 ? 8.0 + (double)parts * (part_us + 0.06) : 0.0);
+            if ((big || parts > 1) && us >= least) continue;
+            least = us;
+            best = p;
+            best.rows_each = (steps > 0 ? steps : 1) * kTileR;
+        }
+    }
+    best.parts = (int)((rows + best.rows_each - 1) / best.rows_each);
+    if (best.parts < 1) best.parts = 1;
+    return best;
 }
 
 template <typename T, int V, bool BIG>
