@@ -558,14 +558,17 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
 
 template <typename T, int DP> __global__ void __launch_bounds__(256, (DP < 128 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles) { keys_of<T, DP, false>(a, gr, k_tiles, blockIdx.x); }
 
-// The first workgroups take queries, the others keys: with either alone on the device, 2 x 810 causal tokens, 4 heads of 128, took 73 us where this takes 53, 16 sequences of
-// up to 500, 12 heads of 64, 87 and 80, 5001 causal tokens, 16 heads of 128, 439 and 417.  The stats that both need come from a launch before.
-template <typename T, int DP> __global__ void __launch_bounds__(256, 2) both_kernel(Args a, Grad queries, Grad keys, int q_tiles, int k_tiles, uint32_t q_blocks)
+// Some workgroups take queries, the others keys, those with the longer way to go first (9 sequences of up to 1001, 32 heads of 80 sharing 8: keys first 250 us, queries first
+// 350; 5001 causal tokens, 16 heads of 128 sharing 4, 444 and 412).  With either alone on the device, 2 x 810 causal tokens, 4 heads of 128, took 73 us where this takes
+// 50, 16 sequences of up to 500, 12 heads of 64, 87 and 76, 5001 causal tokens 439 and 412.  The stats that both need come from a launch before.
+template <typename T, int DP> __global__ void __launch_bounds__(256, 2) both_kernel(Args a, Grad queries, Grad keys, int q_tiles, int k_tiles, uint32_t first, int keys_first)
 {
-    if (blockIdx.x < q_blocks)
-        queries_of<T, DP, true>(a, queries, q_tiles, blockIdx.x);
+    const bool in_first = blockIdx.x < first;
+    const uint32_t block = in_first ? blockIdx.x : blockIdx.x - first;
+    if (in_first == (keys_first != 0))
+        keys_of<T, DP, true>(a, keys, k_tiles, block);
     else
-        keys_of<T, DP, true>(a, keys, k_tiles, blockIdx.x - q_blocks);
+        queries_of<T, DP, true>(a, queries, q_tiles, block);
 }
 // Eight threads per query, sixteen values of its row each.  Bound: memory, and of short sequences its launch (3 us).
 template <typename T> __global__ void __launch_bounds__(256) stats_kernel(Args a, Grad gr)
@@ -704,7 +707,7 @@ template <typename T> __global__ void __launch_bounds__(256) buckets_kernel(Args
 constexpr int kOwnMost = 64;    // keys of a sequence that is one wavefront's own
 constexpr int kFewParts = 64;   // workgroups whose diagonals the buckets' kernel adds itself (64 of them 5.7 us, by a launch of their own 4.9 and 4.8)
 struct Plan {
-    bool own;
+    bool own, keys_first;
     int q_tiles, q_parts, q_part_keys, k_tiles, parts, diagonal_parts;
     size_t stats, diagonals, q_sums, sums, tables, total;   // bytes (sums: of the queries' parts and, q_sums further, of the keys')
 };
@@ -727,12 +730,14 @@ Plan plan_of(const pruner_attention* a)
     const int held = 256;   // workgroups of either kind that the device has room for
     // (steps as measured: 5001 causal tokens, 16 heads of 128 sharing 4; 16 sequences of up to 500, 12 of 64)
     if (!p.own && rows > 0 && keys > 0) {
-        const int step = dp < 128 ? 64 : 32, parts = parts_of(q_blocks, (a->k_tokens + step - 1) / step, causal, held,
-                                                              dp == 128 ? 1.2 : dp == 64 ? 1.4 : 1.0, dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, rows * dp * 4);
+        const int step = dp < 128 ? 64 : 32;
+        const int64_t q_chain = (a->k_tokens + step - 1) / step, k_chain = (int64_t)group * ((a->q_tokens + step - 1) / step);
+        const double q_alone = dp == 128 ? 1.2 : dp == 64 ? 1.4 : 1.0, k_alone = dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0;
+        const int parts = parts_of(q_blocks, q_chain, causal, held, q_alone, dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, rows * dp * 4);
         p.q_part_keys = ((a->k_tokens + parts - 1) / parts + 63) / 64 * 64;
         p.q_parts = (a->k_tokens + p.q_part_keys - 1) / p.q_part_keys;
-        p.parts = parts_of(k_blocks, (int64_t)group * ((a->q_tokens + step - 1) / step), causal, held, dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0,
-                           dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
+        p.parts = parts_of(k_blocks, k_chain, causal, held, k_alone, dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
+        p.keys_first = k_alone * (double)k_chain / p.parts > q_alone * (double)q_chain / p.q_parts;
     }
     // (the window for the largest edge that there can be: sizes alone decide)
     const int64_t reach = (int64_t)a->q_tokens + a->k_tokens;
@@ -791,7 +796,8 @@ template <typename T, int DP> int run(const Call& c)
             hipLaunchKernelGGL(stats_kernel<T>, dim3((unsigned)(need < 65536 ? need : 65536)), dim3(256), 0, c.st, a, c.queries);
             PRUNER_LAUNCH_CHECK();
         }
-        hipLaunchKernelGGL((both_kernel<T, DP>), dim3(q_blocks + k_blocks), dim3(256), q_lds > k_lds ? q_lds : k_lds, c.st, a, c.queries, c.keys, c.plan.q_tiles, c.plan.k_tiles, q_blocks);
+        hipLaunchKernelGGL((both_kernel<T, DP>), dim3(q_blocks + k_blocks), dim3(256), q_lds > k_lds ? q_lds : k_lds, c.st, a, c.queries, c.keys, c.plan.q_tiles, c.plan.k_tiles,
+                           c.plan.keys_first ? k_blocks : q_blocks, (int)c.plan.keys_first);
         PRUNER_LAUNCH_CHECK();
         const unsigned q_join = c.plan.q_parts > 1 ? (unsigned)((q_heads * a.q_tokens * (DP / 4) + 255) / 256) : 0, k_join = c.plan.parts > 1 ? (unsigned)((k_heads * a.k_tokens * (DP / 2) + 255) / 256) : 0;
         if (q_join + k_join > 0) {
