@@ -358,12 +358,12 @@ constexpr int turns_of(int dp, bool shared, int rows) { return !shared ? 1 : dp 
 
 // Into how many parts the long axis of `blocks` workgroups is cut, each of up to `chain` steps, `held` of them on the device at once.  A step takes alone_us
 // microseconds where a workgroup goes through its steps by itself, and full_us where all are at work (and a quarter of a workgroup's steps is left when the others are done); a part has fewer steps to go through in turn, but
-// leaves sums (of sum_bytes) that one more launch reads again, at 4 TB/s (they are written while others compute).
-inline int parts_of(double blocks, int64_t chain, bool causal, double held, double alone_us, double full_us, double sum_bytes)
+// leaves sums (of sum_bytes) that one more launch reads again, at 4 TB/s (they are written while others compute).  other_us: what else the device does in the same launch.
+inline int parts_of(double blocks, int64_t chain, bool causal, double held, double alone_us, double full_us, double sum_bytes, double other_us = 0.0)
 {
     int best = 1;
     double least = 0;
-    const double share = blocks * (double)chain * (causal ? 0.5 : 1.0) / held * full_us;
+    const double share = blocks * (double)chain * (causal ? 0.5 : 1.0) / held * full_us + other_us;
     for (int p = 1; p == 1 || (p <= 64 && 2 * p <= chain); p += p < 8 ? 1 : p / 4) {
         const double steps = (double)((chain + p - 1) / p) * alone_us, both = share + 0.25 * steps, us = (steps > both ? steps : both) + (p > 1 ? 5.0 + p * sum_bytes / 4e6 : 0.0);
         if (p == 1 || us < (best == 1 ? 0.9 : 1.0) * least) {

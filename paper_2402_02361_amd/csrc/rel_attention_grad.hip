@@ -727,16 +727,17 @@ Plan plan_of(const pruner_attention* a)
     p.q_part_keys = a->k_tokens;
     const double rows = (double)a->batch * a->q_heads * a->q_tokens, keys = (double)a->batch * a->kv_heads * a->k_tokens;
     const double q_blocks = (double)a->batch * a->q_heads * p.q_tiles, k_blocks = (double)a->batch * a->kv_heads * p.k_tiles;
-    const int held = 256;   // workgroups of either kind that the device has room for
+    const int held = 512;   // workgroups that the device has room for
     // (steps as measured: 5001 causal tokens, 16 heads of 128 sharing 4; 16 sequences of up to 500, 12 of 64)
     if (!p.own && rows > 0 && keys > 0) {
         const int step = dp < 128 ? 64 : 32;
         const int64_t q_chain = (a->k_tokens + step - 1) / step, k_chain = (int64_t)group * ((a->q_tokens + step - 1) / step);
         const double q_alone = dp == 128 ? 1.2 : dp == 64 ? 1.4 : 1.0, k_alone = dp == 128 ? 1.5 : dp == 64 ? 1.5 : 1.0;
-        const int parts = parts_of(q_blocks, q_chain, causal, held, q_alone, dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, rows * dp * 4);
+        const double q_full = dp == 128 ? 1.9 : dp == 64 ? 2.4 : 1.8, k_full = dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, part = (causal ? 0.5 : 1.0) / held;
+        const int parts = parts_of(q_blocks, q_chain, causal, held, q_alone, q_full, rows * dp * 4, k_blocks * (double)k_chain * part * k_full);
         p.q_part_keys = ((a->k_tokens + parts - 1) / parts + 63) / 64 * 64;
         p.q_parts = (a->k_tokens + p.q_part_keys - 1) / p.q_part_keys;
-        p.parts = parts_of(k_blocks, k_chain, causal, held, k_alone, dp == 128 ? 2.4 : dp == 64 ? 2.5 : 1.8, keys * 2 * dp * 4);
+        p.parts = parts_of(k_blocks, k_chain, causal, held, k_alone, k_full, keys * 2 * dp * 4, q_blocks * (double)q_chain * part * q_full);
         p.keys_first = k_alone * (double)k_chain / p.parts > q_alone * (double)q_chain / p.q_parts;
     }
     // (the window for the largest edge that there can be: sizes alone decide)
