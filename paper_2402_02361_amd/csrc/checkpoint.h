@@ -24,17 +24,19 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
 
-// How many of eight values from a place in a row, where `left` of the row's values remain and `after` rows follow, lie within the matrix.
-__device__ __forceinline__ int room_of(int64_t after, int64_t pitch, int left)
+// How many of eight values from a place in a row, where `left` of the row's values remain, `after` rows follow and `before` values precede it, lie within the
+// matrix; -1 where these are fewer but the eight that end with the last of them do.
+__device__ __forceinline__ int room_of(int64_t after, int64_t pitch, int left, int64_t before)
 {
     if (after >= 8) return 8;
     const int64_t n = after * pitch + left;
-    return n < 8 ? (int)n : 8;
+    return n >= 8 ? 8 : before >= 8 - left ? -1 : (int)n;
 }
 
 // Eight neighbouring values as they lie in memory (T).  V = 8: rows begin at multiples of 16 bytes and hold whole eights.  V = 1: they begin anywhere; an
 // eight moves by accesses that need no alignment.  Of a row's last values the read takes the next row's along, where the matrix has that much room
-// (one by one a row's tail is what such rows then cost: the weight gradient 1601 x 903 over 30000 rows took 522 us).  Values at or beyond `left` are 0
+// (one by one a row's tail is what such rows then cost: the weight gradient 1601 x 903 over 30000 rows took 522 us), or those before them (one by one the gradients of
+// three rows of 102 took 13 us, and take 11).  Values at or beyond `left` are 0
 // after a read and are not written.
 template <typename T, int V> struct Eight {
     static constexpr int kWords = 2 * (int)sizeof(T);
@@ -65,7 +67,18 @@ template <typename T, int V> struct Eight {
                 }
             }
         } else if constexpr (V == 1) {
-            if (left > 0) {   // (the matrix's last values)
+            if (left > 0 && room < 0) {   // (the matrix's last values)
+                const int by = kEach - left;
+#pragma unroll
+                for (int i = 0; i < kWords; i += 4) {
+                    const u32x4 q = *reinterpret_cast<const Loose*>(p - by + i * 4 / (int)sizeof(T));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[i + j] = q[j];
+                }
+                down<4>(by & 4);
+                down<2>(by & 2);
+                down<1>(by & 1);
+            } else if (left > 0) {   // (and there are not eight)
 #pragma unroll 1
                 for (int j = 0; j < left; ++j) {
                     uint32_t v;
@@ -77,6 +90,21 @@ template <typename T, int V> struct Eight {
                     for (int i = 0; i < kWords; ++i) w[i] |= i == j * (int)sizeof(T) / 4 ? v : 0u;
                 }
             }
+        }
+    }
+    template <int VALUES> __device__ __forceinline__ void down(bool move)   // by so many values, zeros behind
+    {
+        constexpr int kFar = VALUES * (int)sizeof(T) / 4;   // words (0: half a word)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            uint32_t moved = 0u;
+            if constexpr (kFar == 0) {
+                moved = w[i] >> 16;
+                if (i + 1 < kWords) moved |= w[i + 1 < kWords ? i + 1 : 0] << 16;
+            } else {
+                if (i + kFar < kWords) moved = w[i + kFar < kWords ? i + kFar : 0];
+            }
+            w[i] = move ? moved : w[i];
         }
     }
     __device__ __forceinline__ void store(T* __restrict__ p, int left) const
@@ -159,7 +187,12 @@ template <int V> struct EightCodes {
             w[0] = q[0];
             w[1] = q[1];
         } else if constexpr (V == 1) {
-            if (left > 0)
+            if (left > 0 && room < 0) {
+                const Loose q = *reinterpret_cast<const Loose*>(p - (kEach - left));
+                const uint64_t all = (((uint64_t)q[1] << 32) | q[0]) >> (8 * (kEach - left));
+                w[0] = (uint32_t)all;
+                w[1] = (uint32_t)(all >> 32);
+            } else if (left > 0)
 #pragma unroll
                 for (int j = 0; j < kEach; ++j)
                     if (j < left) w[j / 4] |= (uint32_t)(uint8_t)p[j] << (8 * (j % 4));

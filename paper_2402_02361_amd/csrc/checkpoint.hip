@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, int6
     const uint32_t row = per_row.of(item), at = item - row * per_row.d;
     const int col = 8 * (int)at, left = dim - col;
     Eight<T, V> in;
-    in.load(x + (int64_t)row * pitch + col, left, room_of(rows - 1 - row, pitch, left));
+    in.load(x + (int64_t)row * pitch + col, left, room_of(rows - 1 - row, pitch, left, (int64_t)row * pitch + col));
     float v[kEach];
     in.to_floats(v);
     EightCodes<V> out;
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__
     const uint32_t row = per_row.of(item), at = item - row * per_row.d;
     const int col = 8 * (int)at, left = dim - col;
     EightCodes<V> in;
-    in.load(codes + (int64_t)row * dim + col, left, room_of(rows - 1 - row, dim, left));
+    in.load(codes + (int64_t)row * dim + col, left, room_of(rows - 1 - row, dim, left, (int64_t)row * dim + col));
     float v[kEach];
     restore_eight(in.w, exps[(int64_t)row * (per_row.d / 4) + at / 4], v);
     Eight<T, V> out;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(WgradShape<BIG>::kThreads, 2) wgrad_kernel(con
             const int64_t r = r0 + s_row + S::kRowStep * u;
             const bool in = r < r_end;
             // (columns past the matrix's may hold anything: their results are not kept)
-            const int n_room = room_of(rows - 1 - r, dy_pitch, n_left), k_room = room_of(rows - 1 - r, dim, k_left);
+            const int n_room = room_of(rows - 1 - r, dy_pitch, n_left, r * dy_pitch + n0 + 8 * s_chunk), k_room = room_of(rows - 1 - r, dim, k_left, r * dim + k0 + 8 * s_chunk);
             dy_in[u].load(dy + r * dy_pitch + n0 + 8 * s_chunk, in && n_left > 0 ? (n_room >= 8 ? 8 : n_left) : 0, n_room);
             x_in[u].load(codes + r * dim + k0 + 8 * s_chunk, in && k_left > 0 ? (k_room >= 8 ? 8 : k_left) : 0, k_room);
             x_exp[u] = in && k_left > 0 ? exps[r * groups + (k0 >> 5) + (s_chunk >> 2)] : 0u;

@@ -7,8 +7,8 @@
 // A row lives in the registers of T threads, eight neighbouring values each, T the power of two that covers it, or beyond 64 the whole wavefronts that do: every matrix is
 // read once and written once, and the statistics are formed again in the backward pass, where they cost no bytes.
 // All in binary32.  Bound: memory: 65536 x 2048 bfloat16 rows' gradients 411 us, 4.9 TB/s, 65536 x 256 49 us, 5.2 TB/s; forward, 16384 x 1100 binary32 rows 64 us, 4.5 TB/s.  A
-// large copy reaches 5.2.  Rows of more than 64 threads wait for each other's sums: gradients over 16384 x 4096 rows 325 us (3.1 TB/s), and rows that begin
-// anywhere for their selections: over 16384 x 1111 rows 126 us, where 1112 take 86.
+// large copy reaches 5.2.  Rows of more than 64 threads wait for each other's sums: gradients over 16384 x 4096 rows 248 us (4.1 TB/s), over 8192 x 8192, where a thread
+// has 128 registers, 400 (2.5); rows that begin anywhere cost selections: over 16384 x 1111 rows 129 us, where 1112 take 86.
 #include "checkpoint.h"
 
 namespace pruner {
@@ -53,11 +53,16 @@ struct RowSum {
 #pragma unroll
             for (int n = 0; n < N; ++n) meet[turn][wave][n] = v[n];
         __syncthreads();
+        // (a lane per wavefront, at most 16, then as above: read one after the other: gradients over 16384 x 4096 rows 341 us where this takes 248, 5000 x 5000
+        // 184 and 124)
+        const int at = threadIdx.x & 15;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            float s = 0.f;
-            for (int w = first; w < first + waves; ++w) s += meet[turn][w][n];
-            v[n] = s;
+            v[n] = at < waves ? meet[turn][first + at][n] : 0.f;
+            v[n] += moved<0xB1>(v[n]);
+            v[n] += moved<0x4E>(v[n]);
+            v[n] += moved<0x141>(v[n]);
+            v[n] += moved<0x140>(v[n]);
         }
         turn ^= 1;
     }
@@ -142,9 +147,9 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
     auto fetch = [&](int64_t row) {
         const int some = row < p.rows ? left : 0;
         const int64_t after = p.rows - 1 - row;
-        x_next.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left));
-        if (f) f_next.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left));
-        if constexpr (GATE_ROWS) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
+        x_next.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left, row * x_pitch + col));
+        if (f) f_next.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left, row * f_pitch + col));
+        if constexpr (GATE_ROWS) g_next.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left, row * p.gate_pitch + col));
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
     for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
@@ -227,15 +232,15 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
     auto fetch = [&](int64_t row) {
         const int some = row < p.rows ? left : 0;
         const int64_t after = p.rows - 1 - row;
-        next.x.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left));
-        next.dy.load(dy + row * dy_pitch + col, some, room_of(after, dy_pitch, left));
-        if (f) next.f.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left));
+        next.x.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left, row * x_pitch + col));
+        next.dy.load(dy + row * dy_pitch + col, some, room_of(after, dy_pitch, left, row * dy_pitch + col));
+        if (f) next.f.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left, row * f_pitch + col));
         if (codes) {
-            next.c.load(codes + row * p.dim + col, some, room_of(after, p.dim, left));
+            next.c.load(codes + row * p.dim + col, some, room_of(after, p.dim, left, row * p.dim + col));
             next.byte = some > 0 ? exps[row * groups + t / 4] : 1u;
         }
-        if (gate_rows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left));
-        if (dh) next.dh.load(dh + row * dh_pitch + col, some, room_of(after, dh_pitch, left));
+        if (gate_rows) next.g.load(static_cast<const T*>(p.gate) + row * p.gate_pitch + col, some, room_of(after, p.gate_pitch, left, row * p.gate_pitch + col));
+        if (dh) next.dh.load(dh + row * dh_pitch + col, some, room_of(after, dh_pitch, left, row * dh_pitch + col));
     };
     fetch((int64_t)blockIdx.x * in_block + slot);
     for (int64_t first = (int64_t)blockIdx.x * in_block; first < p.rows; first += stride) {
