@@ -448,13 +448,22 @@ def _stream_on(stream, t):
     return _raw_stream(t.get_device())
 
 
-def _scratch(workspace, need, device):
+def _made_for(stream, *tensors):
+    """Tensors made for a call on a given stream belong to it: their memory is not given away before what is enqueued there is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _scratch(workspace, need, device, stream):
     """(pointer, bytes) of the given workspace, or of a new one that is held until the call has been made; none where none is needed."""
     if workspace is None:
         if need == 0:
             return None, None, 0
         import torch
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        _made_for(stream, workspace)
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -484,6 +493,7 @@ def checkpoint_pack(x, kept=None, stream=None):
     rows, dim = x.shape
     if kept is None:
         kept = _new_checkpoint(rows, dim, x.device)
+        _made_for(stream, *kept)
     rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, _c_checkpoint(kept, rows, dim), _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_pack")
@@ -497,6 +507,7 @@ def checkpoint_restore(kept, dtype=None, x=None, stream=None):
     rows, dim = kept[0].shape
     if x is None:
         x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
+        _made_for(stream, x)
     assert x.shape == (rows, dim), "x"
     p, pitch = _rows_of(x, "x")
     rc = lib.pruner_checkpoint_restore(_c_checkpoint(kept, rows, dim), _dtype(x.dtype), rows, dim, p, pitch, _stream_on(stream, x))
@@ -516,8 +527,9 @@ def checkpoint_wgrad(dy, kept, dw=None, accumulate=False, workspace=None, stream
     if dw is None:
         assert not accumulate, "accumulate needs dw"
         dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
+        _made_for(stream, dw)
     assert dw.is_cuda and dw.dtype == torch.float32 and dw.is_contiguous() and dw.shape == (n_out, dim), "dw"
-    held, ws, size = _scratch(workspace, lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim), dy.device)
+    held, ws, size = _scratch(workspace, lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim), dy.device, stream)
     rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, _c_checkpoint(kept, rows, dim), rows, n_out, dim, dw.data_ptr(), int(accumulate), ws, size,
                                      _stream_on(stream, dy))
     if rc:
@@ -558,6 +570,7 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
     h = torch.empty_like(x, memory_format=torch.contiguous_format)
     y = torch.empty_like(h) if w_pre is not None else None
     kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
+    _made_for(stream, h, y, *(kept or ()))
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
     rc = lib.pruner_gated_norm(p, px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), _c_checkpoint(kept, rows, dim) if checkpoint else None, _stream_on(stream, x))
     if rc:
@@ -587,7 +600,8 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
         if gate is not None:
             dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
     dw_pre = torch.empty_like(w_pre)
-    held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device)
+    _made_for(stream, dx, df, dgate, dw_post, dw_pre)
+    held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device, stream)
     rc = lib.pruner_gated_norm_grad(p, pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, _c_checkpoint(kept, rows, dim) if kept is not None else None,
                                     _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), ws, size, _stream_on(stream, x))
     if rc:
@@ -655,9 +669,11 @@ def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causa
     batch, q_tokens, q_heads, _ = q.shape
     if o is None:
         o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        _made_for(stream, o)
     assert o.shape == q.shape and o.dtype == q.dtype, "o"
     lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
-    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_workspace_bytes(a), q.device)
+    _made_for(stream, lse)
+    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_workspace_bytes(a), q.device, stream)
     rc = lib.pruner_rel_attention(a, _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
     if rc:
         raise PrunerError(rc, "pruner_rel_attention")
@@ -676,7 +692,8 @@ def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, 
     dense = torch.contiguous_format
     dq, dk, dv = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense), torch.empty_like(v, memory_format=dense)
     dtable = torch.empty_like(table) if table is not None else None
-    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_grad_workspace_bytes(a), q.device)
+    _made_for(stream, dq, dk, dv, dtable)
+    held, ws, size = _scratch(workspace, lib.pruner_rel_attention_grad_workspace_bytes(a), q.device, stream)
     rc = lib.pruner_rel_attention_grad(a, _heads(do, "do"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _heads(dq, "dq"),
                                        _heads(dk, "dk"), _heads(dv, "dv"), _ptr(dtable), ws, size, _stream_on(stream, q))
     if rc:
