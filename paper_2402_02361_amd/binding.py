@@ -4,6 +4,7 @@ Argument marshalling only.  Device buffers are torch tensors on the GPU (PyTorch
 streams, nothing else); descriptors are the dataclasses of the `workloads` package or anything with the
 same attribute names.
 """
+import contextlib
 import ctypes as C
 import math
 import os
@@ -418,13 +419,15 @@ def verify_score(feat, n_stmt, weights, vscore=None, workspace=None, stream=None
 
 
 # ---- operators of a trainable Transformer block
+# A call on a given stream takes what it makes from that stream's memory, and what it returns may be used on the current stream once that has
+# waited.  That its inputs are there when the given stream reads them, and stay until it has, is the caller's to see to, as it is with torch's own calls.
 
 MAX_BIAS_EDGES, MAX_BIAS_DISTANCE, MAX_NORM_DIM, CHECKPOINT_GROUP = 64, 1024, 8192, 32
 _BF16, _F16, _F32 = 0, 1, 2
 _ATTENTION_CAUSAL, _ATTENTION_TWO_SIDED = 1, 2
 
 
-_dtypes, _raw_stream = {}, None
+_dtypes, _raw_stream, _HERE = {}, None, contextlib.nullcontext()
 # The structs of include/pruner.h as bytes, which a call takes like a pointer to them (a ctypes structure takes a call of a few microseconds half of one more).
 _PACK_CHECKPOINT, _PACK_HEADS = struct.Struct("@2P"), struct.Struct("@P3q")
 _PACK_NORM, _PACK_ATTENTION = struct.Struct("@q3i2f4x3Pq"), struct.Struct("@8if4x4Pi4x")
@@ -448,22 +451,32 @@ def _stream_on(stream, t):
     return _raw_stream(t.get_device())
 
 
-def _made_for(stream, *tensors):
-    """Tensors made for a call on a given stream belong to it: their memory is not given away before what is enqueued there is done."""
+def _made_on(stream):
+    """Where a call on a given stream makes tensors: from that stream's own memory.  Of another stream's, what has just been dropped there may
+    still be read or written by work that is under way."""
+    if stream is None:
+        return _HERE
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _returned(stream, *tensors):
+    """Results of a call on a given stream will be used on the current one: once dropped, their memory is kept until what is enqueued there is done."""
     if stream is not None:
+        import torch
         for t in tensors:
             if t is not None:
-                t.record_stream(stream)
+                t.record_stream(torch.cuda.current_stream(t.device))
 
 
 def _scratch(workspace, need, device, stream):
-    """(pointer, bytes) of the given workspace, or of a new one that is held until the call has been made; none where none is needed."""
+    """(tensor, pointer, bytes) of the given workspace, or of a new one that is held until the call has been made; nothing where none is needed."""
     if workspace is None:
         if need == 0:
             return None, None, 0
         import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        _made_for(stream, workspace)
+        with _made_on(stream):
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -492,8 +505,9 @@ def checkpoint_pack(x, kept=None, stream=None):
     p, pitch = _rows_of(x, "x")
     rows, dim = x.shape
     if kept is None:
-        kept = _new_checkpoint(rows, dim, x.device)
-        _made_for(stream, *kept)
+        with _made_on(stream):
+            kept = _new_checkpoint(rows, dim, x.device)
+        _returned(stream, *kept)
     rc = lib.pruner_checkpoint_pack(p, _dtype(x.dtype), rows, dim, pitch, _c_checkpoint(kept, rows, dim), _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_checkpoint_pack")
@@ -506,8 +520,9 @@ def checkpoint_restore(kept, dtype=None, x=None, stream=None):
     lib = load_library()
     rows, dim = kept[0].shape
     if x is None:
-        x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
-        _made_for(stream, x)
+        with _made_on(stream):
+            x = torch.empty((rows, dim), dtype=dtype, device=kept[0].device)
+        _returned(stream, x)
     assert x.shape == (rows, dim), "x"
     p, pitch = _rows_of(x, "x")
     rc = lib.pruner_checkpoint_restore(_c_checkpoint(kept, rows, dim), _dtype(x.dtype), rows, dim, p, pitch, _stream_on(stream, x))
@@ -526,8 +541,9 @@ def checkpoint_wgrad(dy, kept, dw=None, accumulate=False, workspace=None, stream
     dim = kept[0].shape[1]
     if dw is None:
         assert not accumulate, "accumulate needs dw"
-        dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
-        _made_for(stream, dw)
+        with _made_on(stream):
+            dw = torch.empty((n_out, dim), dtype=torch.float32, device=dy.device)
+        _returned(stream, dw)
     assert dw.is_cuda and dw.dtype == torch.float32 and dw.is_contiguous() and dw.shape == (n_out, dim), "dw"
     held, ws, size = _scratch(workspace, lib.pruner_checkpoint_wgrad_workspace_bytes(rows, n_out, dim), dy.device, stream)
     rc = lib.pruner_checkpoint_wgrad(p, _dtype(dy.dtype), pitch, _c_checkpoint(kept, rows, dim), rows, n_out, dim, dw.data_ptr(), int(accumulate), ws, size,
@@ -567,10 +583,11 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
     if f is not None:
         assert f.dtype == x.dtype and f.shape == x.shape, "f"
         pf, f_pitch = _rows_of(f, "f")
-    h = torch.empty_like(x, memory_format=torch.contiguous_format)
-    y = torch.empty_like(h) if w_pre is not None else None
-    kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
-    _made_for(stream, h, y, *(kept or ()))
+    with _made_on(stream):
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+        y = torch.empty_like(h) if w_pre is not None else None
+        kept = _new_checkpoint(rows, dim, x.device) if checkpoint else None
+    _returned(stream, h, y, *(kept or ()))
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
     rc = lib.pruner_gated_norm(p, px, x_pitch, pf, f_pitch, _ptr(h), _ptr(y), _c_checkpoint(kept, rows, dim) if checkpoint else None, _stream_on(stream, x))
     if rc:
@@ -592,15 +609,16 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
     pdh, dh_pitch = _rows_of(dh, "dh") if dh is not None else (None, 0)
     pf, f_pitch = _rows_of(f, "f") if f is not None and kept is None else (None, 0)
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
-    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
     df = dgate = dw_post = None
-    if f is not None:
-        df = torch.empty_like(dx)
-        dw_post = torch.empty_like(w_post)
-        if gate is not None:
-            dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
-    dw_pre = torch.empty_like(w_pre)
-    _made_for(stream, dx, df, dgate, dw_post, dw_pre)
+    with _made_on(stream):
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        if f is not None:
+            df = torch.empty_like(dx)
+            dw_post = torch.empty_like(w_post)
+            if gate is not None:
+                dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
+        dw_pre = torch.empty_like(w_pre)
+    _returned(stream, dx, df, dgate, dw_post, dw_pre)
     held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device, stream)
     rc = lib.pruner_gated_norm_grad(p, pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, _c_checkpoint(kept, rows, dim) if kept is not None else None,
                                     _ptr(dx), _ptr(df), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), ws, size, _stream_on(stream, x))
@@ -667,12 +685,13 @@ def rel_attention(q, k, v, table=None, edges=None, q_len=None, k_len=None, causa
     lib = load_library()
     a, held_edges = _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale)
     batch, q_tokens, q_heads, _ = q.shape
-    if o is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
-        _made_for(stream, o)
+    made_o = o is None
+    with _made_on(stream):
+        if made_o:
+            o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
+    _returned(stream, o if made_o else None, lse)
     assert o.shape == q.shape and o.dtype == q.dtype, "o"
-    lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
-    _made_for(stream, lse)
     held, ws, size = _scratch(workspace, lib.pruner_rel_attention_workspace_bytes(a), q.device, stream)
     rc = lib.pruner_rel_attention(a, _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
     if rc:
@@ -690,9 +709,10 @@ def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, 
     assert do.shape == q.shape and do.dtype == q.dtype and o.shape == q.shape and o.dtype == q.dtype, "do, o"
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (batch, q_heads, q_tokens), "lse"
     dense = torch.contiguous_format
-    dq, dk, dv = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense), torch.empty_like(v, memory_format=dense)
-    dtable = torch.empty_like(table) if table is not None else None
-    _made_for(stream, dq, dk, dv, dtable)
+    with _made_on(stream):
+        dq, dk, dv = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense), torch.empty_like(v, memory_format=dense)
+        dtable = torch.empty_like(table) if table is not None else None
+    _returned(stream, dq, dk, dv, dtable)
     held, ws, size = _scratch(workspace, lib.pruner_rel_attention_grad_workspace_bytes(a), q.device, stream)
     rc = lib.pruner_rel_attention_grad(a, _heads(do, "do"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(o, "o"), _ptr(lse), _heads(dq, "dq"),
                                        _heads(dk, "dk"), _heads(dv, "dv"), _ptr(dtable), ws, size, _stream_on(stream, q))

@@ -1,0 +1,136 @@
+"""A call of the block's operators on a given stream takes no memory from work that is still under way on the current one, and what it returned is not
+given away there while the current stream still reads it."""
+import pytest
+import torch
+
+import paper_2402_02361_amd as P
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def _randn(gen, *shape, dtype=BF):
+    return torch.randn(*shape, generator=gen).to(dtype).cuda()
+
+
+def _attention(seed):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v = (_randn(gen, 1, 1500, 2, 64) for _ in range(3))
+    return lambda stream: P.rel_attention(q, k, v, causal=True, want_lse=True, stream=stream)
+
+
+def _attention_grad(seed):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v, do = (_randn(gen, 1, 1500, 2, 64) for _ in range(4))
+    edges = P.relative_edges(8, 64)
+    table = _randn(gen, len(edges) + 1, 2)
+    o, lse = P.rel_attention(q, k, v, table, edges, causal=True, want_lse=True)
+    return lambda stream: P.rel_attention_grad(do, q, k, v, o, lse, table, edges, causal=True, stream=stream)
+
+
+def _norm(seed):
+    gen = torch.Generator().manual_seed(seed)
+    x, f = (_randn(gen, 2000, 320) for _ in range(2))
+    w = _randn(gen, 320, dtype=torch.float32)
+
+    def call(stream):
+        h, y, kept = P.gated_norm(x, f, w, w, checkpoint=True, stream=stream)
+        return (h, y, *kept)
+
+    return call
+
+
+def _norm_grad(seed):
+    gen = torch.Generator().manual_seed(seed)
+    x, f, dy, gate = (_randn(gen, 2000, 320) for _ in range(4))
+    w = _randn(gen, 320, dtype=torch.float32)
+    return lambda stream: P.gated_norm_grad(None, dy, x, f, w, w, gate=gate, stream=stream)
+
+
+def _pack(seed):
+    x = _randn(torch.Generator().manual_seed(seed), 3000, 300)
+    return lambda stream: tuple(P.checkpoint_pack(x, stream=stream))
+
+
+def _restore(seed):
+    kept = P.checkpoint_pack(_randn(torch.Generator().manual_seed(seed), 3000, 300))
+    return lambda stream: P.checkpoint_restore(kept, BF, stream=stream)
+
+
+def _wgrad(seed):
+    gen = torch.Generator().manual_seed(seed)
+    dy, kept = _randn(gen, 6000, 200), P.checkpoint_pack(_randn(gen, 6000, 136))
+    return lambda stream: P.checkpoint_wgrad(dy, kept, stream=stream)
+
+
+CALLS = [_attention, _attention_grad, _norm, _norm_grad, _pack, _restore, _wgrad]
+
+
+def _tensors(r):
+    return [t for t in (r if isinstance(r, tuple) else (r,)) if t is not None]
+
+
+def _same(a, b):
+    return len(a) == len(b) and all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.fixture(scope="module")
+def busy():
+    """Several milliseconds of work on the current stream."""
+    a, out = torch.randn(4096, 4096, device="cuda", dtype=BF), torch.empty(4096, 4096, device="cuda", dtype=BF)
+    return lambda: [torch.mm(a, a, out=out) for _ in range(60)]
+
+
+@pytest.mark.parametrize("make", CALLS)
+def test_memory_that_pending_work_reads_is_left_alone(make, busy):
+    """Results of a call are to be copied on the current stream, which is busy, and are dropped: the same call on an idle stream, which waits for nothing,
+    asks for tensors of the same sizes."""
+    call = make(1)
+    want = [t.clone() for t in _tensors(call(None))]
+    held = _tensors(call(None))
+    copies = [torch.empty_like(t) for t in held]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy()
+    for c, t in zip(copies, held):
+        c.copy_(t)
+    t = held = None
+    got = _tensors(call(side))
+    torch.cuda.synchronize()
+    assert _same(copies, want) and _same(got, want)
+
+
+@pytest.mark.parametrize("make", CALLS)
+def test_memory_that_pending_work_writes_is_left_alone(make, busy):
+    """Tensors of the results' sizes are to be filled on the current stream, which is busy, and are dropped before that."""
+    call = make(2)
+    want = [t.clone() for t in _tensors(call(None))]
+    held = [torch.empty_like(t) for t in want]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy()
+    for t in held:
+        t.fill_(7)
+    t = held = None
+    got = _tensors(call(side))
+    torch.cuda.synchronize()
+    assert _same(got, want)
+
+
+@pytest.mark.parametrize("make", CALLS)
+def test_results_that_the_current_stream_reads_are_kept(make, busy):
+    """Results of a call on a stream are read on the current one, after it has waited, and dropped: the next call on that stream gets other memory."""
+    call, other = make(3), make(4)
+    want, next_want = [t.clone() for t in _tensors(call(None))], [t.clone() for t in _tensors(other(None))]
+    copies = [torch.empty_like(t) for t in want]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = _tensors(call(side))
+    torch.cuda.current_stream().wait_stream(side)
+    busy()
+    for c, t in zip(copies, got):
+        c.copy_(t)
+    t = got = None
+    next_got = _tensors(other(side))
+    torch.cuda.synchronize()
+    assert _same(copies, want) and _same(next_got, next_want)
