@@ -216,10 +216,45 @@ def _stream(stream):
     return s.cuda_stream   # (a number: the prototypes make the pointer)
 
 
-def _workspace(workspace, need, device):
+# A call on a given stream takes what it makes from that stream's memory, and what it returns may be used on the current stream once that has
+# waited.  That its inputs are there when the given stream reads them, and stay until it has, is the caller's to see to, as it is with torch's own calls.
+_HERE = contextlib.nullcontext()
+
+
+def _made_on(stream):
+    """Where a call on a given stream makes tensors: from that stream's own memory.  Of another stream's, what has just been dropped there may
+    still be read or written by work that is under way."""
+    if stream is None:
+        return _HERE
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _returned(stream, *tensors):
+    """Results of a call on a given stream will be used on the current one: once dropped, their memory is kept until what is enqueued there is done."""
+    if stream is not None:
+        import torch
+        for t in tensors:
+            if t is not None:
+                t.record_stream(torch.cuda.current_stream(t.device))
+
+
+def _new(stream, shape, dtype, device):
+    """A tensor that a call makes and returns."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _made_on(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    _returned(stream, t)
+    return t
+
+
+def _workspace(workspace, need, device, stream):
     import torch
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        with _made_on(stream):
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
     return workspace
 
 
@@ -236,10 +271,10 @@ def draft_score(subgraphs, seg_off, tiles, flags=0, score=None, symbols=False, w
     n_sg, n = len(seg) - 1, int(seg[-1])
     arr = subgraphs if isinstance(subgraphs, C.Array) else to_c_subgraphs(subgraphs)
     if score is None:
-        score = torch.empty(n, dtype=torch.float32, device=tiles.device)
-    sym = torch.empty((NSYM, n), dtype=torch.int64, device=tiles.device) if symbols is True else (symbols or None)
+        score = _new(stream, n, torch.float32, tiles.device)
+    sym = _new(stream, (NSYM, n), torch.int64, tiles.device) if symbols is True else (symbols or None)
     need = workspace_bytes(WS_DRAFT, n, n_sg, 0)
-    ws = _workspace(workspace, need, tiles.device)
+    ws = _workspace(workspace, need, tiles.device, stream)
     rc = lib.pruner_draft_score(arr, n_sg, seg_p, _ptr(tiles), tiles.shape[1], flags, _ptr(score), _ptr(sym),
                                 _ptr(ws), ws.numel(), _stream(stream))
     if rc:
@@ -255,11 +290,11 @@ def topk(score, seg_off, k, idx_out=None, val_out=None, want_values=True, worksp
     seg, seg_p = _seg(seg_off)
     n_sg, n = len(seg) - 1, int(seg[-1])
     if idx_out is None:
-        idx_out = torch.empty((max(n_sg, 0), max(k, 0)), dtype=torch.int32, device=score.device)
+        idx_out = _new(stream, (max(n_sg, 0), max(k, 0)), torch.int32, score.device)
     if val_out is None and want_values:
-        val_out = torch.empty((max(n_sg, 0), max(k, 0)), dtype=torch.float32, device=score.device)
+        val_out = _new(stream, (max(n_sg, 0), max(k, 0)), torch.float32, score.device)
     need = workspace_bytes(WS_TOPK, n, n_sg, k)
-    ws = _workspace(workspace, need, score.device)
+    ws = _workspace(workspace, need, score.device, stream)
     rc = lib.pruner_topk(_ptr(score), seg_p, n_sg, k, _ptr(idx_out), _ptr(val_out), _ptr(ws), ws.numel(), _stream(stream))
     if rc:
         raise PrunerError(rc, "pruner_topk")
@@ -290,13 +325,13 @@ def prior_filter(subgraphs, seg_off, tiles, k, flags=0, score=None, idx_out=None
     n_sg, n = len(seg) - 1, int(seg[-1])
     arr = subgraphs if isinstance(subgraphs, C.Array) else to_c_subgraphs(subgraphs)
     if score is None:
-        score = torch.empty(n, dtype=torch.float32, device=tiles.device)
+        score = _new(stream, n, torch.float32, tiles.device)
     if idx_out is None:
-        idx_out = torch.empty((max(n_sg, 0), max(k, 0)), dtype=torch.int32, device=tiles.device)
+        idx_out = _new(stream, (max(n_sg, 0), max(k, 0)), torch.int32, tiles.device)
     if val_out is None and want_values:
-        val_out = torch.empty((max(n_sg, 0), max(k, 0)), dtype=torch.float32, device=tiles.device)
+        val_out = _new(stream, (max(n_sg, 0), max(k, 0)), torch.float32, tiles.device)
     need = workspace_bytes(WS_PRIOR_FILTER, n, n_sg, k)
-    ws = _workspace(workspace, need, tiles.device)
+    ws = _workspace(workspace, need, tiles.device, stream)
     ev = C.c_void_p(scored_event.cuda_event) if scored_event is not None else None
     rc = lib.pruner_prior_filter(arr, n_sg, seg_p, _ptr(tiles), tiles.shape[1], flags, k, _ptr(score), _ptr(idx_out), _ptr(val_out),
                                  _ptr(ws), ws.numel(), _stream(stream), ev)
@@ -315,13 +350,13 @@ def lse(subgraphs, seg_off, tiles, k, n_steps, seed, mutate_q16, flags=0, score=
     n_sg, n = len(seg) - 1, int(seg[-1])
     arr = subgraphs if isinstance(subgraphs, C.Array) else to_c_subgraphs(subgraphs)
     if score is None:
-        score = torch.empty(n, dtype=torch.float32, device=tiles.device)
+        score = _new(stream, n, torch.float32, tiles.device)
     rows = tiles.shape[0]
-    spec_tiles = torch.empty((rows, max(n_sg * k, 0)), dtype=torch.uint16, device=tiles.device)
-    spec_score = torch.empty((max(n_sg, 0), max(k, 0)), dtype=torch.float32, device=tiles.device)
-    spec_count = torch.empty(max(n_sg, 0), dtype=torch.int32, device=tiles.device)
+    spec_tiles = _new(stream, (rows, max(n_sg * k, 0)), torch.uint16, tiles.device)
+    spec_score = _new(stream, (max(n_sg, 0), max(k, 0)), torch.float32, tiles.device)
+    spec_count = _new(stream, max(n_sg, 0), torch.int32, tiles.device)
     need = workspace_bytes(WS_LSE, n, n_sg, k)
-    ws = _workspace(workspace, need, tiles.device)
+    ws = _workspace(workspace, need, tiles.device, stream)
     rc = lib.pruner_lse(arr, n_sg, seg_p, _ptr(tiles), tiles.shape[1], rows, flags, k, n_steps, seed & 0xFFFFFFFFFFFFFFFF, mutate_q16,
                         _ptr(score), _ptr(spec_tiles), _ptr(spec_score), _ptr(spec_count), _ptr(ws), ws.numel(), _stream(stream))
     if rc:
@@ -337,10 +372,10 @@ def random_init(subgraphs, seg_off, rows, seed, tiles=None, workspace=None, stre
     n_sg, n = len(seg) - 1, int(seg[-1])
     arr = subgraphs if isinstance(subgraphs, C.Array) else to_c_subgraphs(subgraphs)
     if tiles is None:
-        tiles = torch.empty((rows, n), dtype=torch.uint16, device=device)
+        tiles = _new(stream, (rows, n), torch.uint16, device)
     assert tiles.is_cuda and tiles.dtype == torch.uint16 and tiles.dim() == 2 and tiles.is_contiguous() and tiles.shape[0] == rows
     need = int(lib.pruner_random_init_workspace_bytes(arr, n_sg))
-    ws = _workspace(workspace, max(need, 256), tiles.device)
+    ws = _workspace(workspace, max(need, 256), tiles.device, stream)
     rc = lib.pruner_random_init(arr, n_sg, seg_p, _ptr(tiles), tiles.shape[1], rows, seed & 0xFFFFFFFFFFFFFFFF, _ptr(ws), ws.numel(),
                                 _stream(stream))
     if rc:
@@ -360,11 +395,11 @@ def pacm_score(feat, n_stmt, flow, n_blk, weights, y=None, workspace=None, strea
     assert n_stmt.is_cuda and n_stmt.dtype == torch.int32 and n_stmt.is_contiguous() and n_stmt.numel() == n_d
     assert n_blk.is_cuda and n_blk.dtype == torch.int32 and n_blk.is_contiguous() and n_blk.numel() == n_d
     if y is None:
-        y = torch.empty(n_d, dtype=torch.float32, device=feat.device)
+        y = _new(stream, n_d, torch.float32, feat.device)
     names = ("W1", "b1", "W2", "b2", "We", "be", "Wq", "Wk", "Wv", "Wo", "Wh", "bh", "wo")
     m = CPacm(*[weights[k].data_ptr() for k in names], float(weights["bo"]))
     need = workspace_bytes(WS_PACM, n_d, 0, 0)
-    ws = _workspace(workspace, need, feat.device)
+    ws = _workspace(workspace, need, feat.device, stream)
     rc = lib.pruner_pacm_score(_ptr(feat), _ptr(n_stmt), _ptr(flow), _ptr(n_blk), n_d, C.byref(m), _ptr(y), _ptr(ws), ws.numel(), _stream(stream))
     if rc:
         raise PrunerError(rc, "pruner_pacm_score")
@@ -407,11 +442,11 @@ def verify_score(feat, n_stmt, weights, vscore=None, workspace=None, stream=None
     assert n_stmt.is_cuda and n_stmt.dtype == torch.int32 and n_stmt.is_contiguous()
     n_d = feat.shape[0]
     if vscore is None:
-        vscore = torch.empty(n_d, dtype=torch.float32, device=feat.device)
+        vscore = _new(stream, n_d, torch.float32, feat.device)
     m = CMlp(weights["W1"].data_ptr(), weights["b1"].data_ptr(), weights["W2"].data_ptr(), weights["b2"].data_ptr(),
              weights["w3"].data_ptr(), float(weights["b3"]))
     need = workspace_bytes(WS_VERIFY, n_d, 0, 0)
-    ws = _workspace(workspace, need, feat.device)
+    ws = _workspace(workspace, need, feat.device, stream)
     rc = lib.pruner_verify_score(_ptr(feat), _ptr(n_stmt), n_d, C.byref(m), _ptr(vscore), _ptr(ws), ws.numel(), _stream(stream))
     if rc:
         raise PrunerError(rc, "pruner_verify_score")
@@ -419,15 +454,13 @@ def verify_score(feat, n_stmt, weights, vscore=None, workspace=None, stream=None
 
 
 # ---- operators of a trainable Transformer block
-# A call on a given stream takes what it makes from that stream's memory, and what it returns may be used on the current stream once that has
-# waited.  That its inputs are there when the given stream reads them, and stay until it has, is the caller's to see to, as it is with torch's own calls.
 
 MAX_BIAS_EDGES, MAX_BIAS_DISTANCE, MAX_NORM_DIM, CHECKPOINT_GROUP = 64, 1024, 8192, 32
 _BF16, _F16, _F32 = 0, 1, 2
 _ATTENTION_CAUSAL, _ATTENTION_TWO_SIDED = 1, 2
 
 
-_dtypes, _raw_stream, _HERE = {}, None, contextlib.nullcontext()
+_dtypes, _raw_stream = {}, None
 # The structs of include/pruner.h as bytes, which a call takes like a pointer to them (a ctypes structure takes a call of a few microseconds half of one more).
 _PACK_CHECKPOINT, _PACK_HEADS = struct.Struct("@2P"), struct.Struct("@P3q")
 _PACK_NORM, _PACK_ATTENTION = struct.Struct("@q3i2f4x3Pq"), struct.Struct("@8if4x4Pi4x")
@@ -449,24 +482,6 @@ def _stream_on(stream, t):
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
     return _raw_stream(t.get_device())
-
-
-def _made_on(stream):
-    """Where a call on a given stream makes tensors: from that stream's own memory.  Of another stream's, what has just been dropped there may
-    still be read or written by work that is under way."""
-    if stream is None:
-        return _HERE
-    import torch
-    return torch.cuda.stream(stream)
-
-
-def _returned(stream, *tensors):
-    """Results of a call on a given stream will be used on the current one: once dropped, their memory is kept until what is enqueued there is done."""
-    if stream is not None:
-        import torch
-        for t in tensors:
-            if t is not None:
-                t.record_stream(torch.cuda.current_stream(t.device))
 
 
 def _scratch(workspace, need, device, stream):
