@@ -443,8 +443,9 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  * Query head h reads key/value head h / (q_heads / kv_heads).
  *   bucket(r) = the number of edges <= |r|, plus n_edges + 1 if r > 0 (two-sided: table [2 (n_edges + 1)][q_heads]); one-sided: the number of
  *   edges <= max(-r, 0) (table [n_edges + 1][q_heads]); edges ascend strictly, 1 <= edge <= PRUNER_MAX_BIAS_DISTANCE.
- * Products accumulate in binary32, softmax statistics are binary32; the weights a_ij (and in the backward pass their gradients) are rounded to
- * the type before the second product.
+ * Products accumulate in binary32, softmax statistics are binary32; the weights a_ij (and in the backward pass the scores' gradients) are rounded to
+ * the type before the second product, in the backward pass in binary16 times powers of two, so that small ones keep their digits.  The sum of dout o over a
+ * row that the scores' gradients need is taken from o as it is given, rounded to the type (of sequences of few queries and keys from the weights themselves).
  *
  *   q, o, dout, dq   pruner_heads: token t of sequence b, head h at p + (b batch + t token + h head) elements, head_dim of them contiguous;
  *   k, v, dk, dv     head_dim a multiple of 8, 8..128; pointers 16-byte aligned, strides multiples of 8; token strides up to 2^22
