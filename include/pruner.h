@@ -441,6 +441,8 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  * beyond ql) has o = 0, lse = -infinity, and passes no gradient.  What rows beyond the lengths hold does not matter.  (A NaN or an infinity in a value
  * or a gradient within the lengths may reach every row of its sequence: its weight there is 0, but it is multiplied.)
  * Query head h reads key/value head h / (q_heads / kv_heads).
+ * Scores with their bias are binary32, and so is lse: beside a mask's -1e9 or the type's lowest value a score vanishes, and a row that sees nothing else weighs
+ * its keys alike, in the gradients too (where |lse| > 1024 they sum the row's weights again, which takes longer).
  *   bucket(r) = the number of edges <= |r|, plus n_edges + 1 if r > 0 (two-sided: table [2 (n_edges + 1)][q_heads]); one-sided: the number of
  *   edges <= max(-r, 0) (table [n_edges + 1][q_heads]); edges ascend strictly, 1 <= edge <= PRUNER_MAX_BIAS_DISTANCE.
  * Products accumulate in binary32, softmax statistics are binary32; the weights a_ij (and in the backward pass the scores' gradients) are rounded to

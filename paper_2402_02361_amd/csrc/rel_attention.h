@@ -25,7 +25,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
-constexpr float kHuge = 1e30f;   // a bias beyond this is added to a score before anything else is done with either
+constexpr float kLarge = 1024.f;   // a bias beyond this is added to a score before anything else is done with either, as where biases lie in a window; see also row_sums
 #define ATT_INF __builtin_inff()
 
 __device__ __forceinline__ floatx16 mfma(u32x4 a, u32x4 b, floatx16 c, __bf16)

@@ -111,7 +111,7 @@ __device__ __forceinline__ bool finish_scores(floatx16 (&s)[N], const Args& a, c
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = __builtin_fmaf(s[n][i], a.scale, w[32 * n + 8 * (i >> 2) + (i & 3)]);
-    } else if (!(__builtin_fabsf(bias) < kHuge)) {
+    } else if (!(__builtin_fabsf(bias) < kLarge)) {
         fused = false;
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -339,7 +339,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
                 fused = false;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[0][i] = __builtin_fmaf(s[0][i], a.scale, mine_of[n[8 * (i >> 2) + (i & 3)] * a.group]);
-            } else if (__any(!(__builtin_fabsf(bias) < kHuge))) {   // (lanes have biases of different heads)
+            } else if (__any(!(__builtin_fabsf(bias) < kLarge))) {   // (lanes have biases of different heads)
                 fused = false;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[0][i] = __builtin_fmaf(s[0][i], a.scale, bias);

@@ -7,7 +7,7 @@
 //   keys      a wavefront owns 32 keys: S and dP leave a key's values in its two lanes; dV^T += dO^T P, dK^T += Q^T dS.  It goes
 //             through the query tiles of all heads that share the key head.
 //   Where either has too few tiles for the device, their long axis is cut into parts, whose sums go to the workspace (join_kernel adds them in order).
-//   stats_kernel, both_kernel    lse and delta of every query, then queries and keys in one launch.
+//   stats_kernel, both_kernel    lse and delta of every query (and what its weights sum to, where lse does not tell), then queries and keys in one launch.
 //   queries_kernel, keys_kernel  the same for sequences of few queries and keys, each by a wavefront; delta is the sum of P dP there.
 //   diagonals_kernel, buckets_kernel   the workgroups' diagonals added in order, and the diagonals of a bucket (where the workgroups are few, by the
 //             latter alone).
@@ -74,23 +74,28 @@ template <typename T, int BLOCKS> struct Holder {
 struct Grad {
     Heads dout, o, out0, out1;   // out0, out1: dq, or dk and dv
     const float* lse;
-    float* stats;                // [3][batch][q_heads][stat_rows]: see leave_stats
+    float* stats;                // [kStats][batch][q_heads][stat_rows]: see leave_stats
     int stat_rows;               // q_tokens rounded up to 32
     float* diagonals;            // [part][q_heads][window + 2]
     float* sums;                 // of the parts: [part][batch][q_heads][q_tokens][DP], or [part][batch][kv_heads][k_tokens][2][DP]
     int parts, part_keys;        // part_keys: of the queries' kernel, a multiple of 64
 };
 
-// What the keys' kernel needs of a query: lse (plus infinity without a key, or where there is no query: every weight is then exp(-infinity)), what is added to the exponent of 2, and
-// -delta, both as they go with the form in which the weights are held.
-template <typename T> __device__ __forceinline__ void leave_stats(const Grad& gr, int64_t heads, int bh, int i, float lse, float delta)
+// What the keys' kernel needs of a query: lse (plus infinity without a key, or where there is no query: every weight is then exp(-infinity)), what is added to the exponent of 2, -delta,
+// as they go with the form in which the weights are held, and what the weights exp(s - lse) are multiplied by.  more: log2 of what these sum to.
+constexpr int kStats = 4;
+template <typename T> __device__ __forceinline__ void leave_stats(const Grad& gr, int64_t heads, int bh, int i, float lse, float delta, float more)
 {
     if (i >= gr.stat_rows) return;
     const int64_t all = heads * gr.stat_rows, row = (int64_t)bh * gr.stat_rows + i;
     gr.stats[row] = lse;
-    gr.stats[all + row] = Held<T>::kShift - lse * kLog2e;
+    gr.stats[all + row] = Held<T>::kShift - lse * kLog2e - more;
     gr.stats[2 * all + row] = -delta * Held<T>::kUnit;
+    gr.stats[3 * all + row] = exp2_of(-more);
 }
+// Whether a row's weights have to be summed again because of lse binary32 keeps too few digits (at 1024 they sum to 1 within 6e-5; a row that sees nothing but a mask's -1e9 has
+// lse = -1e9, whatever the number of its keys, and weights of 1 each).
+__device__ __forceinline__ bool sums_unknown(float lse) { return __builtin_fabsf(lse) > kLarge && __builtin_fabsf(lse) < ATT_INF; }
 
 // Sums of a 32 x 32 result along its diagonals, sixteen rows at a time: element (row, column) goes to place row of line row - column + 31, so a
 // line is a diagonal; lane d adds line d's sixteen places (those that no element reaches stay zero) and adds that to its diagonal's sum.  Lines are 18
@@ -187,13 +192,14 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queri
     u32x4 qf[Tile<DP>::kSteps], df[Tile<DP>::kSteps];
     load_row<T, DP>(qf, a.q.at<T>(b, h) + (int64_t)i * a.q.token, mine, a.head_dim, half);
     load_row<T, DP>(df, gr.dout.at<T>(b, h) + (int64_t)i * gr.dout.token, mine, a.head_dim, half);
-    float delta = 0.f, lse = ATT_INF;
+    float delta = 0.f, lse = ATT_INF, more = 0.f;
     const int64_t row = (int64_t)bh * a.q_tokens + i;
     if (mine) {
         if constexpr (SHARED) {
             const int64_t stat = (int64_t)bh * gr.stat_rows + i;
             lse = gr.stats[stat];
             delta = gr.stats[2 * (int64_t)heads * gr.stat_rows + stat] * (-1.f / Held<T>::kUnit);
+            more = -__builtin_amdgcn_logf(gr.stats[3 * (int64_t)heads * gr.stat_rows + stat]);   // (base 2; 0 of 1)
         } else {
             lse = gr.lse[row];
             lse = lse == -ATT_INF ? ATT_INF : lse;   // (no key: every weight is exp(-infinity))
@@ -229,15 +235,15 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queri
             const int r_lo = k0 - (kl - ql + q0 + 31), r_hi = k0 + 31 - (kl - ql + q0);
             const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
             const float bias = place == kRight ? bias_right : bias_left;
-            if (place == kNear || !(__builtin_fabsf(bias) < kHuge)) {
+            if (place == kNear || !(__builtin_fabsf(bias) < kLarge)) {
                 const float* const w = biases + (k0 - p - window.first + 4 * half);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float t = __builtin_fmaf(s[e], a.scale, place == kNear ? w[8 * (e >> 2) + (e & 3)] : bias);
-                    s[e] = exp2_of((t - lse) * kLog2e);
+                    s[e] = exp2_of(__builtin_fmaf(t - lse, kLog2e, -more));
                 }
             } else {
-                const float c = a.scale * kLog2e, d = (bias - lse) * kLog2e;
+                const float c = a.scale * kLog2e, d = __builtin_fmaf(bias - lse, kLog2e, -more);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = exp2_of(__builtin_fmaf(s[e], c, d));
             }
@@ -250,6 +256,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queri
         settle();
         if constexpr (!SHARED) {
             // delta as the sum of P dP: o is rounded, and with a few keys what it lost is as large as the gradient's own rounding
+            float total = 0.f;
             for (int key0 = 0; key0 < end; key0 += kN) {
                 wait_for<0>();
                 wave_fence();
@@ -257,13 +264,21 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queri
                     floatx16 s, dp;
                     weigh(tiles, 0, key0, s, dp);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) delta = __builtin_fmaf(s[e], dp[e], delta);
+                    for (int e = 0; e < 16; ++e) {
+                        delta = __builtin_fmaf(s[e], dp[e], delta);
+                        total += s[e];
+                    }
                 }
                 wait_for_reads();
                 wave_fence();
                 if (end > kN) request(key0 + kN < end ? key0 + kN : 0, 0);
             }
             delta = sum_of_halves(delta);
+            total = sum_of_halves(total);
+            if (sums_unknown(lse)) {
+                more = __builtin_amdgcn_logf(total);   // (base 2)
+                delta /= total;
+            }
         }
         int turn = 0;
         for (int key0 = begin; key0 < end; key0 += kN) {
@@ -323,7 +338,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queri
         }
         wait_for<0>();   // (nothing may arrive in LDS that is used for other things, or no longer this workgroup's)
     }
-    if (!SHARED && half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
+    if (!SHARED && half == 0) leave_stats<T>(gr, heads, bh, i, lse, delta, more);
     holder.release(dq);
     if (i < a.q_tokens) {
         if (SHARED && gr.parts > 1)
@@ -371,8 +386,8 @@ template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this took 228)
     static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
     static constexpr int kTurns = SHARED ? (kWide ? 2 : 3) : 1;
-    static constexpr int kStat = 64;                          // floats of a tile's stats, three of them
-    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + 3 * kStat * 4;
+    static constexpr int kStat = 64;                          // floats of one of a tile's stats
+    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + kStats * kStat * 4;
     static constexpr int kHeldBytes = kWide ? Tile<DP>::kSteps * 1024 : 0;   // of a wavefront
     static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
 };
@@ -418,7 +433,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
     qf.set(a.q.token, a.head_dim, thread, SHARED ? wave : 0);
     of.set(gr.dout.token, a.head_dim, thread, SHARED ? wave : 0);
     const int64_t all = (int64_t)a.batch * a.q_heads * gr.stat_rows;
-    // Of those that share a tile, wavefronts 0 to 2 ask for a stat each.
+    static_assert(!SHARED || Shape::kWaves == kStats, "of those that share a tile each asks for one of its stats");
     auto request = [&](int n, int turn) {
         const bool some = n < to;
         const int h = some ? hk * a.group + n / each : 0, i0 = some ? (first_tile + n % each) * kQ : 0, left = some ? ql - i0 : 0;
@@ -430,10 +445,10 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
                       buffer_of(gr.stats + w * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
         };
         if constexpr (SHARED) {
-            if (wave < 3) stat(wave);
+            stat(wave);
         } else {
 #pragma unroll
-            for (int w = 0; w < 3; ++w) stat(w);
+            for (int w = 0; w < kStats; ++w) stat(w);
         }
     };
     constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
@@ -486,11 +501,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
                 head_filled = g;
             }
             if constexpr (SHARED) {
-                constexpr int kLater = (kTurns - 2) * 2 * Flow<T, DP, kQ, kThreads>::kEach;
-                if (kLater > 0 && wave < 3)
-                    wait_for<kLater + (kTurns - 2)>();
-                else
-                    wait_for<kLater>();
+                wait_for<(kTurns - 2) * (2 * Flow<T, DP, kQ, kThreads>::kEach + 1)>();
                 __syncthreads();   // (and the tile before is done with)
                 request(n + kTurns - 1, turn == 0 ? kTurns - 1 : turn - 1);
             } else {
@@ -530,7 +541,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
                 if constexpr (!kWide) columns.start(turned);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
-                if (place == kNear || !(__builtin_fabsf(bias) < kHuge)) {
+                if (place == kNear || !(__builtin_fabsf(bias) < kLarge)) {
                     const float* const w = biases + (j - p0 - window.first - 4 * half);
 #pragma unroll
                     for (int g4 = 0; g4 < 4; ++g4) {
@@ -539,6 +550,14 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
                         for (int e = 0; e < 4; ++e) {
                             const float t = __builtin_fmaf(s[4 * g4 + e], a.scale, place == kNear ? w[-(8 * g4 + e)] : bias);
                             s[4 * g4 + e] = exp2_of(__builtin_fmaf(t - lse[e], kLog2e, Held<T>::kShift));
+                        }
+                    }
+                    if (__any(st[3 * kStat + 32 * m + l32] != 1.f)) {   // (rare; kept with the others, these take sixteen registers)
+#pragma unroll
+                        for (int g4 = 0; g4 < 4; ++g4) {
+                            const f32x4 x = *reinterpret_cast<const f32x4*>(st + 3 * kStat + 32 * m + 8 * g4 + 4 * half);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[4 * g4 + e] *= x[e];
                         }
                     }
                 } else {
@@ -614,6 +633,38 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) both_ker
     else
         queries_of<T, DP, true>(a, queries, q_tiles, block);
 }
+// Log2 of what the weights exp(s - lse) of a wavefront's eight queries from i0 on sum to (lane: query i0 + lane / 8), for rows of which lse does not tell.  Queries are columns
+// eight at a time, four times over, keys rows of 32 straight from memory, and scores are formed step by step as queries_of forms them, so that both round alike.  Not fast, as such
+// rows are few: where all are, 5001 causal tokens, 16 heads of 128 sharing 4, take 3.3 ms and not 0.47, 16 sequences of 500, 12 heads of 64, 0.53 and not 0.09.
+template <typename T> __device__ __forceinline__ float row_sums(const Args& a, int b, int h, int i0, float lse_of_lane, int lane)
+{
+    const int half = lane >> 5, l32 = lane & 31, hk = h / a.group, ql = a.queries(b), kl = a.keys(b), i = i0 + (l32 & 7), p = kl - ql + i;
+    const float lse = __shfl(lse_of_lane, 8 * (l32 & 7), kWave);
+    const bool mine = i < ql;
+    const T* const q = a.q.at<T>(b, h) + (int64_t)i * a.q.token;
+    const int limit = a.causal ? (p + 1 < kl ? p + 1 : kl) : kl, last = i0 + 7 < ql ? i0 + 7 : ql - 1, end = a.causal ? (kl - ql + last + 1 < kl ? kl - ql + last + 1 : kl) : kl;
+    float total = 0.f;
+    for (int k0 = 0; k0 < end; k0 += 32) {
+        const int j = k0 + l32;
+        const T* const k = a.k.at<T>(b, hk) + (int64_t)j * a.k.token;
+        floatx16 s = zero16();
+        for (int d = 0; d < a.head_dim; d += 16) {
+            const int at = d + 8 * half;
+            u32x4 kf{0u, 0u, 0u, 0u}, qf{0u, 0u, 0u, 0u};
+            if (at < a.head_dim && j < kl) kf = *reinterpret_cast<const u32x4*>(k + at);
+            if (at < a.head_dim && mine) qf = *reinterpret_cast<const u32x4*>(q + at);
+            s = mfma(kf, qf, s, T{});
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int key = k0 + row_of(e, half);
+            if (key < limit) total += exp2_of((__builtin_fmaf(s[e], a.scale, a.table ? a.bias<T>(a.bucket(key - p), h) : 0.f) - lse) * kLog2e);
+        }
+    }
+    total = sum_of_halves(total);
+    return __builtin_amdgcn_logf(__shfl(total, lane >> 3, kWave));
+}
+
 // Eight threads per query, sixteen values of its row each.  Bound: memory, and of short sequences its launch (3 us).
 template <typename T> __global__ void __launch_bounds__(256) stats_kernel(Args a, Grad gr)
 {
@@ -621,7 +672,7 @@ template <typename T> __global__ void __launch_bounds__(256) stats_kernel(Args a
     const int t = threadIdx.x & 7;
     for (int64_t item = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); item < heads * gr.stat_rows; item += (int64_t)gridDim.x * 32) {   // (eight threads together)
         const int bh = (int)(item / gr.stat_rows), i = (int)(item % gr.stat_rows), b = bh / a.q_heads, h = bh % a.q_heads;
-        float delta = 0.f, lse = ATT_INF;
+        float delta = 0.f, lse = ATT_INF, more = 0.f;
         if (i < a.queries(b)) {
             const T* const o = gr.o.at<T>(b, h) + (int64_t)i * gr.o.token;
             const T* const d = gr.dout.at<T>(b, h) + (int64_t)i * gr.dout.token;
@@ -642,7 +693,12 @@ template <typename T> __global__ void __launch_bounds__(256) stats_kernel(Args a
         }
 #pragma unroll
         for (int n = 1; n < 8; n <<= 1) delta += __shfl_xor(delta, n, kWave);
-        if (t == 0) leave_stats<T>(gr, heads, bh, i, lse, delta);
+        const bool unknown = sums_unknown(lse);
+        if (__any(unknown)) {   // (a wavefront's eight queries are of one head: stat_rows is a multiple of 32)
+            const float sum = row_sums<T>(a, b, h, __builtin_amdgcn_readfirstlane(i), lse, threadIdx.x & 63);
+            more = unknown ? sum : 0.f;
+        }
+        if (t == 0) leave_stats<T>(gr, heads, bh, i, lse, delta, more);
     }
 }
 
@@ -789,7 +845,7 @@ Plan plan_of(const pruner_attention* a)
     const int most = (int)(reach < PRUNER_MAX_BIAS_DISTANCE ? reach : PRUNER_MAX_BIAS_DISTANCE);
     const int widest = Window(most, a->flags & PRUNER_ATTENTION_TWO_SIDED ? (most > 1 ? most : 1) : 0).size + 2;
     p.diagonal_parts = p.own ? a->batch : a->batch * p.q_tiles * p.q_parts;
-    p.stats = round_up((size_t)a->batch * a->q_heads * round_up((size_t)a->q_tokens, 32) * 3 * 4, 256);
+    p.stats = round_up((size_t)a->batch * a->q_heads * round_up((size_t)a->q_tokens, 32) * kStats * 4, 256);
     p.diagonals = a->table ? round_up((size_t)p.diagonal_parts * a->q_heads * widest * 4, 256) : 0;
     p.tables = a->table ? round_up((size_t)a->q_heads * widest * 4, 256) : 0;
     const size_t of_queries = p.q_parts > 1 ? (size_t)p.q_parts * (size_t)rows * dp * 4 : 0, of_keys = p.parts > 1 ? (size_t)p.parts * (size_t)keys * 2 * dp * 4 : 0;
