@@ -402,13 +402,14 @@ int pruner_checkpoint_wgrad(const void* dy, int32_t dtype, int64_t dy_pitch, con
  * All of it in binary32 on the unrounded h; h and y are rounded once, to the type.
  *   x, f, h, y     device, dtype; x and f with pitches, outputs contiguous.  f NULL: u = 0 (the first norm of a model).
  *                  h or y NULL: not wanted.
- *   w_post, w_pre  device float [dim]; w_post may be NULL with f
+ *   w_post, w_pre  device float [dim]; w_post may be NULL with f, w_pre where neither y nor its checkpoint is wanted
  *   gate           NULL (sigmoid(gate) is then 1), or with gate_pitch > 0 device [rows][gate_pitch] of dtype, or with gate_pitch = 0 device
  *                  float [dim], one for all rows
  *   kept_y         NULL, or room for the checkpoint of y as it is stored (y in its type)
  * rows >= 0, 1 <= dim <= PRUNER_MAX_NORM_DIM.  No workspace.
  *
- * pruner_gated_norm_grad: dh and dy are the gradients of the two outputs (dh NULL: zero), f or kept_f (exactly one, or neither if the forward
+ * pruner_gated_norm_grad: dh and dy are the gradients of the two outputs (dh NULL: zero; w_pre NULL, the forward pass formed no y: dy and dw_pre are NULL as
+ * well, and dh is not), f or kept_f (exactly one, or neither if the forward
  * pass had no f) the block's output or its checkpoint; the statistics are formed again from x, f and the gate.
  *   dx, df, dgate           device, contiguous, of dtype; dgate float [dim] for one gate of all rows, NULL without gate; df NULL without f
  *   dw_post, dw_pre         device float [dim] (dw_post NULL without f); sums over rows in binary32, in an order that depends on

@@ -611,8 +611,8 @@ def gated_norm(x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False
 
 
 def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6, center=False, workspace=None, stream=None):
-    """pruner_gated_norm_grad.  dh (or None: zero), dy: the gradients of gated_norm's h and y; f: the block's output, its Checkpoint, or None as in the
-    forward pass.  Returns (dx, df, dgate, dw_post, dw_pre); those of what was None are None."""
+    """pruner_gated_norm_grad.  dh (or None: zero), dy: the gradients of gated_norm's h and y (dy and w_pre None where y was not formed; dh is then
+    needed); f: the block's output, its Checkpoint, or None as in the forward pass.  Returns (dx, df, dgate, dw_post, dw_pre); those of what was None are None."""
     import torch
     lib = load_library()
     rows, dim = x.shape
@@ -620,7 +620,8 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
     px, x_pitch = _rows_of(x, "x")
     for t, what in ((dh, "dh"), (dy, "dy"), (f if kept is None else None, "f")):
         assert t is None or (t.dtype == x.dtype and t.shape == x.shape), what
-    pdy, dy_pitch = _rows_of(dy, "dy")
+    assert (dy is None) == (w_pre is None) and (dy is not None or dh is not None), "dy and w_pre go together, without them dh is needed"
+    pdy, dy_pitch = _rows_of(dy, "dy") if dy is not None else (None, 0)
     pdh, dh_pitch = _rows_of(dh, "dh") if dh is not None else (None, 0)
     pf, f_pitch = _rows_of(f, "f") if f is not None and kept is None else (None, 0)
     p = _c_norm(x, f is not None, w_post, w_pre, gate, alpha, eps, center)
@@ -632,7 +633,7 @@ def gated_norm_grad(dh, dy, x, f, w_post, w_pre, gate=None, alpha=1.0, eps=1e-6,
             dw_post = torch.empty_like(w_post)
             if gate is not None:
                 dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
-        dw_pre = torch.empty_like(w_pre)
+        dw_pre = torch.empty_like(w_pre) if w_pre is not None else None
     _returned(stream, dx, df, dgate, dw_post, dw_pre)
     held, ws, size = _scratch(workspace, lib.pruner_gated_norm_grad_workspace_bytes(rows, dim), x.device, stream)
     rc = lib.pruner_gated_norm_grad(p, pdh, dh_pitch, pdy, dy_pitch, px, x_pitch, pf, f_pitch, _c_checkpoint(kept, rows, dim) if kept is not None else None,

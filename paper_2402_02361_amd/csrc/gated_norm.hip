@@ -3,7 +3,7 @@
 //     norm(v) = (v - m) r, r = 1 / sqrt(mean((v - m)^2) + eps), m = mean(v) or 0
 // Backward, with <.> the mean over a row and N(d, z, r) = r (d - [<d>] - z <d z>) (the middle term with the mean only):
 //     dH = dh + N(dy w_pre, z2, r2);   dx = alpha dH;   dgate = dH u s (1 - s);   df = N(dH s w_post, z1, r1)
-//     dw_pre = sum over rows of dy z2;   dw_post = sum over rows of dH s z1
+//     dw_pre = sum over rows of dy z2;   dw_post = sum over rows of dH s z1;   without a norm after (no y): dH = dh
 // A row lives in the registers of T threads, eight neighbouring values each, T the power of two that covers it, or beyond 64 the whole wavefronts that do: every matrix is
 // read once and written once, and the statistics are formed again in the backward pass, where they cost no bytes.
 // All in binary32.  Bound: memory: 65536 x 2048 bfloat16 rows' gradients 411 us, 4.9 TB/s, 65536 x 256 49 us, 5.2 TB/s; forward, 16384 x 1100 binary32 rows 64 us, 4.5 TB/s.  A
@@ -199,8 +199,8 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(Norm p, const T* __restrict
 }
 
 // sums: [3][dim] of every workgroup (dw_post, dw_pre, dgate of one gate for all rows)
-// VECTOR: the gate is one for all rows
-template <typename T, int V, int BLOCK, bool VECTOR>
+// VECTOR: the gate is one for all rows.  Y: there is a norm after (asked for in the kernel this took 65536 x 2048 rows 421 us where it takes 400, and 8192 x 8192 319 and 400).
+template <typename T, int V, int BLOCK, bool VECTOR, bool Y>
 __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __restrict__ dh, int64_t dh_pitch, const T* __restrict__ dy, int64_t dy_pitch,
                                                          const T* __restrict__ x, int64_t x_pitch, const T* __restrict__ f, int64_t f_pitch,
                                                          const int8_t* __restrict__ codes, const uint8_t* __restrict__ exps, T* __restrict__ dx, T* __restrict__ df,
@@ -232,8 +232,10 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
     auto fetch = [&](int64_t row) {
         const int some = row < p.rows ? left : 0;
         const int64_t after = p.rows - 1 - row;
-        next.x.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left, row * x_pitch + col));
-        next.dy.load(dy + row * dy_pitch + col, some, room_of(after, dy_pitch, left, row * dy_pitch + col));
+        if constexpr (Y) {   // (x stands only in what the norm after sees)
+            next.x.load(x + row * x_pitch + col, some, room_of(after, x_pitch, left, row * x_pitch + col));
+            next.dy.load(dy + row * dy_pitch + col, some, room_of(after, dy_pitch, left, row * dy_pitch + col));
+        }
         if (f) next.f.load(f + row * f_pitch + col, some, room_of(after, f_pitch, left, row * f_pitch + col));
         if (codes) {
             next.c.load(codes + row * p.dim + col, some, room_of(after, p.dim, left, row * p.dim + col));
@@ -270,18 +272,22 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
 #pragma unroll
             for (int j = 0; j < kEach; ++j) v[j] = __builtin_fmaf(s[j], z1[j] * w_post[j], v[j]);
         }
-        const float r2 = normalise<V>(sum, v, z2, mine, p.per_dim, p.center, p.eps);
-        now.dy.to_floats(d);
+        if constexpr (Y) {
+            const float r2 = normalise<V>(sum, v, z2, mine, p.per_dim, p.center, p.eps);
+            now.dy.to_floats(d);
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            sum_pre[j] = __builtin_fmaf(d[j], z2[j], sum_pre[j]);
-            d[j] *= w_pre[j];
-        }
-        back<V>(sum, d, z2, r2, mine, p.per_dim, p.center);
-        if (dh) {
-            now.dh.to_floats(w);
+            for (int j = 0; j < kEach; ++j) {
+                sum_pre[j] = __builtin_fmaf(d[j], z2[j], sum_pre[j]);
+                d[j] *= w_pre[j];
+            }
+            back<V>(sum, d, z2, r2, mine, p.per_dim, p.center);
+            if (dh) {
+                now.dh.to_floats(w);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) d[j] += w[j];
+                for (int j = 0; j < kEach; ++j) d[j] += w[j];
+            }
+        } else {
+            now.dh.to_floats(d);
         }
         Eight<T, V> out;
 #pragma unroll
@@ -329,7 +335,7 @@ __global__ void __launch_bounds__(BLOCK) norm_grad_kernel(Norm p, const T* __res
                 if (j < left) to[col + j] = mine[j];
     };
     float* const to = sums + (int64_t)blockIdx.x * 3 * p.dim;
-    leave(sum_pre, to + p.dim);
+    if constexpr (Y) leave(sum_pre, to + p.dim);
     if (has_f) {
         leave(sum_post, to);
         if constexpr (VECTOR) leave(sum_gate, to + 2 * p.dim);
@@ -429,12 +435,13 @@ template <typename T, int V>
 int run_norm_grad(const pruner_norm* p, const Shape& s, const void* dh, int64_t dh_pitch, const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, const void* f,
                   int64_t f_pitch, const pruner_checkpoint* kept, void* dx, void* df, void* dgate, float* sums, int* parts, hipStream_t st)
 {
-    const bool vector = p->gate && !p->gate_pitch;
-    auto* const kernel = s.block > 512   ? (vector ? &norm_grad_kernel<T, V, 1024, true> : &norm_grad_kernel<T, V, 1024, false>)
-                         : s.block > 256 ? (vector ? &norm_grad_kernel<T, V, 512, true> : &norm_grad_kernel<T, V, 512, false>)
-                                         : (vector ? &norm_grad_kernel<T, V, 256, true> : &norm_grad_kernel<T, V, 256, false>);
-    static Held held[2][17];
-    const int64_t blocks = held[vector][s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
+    const bool vector = p->gate && !p->gate_pitch, has_y = p->w_pre;
+    auto* const kernel = !has_y          ? (vector ? &norm_grad_kernel<T, V, 1024, true, false> : &norm_grad_kernel<T, V, 1024, false, false>)   // (128 registers are enough)
+                         : s.block > 512 ? (vector ? &norm_grad_kernel<T, V, 1024, true, true> : &norm_grad_kernel<T, V, 1024, false, true>)
+                         : s.block > 256 ? (vector ? &norm_grad_kernel<T, V, 512, true, true> : &norm_grad_kernel<T, V, 512, false, true>)
+                                         : (vector ? &norm_grad_kernel<T, V, 256, true, true> : &norm_grad_kernel<T, V, 256, false, true>);
+    static Held held[2][2][17];
+    const int64_t blocks = held[has_y][vector][s.block / kWave].get(reinterpret_cast<const void*>(kernel), s.block, s.blocks);
     if (blocks < 0) return PRUNER_EHIP;
     *parts = (int)blocks;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(s.block), 0, st, norm_of(p, s.threads), static_cast<const T*>(dh), dh_pitch, static_cast<const T*>(dy),
@@ -481,12 +488,14 @@ extern "C" int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int6
 {
     if (!norm_ok(p) || (f && kept_f)) return PRUNER_EINVAL;
     const bool has_f = f || kept_f || (p->rows == 0 && dw_post);   // (a matrix without rows may have no address: its sums are zero)
-    if (!vector_ok(dw_pre) || !vector_ok(p->w_pre) || (has_f && (!vector_ok(dw_post) || !vector_ok(p->w_post)))) return PRUNER_EINVAL;
+    const bool has_y = p->w_pre != nullptr;
+    if (has_y ? !vector_ok(dw_pre) || !vector_ok(p->w_pre) : dw_pre || dy || (p->rows > 0 && !dh)) return PRUNER_EINVAL;
+    if (has_f && (!vector_ok(dw_post) || !vector_ok(p->w_post))) return PRUNER_EINVAL;
     const size_t bytes = type_bytes(p->dtype);
     const bool gate_rows = has_f && p->gate && p->gate_pitch, gate_vector = has_f && p->gate && !p->gate_pitch;
     if (has_f && p->gate && (!dgate || !aligned(dgate, gate_vector ? 4 : bytes))) return PRUNER_EINVAL;
     if (p->rows > 0) {
-        if (!matrix_ok(x, x_pitch, p) || !matrix_ok(dy, dy_pitch, p) || (dh && !matrix_ok(dh, dh_pitch, p)) || (f && !matrix_ok(f, f_pitch, p)) || (kept_f && !kept_ok(kept_f)) ||
+        if (!matrix_ok(x, x_pitch, p) || (has_y && !matrix_ok(dy, dy_pitch, p)) || (dh && !matrix_ok(dh, dh_pitch, p)) || (f && !matrix_ok(f, f_pitch, p)) || (kept_f && !kept_ok(kept_f)) ||
             !gate_ok(p))
             return PRUNER_EINVAL;
         if (!dx || !aligned(dx, bytes) || (has_f && (!df || !aligned(df, bytes)))) return PRUNER_EINVAL;
