@@ -250,9 +250,10 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
 
 // The same without registers on the way: bounds-checked buffer loads whose data go to LDS (64 lanes' 16 bytes side by side from M0 on), for a tile that all
 // wavefronts of a workgroup share, or one's own.  What was requested has arrived after wait_for<n>(), n the number of this wavefront's later requests, and is
-// there for the others after a barrier.  Tiles that these fill lie in the first 64 KB of LDS.  (A row's chunks are permuted on the way: a
+// there for the others after a barrier.  What these fill lies in the first kRequestRoom bytes of LDS (a place of 16 bits).  (A row's chunks are permuted on the way: a
 // lane asks for the chunk whose place it fills.)  The requests are written out because the compiler, seeing them, would wait for all
 // of them before any read of LDS; they return nothing in registers.
+constexpr int kRequestRoom = 65536;
 __device__ __forceinline__ void request_16(uint32_t lds, uint32_t at, u32x4 from, uint32_t offset)
 {
     asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(from), "s"(offset) : "memory");

@@ -128,6 +128,7 @@ template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, (DP == 128 ? 2 : 3)) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
 {
     constexpr int kN = SHARED ? kKeys : kOwnKeys, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);
+    static_assert((SHARED ? kTurns : 4) * 2 * kTileBytes <= kRequestRoom, "tiles lie where requests reach");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;

@@ -126,6 +126,7 @@ __device__ __forceinline__ void add_diagonals(float* skew, float* sums, const fl
 template <typename T, int DP, bool SHARED> __device__ __forceinline__ void queries_of(const Args& a, const Grad& gr, int q_tiles, uint32_t block)
 {
     constexpr int kN = SHARED && DP < 128 ? 64 : kOwn, kThreads = SHARED ? 256 : 64, kTileBytes = kN * Tile<DP>::kRowBytes, kTurns = turns_of(DP, SHARED, kN);   // (64 keys of 128 would leave no room for a second workgroup)
+    static_assert((SHARED ? kTurns : 4) * 2 * kTileBytes <= kRequestRoom, "tiles lie where requests reach");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31, thread = SHARED ? (int)threadIdx.x : lane;
     const uint32_t heads = (uint32_t)a.batch * a.q_heads;
@@ -386,10 +387,14 @@ template <typename T, int DP, bool SHARED> struct KeysShape {
     static constexpr int kWaves = 4;                          // of a workgroup (wide: eight would share a tile's requests, but wait for each other: 252 us where this took 228)
     static constexpr int kQ = SHARED && !kWide ? 64 : 32;     // queries of a tile
     static constexpr int kTurns = SHARED ? (kWide ? 2 : 3) : 1;
-    static constexpr int kStat = 64;                          // floats of one of a tile's stats
-    static constexpr int kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + kStats * kStat * 4;
+    // Shared tiles have their stats behind them; own tiles, which 128 wide fill what requests reach, lie side by side and their stats, which arrive through registers, behind
+    // them all (three wavefronts instead: 783 sequences of 6 queries and 55 keys, 16 heads of 128 sharing two, 250 us where this takes 225).
+    static constexpr int kStat = SHARED ? 64 : 32;            // floats of one of a tile's stats
+    static constexpr int kStatBytes = kStats * kStat * 4, kTileBytes = kQ * Tile<DP>::kRowBytes, kTurnBytes = 2 * kTileBytes + (SHARED ? kStatBytes : 0);
     static constexpr int kHeldBytes = kWide ? Tile<DP>::kSteps * 1024 : 0;   // of a wavefront
     static constexpr int kKeys = SHARED ? 32 * kWaves : 32;
+    static_assert((SHARED ? kTurns : kWaves) * kTurnBytes <= kRequestRoom, "tiles lie where requests reach");
+    static constexpr int kBytes = SHARED ? kTurns * kTurnBytes + kWaves * kHeldBytes : kWaves * (kTurnBytes + kStatBytes);   // of LDS before the biases
 };
 template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_of(const Args& a, const Grad& gr, int k_tiles, uint32_t block)
 {
@@ -407,7 +412,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
         part = it.tile % gr.parts;
         k0 = (k_tiles - 1 - it.tile / gr.parts) * Shape::kKeys + 32 * wave;   // (under a causal mask the first keys are seen by the most queries)
     } else {
-        const int64_t unit = (int64_t)block * 4 + wave;
+        const int64_t unit = (int64_t)block * Shape::kWaves + wave;
         if (unit >= (int64_t)heads * k_tiles) return;
         bh = (int)(unit / k_tiles);
         k0 = (int)(unit % k_tiles) * 32;
@@ -418,7 +423,8 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
     const int window_floats = a.table ? (window.size + 3) & ~3 : 0;
     char* const turns = lds + (SHARED ? 0 : wave * kTurnBytes);
     char* const held = lds + Shape::kTurns * kTurnBytes + wave * Shape::kHeldBytes + 16 * lane;
-    float* const biases = reinterpret_cast<float*>(lds + (SHARED ? Shape::kTurns * kTurnBytes + Shape::kWaves * Shape::kHeldBytes : 4 * kTurnBytes)) + (SHARED ? 0 : wave * window_floats);
+    float* const own_stats = reinterpret_cast<float*>(lds + Shape::kWaves * kTurnBytes + wave * Shape::kStatBytes);
+    float* const biases = reinterpret_cast<float*>(lds + Shape::kBytes) + (SHARED ? 0 : wave * window_floats);
 
     // query tiles that see any of this workgroup's keys
     const int first_key = SHARED ? k0 - 32 * wave : k0, shift = kl - ql;
@@ -433,6 +439,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
     qf.set(a.q.token, a.head_dim, thread, SHARED ? wave : 0);
     of.set(gr.dout.token, a.head_dim, thread, SHARED ? wave : 0);
     const int64_t all = (int64_t)a.batch * a.q_heads * gr.stat_rows;
+    float stat_in[2] = {0.f, 0.f};   // own tiles: this lane's values of the next tile's stats
     static_assert(!SHARED || Shape::kWaves == kStats, "of those that share a tile each asks for one of its stats");
     auto request = [&](int n, int turn) {
         const bool some = n < to;
@@ -440,15 +447,12 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
         const uint32_t place = (uint32_t)((SHARED ? turn : wave) * kTurnBytes);
         qf.request(a.q.at<T>(b, h) + (int64_t)i0 * a.q.token, left, place);
         of.request(gr.dout.at<T>(b, h) + (int64_t)i0 * gr.dout.token, left, place + kTileBytes);
-        auto stat = [&](int w) {
-            request_4(place + 2 * kTileBytes + 4 * kStat * w, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u,
-                      buffer_of(gr.stats + w * all + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0, some ? 4 * (gr.stat_rows - i0) : 0));
-        };
+        const float* const stats = gr.stats + ((int64_t)b * a.q_heads + h) * gr.stat_rows + i0;
         if constexpr (SHARED) {
-            stat(wave);
-        } else {
+            request_4(place + 2 * kTileBytes + 4 * kStat * wave, lane < kQ ? 4u * (uint32_t)lane : 0x80000000u, buffer_of(stats + wave * all, some ? 4 * (gr.stat_rows - i0) : 0));
+        } else if (some) {   // (32 rows of a tile, as many of stats: stat_rows is a multiple of 32)
 #pragma unroll
-            for (int w = 0; w < kStats; ++w) stat(w);
+            for (int w = 0; w < 2; ++w) stat_in[w] = stats[(2 * w + half) * all + l32];
         }
     };
     constexpr int kAhead = SHARED ? kTurns - 1 : 1;   // tiles on their way before the first is worked on
@@ -506,11 +510,13 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
                 request(n + kTurns - 1, turn == 0 ? kTurns - 1 : turn - 1);
             } else {
                 wait_for<0>();
+#pragma unroll
+                for (int w = 0; w < 2; ++w) own_stats[(2 * w + half) * kStat + l32] = stat_in[w];
                 wave_fence();
             }
             if constexpr (kWide) at.forget();
             const char* const qt = turns + (SHARED ? turn * kTurnBytes : 0);
-            const float* const st = reinterpret_cast<const float*>(qt + 2 * kTileBytes);
+            const float* const st = SHARED ? reinterpret_cast<const float*>(qt + 2 * kTileBytes) : own_stats;
 #pragma unroll
             for (int m = 0; m < kQ / 32; ++m) {
                 const int p0 = shift + i0 + 32 * m;   // position of the block's first query
@@ -619,7 +625,7 @@ template <typename T, int DP, bool SHARED> __device__ __forceinline__ void keys_
     }
 }
 
-template <typename T, int DP> __global__ void __launch_bounds__(256, (DP < 128 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles) { keys_of<T, DP, false>(a, gr, k_tiles, blockIdx.x); }
+template <typename T, int DP> __global__ void __launch_bounds__(256, (DP == 32 ? 3 : DP == 64 ? 2 : 1)) keys_kernel(Args a, Grad gr, int k_tiles) { keys_of<T, DP, false>(a, gr, k_tiles, blockIdx.x); }
 
 // Some workgroups take queries, the others keys, those with the longer way to go first (9 sequences of up to 1001, 32 heads of 80 sharing 8: keys first 250 us, queries first
 // 350; 5001 causal tokens, 16 heads of 128 sharing 4, 444 and 412).  With either alone on the device, 2 x 810 causal tokens, 4 heads of 128, took 73 us where this takes
@@ -883,14 +889,16 @@ template <typename T, int DP> int run(const Call& c)
             PRUNER_LAUNCH_CHECK();
         }
         if (a.k_tokens > 0) {
-            hipLaunchKernelGGL((keys_kernel<T, DP>), dim3((unsigned)((k_heads * c.plan.k_tiles + 3) / 4)), dim3(256), 4 * (window + KeysShape<T, DP, false>::kTurnBytes), c.st, a, c.keys, c.plan.k_tiles);
+            typedef KeysShape<T, DP, false> Shape;
+            hipLaunchKernelGGL((keys_kernel<T, DP>), dim3((unsigned)((k_heads * c.plan.k_tiles + Shape::kWaves - 1) / Shape::kWaves)), dim3(64 * Shape::kWaves),
+                               Shape::kBytes + Shape::kWaves * window, c.st, a, c.keys, c.plan.k_tiles);
             PRUNER_LAUNCH_CHECK();
         }
     } else if (q_heads > 0) {
         typedef KeysShape<T, DP, true> Shape;
         static_assert(Shape::kWaves == 4, "workgroups of 256 threads");
         constexpr int kStep = DP < 128 ? 64 : 32;
-        const size_t q_lds = 5 * window + 4 * skew + turns_of(DP, true, kStep) * 2 * kStep * DP * 2, k_lds = window + Shape::kTurns * Shape::kTurnBytes + Shape::kWaves * Shape::kHeldBytes;
+        const size_t q_lds = 5 * window + 4 * skew + turns_of(DP, true, kStep) * 2 * kStep * DP * 2, k_lds = window + Shape::kBytes;
         const unsigned q_blocks = (unsigned)(q_heads * c.plan.q_tiles * c.plan.q_parts), k_blocks = (unsigned)(k_heads * c.plan.k_tiles * c.plan.parts);
         if (a.q_tokens > 0) {
             const int64_t need = (q_heads * c.queries.stat_rows + 31) / 32;
