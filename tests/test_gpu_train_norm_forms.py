@@ -82,3 +82,19 @@ def test_what_goes_together():
     for a in ((None, None, x, f, w1, None), (dh, dy, x, f, w1, None), (dh, None, x, f, w1, w2), (None, None, x, f, w1, w2)):
         with pytest.raises(AssertionError):
             P.gated_norm_grad(*a)
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-18, 1e-19, 3e-20, 1e-20])
+def test_tiny_values_without_eps(size):
+    """Mean squares below binary32's smallest normal number: they keep a step of 2^-149, of which a value's square is off by half, beside the usual roundings."""
+    gen = torch.Generator().manual_seed(1)
+    f, dh = torch.randn(5, 200, generator=gen).cuda() * size, torch.randn(5, 200, generator=gen).cuda()
+    w, x = torch.ones(200, device="cuda"), torch.zeros(5, 200, device="cuda")
+    h, _, _ = P.gated_norm(x, f, w, None, eps=0.0)
+    _, df, _, dw, _ = P.gated_norm_grad(dh, None, x, f, w, None, eps=0.0)
+    want = ref.norm(*(ref.cpu(t) for t in (x, f, w, w)), eps=0.0, dh=ref.cpu(dh), dy=np.zeros((5, 200)))
+    off = 2.0 ** -149 / size ** 2 + 64 * ref.F32
+    assert (np.abs(ref.cpu(h) - want["h"]) <= off * np.abs(want["h"])).all()
+    # (twice for r and z, and as much again for <d z>)
+    assert (np.abs(ref.cpu(df) - want["df"]) <= 4 * off * want["df_abs"]).all()
+    assert (np.abs(ref.cpu(dw) - want["dw_post"]) <= off * want["dw_post_abs"]).all()
