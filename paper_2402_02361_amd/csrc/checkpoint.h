@@ -17,8 +17,6 @@ constexpr int kGroup = PRUNER_CHECKPOINT_GROUP;
 constexpr int kEach = 8;                        // values of a row that a thread holds; four threads hold a group
 static_assert(kGroup == 4 * kEach, "a group is four threads' values");
 
-template <typename T> __device__ __forceinline__ float widened(T v) { return (float)v; }
-
 __device__ __forceinline__ uint32_t pair_of(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
 __device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2)); }
 __device__ __forceinline__ f32x2 pair_to(uint32_t w, __bf16) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)}; }

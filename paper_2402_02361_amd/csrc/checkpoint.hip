@@ -7,7 +7,7 @@ namespace {
 
 using namespace ckpt;
 
-// n / d for n below 2^31 and 1 <= d < 2^31, by a multiplication: q = (hi(n m) + n) >> s with m = floor(2^32 (2^s - d) / d) + 1, s = ceil(log2 d).
+// n / d for n below 2^31 and 1 <= d < 2^31, by a multiplication (Granlund and Montgomery, Division by invariant integers using multiplication, 1994): q = (hi(n m) + n) >> s with m = floor(2^32 (2^s - d) / d) + 1, s = ceil(log2 d).
 struct Divisor {
     uint32_t d, m, s;
     explicit Divisor(uint32_t by) : d(by), m(0), s(0)

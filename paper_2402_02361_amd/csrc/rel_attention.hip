@@ -453,11 +453,14 @@ Plan plan_of(const pruner_attention* a)
         const int dp = padded_dim(a->head_dim);
         int64_t parts;
         if (p.route == Route::kRows) {
-            const int fewest = 512;   // keys of a part at least
+            // keys of a part at least (256, 512 and 1024, us a call: one token against 5000 keys, 8 heads of 64, 18, 17, 18; 2 tokens of 4 sequences against 3000, 16 heads of 128 sharing 4,
+            // 18, 18, 20; one against 60000, 8 heads of 128 sharing one, 100, 58, 39)
+            const int fewest = 512;
             parts = (kEnoughRows + groups - 1) / groups;
             const int64_t most = ((int64_t)a->k_tokens + fewest - 1) / fewest;
             parts = parts < most ? parts : most;
-        } else {   // (steps as measured: 8192 causal tokens, 16 heads of 128; 5417, 4 of 64)
+        } else {   // (steps as measured: 8192 causal tokens, 16 heads of 128; 5417, 4 of 64; those of 32 wide heads: 200 queries and
+                   // 9000 keys, 4 heads, 34 us by 64 wide heads' steps, 28 by these, 1500 causal tokens, 2 heads, 17 either way)
             parts = parts_of((double)groups, (a->k_tokens + kKeys - 1) / kKeys, a->flags & PRUNER_ATTENTION_CAUSAL, dp == 128 ? 512 : 768, dp == 128 ? 1.5 : dp == 64 ? 1.1 : 0.8,
                              dp == 32 ? 1.6 : 2.2, (double)p.rows * dp * 4);
         }

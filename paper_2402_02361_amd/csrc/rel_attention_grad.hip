@@ -823,7 +823,7 @@ Plan plan_of(const pruner_attention* a)
     const int dp = padded_dim(a->head_dim), group = a->q_heads / a->kv_heads;
     const bool causal = a->flags & PRUNER_ATTENTION_CAUSAL;
     // A workgroup's four wavefronts share tiles, or, where queries and keys are few, each has a sequence and head of its own (us in all, shared and own: 2048 sequences of 8 queries
-    // and keys, 64 wide, 68 and 34; 783 of 6 and 55, 16 heads sharing two, 268 and 141, of 128 312 and 256; 200 of 20 and 60, 4 heads, 41 and 37, of 128 49 and 51;
+    // and keys, 64 wide, 67 and 32; 783 of 6 and 55, 16 heads sharing two, 264 and 125, of 128 311 and 225; 200 of 20 and 60, 4 heads, 41 and 34, of 128 51 and 49;
     // 200 of 20 and 120 46 and 50).
     p.own = a->q_tokens <= 32 && a->k_tokens <= kOwnMost;
     p.q_tiles = (a->q_tokens + 127) / 128;
