@@ -459,9 +459,9 @@ int pruner_gated_norm_grad(const pruner_norm* p, const void* dh, int64_t dh_pitc
  *   dtable           device, of dtype, the table's shape, or NULL without table; sums over pairs in binary32 in an order that depends on the
  *                    sizes and the device alone, rounded once
  * Outputs are written for every row of q_tokens and k_tokens.  dk and dv are the sums over the query heads that share a key head.
- * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, batch x q_heads x (q_tokens + 64) below 2^30, for the gradients
- * with batch x kv_heads x (k_tokens + 64) added to it.
- * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes only.  0: none is
+ * batch >= 0, q_tokens, k_tokens >= 0 and below 2^30, q_heads up to 2^20, batch x q_heads x (q_tokens + 64) below 2^30; for the gradients
+ * with batch x kv_heads x (k_tokens + 64) added to it, and q_heads up to 65535.
+ * workspace: pruner_rel_attention_workspace_bytes(a), pruner_rel_attention_grad_workspace_bytes(a); they read the sizes and whether there is a table.  0: none is
  * needed and workspace may be NULL.
  * Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
  */

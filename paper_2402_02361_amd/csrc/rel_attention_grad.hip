@@ -14,7 +14,7 @@
 // S and dP are formed twice (14 products of a pair's depth where 10 would do), so that nothing is added across workgroups but in a fixed order.
 //
 // Bound: the matrix cores with the exponentials and LDS reads between their products.  5001 causal tokens, 16 heads of 128 sharing 4: 414 us in all, queries alone on the device
-// 190 (820 TFLOP/s), keys 240 (860), where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 79 us in all, bound by a
+// 190 (820 TFLOP/s), keys 240 (860), where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 75 us in all, bound by a
 // workgroup's chain of tiles and its start (5 us).
 #include "rel_attention.h"
 
