@@ -37,8 +37,8 @@ def _prior_filter(P, seed):
 
 def _lse(P, seed):
     seg, tiles = lse_population(SG, LENS, seed=seed)
-    populations = [dev(tiles) for _ in range(2)]   # (each call moves its population on)
-    return lambda stream: P.lse(SG, seg, populations.pop(), 100, 3, seed, 52429, stream=stream)
+    populations = {given: dev(tiles) for given in (False, True)}   # (each call moves its population on, which is the caller's to keep until then)
+    return lambda stream: P.lse(SG, seg, populations[stream is not None], 100, 3, seed, 52429, stream=stream)
 
 
 def _random_init(P, seed):
