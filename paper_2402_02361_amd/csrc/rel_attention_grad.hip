@@ -13,6 +13,9 @@
 //             latter alone).
 // S and dP are formed twice (14 products of a pair's depth where 10 would do), so that nothing is added across workgroups but in a fixed order.
 //
+// P and dS are rounded to the operands' type for the products that sum them, at the rate of the matrix cores' 16-bit forms, and delta is taken from o as it is given, rounded (a pass over the
+// keys would have it from P dP, as own tiles have): dq is off by 2.4e-3 of itself with 5001 causal tokens in bfloat16, where its own rounding makes 1.66e-3, dS's 2.34e-3 with that and delta's
+// 1.71e-3; with 150 causal tokens 2.53e-3, 2.35e-3 and 1.92e-3.
 // Bound: the matrix cores with the exponentials and LDS reads between their products.  5001 causal tokens, 16 heads of 128 sharing 4: 414 us in all, queries alone on the device
 // 190 (820 TFLOP/s), keys 240 (860), where a large matrix product reaches 1445.  16 sequences of up to 500, 12 heads of 64: 75 us in all, bound by a
 // workgroup's chain of tiles and its start (5 us).

@@ -134,3 +134,25 @@ def test_results_that_the_current_stream_reads_are_kept(make, busy):
     next_got = _tensors(other(side))
     torch.cuda.synchronize()
     assert _same(copies, want) and _same(next_got, next_want)
+
+
+@pytest.mark.parametrize("make", CALLS)
+def test_on_another_stream_of_a_graph(make):
+    """Captured on a stream that branches off the capturing one and joins it again; replayed with other work between."""
+    call = make(5)
+    want = [t.clone() for t in _tensors(call(None))]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = _tensors(call(side))
+        torch.cuda.current_stream().wait_stream(side)
+        sums = [t.clone() for t in got]
+    for _ in range(3):
+        for t in (*got, *sums):
+            t.fill_(7)
+        (torch.ones(1000, 1000, device="cuda") @ torch.ones(1000, 1000, device="cuda")).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(got, want) and _same(sums, want)
