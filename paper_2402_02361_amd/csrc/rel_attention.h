@@ -256,11 +256,11 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
 constexpr int kRequestRoom = 65536;
 __device__ __forceinline__ void request_16(uint32_t lds, uint32_t at, u32x4 from, uint32_t offset)
 {
-    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(from), "s"(offset) : "memory");
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(from), "s"(offset) : "memory", "m0");
 }
 __device__ __forceinline__ void request_4(uint32_t lds, uint32_t at, u32x4 from)   // 4 bytes a lane
 {
-    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(from) : "memory");
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(from) : "memory", "m0");
 }
 template <int N> __device__ __forceinline__ void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // Before a loop: all that was loaded into registers has come.  (Where the compiler finds a first use inside the loop, it waits there each time, and with
