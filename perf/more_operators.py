@@ -18,8 +18,9 @@ How weights and caches lie (both sides read it):
   weights  codes int32 [n_out / 16][dim / 128][4][16][4] (rounded up): the word (g, row, j) of a block holds the weights of columns
            32 j + 8 g + i, i = 0 .. 7, of that row, four bits each from bit 4 (i / 2) + 16 (i % 2) on; a weight is (code - 8) scale.
            scales bfloat16 [n_out / 16][dim / 128][4][128 / group][4]: of group u and row 4 a + r of a block at (a, u, r)
-  caches   codes uint8 (e4m3), keys [pages][kv_heads][page_tokens][head_dim], values [pages][kv_heads][head_dim][page_tokens]; a value is
-           code 2^(exp - 127), exps uint8 [pages][kv_heads]; pages int32 [batch][pages of a sequence]
+  caches   codes uint8 (e4m3), keys [pages][kv_heads][head_dim / 16][page_tokens][16], the last of them 16 neighbouring columns, values
+           [pages][kv_heads][page_tokens / 16][head_dim][16], the last of them 16 neighbouring tokens; a value is code 2^(exp - 127),
+           exps uint8 [pages][kv_heads]; pages int32 [batch][pages of a sequence]
 """
 import math
 
@@ -190,16 +191,23 @@ def _exponents(top):
     return torch.where(top > 0, e.int() - 9 + (m > 0.875).int(), torch.full_like(e.int(), -126)).clamp(min=-126)
 
 
+def _lay(x, turned):
+    """[pages, heads, place, column] as it lies in a cache."""
+    p, h, t, d = x.shape
+    return x.view(p, h, t // 16, 16, d).transpose(3, 4).contiguous() if turned else x.view(p, h, t, d // 16, 16).transpose(2, 3).contiguous()
+
+
 def _fill(gen, pages, heads, page_tokens, head_dim, turned):
     """Codes and exponents of a pool of pages: channels of different sizes, pages of different sizes."""
-    codes = torch.empty((pages, heads, head_dim, page_tokens) if turned else (pages, heads, page_tokens, head_dim), dtype=torch.uint8, device="cuda")
+    codes = torch.empty((pages, heads, page_tokens // 16, head_dim, 16) if turned else (pages, heads, head_dim // 16, page_tokens, 16), dtype=torch.uint8, device="cuda")
     exps = torch.empty((pages, heads), dtype=torch.uint8, device="cuda")
-    channel = torch.exp(_randn(gen, heads, head_dim, 1) * 0.7) if turned else torch.exp(_randn(gen, heads, 1, head_dim) * 0.7)
+    channel = torch.exp(_randn(gen, heads, 1, head_dim) * 0.7)
     step = max(1, (1 << 27) // (heads * page_tokens * head_dim))
     for p in range(0, pages, step):
-        x = torch.randn(codes[p:p + step].shape, generator=gen, device="cuda") * channel * torch.exp(_randn(gen, min(step, pages - p), 1, 1, 1) * 0.2)
+        n = min(step, pages - p)
+        x = torch.randn((n, heads, page_tokens, head_dim), generator=gen, device="cuda") * channel * torch.exp(_randn(gen, n, 1, 1, 1) * 0.2)
         e = _exponents(x.abs().amax((2, 3)))
-        codes[p:p + step] = (x * _two_to(-e)[..., None, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+        codes[p:p + step] = _lay((x * _two_to(-e)[..., None, None]).to(torch.float8_e4m3fn).view(torch.uint8), turned)
         exps[p:p + step] = (e + 127).to(torch.uint8)
     return codes, exps
 
@@ -362,25 +370,25 @@ def _plain_cache(s):
         old = codes[first].view(torch.float8_e4m3fn).float()
         was = exps[first].int() - 127
         now = torch.where(kept[:, :1], torch.maximum(most[first], was), most[first])
-        again = (old * _two_to(was - now)[..., None, None]).to(torch.float8_e4m3fn).view(torch.uint8)
-        where = kept[:, None, None, :] if turned else kept[:, None, :, None]
+        again = (old * _two_to(was - now)[..., None, None, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+        where = kept.view(-1, 1, t // 16, 1, 16) if turned else kept.view(-1, 1, 1, t, 1)
         codes[first] = torch.where(where, again, codes[first])
         most[first] = now
         exps[page] = (most[page] + 127).to(torch.uint8)
         new = (x * _two_to(-most[page])[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)   # [batch, tokens, heads, dim]
         if turned:
-            codes[page, :, :, place] = new
+            codes[page, :, place // 16, :, place % 16] = new
         else:
-            codes[page, :, place] = new
+            codes[page, :, :, place] = new.unflatten(-1, (-1, 16))
     return _plain_restore(s)
 
 
 def _dense(s, codes, exps, turned, b):
     """Sequences' values [.., heads, places, dim] in binary32."""
     of = s["pages"][b].long().clamp(min=0)
-    x = codes[of].view(torch.float8_e4m3fn).float() * _two_to(exps[of].int() - 127)[..., None, None]
-    x = (x.transpose(-1, -2) if turned else x).transpose(-3, -4)
-    return x.reshape(*x.shape[:-3], -1, x.shape[-1])
+    x = codes[of].view(torch.float8_e4m3fn).float() * _two_to(exps[of].int() - 127)[..., None, None, None]
+    x = (x.transpose(-1, -2) if turned else x.transpose(-2, -3)).movedim(-4, -5)      # [.., heads, page, unit, 16, column] or [.., heads, page, place, unit, 16]
+    return x.reshape(*x.shape[:-4], -1, s["case"]["head_dim"])
 
 
 def _plain_restore(s):
@@ -521,8 +529,8 @@ def _exact_cache(s, codes, exps, name, turned):
             lo, hi = i * t, min((i + 1) * t, before + n)
             if hi <= lo:
                 break
-            held = _value(s[codes][page])
-            held = held.transpose(1, 2) if turned else held                           # [heads, place, dim]
+            held = _value(s[codes][page]).transpose(2, 3) if turned else _value(s[codes][page]).transpose(1, 2)
+            held = held.reshape(c["kv_heads"], t, c["head_dim"])
             e = s[exps][page].double()[:, None, None] - 127
             kept, values = max(0, min(before, hi) - lo), torch.zeros(c["kv_heads"], hi - lo, c["head_dim"], dtype=torch.float64, device="cuda")
             if lo + kept < hi:
@@ -547,8 +555,8 @@ def _exact_attention(s):
         of = s["pages"][b, :-(-m // t)].long()
         r = torch.arange(m, device="cuda")[None, :] - (torch.arange(n, device="cuda")[:, None] + m - n)
         for h in range(c["kv_heads"]):
-            k = (_value(s["k_codes"][of, h]) * _power(s["k_exps"][of, h].long() - 127)[:, None, None]).reshape(-1, c["head_dim"])[:m]
-            v = (_value(s["v_codes"][of, h]) * _power(s["v_exps"][of, h].long() - 127)[:, None, None]).transpose(1, 2).reshape(-1, c["head_dim"])[:m]
+            k = (_value(s["k_codes"][of, h]) * _power(s["k_exps"][of, h].long() - 127)[:, None, None, None]).transpose(1, 2).reshape(-1, c["head_dim"])[:m]
+            v = (_value(s["v_codes"][of, h]) * _power(s["v_exps"][of, h].long() - 127)[:, None, None, None]).transpose(2, 3).reshape(-1, c["head_dim"])[:m]
             for g in range(h * group, (h + 1) * group):
                 w = s["scale"] * (s["q"][b, :n, g].double() @ k.t())
                 if c["sides"]:
