@@ -490,6 +490,105 @@ int pruner_rel_attention_grad(const pruner_attention* a, const pruner_heads* dou
                               const pruner_heads* o, const float* lse, const pruner_heads* dq, const pruner_heads* dk, const pruner_heads* dv, void* dtable,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- a sequence read token by token ---------------------------------------------------------------------------------------
+   What a step of one or a few new tokens per sequence needs besides: positions by rotation, keys and values kept in 8 bits in
+   pages, attention over them, and linear layers whose weights are held in 4 bits.  The calls share one way of naming tokens: of
+   sequence b, k_len[b] tokens are there after the step and the last q_len[b] of them are new. */
+
+/*
+ * Positions by rotation: columns of a head turn in pairs by an angle that grows with the position p,
+ *     (a, b) -> amplitude (a cos(p f_i) - b sin(p f_i), b cos(p f_i) + a sin(p f_i)),   i = 0 .. rotary_dim / 2 - 1;
+ * pair i is columns (i, i + rotary_dim / 2), or with PRUNER_ROTARY_INTERLEAVED columns (2 i, 2 i + 1); the columns from rotary_dim on stay
+ * as they are.  pruner_rotary_grad is the gradient: the same by -p f_i.  Frequencies for contexts longer than a model was trained on are the caller's to scale.
+ * Angles are reduced exactly, sines and cosines are binary32 (off by a rounding or two), and so is the product, rounded once to the type.
+ *   q, k, q_out, k_out  pruner_heads of any strides >= 0 (queries q_heads, keys kv_heads; a count of 0: none, its pointers are not read), head_dim contiguous, at their
+ *                       type's size; an output may be its input (with the same strides), and overlaps it in no other way
+ *   freqs               host double [rotary_dim / 2], |f| <= PRUNER_MAX_ROTARY_FREQUENCY
+ *   positions           device int32 [batch][tokens], or NULL: token t of sequence b stands at k_len[b] - q_len[b] + t (k_len NULL: at t; q_len NULL: tokens).
+ *                       Any value, negative ones too.
+ * Every one of the batch x tokens rows is turned.  head_dim 2..512, rotary_dim even, 2..min(head_dim, 256); batch x tokens below 2^30, heads up to 65535.
+ * No workspace.  Errors: PRUNER_EINVAL.
+ */
+#define PRUNER_ROTARY_INTERLEAVED 1
+#define PRUNER_MAX_ROTARY_DIM 256
+#define PRUNER_MAX_ROTARY_HEAD 512
+#define PRUNER_MAX_ROTARY_FREQUENCY 64.0
+typedef struct pruner_rotation {
+    int32_t dtype;                     /* PRUNER_BF16, PRUNER_F16 or PRUNER_F32 */
+    int32_t batch, tokens, q_heads, kv_heads, head_dim, rotary_dim, flags;
+    float amplitude;
+    const double* freqs;
+    const int32_t *positions, *q_len, *k_len;
+} pruner_rotation;
+int pruner_rotary(const pruner_rotation* r, const pruner_heads* q, const pruner_heads* k, const pruner_heads* q_out, const pruner_heads* k_out, void* stream);
+int pruner_rotary_grad(const pruner_rotation* r, const pruner_heads* dq_out, const pruner_heads* dk_out, const pruner_heads* dq, const pruner_heads* dk, void* stream);
+
+/*
+ * A cache of keys and values in 8 bits.  It is a pool of pages of page_tokens tokens; token t of sequence b lies in page table[b][t / page_tokens] at place
+ * t % page_tokens.  A page of a head holds e4m3 codes (sign, four bits of exponent, three of fraction; 448 is the largest) and one exponent byte for the keys and
+ * one for the values; a value is code x 2^(byte - 127), byte 1..254.
+ *   k_codes  device uint8 [pages][kv_heads][head_dim / 16][page_tokens][16]: the last index is 16 neighbouring columns
+ *   v_codes  device uint8 [pages][kv_heads][page_tokens / 16][head_dim][16]: the last index is 16 neighbouring tokens
+ *   k_exps, v_exps  device uint8 [pages][kv_heads]
+ *   table    device int32 [batch][seq_pages], or NULL: page i of sequence b is b seq_pages + i (pages >= batch x seq_pages).  A number outside 0 .. pages - 1 is a page that is not
+ *            there: its tokens are not stored, not seen and read back as zeros.
+ * codes 16-byte aligned; page_tokens a power of two, 16..PRUNER_MAX_PAGE_TOKENS; head_dim a multiple of 16, 16..128; kv_heads 1..65535; seq_pages x page_tokens below 2^30.
+ * A sequence may share full pages with others; a page that gets tokens is one sequence's alone.
+ *
+ * pruner_cache_append stores tokens: row t of k and v (t < q_len[b]) becomes token k_len[b] - q_len[b] + t.  Of each page that gets tokens
+ *     e = the smallest integer >= -126 with max |x| <= 448 x 2^e over the new tokens there, not below the page's own if it holds older tokens,
+ *     code = x / 2^e to the nearest (ties to even);   byte = e + 127;
+ * codes of older tokens are rounded again if the exponent has grown.  An infinity or a NaN becomes e4m3's NaN and does not count for e.  Tokens that would lie before the
+ * first place or behind the last page are left out.  What lies behind the new tokens stays as it is.
+ *   k, v   pruner_heads [batch][tokens][kv_heads][head_dim] of any strides >= 0, of any of the three types, at their type's size
+ *   q_len  device int32 [batch] or NULL: tokens for all (values outside 0..tokens are clamped);  k_len  device int32 [batch] or NULL: q_len (sequences begin)
+ * pruner_cache_restore reads tokens 0 .. k_len[b] - 1 back (k_len NULL: tokens for all; clamped to 0..tokens); rows from there on are zeros.  Values are exact
+ * within the type's range.  tokens up to seq_pages x page_tokens.
+ * No workspace.  2 x batch x kv_heads x (pages that a call's tokens can touch) below 2^24.  Errors: PRUNER_EINVAL.
+ *
+ * pruner_cache_attention is pruner_rel_attention over a cache: the same formulas, masks, biases, types and limits (head_dim a multiple of 16; a->kv_heads and
+ * a->head_dim are the cache's; a->k_tokens at most seq_pages x page_tokens), q, o and lse as there.  Tokens of a page that is not there are not seen; a NaN among the codes of
+ * a sequence's tokens may reach every row of the sequence.  What lies behind a sequence's tokens does not matter.
+ * workspace: pruner_cache_attention_workspace_bytes(a), which reads the sizes only.  Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
+ */
+#define PRUNER_MAX_PAGE_TOKENS 256
+typedef struct pruner_cache {
+    uint8_t *k_codes, *v_codes, *k_exps, *v_exps;
+    const int32_t* table;
+    int32_t pages, page_tokens, kv_heads, head_dim, seq_pages;
+} pruner_cache;
+int pruner_cache_append(const pruner_cache* c, int32_t dtype, int32_t batch, int32_t tokens, const pruner_heads* k, const pruner_heads* v, const int32_t* q_len,
+                        const int32_t* k_len, void* stream);
+int pruner_cache_restore(const pruner_cache* c, int32_t dtype, int32_t batch, int32_t tokens, const int32_t* k_len, const pruner_heads* k, const pruner_heads* v, void* stream);
+size_t pruner_cache_attention_workspace_bytes(const pruner_attention* a);
+int pruner_cache_attention(const pruner_attention* a, const pruner_cache* c, const pruner_heads* q, const pruner_heads* o, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * Linear layers of few rows whose weights are held in 4 bits: y = x W^T + bias, W[n][k] = (code - 8) x scale, codes 0..15, one scale for `group` neighbouring inputs of an output.
+ * pruner_weights_pack makes them (inputs beyond dim have code 8; the last group of an output may be shorter):
+ *     scale = bfloat16(max |w| / 7),   code - 8 = w / scale to the nearest (ties to even), within -8..7; scale 0 where that is 0;
+ *     a group that holds an infinity or a NaN has a NaN for its scale and restores as NaN.
+ *   codes   device, 16-byte aligned [ceil(n_out / 16)][ceil(dim / 128)][4][16][4] words of 32 bits: the word (g, r, j) of a block holds inputs 32 j + 8 g + i, i = 0..7, of the block's
+ *           output r, input i at bit 4 (i / 2) + 16 (i % 2)
+ *   scales  device bfloat16 bits, 8-byte aligned [ceil(n_out / 16)][ceil(dim / 128)][4][128 / group][4]: of output 4 a + r and the block's group u at (a, u, r)
+ *   group   32, 64 or 128;  n_out and dim 1..2^24
+ * pruner_weights_pack and pruner_weights_restore: w device [n_out][pitch] of any of the three types (restored values are rounded to it).
+ * pruner_weights_linear: x device [rows][x_pitch], y device [rows][y_pitch], PRUNER_BF16 or PRUNER_F16; bias device float [n_out] or NULL; rows 0..PRUNER_MAX_LINEAR_ROWS (made for few: the
+ * weights are read once for every 16 or 32).  Products with codes are exact and sums binary32, rounded once.  (bfloat16: sums are of x times 128 + code, less 136 times x: an
+ * infinity in x gives a NaN, and so may values beyond 2^120.)
+ * No workspace.  Errors: PRUNER_EINVAL (pointers; w, x, y at their type's size, bias 4 bytes; sizes, types, a pitch below the row).
+ */
+#define PRUNER_MAX_LINEAR_ROWS (1 << 20)
+typedef struct pruner_weights {
+    void* codes;
+    uint16_t* scales;
+    int32_t n_out, dim, group;
+} pruner_weights;
+int pruner_weights_pack(const void* w, int32_t dtype, int64_t pitch, const pruner_weights* packed, void* stream);
+int pruner_weights_restore(const pruner_weights* packed, int32_t dtype, void* w, int64_t pitch, void* stream);
+int pruner_weights_linear(const pruner_weights* packed, const void* x, int32_t dtype, int64_t rows, int64_t x_pitch, const float* bias, void* y, int64_t y_pitch, void* stream);
+
 #define PRUNER_WS_DRAFT 0
 #define PRUNER_WS_TOPK 1
 #define PRUNER_WS_VERIFY 2

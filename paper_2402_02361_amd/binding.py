@@ -80,10 +80,43 @@ class CAttention(C.Structure):
                 ("edges", C.c_void_p), ("n_edges", C.c_int32)]
 
 
+class CRotation(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("tokens", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("flags", C.c_int32), ("amplitude", C.c_float), ("freqs", C.c_void_p), ("positions", C.c_void_p), ("q_len", C.c_void_p), ("k_len", C.c_void_p)]
+
+
+class CCache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_exps", C.c_void_p), ("v_exps", C.c_void_p), ("table", C.c_void_p), ("pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("seq_pages", C.c_int32)]
+
+
+class CWeights(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("n_out", C.c_int32), ("dim", C.c_int32), ("group", C.c_int32)]
+
+
 class Checkpoint(NamedTuple):
     """A matrix of activations in 8 bits: codes int8 [rows, dim], exps uint8 [rows, ceil(dim / 32)]."""
     codes: object
     exps: object
+
+
+class Cache(NamedTuple):
+    """Keys and values in 8 bits in a pool of pages: k_codes uint8 [pages, kv_heads, head_dim / 16, page_tokens, 16], v_codes uint8 [pages, kv_heads, page_tokens / 16, head_dim, 16],
+    k_exps, v_exps uint8 [pages, kv_heads]; table int32 [batch, pages of a sequence], or a number: sequences have that many pages each, one after the other."""
+    k_codes: object
+    v_codes: object
+    k_exps: object
+    v_exps: object
+    table: object
+
+
+class PackedWeights(NamedTuple):
+    """A linear layer's weights in 4 bits: codes int32 [ceil(n_out / 16), ceil(dim / 128), 4, 16, 4], scales bfloat16 [ceil(n_out / 16), ceil(dim / 128), 4, 128 / group, 4]."""
+    codes: object
+    scales: object
+    n_out: int
+    dim: int
+    group: int
 
 
 _lib = None
@@ -155,6 +188,23 @@ def load_library():
         lib.pruner_rel_attention_grad_workspace_bytes.argtypes = [C.c_void_p]
         lib.pruner_rel_attention_grad.restype = C.c_int
         lib.pruner_rel_attention_grad.argtypes = [C.c_void_p] * 10 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        for name in ("pruner_rotary", "pruner_rotary_grad"):
+            getattr(lib, name).restype = C.c_int
+            getattr(lib, name).argtypes = [C.c_void_p] * 6
+        lib.pruner_cache_append.restype = C.c_int
+        lib.pruner_cache_append.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 5
+        lib.pruner_cache_restore.restype = C.c_int
+        lib.pruner_cache_restore.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 4
+        lib.pruner_cache_attention_workspace_bytes.restype = C.c_size_t
+        lib.pruner_cache_attention_workspace_bytes.argtypes = [C.c_void_p]
+        lib.pruner_cache_attention.restype = C.c_int
+        lib.pruner_cache_attention.argtypes = [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        lib.pruner_weights_pack.restype = C.c_int
+        lib.pruner_weights_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p]
+        lib.pruner_weights_restore.restype = C.c_int
+        lib.pruner_weights_restore.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        lib.pruner_weights_linear.restype = C.c_int
+        lib.pruner_weights_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         lib.pruner_workspace_bytes.restype = C.c_size_t
         lib.pruner_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
         lib.pruner_strerror.restype = C.c_char_p
@@ -464,6 +514,7 @@ _dtypes, _raw_stream = {}, None
 # The structs of include/pruner.h as bytes, which a call takes like a pointer to them (a ctypes structure takes a call of a few microseconds half of one more).
 _PACK_CHECKPOINT, _PACK_HEADS = struct.Struct("@2P"), struct.Struct("@P3q")
 _PACK_NORM, _PACK_ATTENTION = struct.Struct("@q3i2f4x3Pq"), struct.Struct("@8if4x4Pi4x")
+_PACK_ROTATION, _PACK_CACHE, _PACK_WEIGHTS = struct.Struct("@8if4x4P"), struct.Struct("@5P5i4x"), struct.Struct("@2P3i4x")
 
 
 def _dtype(t):
@@ -671,9 +722,14 @@ def _lengths(t, batch, what):
 
 
 def _c_attention(q, k, v, table, edges, q_len, k_len, causal, scale):
-    batch, q_tokens, q_heads, head_dim = q.shape
+    batch, _, _, head_dim = q.shape
     k_tokens, kv_heads = k.shape[1], k.shape[2]
     assert k.shape == (batch, k_tokens, kv_heads, head_dim) and v.shape == k.shape and k.dtype == q.dtype and v.dtype == q.dtype, "q, k, v"
+    return _c_attention_of(q, k_tokens, kv_heads, table, edges, q_len, k_len, causal, scale)
+
+
+def _c_attention_of(q, k_tokens, kv_heads, table, edges, q_len, k_len, causal, scale):
+    batch, q_tokens, q_heads, head_dim = q.shape
     flags = _ATTENTION_CAUSAL if causal else 0
     n_edges = 0
     if table is not None:
@@ -735,3 +791,211 @@ def rel_attention_grad(do, q, k, v, o, lse, table=None, edges=None, q_len=None, 
     if rc:
         raise PrunerError(rc, "pruner_rel_attention_grad")
     return dq, dk, dv, dtable
+
+
+# ---- a sequence read token by token
+
+MAX_ROTARY_DIM, MAX_ROTARY_HEAD, MAX_ROTARY_FREQUENCY, MAX_PAGE_TOKENS, MAX_LINEAR_ROWS = 256, 512, 64.0, 256, 1 << 20
+_ROTARY_INTERLEAVED = 1
+
+
+def rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, trained=None, low=1.0, high=4.0):
+    """Angle per position of each of rotary_dim / 2 pairs: base^(-2 i / rotary_dim) (float64 numpy array).  factor: positions are to reach that many times as far as in training: with
+    trained None every frequency is divided by it; else only those that turn fewer than `low` times over `trained` positions, those that turn `high` times or more stay, and in between the two
+    mix in proportion."""
+    assert rotary_dim % 2 == 0 and 2 <= rotary_dim <= MAX_ROTARY_DIM and base > 0 and factor > 0, "rotary_dim, base, factor"
+    f = float(base) ** (-2.0 * np.arange(rotary_dim // 2, dtype=np.float64) / rotary_dim)
+    if trained is None:
+        return f / factor
+    assert trained > 0 and high > low, "trained, low, high"
+    kept = np.clip((trained * f / (2.0 * math.pi) - low) / (high - low), 0.0, 1.0)
+    return f * (kept + (1.0 - kept) / factor)
+
+
+def _rotary(name, q, k, freqs, positions, q_len, k_len, interleaved, amplitude, out, stream):
+    import torch
+    lib = load_library()
+    batch, tokens, q_heads, head_dim = q.shape
+    assert q.is_cuda, "q"
+    assert k is None or (k.is_cuda and k.dtype == q.dtype and k.dim() == 4 and k.shape[:2] == q.shape[:2] and k.shape[3] == head_dim), "k"
+    if not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
+        freqs = np.ascontiguousarray(freqs, dtype=np.float64)
+    assert freqs.ndim == 1 and 2 <= 2 * len(freqs) <= head_dim, "freqs"
+    if positions is not None:
+        assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (batch, tokens), "positions"
+    if out is None:
+        with _made_on(stream):
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k is not None else None
+        _returned(stream, q_out, k_out)
+    else:
+        q_out, k_out = out
+        assert q_out.is_cuda and q_out.shape == q.shape and q_out.dtype == q.dtype, "out"
+        assert (k is None) == (k_out is None) and (k is None or (k_out.is_cuda and k_out.shape == k.shape and k_out.dtype == k.dtype)), "out"
+    r = _PACK_ROTATION.pack(_dtype(q.dtype), batch, tokens, q_heads, k.shape[2] if k is not None else 0, head_dim, 2 * len(freqs), _ROTARY_INTERLEAVED if interleaved else 0, amplitude,
+                            freqs.__array_interface__["data"][0], positions.data_ptr() if positions is not None else 0, _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"))
+    rc = getattr(lib, name)(r, _heads(q, "q"), _heads(k, "k") if k is not None else None, _heads(q_out, "out"), _heads(k_out, "out") if k is not None else None, _stream_on(stream, q))
+    if rc:
+        raise PrunerError(rc, name)
+    return q_out, k_out
+
+
+def rotary(q, k, freqs, positions=None, q_len=None, k_len=None, interleaved=False, amplitude=1.0, out=None, stream=None):
+    """pruner_rotary: queries and keys turned by their positions.  q: bfloat16, float16 or float32 CUDA [batch, tokens, q_heads, head_dim], k [batch, tokens, kv_heads, head_dim] or None, any
+    strides with contiguous heads; freqs: angle per position of each pair (host, e.g. from rotary_frequencies), the first 2 len(freqs) columns turn; positions int32 CUDA
+    [batch, tokens], or None: token t stands at k_len - q_len + t (int32 CUDA [batch] each; k_len None: at t, q_len None: tokens).  interleaved: pairs are neighbouring columns, else
+    columns half of them apart.  out: (q_out, k_out), the inputs themselves among others.  Returns (q_out, k_out)."""
+    return _rotary("pruner_rotary", q, k, freqs, positions, q_len, k_len, interleaved, amplitude, out, stream)
+
+
+def rotary_grad(dq, dk, freqs, positions=None, q_len=None, k_len=None, interleaved=False, amplitude=1.0, out=None, stream=None):
+    """pruner_rotary_grad: the gradients of rotary's q and k from those of its outputs, the rest as it was called."""
+    return _rotary("pruner_rotary_grad", dq, dk, freqs, positions, q_len, k_len, interleaved, amplitude, out, stream)
+
+
+def new_cache(pages, kv_heads, head_dim, table, page_tokens=64, device="cuda", stream=None):
+    """A Cache with room for `pages` pages; table: int32 CUDA [batch, pages of a sequence], or a number of pages that each sequence has for itself."""
+    import torch
+    assert pages >= 0 and kv_heads >= 1 and head_dim % 16 == 0 and page_tokens % 16 == 0, "pages, kv_heads, head_dim, page_tokens"
+    with _made_on(stream):
+        made = (torch.empty((pages, kv_heads, head_dim // 16, page_tokens, 16), dtype=torch.uint8, device=device),
+                torch.empty((pages, kv_heads, page_tokens // 16, head_dim, 16), dtype=torch.uint8, device=device),
+                torch.empty((pages, kv_heads), dtype=torch.uint8, device=device), torch.empty((pages, kv_heads), dtype=torch.uint8, device=device))
+    _returned(stream, *made)
+    return Cache(*made, table)
+
+
+def _c_cache(cache, batch):
+    """(the struct, kv_heads, head_dim, the tokens that a sequence has room for)"""
+    import torch
+    k, v, k_exps, v_exps, table = cache
+    pages, kv_heads, units, page_tokens, unit = k.shape
+    head_dim = 16 * units
+    assert k.is_cuda and k.dtype == torch.uint8 and k.is_contiguous() and unit == 16, "k_codes"
+    assert v.is_cuda and v.dtype == torch.uint8 and v.is_contiguous() and v.shape == (pages, kv_heads, page_tokens // 16, head_dim, 16), "v_codes"
+    for t, what in ((k_exps, "k_exps"), (v_exps, "v_exps")):
+        assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == (pages, kv_heads), what
+    if isinstance(table, int):
+        at, seq_pages = 0, table
+    else:
+        assert table.is_cuda and table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2 and table.shape[0] == batch, "table"
+        at, seq_pages = table.data_ptr(), table.shape[1]
+    return (_PACK_CACHE.pack(k.data_ptr(), v.data_ptr(), k_exps.data_ptr(), v_exps.data_ptr(), at, pages, page_tokens, kv_heads, head_dim, seq_pages), kv_heads, head_dim,
+            seq_pages * page_tokens)
+
+
+def cache_append(cache, k, v, q_len=None, k_len=None, stream=None):
+    """pruner_cache_append: row t of k and v (bfloat16, float16 or float32 CUDA [batch, tokens, kv_heads, head_dim], any strides with contiguous heads) becomes token k_len - q_len + t
+    of its sequence, t < q_len.  q_len, k_len: int32 CUDA [batch]; q_len None: tokens, k_len None: q_len."""
+    lib = load_library()
+    batch, tokens = k.shape[:2]
+    c, kv_heads, head_dim, _ = _c_cache(cache, batch)
+    assert k.shape == (batch, tokens, kv_heads, head_dim) and v.shape == k.shape and v.dtype == k.dtype, "k, v"
+    rc = lib.pruner_cache_append(c, _dtype(k.dtype), batch, tokens, _heads(k, "k"), _heads(v, "v"), _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"), _stream_on(stream, k))
+    if rc:
+        raise PrunerError(rc, "pruner_cache_append")
+
+
+def cache_restore(cache, tokens, k_len, dtype, stream=None):
+    """pruner_cache_restore: (k, v) [batch, tokens, kv_heads, head_dim] of `dtype`, the cache's first `tokens` tokens of each sequence; rows from k_len (int32 CUDA [batch]) on are zeros."""
+    import torch
+    lib = load_library()
+    batch = k_len.numel()
+    c, kv_heads, head_dim, _ = _c_cache(cache, batch)
+    with _made_on(stream):
+        k = torch.empty((batch, tokens, kv_heads, head_dim), dtype=dtype, device=k_len.device)
+        v = torch.empty_like(k)
+    _returned(stream, k, v)
+    rc = lib.pruner_cache_restore(c, _dtype(dtype), batch, tokens, _lengths(k_len, batch, "k_len"), _heads(k, "k"), _heads(v, "v"), _stream_on(stream, k_len))
+    if rc:
+        raise PrunerError(rc, "pruner_cache_restore")
+    return k, v
+
+
+def cache_attention(q, cache, table=None, edges=None, q_len=None, k_len=None, causal=True, scale=None, o=None, want_lse=False, k_tokens=None, workspace=None, stream=None):
+    """pruner_cache_attention: rel_attention over a Cache.  q [batch, q_tokens, q_heads, head_dim], the last q_len tokens of sequences of k_len (int32 CUDA [batch]; k_len None: as many as
+    the cache has room for, or k_tokens).  k_tokens: the most that any sequence has, where that is known and less than there is room for (a shorter axis is cut into fewer parts); the rest as
+    for rel_attention.  Returns o, with want_lse=True (o, lse)."""
+    import torch
+    lib = load_library()
+    batch, q_tokens, q_heads, head_dim = q.shape
+    c, kv_heads, width, room = _c_cache(cache, batch)
+    assert q.is_cuda and head_dim == width, "q"
+    a, held_edges = _c_attention_of(q, room if k_tokens is None else k_tokens, kv_heads, table, edges, q_len, k_len, causal, scale)
+    made_o = o is None
+    with _made_on(stream):
+        if made_o:
+            o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
+    _returned(stream, o if made_o else None, lse)
+    assert o.shape == q.shape and o.dtype == q.dtype, "o"
+    held, ws, size = _scratch(workspace, lib.pruner_cache_attention_workspace_bytes(a), q.device, stream)
+    rc = lib.pruner_cache_attention(a, c, _heads(q, "q"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
+    if rc:
+        raise PrunerError(rc, "pruner_cache_attention")
+    return (o, lse) if want_lse else o
+
+
+def _c_weights(w):
+    import torch
+    codes, scales, n_out, dim, group = w
+    tiles, blocks = -(-n_out // 16), -(-dim // 128)
+    assert group in (32, 64, 128), "group"
+    assert codes.is_cuda and codes.dtype == torch.int32 and codes.is_contiguous() and codes.shape == (tiles, blocks, 4, 16, 4), "codes"
+    assert scales.is_cuda and scales.dtype == torch.bfloat16 and scales.is_contiguous() and scales.shape == (tiles, blocks, 4, 128 // group, 4), "scales"
+    return _PACK_WEIGHTS.pack(codes.data_ptr(), scales.data_ptr(), n_out, dim, group)
+
+
+def weights_pack(w, group=32, packed=None, stream=None):
+    """pruner_weights_pack.  w: bfloat16, float16 or float32 CUDA [n_out, dim] (rows may be further apart); `group` neighbouring inputs (32, 64 or 128) share a scale.  Returns PackedWeights."""
+    import torch
+    lib = load_library()
+    p, pitch = _rows_of(w, "w")
+    n_out, dim = w.shape
+    if packed is None:
+        tiles, blocks = -(-n_out // 16), -(-dim // 128)
+        with _made_on(stream):
+            packed = PackedWeights(torch.empty((tiles, blocks, 4, 16, 4), dtype=torch.int32, device=w.device),
+                                   torch.empty((tiles, blocks, 4, 128 // group, 4), dtype=torch.bfloat16, device=w.device), n_out, dim, group)
+        _returned(stream, packed.codes, packed.scales)
+    assert packed.n_out == n_out and packed.dim == dim, "packed"
+    rc = lib.pruner_weights_pack(p, _dtype(w.dtype), pitch, _c_weights(packed), _stream_on(stream, w))
+    if rc:
+        raise PrunerError(rc, "pruner_weights_pack")
+    return packed
+
+
+def weights_restore(packed, dtype=None, w=None, stream=None):
+    """pruner_weights_restore.  Returns w [n_out, dim] (of `dtype`, or a given tensor's)."""
+    import torch
+    lib = load_library()
+    if w is None:
+        with _made_on(stream):
+            w = torch.empty((packed.n_out, packed.dim), dtype=dtype, device=packed.codes.device)
+        _returned(stream, w)
+    assert w.shape == (packed.n_out, packed.dim), "w"
+    p, pitch = _rows_of(w, "w")
+    rc = lib.pruner_weights_restore(_c_weights(packed), _dtype(w.dtype), p, pitch, _stream_on(stream, w))
+    if rc:
+        raise PrunerError(rc, "pruner_weights_restore")
+    return w
+
+
+def weights_linear(x, packed, bias=None, y=None, stream=None):
+    """pruner_weights_linear: y = x W^T + bias.  x: bfloat16 or float16 CUDA [rows, dim] (rows may be further apart), packed: PackedWeights, bias float32 [n_out] or None.
+    Returns y [rows, n_out]."""
+    import torch
+    lib = load_library()
+    p, pitch = _rows_of(x, "x")
+    rows, dim = x.shape
+    assert dim == packed.dim, "x"
+    if y is None:
+        with _made_on(stream):
+            y = torch.empty((rows, packed.n_out), dtype=x.dtype, device=x.device)
+        _returned(stream, y)
+    assert y.shape == (rows, packed.n_out) and y.dtype == x.dtype, "y"
+    py, y_pitch = _rows_of(y, "y")
+    rc = lib.pruner_weights_linear(_c_weights(packed), p, _dtype(x.dtype), rows, pitch, _vector(bias, packed.n_out, "bias") if bias is not None else None, py, y_pitch, _stream_on(stream, x))
+    if rc:
+        raise PrunerError(rc, "pruner_weights_linear")
+    return y

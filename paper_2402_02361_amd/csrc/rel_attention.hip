@@ -19,7 +19,7 @@
 // The weights are rounded to the operands' type for the second product, which is the rate of the matrix cores' 16-bit forms; their sum is of the unrounded ones.  8192 causal tokens in
 // bfloat16: o is off by 2.0e-3 of itself, where its own rounding makes 1.5e-3; 16 sequences of up to 777 in binary16 2.8e-4 and 2.1e-4.
 // rows_kernel is bound by memory: one token against 32 caches of up to 32768, 8 heads of 128, 400 us and 12 to join, 5.2 TB/s.
-#include "rel_attention.h"
+#include "attention_softmax.h"
 
 namespace pruner {
 namespace att {
@@ -27,68 +27,6 @@ namespace {
 
 constexpr int kKeys = 64;          // keys of a shared tile
 constexpr int kOwnKeys = 32;       // keys of a wavefront's own tile
-constexpr float kSlack = 8.f;      // a running maximum may lag this far behind: weights stay below e^8, within binary16
-
-// What a part of the key axis leaves per row: its weighted sum (binary32, unnormalised) and (maximum, sum).
-struct Parts {
-    float* sums;    // [part][row][DP]
-    float2* stats;  // [part][row]
-    int count, keys;   // parts, keys of a part (a multiple of 64)
-};
-
-// The running softmax of one query over 32-key blocks of scores.
-template <typename T, int DP> struct Running {
-    float m, l;
-    floatx16 o[Tile<DP>::kBlocks];
-    __device__ __forceinline__ void clear()
-    {
-        m = -ATT_INF;
-        l = 0.f;
-#pragma unroll
-        for (int b = 0; b < Tile<DP>::kBlocks; ++b) o[b] = zero16();
-    }
-    // s: scores; where fused, scaled by `scale` and shifted by `bias` on the way, else they are what the softmax takes.  On return s holds the weights.
-    template <int N> __device__ __forceinline__ void weigh(floatx16 (&s)[N], bool fused, float scale, float bias)
-    {
-        float top = s[0][0];
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, s[n][i]);
-        top = max_of_halves(top);
-        if (fused) top = __builtin_fmaf(top, scale, bias);
-        if (__any(top > m + kSlack)) {   // (from minus infinity: any score)
-            const float now = __builtin_fmaxf(m, top), factor = now == -ATT_INF ? 1.f : exp2_of((m - now) * kLog2e);
-            m = now;
-            l *= factor;
-#pragma unroll
-            for (int b = 0; b < Tile<DP>::kBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[b][i] *= factor;
-        }
-        const float from = m == -ATT_INF ? 0.f : m;   // (no key yet: every weight is exp(-infinity))
-        float sum = 0.f;
-        if (fused) {
-            const float c = scale * kLog2e, d = (bias - from) * kLog2e;
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[n][i] = exp2_of(__builtin_fmaf(s[n][i], c, d));
-                    sum += s[n][i];
-                }
-        } else {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[n][i] = exp2_of((s[n][i] - from) * kLog2e);
-                    sum += s[n][i];
-                }
-        }
-        l += sum;
-    }
-};
 
 // Keys at or beyond `limit` leave the softmax.
 template <int N> __device__ __forceinline__ void mask_scores(floatx16 (&s)[N], int key0, int limit, int half)
@@ -123,8 +61,6 @@ __device__ __forceinline__ bool finish_scores(floatx16 (&s)[N], const Args& a, c
     if (masked) mask_scores(s, key0, limit, half);
     return fused;
 }
-
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -ATT_INF : __builtin_fmaf(__builtin_amdgcn_logf(l), kLn2, m); }   // (logf: base 2)
 
 template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(256, (DP == 128 ? 2 : 3)) tile_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int q_tiles)
@@ -261,20 +197,10 @@ __global__ void __launch_bounds__(256, (DP == 128 ? 2 : 3)) tile_kernel(Args a, 
     if (lse && half == 0) lse[row] = i < ql ? lse_of(run.m, l) : -ATT_INF;
 }
 
-// LDS of rows_kernel before the tiles: the biases of the group's heads, and the bucket of every r that a tile which is not wholly at one end can ask for.
-struct RowsLds {
-    int n_buckets, biases, buckets;   // bytes
-    __host__ __device__ explicit RowsLds(const Args& a)
-        : n_buckets(a.table ? (a.n_edges + 1) * (a.two_sided ? 2 : 1) : 0), biases((n_buckets * a.group * 4 + 15) & ~15),
-          buckets(a.table ? (Window(a.left, a.right).size + 15) & ~15 : 0)
-    {
-    }
-};
-
 // Query t of head hk * group + g is column t * group + g.
 template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts)
 {
-    constexpr int kTileBytes = kOwnKeys * Tile<DP>::kRowBytes, kStride = DP + 4;   // (sums: rows of DP + 4 floats, so that neighbouring rows lie in other banks)
+    constexpr int kTileBytes = kOwnKeys * Tile<DP>::kRowBytes;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int columns = a.q_tokens * a.group;
@@ -359,75 +285,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
             wave_fence();
         }
     }
-    // the four wavefronts' sums, one after the other
-    __syncthreads();
-    float2* const stats = reinterpret_cast<float2*>(lds);           // [4][32]
-    float* const sums = reinterpret_cast<float*>(lds + 4 * 32 * 8); // [4][columns][kStride]
-    const float l = sum_of_halves(run.l);
-    if (half == 0) stats[wave * 32 + l32] = make_float2(run.m, mine ? l : 0.f);
-    if (l32 < columns) store_row32<DP>(sums + (wave * columns + l32) * kStride, run.o, half);
-    __syncthreads();
-    for (int item = threadIdx.x; item < columns * (DP / 4); item += 256) {
-        const int c = item / (DP / 4), d = 4 * (item % (DP / 4));
-        float m = -ATT_INF;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = __builtin_fmaxf(m, stats[w * 32 + c].y != 0.f ? stats[w * 32 + c].x : -ATT_INF);
-        float total = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float2 st = stats[w * 32 + c];
-            if (st.y == 0.f) continue;
-            const float f = exp2_of((st.x - m) * kLog2e);
-            total = __builtin_fmaf(f, st.y, total);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(sums + (w * columns + c) * kStride + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
-        }
-        const int tt = c / a.group, hh = hk * a.group + c % a.group;
-        const int64_t row = ((int64_t)b * a.q_heads + hh) * a.q_tokens + tt;
-        if (parts.count > 1) {
-            const int64_t slot = (int64_t)part * a.batch * a.q_heads * a.q_tokens + row;
-            *reinterpret_cast<f32x4*>(parts.sums + slot * DP + d) = o;
-            if (d == 0) parts.stats[slot] = make_float2(m, total);
-        } else {
-            const float f = total != 0.f ? 1.f / total : 0.f;
-            if (d < a.head_dim)
-                *reinterpret_cast<u32x2*>(out.at<T>(b, hh) + (int64_t)tt * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
-            if (lse && d == 0) lse[row] = lse_of(m, total);
-        }
-    }
-}
-
-// Four neighbouring values of a row per thread.
-template <typename T, int DP> __global__ void __launch_bounds__(256) join_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts)
-{
-    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = item / (DP / 4);
-    const int d = 4 * (int)(item % (DP / 4));
-    if (row >= rows) return;
-    float m = -ATT_INF, total = 0.f;
-#pragma unroll 8
-    for (int n = 0; n < parts.count; ++n) {
-        const float2 st = parts.stats[n * rows + row];
-        m = __builtin_fmaxf(m, st.y != 0.f ? st.x : -ATT_INF);
-    }
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int n = 0; n < parts.count; ++n) {
-        const float2 st = parts.stats[n * rows + row];
-        const f32x4 x = *reinterpret_cast<const f32x4*>(parts.sums + (n * rows + row) * DP + d);
-        const bool any = st.y != 0.f;   // (a part that no key reached counts for nothing, whatever it left)
-        const float f = any ? exp2_of((st.x - m) * kLog2e) : 0.f;
-        total = __builtin_fmaf(f, st.y, total);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, any ? x[e] : 0.f, o[e]);
-    }
-    const float f = total != 0.f ? 1.f / total : 0.f;
-    const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads;
-    if (d < a.head_dim)
-        *reinterpret_cast<u32x2*>(out.at<T>(b, h) + (int64_t)i * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
-    if (lse && d == 0) lse[row] = lse_of(m, total);
+    meet<T, DP>(run, lds, a, out, lse, parts, b, hk, part, columns, mine);
 }
 
 // Which kernel, and into how many parts the keys are cut.

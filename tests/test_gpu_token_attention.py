@@ -1,0 +1,251 @@
+"""cache_attention against the definition of rel_attention in 64 bits on the values that the cache's codes stand for."""
+import numpy as np
+import pytest
+import torch
+
+import block_reference as block
+import paper_2402_02361_amd as P
+import token_reference as ref
+
+pytestmark = pytest.mark.gpu
+BF, HALF = torch.bfloat16, torch.float16
+E = np.array([1, 2, 3, 4, 6, 9, 14, 22], np.int32)
+
+
+def _ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def _cache(seed, batch, tokens, heads, head_dim, page_tokens, k_len=None, missing=()):
+    """A cache whose pages hold random codes and exponents up to the sequences' lengths, and NaN codes and exponents of any size behind them; missing: (sequence, page) that are not there.
+    Returns it with its values [batch, tokens, heads, head_dim] and which tokens are there."""
+    rng = np.random.default_rng(seed)
+    seq_pages = -(-tokens // page_tokens)
+    k_len = [tokens] * batch if k_len is None else [int(np.clip(n, 0, tokens)) for n in k_len]
+    pages = batch * seq_pages + 2
+    table = rng.permutation(pages)[:batch * seq_pages].reshape(batch, seq_pages).astype(np.int32)
+    codes = [ref.to_e4m3(rng.standard_normal((pages, heads, page_tokens, head_dim)) * 120 * np.exp(0.3 * rng.standard_normal((1, heads, 1, head_dim)))) for _ in range(2)]
+    codes = [np.where((c & 127) == 127, 120, c).astype(np.uint8) for c in codes]
+    exps = [rng.integers(119, 122, (pages, heads)).astype(np.uint8) for _ in range(2)]
+    used = np.zeros((pages, page_tokens), bool)
+    for b in range(batch):
+        for i in range(seq_pages):
+            used[table[b, i]] = i * page_tokens + np.arange(page_tokens) < k_len[b]
+            if (b, i) in missing:
+                table[b, i] = (-1, pages, 1 << 30)[i % 3]
+            elif i * page_tokens >= k_len[b]:
+                exps[0][table[b, i]], exps[1][table[b, i]] = 255, 250
+                if i % 2:
+                    table[b, i] = -1
+    for c in codes:
+        c[~used[:, None, :].repeat(heads, 1)] = 127 if seed % 2 else 255
+    values, there = zip(*(ref.dense(c, e, table, tokens, k_len) for c, e in zip(codes, exps)))
+    k = np.ascontiguousarray(codes[0].reshape(pages, heads, page_tokens, head_dim // 16, 16).transpose(0, 1, 3, 2, 4))
+    v = np.ascontiguousarray(codes[1].reshape(pages, heads, page_tokens // 16, 16, head_dim).transpose(0, 1, 2, 4, 3))
+    return P.Cache(*(torch.from_numpy(t).cuda() for t in (k, v, *exps)), _ints(table)), values[0], values[1], there[0]
+
+
+def _randn(gen, *shape, dtype, scale=1.0):
+    return (torch.randn(*shape, generator=gen) * scale).to(dtype).cuda()
+
+
+def _reference(q, k, v, there, table, edges, q_len, k_len, causal, scale):
+    """block.attention, with the tokens of missing pages out of sight (as keys whose scores are minus infinity: they are taken out of each sequence, their distances kept)."""
+    if there is None:
+        return block.attention(q, k, v, table, edges, q_len, k_len, causal, scale)
+    batch, lq, hq, d = q.shape
+    out = {"o": np.zeros(q.shape), "o_abs": np.zeros(q.shape), "v_abs": np.zeros(q.shape), "lse": np.full((batch, hq, lq), -np.inf)}
+    group = hq // k.shape[2]
+    two_sided = table is not None and table.shape[0] == 2 * (len(edges) + 1)
+    for b in range(batch):
+        ql, kl = int(q_len[b]), int(k_len[b])
+        r = np.arange(kl)[None, :] - (kl - ql + np.arange(ql))[:, None]
+        seen = ((r <= 0) if causal else np.ones_like(r, bool)) & there[b, :kl][None, :]
+        for h in range(hq):
+            s = scale * (q[b, :ql, h] @ k[b, :kl, h // group].T) + (table[block.buckets(r, edges, two_sided), h] if table is not None else 0)
+            for i in range(ql):
+                if not seen[i].any():
+                    continue
+                e = np.exp(s[i, seen[i]] - s[i, seen[i]].max())
+                p, vv = e / e.sum(), v[b, :kl, h // group][seen[i]]
+                out["o"][b, i, h], out["o_abs"][b, i, h], out["v_abs"][b, i, h] = p @ vv, p @ np.abs(vv), np.abs(vv).sum(0)
+                out["lse"][b, h, i] = np.log(e.sum()) + s[i, seen[i]].max()
+    return out
+
+
+def _within(got, lse, want, dtype):
+    g, bound = block.cpu(got), block.attention_bounds(want, dtype)["o"]
+    assert np.isfinite(g).all()
+    worst = np.abs(g - want["o"]) / np.maximum(bound, 1e-300)
+    assert (worst <= 1).all(), f"{worst.max():.3g} of its bound at {np.unravel_index(worst.argmax(), worst.shape)}"
+    t, none = block.cpu(lse), np.isinf(want["lse"])
+    assert np.array_equal(none, np.isinf(t)) and (np.abs(t[~none] - want["lse"][~none]) <= 1e-5 + 2e-6 * np.abs(want["lse"][~none])).all()
+
+
+def _check(dtype, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, page_tokens, sides=0, edges=E, q_len=None, k_len=None, causal=True, seed=0, missing=()):
+    gen = torch.Generator().manual_seed(seed)
+    cache, k, v, there = _cache(seed, batch, k_tokens, kv_heads, head_dim, page_tokens, k_len, missing)
+    q = _randn(gen, batch, q_tokens, q_heads, head_dim, dtype=dtype)
+    table = _randn(gen, sides * (len(edges) + 1), q_heads, dtype=dtype, scale=0.7) if sides else None
+    ql = [q_tokens] * batch if q_len is None else [int(np.clip(n, 0, q_tokens)) for n in q_len]
+    kl = [k_tokens] * batch if k_len is None else [int(np.clip(n, 0, k_tokens)) for n in k_len]
+    for b in range(batch):
+        q[b, ql[b]:] = float("nan")
+    scale = 0.5 * head_dim ** -0.5
+    kw = dict(q_len=None if q_len is None else _ints(q_len), k_len=None if k_len is None else _ints(k_len), causal=causal, scale=scale)
+    o, lse = P.cache_attention(q, cache, table, edges if sides else None, want_lse=True, k_tokens=k_tokens, **kw)
+    clean = np.where(np.arange(q_tokens)[None, :, None, None] < np.array(ql)[:, None, None, None], block.cpu(q), 0.0)
+    want = _reference(clean, k, v, there if missing else None, block.cpu(table), edges, ql, kl, causal, scale)
+    _within(o, lse, want, dtype)
+    return q, cache, table, {**kw, "k_len": _ints(kl)}, o, lse   # (the cache has room for more tokens than it holds)
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("batch,q_tokens,k_tokens,q_heads,kv_heads,head_dim,page_tokens", [
+    (1, 1, 1, 1, 1, 16, 16), (3, 1, 300, 8, 8, 64, 64), (2, 1, 2000, 8, 1, 128, 32), (2, 5, 700, 12, 3, 80, 16), (4, 2, 65, 4, 2, 48, 128), (1, 3, 5000, 7, 1, 32, 256), (2, 32, 200, 1, 1, 112, 64),
+    (1, 1, 6000, 32, 1, 96, 64), (5, 8, 40, 4, 1, 128, 16)])
+@pytest.mark.parametrize("sides", [0, 1])
+def test_few_tokens(dtype, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, page_tokens, sides):
+    k_len = [max(1, k_tokens - 61 * b) if b % 2 == 0 else max(1, k_tokens // (b + 1)) for b in range(batch)]
+    edges = P.relative_edges(16, 128) if k_tokens > 128 else E
+    _check(dtype, batch, q_tokens, k_tokens, q_heads, kv_heads, head_dim, page_tokens, sides, edges, k_len=k_len, seed=k_tokens + sides)
+
+
+@pytest.mark.parametrize("causal,sides", [(True, 0), (True, 1), (False, 2), (False, 0), (True, 2)])
+@pytest.mark.parametrize("shape", [(1, 33, 33, 1, 1, 64, 16), (2, 40, 200, 14, 2, 96, 64), (1, 130, 130, 3, 1, 128, 32), (1, 9, 1500, 12, 3, 64, 128), (1, 300, 700, 4, 2, 80, 16), (3, 70, 90, 2, 2, 16, 64),
+                                   (1, 200, 70, 1, 1, 32, 16)])
+def test_many_tokens(shape, causal, sides):
+    _check((BF, HALF)[(sum(shape) + sides) % 2], *shape, sides, causal=causal, seed=sum(shape))
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("q_len,k_len", [([0, 5, 40, 17], [0, 5, 40, 17]), ([9, 40, 3, 0], [4, 0, 40, 12]), ([40, 40, 1, 20], [10, 39, 1, 40]), ([-4, 99, 7, 2], [40, 1000, -1, 16])])
+@pytest.mark.parametrize("tokens", [40, 6])
+def test_lengths_leave_rows_empty_and_padding_does_not_matter(dtype, q_len, k_len, tokens):
+    for causal in (False, True):
+        _check(dtype, 4, tokens, 40, 4, 2, 64, 16, 2, q_len=q_len, k_len=k_len, causal=causal, seed=1)
+
+
+@pytest.mark.parametrize("page_tokens", [16, 32, 64, 128])
+@pytest.mark.parametrize("q_tokens", [1, 20, 100])
+def test_pages_that_are_not_there(page_tokens, q_tokens):
+    """Their tokens are not seen: first ones, ones inside a step, last ones, all of a sequence."""
+    k_len = [400, 390, 401, 130]
+    gone = [(0, 0), (0, 2), (1, 1), (2, 400 // page_tokens)] + [(3, i) for i in range(26)]
+    _check(BF, 4, q_tokens, 401, 4, 2, 64, page_tokens, 1, k_len=k_len, seed=2, missing=[g for g in gone if g[1] < -(-401 // page_tokens)])
+
+
+@pytest.mark.parametrize("far", [1, 40, 500, 1024])
+@pytest.mark.parametrize("q_tokens", [2, 150])
+def test_long_distances(far, q_tokens):
+    _check(HALF, 1, q_tokens, 1600, 4, 2, 32, 64, 1, P.relative_edges(min(far, 20), far), seed=3)
+
+
+@pytest.mark.parametrize("q_heads,q_tokens", [(100, 1), (129, 3), (260, 2), (128, 40), (31, 2), (33, 1)])
+def test_large_groups_of_heads(q_heads, q_tokens):
+    """One key head for all: columns of one query, and of parts of queries, per workgroup; their heads' biases."""
+    _check(BF, 2, q_tokens, 300, q_heads, 1, 32, 64, 1, k_len=[300, 77], seed=4)
+
+
+@pytest.mark.parametrize("q_tokens", [1, 100])
+def test_long_axes_in_parts(q_tokens):
+    _check(BF, 2, q_tokens, 20000, 4, 2, 64, 64, 1, k_len=[20000, 513], seed=5)
+
+
+def test_no_edges_and_masks_through_the_table():
+    """A bias of minus infinity removes its pairs; the type's lowest value leaves a row's weights as they are where all of the row has it."""
+    _check(HALF, 2, 3, 70, 2, 2, 64, 16, 2, (), seed=6)
+    _check(HALF, 2, 50, 70, 2, 2, 64, 16, 1, (), seed=6)
+    for tokens in (3, 60):
+        q, cache, _, kw, _, _ = _check(BF, 1, tokens, 100, 2, 2, 64, 16, seed=7)
+        _, k, v, _ = _cache(7, 1, 100, 2, 64, 16)
+        for value in (float("-inf"), torch.finfo(BF).min):
+            table = torch.randn(len(E) + 1, 2, generator=torch.Generator().manual_seed(8)).to(BF).cuda()
+            table[:5, 0], table[:, 1] = value, value
+            o, lse = P.cache_attention(q, cache, table, E, want_lse=True, **kw)
+            want = block.attention(block.cpu(q), k, v, block.cpu(table), E, causal=True, scale=kw["scale"])
+            g = block.cpu(o)
+            assert np.isfinite(g).all() and (np.abs(g - want["o"])[:, :, 0] <= block.attention_bounds(want, BF)["o"][:, :, 0]).all()
+            if value == float("-inf"):
+                assert not o[:, :, 1].any() and torch.isinf(lse[:, 1]).all()
+            else:
+                for i in range(tokens):
+                    assert np.abs(g[0, i, 1] - v[0, :100 - tokens + i + 1, 1].mean(0)).max() <= 2.0 ** -7 * np.abs(v).max()
+
+
+def test_the_same_as_attention_over_the_values_themselves():
+    """rel_attention over what cache_restore gives, for a cache that cache_append filled: to the roundings of the two."""
+    gen = torch.Generator().manual_seed(9)
+    for q_tokens in (1, 30, 120):
+        k, v = _randn(gen, 2, 150, 2, 64, dtype=BF), _randn(gen, 2, 150, 2, 64, dtype=BF)
+        n, m = _ints([150, 131]), _ints([min(q_tokens, 131)] * 2)
+        cache = P.new_cache(8, 2, 64, 4, 64)
+        P.cache_append(cache, k, v, q_len=n, k_len=n)
+        q = _randn(gen, 2, q_tokens, 8, 64, dtype=BF)
+        table = _randn(gen, len(E) + 1, 8, dtype=BF)
+        a, la = P.cache_attention(q, cache, table, E, q_len=m, k_len=n, want_lse=True)
+        b, lb = P.rel_attention(q, *P.cache_restore(cache, 150, n, BF), table, E, q_len=m, k_len=n, causal=True, want_lse=True)
+        assert (a.float() - b.float()).abs().max() <= 2.0 ** -7 * 4 and (la - lb)[torch.isfinite(lb)].abs().max() <= 1e-4
+
+
+def test_nan_in_a_key_that_is_seen_reaches_the_queries_that_see_it():
+    q, cache, _, kw, _, _ = _check(BF, 1, 60, 100, 1, 1, 64, 16, seed=10)
+    page = int(cache.table[0, 70 // 16])
+    cache.k_codes[page, 0, 1, 70 % 16, 3] = 127
+    o = P.cache_attention(q, cache, **kw)
+    assert torch.isfinite(o[0, :30]).all() and torch.isnan(o[0, 30:]).all()
+
+
+def test_strides_and_orders():
+    q, cache, table, kw, want, _ = _check(BF, 2, 40, 70, 4, 2, 64, 32, 1, seed=11)
+    q = torch.nan_to_num(q)
+    want = P.cache_attention(q, cache, table, E, **kw)
+    heads_first = lambda t: t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)  # noqa: E731
+    wide = lambda t: torch.cat([t, t + 1], 3)[..., :t.shape[3]]  # noqa: E731
+    o = torch.empty(2, 4, 40, 64, dtype=BF, device="cuda").permute(0, 2, 1, 3)
+    assert P.cache_attention(heads_first(q), cache, table, E, o=o, **kw) is o and torch.equal(o, want)
+    assert torch.equal(P.cache_attention(wide(q), cache, table, E, **kw), want)
+    assert torch.equal(P.cache_attention(wide(q)[:, :3], cache, table, E, **kw), P.cache_attention(q[:, :3].contiguous(), cache, table, E, **kw))
+    with pytest.raises(P.PrunerError):
+        P.cache_attention(torch.cat([q, q], 3)[..., 4:68], cache, table, E, **kw)   # rows that begin between multiples of 16 bytes
+
+
+@pytest.mark.parametrize("q_tokens,k_tokens", [(1, 3000), (100, 333), (60, 9000)])
+def test_the_same_bits_every_time_on_another_stream_and_in_a_graph(q_tokens, k_tokens):
+    q, cache, table, kw, o, lse = _check(BF, 2, q_tokens, k_tokens, 6, 2, 64, 64, 1, seed=12)
+    for n in range(4):
+        stream = torch.cuda.Stream() if n % 2 else None
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        got = P.cache_attention(q, cache, table, E, want_lse=True, stream=stream, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], o) and torch.equal(got[1], lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = P.cache_attention(q, cache, table, E, want_lse=True, **kw)
+    for _ in range(3):
+        for t in got:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], o) and torch.equal(got[1], lse)
+
+
+def test_empty_calls():
+    q, cache, table, kw, _, _ = _check(BF, 2, 3, 70, 4, 2, 64, 32, 1, seed=13)
+    o, lse = P.cache_attention(q, cache, table, E, want_lse=True, k_len=_ints([0, 0]))
+    assert not o.any() and torch.isinf(lse).all()
+    assert P.cache_attention(q[:, :0], cache, table, E).shape[1] == 0
+    assert P.cache_attention(q[:0], cache._replace(table=cache.table[:0])).shape[0] == 0
+    assert not P.cache_attention(q, cache, table, E, k_tokens=0).any()
+
+
+def test_refusals_of_the_binding():
+    q, cache, table, kw, _, _ = _check(BF, 2, 3, 70, 4, 2, 64, 32, 1, seed=14)
+    for bad in (dict(table=table.float()), dict(table=table[:5]), dict(q=q[..., :48].contiguous()), dict(q=q[:1]), dict(q=q.cpu()), dict(q_len=torch.ones(2, dtype=torch.int64).cuda()),
+                dict(o=torch.zeros_like(q).half()), dict(cache=cache._replace(k_codes=cache.k_codes[:, :1]))):
+        with pytest.raises(AssertionError):
+            P.cache_attention(**{**dict(q=q, cache=cache, table=table, edges=E), **bad})
+    for bad in (dict(scale=0.0), dict(edges=E[::-1].copy()), dict(q=q[:, :, :1].expand(2, 3, 3, 64), table=None), dict(q=q.float(), table=None), dict(k_tokens=97)):
+        with pytest.raises(P.PrunerError):
+            P.cache_attention(**{**dict(q=q, cache=cache, table=table, edges=E), **bad})
