@@ -83,50 +83,62 @@ struct RowsLds {
     }
 };
 
-// The sums of a workgroup's four wavefronts, each of which has seen keys of its own for the same columns (query t of head hk * group + g is column
-// t * group + g), one after the other: the rows' results, or what this part leaves of them.  lds: (DP + 4) * 4 * columns floats and 1 KB.  mine: this lane's column has a query.
+// Where a workgroup's four wavefronts, each of which has seen keys of its own for the same columns (query t of head hk * group + g is column t * group + g), leave what they have: a column's
+// (maximum, sum), and its weighted sums in rows of DP + 4 floats, so that neighbouring rows lie in other banks.
+template <int DP> struct Meeting {
+    static constexpr int kStride = DP + 4;
+    float2* stats;   // [4][32]
+    float* sums;     // [4][columns][kStride]
+    __device__ __forceinline__ explicit Meeting(char* lds) : stats(reinterpret_cast<float2*>(lds)), sums(reinterpret_cast<float*>(lds + 4 * 32 * 8)) {}
+    static constexpr size_t bytes(int columns) { return 4 * 32 * 8 + (size_t)4 * columns * kStride * 4; }
+    // The rows' results, or what this part leaves of them.
+    template <typename T> __device__ __forceinline__ void join(const Args& a, const Heads& out, float* __restrict__ lse, const Parts& parts, int b, int hk, int part, int columns) const
+    {
+        for (int item = threadIdx.x; item < columns * (DP / 4); item += 256) {
+            const int c = item / (DP / 4), d = 4 * (item % (DP / 4));
+            float m = -ATT_INF;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = __builtin_fmaxf(m, stats[w * 32 + c].y != 0.f ? stats[w * 32 + c].x : -ATT_INF);
+            float total = 0.f;
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float2 st = stats[w * 32 + c];
+                if (st.y == 0.f) continue;
+                const float f = exp2_of((st.x - m) * kLog2e);
+                total = __builtin_fmaf(f, st.y, total);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(sums + (w * columns + c) * kStride + d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
+            }
+            const int tt = c / a.group, hh = hk * a.group + c % a.group;
+            const int64_t row = ((int64_t)b * a.q_heads + hh) * a.q_tokens + tt;
+            if (parts.count > 1) {
+                const int64_t slot = (int64_t)part * a.batch * a.q_heads * a.q_tokens + row;
+                *reinterpret_cast<f32x4*>(parts.sums + slot * DP + d) = o;
+                if (d == 0) parts.stats[slot] = make_float2(m, total);
+            } else {
+                const float f = total != 0.f ? 1.f / total : 0.f;
+                if (d < a.head_dim)
+                    *reinterpret_cast<u32x2*>(out.at<T>(b, hh) + (int64_t)tt * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
+                if (lse && d == 0) lse[row] = lse_of(m, total);
+            }
+        }
+    }
+};
+
+// What a wavefront of 32 columns leaves, and the joint result.  mine: this lane's column has a query.
 template <typename T, int DP>
 __device__ __forceinline__ void meet(const Running<T, DP>& run, char* lds, const Args& a, const Heads& out, float* __restrict__ lse, const Parts& parts, int b, int hk, int part, int columns, bool mine)
 {
-    constexpr int kStride = DP + 4;   // (rows of DP + 4 floats, so that neighbouring rows lie in other banks)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const Meeting<DP> at(lds);
     __syncthreads();
-    float2* const stats = reinterpret_cast<float2*>(lds);           // [4][32]
-    float* const sums = reinterpret_cast<float*>(lds + 4 * 32 * 8); // [4][columns][kStride]
     const float l = sum_of_halves(run.l);
-    if (half == 0) stats[wave * 32 + l32] = make_float2(run.m, mine ? l : 0.f);
-    if (l32 < columns) store_row32<DP>(sums + (wave * columns + l32) * kStride, run.o, half);
+    if (half == 0) at.stats[wave * 32 + l32] = make_float2(run.m, mine ? l : 0.f);
+    if (l32 < columns) store_row32<DP>(at.sums + (wave * columns + l32) * Meeting<DP>::kStride, run.o, half);
     __syncthreads();
-    for (int item = threadIdx.x; item < columns * (DP / 4); item += 256) {
-        const int c = item / (DP / 4), d = 4 * (item % (DP / 4));
-        float m = -ATT_INF;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = __builtin_fmaxf(m, stats[w * 32 + c].y != 0.f ? stats[w * 32 + c].x : -ATT_INF);
-        float total = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float2 st = stats[w * 32 + c];
-            if (st.y == 0.f) continue;
-            const float f = exp2_of((st.x - m) * kLog2e);
-            total = __builtin_fmaf(f, st.y, total);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(sums + (w * columns + c) * kStride + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e]);
-        }
-        const int tt = c / a.group, hh = hk * a.group + c % a.group;
-        const int64_t row = ((int64_t)b * a.q_heads + hh) * a.q_tokens + tt;
-        if (parts.count > 1) {
-            const int64_t slot = (int64_t)part * a.batch * a.q_heads * a.q_tokens + row;
-            *reinterpret_cast<f32x4*>(parts.sums + slot * DP + d) = o;
-            if (d == 0) parts.stats[slot] = make_float2(m, total);
-        } else {
-            const float f = total != 0.f ? 1.f / total : 0.f;
-            if (d < a.head_dim)
-                *reinterpret_cast<u32x2*>(out.at<T>(b, hh) + (int64_t)tt * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
-            if (lse && d == 0) lse[row] = lse_of(m, total);
-        }
-    }
+    at.template join<T>(a, out, lse, parts, b, hk, part, columns);
 }
 
 // Four neighbouring values of a row per thread.

@@ -15,91 +15,6 @@ namespace {
 
 constexpr int kTile = 64;   // keys of a step
 
-// 64 keys' codes on their way to a wavefront: two blocks of 32.  Rows past the sequence's end, or whose page is not there, hold anything; of values they are cleared
-// before use (their weight is 0, but anything may be a NaN).
-template <typename T, int DP> struct Codes {
-    static constexpr int kChunks = DP / 32;
-    u32x4 k[2][kChunks], v[2][kChunks];
-    float k_scale[2], v_scale[2];
-    int k_page[2], v_page[2], there[2];   // there: tokens of this lane's sixteen
-    __device__ __forceinline__ static int key_of(int lane) { return ((lane >> 2 & 1) << 4) | ((lane >> 3 & 3) << 2) | (lane & 3); }   // this lane's row of the keys' operand
-    __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int kl, int lane)
-    {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int at = key0 + 32 * n + key_of(lane), first = key0 + 32 * n + 16 * (lane >> 5);
-            k_page[n] = at < kl ? c.page_of(b, at) : -1;
-            v_page[n] = first < kl ? c.page_of(b, first) : -1;
-        }
-    }
-    __device__ __forceinline__ void load_keys(const cache::Cache& c, int h, int key0, int lane)
-    {
-        const int half = lane >> 5, units = c.head_dim / cache::kUnit;
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int64_t head = c.head_of(k_page[n] < 0 ? 0 : k_page[n], h);
-            const uint8_t* const p = c.k + head * c.page_bytes() + (((key0 + 32 * n + key_of(lane)) & (c.page_tokens() - 1)) << 4);
-            k_scale[n] = cache::two_to(c.k_exps[head]);
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-                const int unit = 2 * i + half < units ? 2 * i + half : units - 1;   // (past the last one: the query's columns are 0 there)
-                k[n][i] = *reinterpret_cast<const u32x4*>(p + ((int64_t)unit << (c.shift + 4)));
-            }
-        }
-    }
-    __device__ __forceinline__ void load_values(const cache::Cache& c, int h, int key0, int kl, int lane)
-    {
-        const int half = lane >> 5, l32 = lane & 31;
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int first = key0 + 32 * n + 16 * half, left = kl - first;
-            there[n] = v_page[n] < 0 ? 0 : left < 16 ? left : 16;
-            const int64_t head = c.head_of(v_page[n] < 0 ? 0 : v_page[n], h);
-            const uint8_t* const p = c.v + head * c.page_bytes() + ((int64_t)((first & (c.page_tokens() - 1)) >> 4) * c.head_dim << 4);
-            v_scale[n] = cache::two_to(c.v_exps[head]);
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) {
-                const int d = 32 * i + l32 < c.head_dim ? 32 * i + l32 : c.head_dim - 1;   // (columns past the last are not stored)
-                v[n][i] = *reinterpret_cast<const u32x4*>(p + (d << 4));
-            }
-        }
-    }
-    __device__ __forceinline__ void clear_values()   // those that are not there
-    {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int bytes = there[n] - 4 * w;
-                const uint32_t keep = bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) v[n][i][w] &= keep;
-            }
-    }
-    __device__ __forceinline__ void scores(floatx16 (&s)[2], const u32x4 (&q)[2 * kChunks]) const
-    {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) s[n] = zero16();
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) s[n] = mfma(cache::eight_from<T>(k[n][i][2 * u], k[n][i][2 * u + 1], k_scale[n]), q[2 * i + u], s[n], T{});
-    }
-    __device__ __forceinline__ void add(floatx16 (&o)[kChunks], const floatx16 (&s)[2]) const
-    {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32x4 w = weights_of<T>(s[n], u);
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) o[i] = mfma(cache::eight_from<T>(v[n][i][2 * u], v[n][i][2 * u + 1], v_scale[n]), w, o[i], T{});
-            }
-    }
-};
-
 constexpr int kBiasHeads = 128;   // heads whose biases a workgroup holds: its columns', at most
 
 // A wavefront's 32 columns (those past the last are the last once more, and not its own).
@@ -141,143 +56,433 @@ struct BiasLds {
     }
 };
 
-// One step: scores with bias and mask, weights, their sums of values; the next step's codes are asked for as soon as these are used.
-template <typename T, int DP>
-__device__ __forceinline__ void step(Running<T, DP>& run, Codes<T, DP>& codes, const u32x4 (&qf)[DP / 16], const Args& a, const cache::Cache& c, const Columns& at, const char* lds,
-                                     const BiasLds& places, const Window& window, float bias_left, float bias_right, int b, int hk, int ql, int kl, int key0, int next, int after, int end, int lane)
+// ---- few columns: products of 16 x 16 x 32
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c, __bf16)
 {
-    const int half = lane >> 5;
-    floatx16 s[2];
-    codes.scores(s, qf);
-    int there[2] = {codes.there[0], codes.there[1]};
-    const bool short_of = __any(there[0] < 16 || there[1] < 16);
-    if (short_of) codes.clear_values();
-    if (next < end) codes.load_keys(c, hk, next, lane);
-    const int r_lo = key0 - (kl - ql + at.q_last), r_hi = key0 + kTile - 1 - (kl - ql + at.q_first);
-    const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
-    const float bias = place == kRight ? bias_right : bias_left;
-    bool fused = true;
-    if (place == kNear) {
-        const uint8_t* const n = reinterpret_cast<const uint8_t*>(lds + places.biases) + (key0 - at.p - window.first + 16 * half);
-        const float* const of = reinterpret_cast<const float*>(lds) + at.bias;
-        fused = false;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, of[n[32 * x + i] * places.heads]);
-    } else if (__any(!(__builtin_fabsf(bias) < kLarge))) {   // (lanes have biases of different heads)
-        fused = false;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, bias);
-    }
-    if (short_of || key0 + kTile > at.all_see)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int seen = at.limit - (key0 + 32 * x + 16 * half), left = seen < there[x] ? seen : there[x];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[x][i] = i < left ? s[x][i] : -ATT_INF;
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c, _Float16)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Of a lane and the three of the same column in the other rows of sixteen.
+__device__ __forceinline__ float max_of_rows(float v)
+{
+    const TwoFloats t = across_rows(v);
+    return max_of_halves(__builtin_fmaxf(t.a, t.b));
+}
+__device__ __forceinline__ float sum_of_rows(float v)
+{
+    const TwoFloats t = across_rows(v);
+    return sum_of_halves(t.a + t.b);
+}
+
+// 64 keys' codes: keys in four operands of 16 rows, row 4 u + j of operand t being key 16 u + 4 t + j, so that lane (n = lane & 15, g = lane >> 4) of the results has column n's scores of the sixteen
+// keys 16 g + 4 t + j; of values it has the sixteen of those keys.  WHOLE: the 64 keys lie in one page, whose place all lanes share.
+template <typename T, int DP, bool WHOLE> struct Few {
+    static constexpr int kChunks = (DP + 63) / 64, kBlocks = DP / 16;
+    u32x4 k[4][kChunks], v[kBlocks];
+    float k_scale, v_scale;
+    int k_page, v_page, there;
+    __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most, int lane)   // most: the sequences' room (their lengths may still be on the way)
+    {
+        if constexpr (WHOLE) {
+            k_page = v_page = key0 < most ? c.page_of(b, key0) : -1;
+        } else {
+            const int k_at = key0 + 16 * (lane >> 2 & 3), v_at = key0 + 16 * (lane >> 4);
+            k_page = k_at < most ? c.page_of(b, k_at) : -1;
+            v_page = v_at < most ? c.page_of(b, v_at) : -1;
         }
-    run.weigh(s, fused, a.scale, bias);
-    codes.add(run.o, s);
-    if (next < end) {
-        codes.load_values(c, hk, next, kl, lane);
-        codes.find(c, b, after, after < end ? kl : 0, lane);
     }
-}
-
-template <typename T, int DP> __device__ __forceinline__ void load_query(u32x4 (&f)[DP / 16], const Args& a, int b, const Columns& at, int half)
-{
-    const T* const p = a.q.at<T>(b, at.h) + (int64_t)at.t * a.q.token;
+    __device__ __forceinline__ void load_keys(const cache::Cache& c, int h, int key0, int lane)
+    {
+        const int64_t head = c.head_of(k_page < 0 ? 0 : k_page, h);
+        const int g = lane >> 4, in = c.page_tokens() - 1, place = WHOLE ? key0 & in : (key0 + 16 * (lane >> 2 & 3)) & in, units = c.head_dim / cache::kUnit;
+        const uint8_t* const p = c.k + head * c.page_bytes() + 16 * place;
+        k_scale = cache::two_to(c.k_exps[head]);
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-        const int d = 32 * (i / 2) + 16 * half + 8 * (i % 2);
-        f[i] = u32x4{0u, 0u, 0u, 0u};
-        if (at.mine && d < a.head_dim) f[i] = *reinterpret_cast<const u32x4*>(p + d);
+        for (int i = 0; i < kChunks; ++i) {
+            const int unit = 4 * i + g < units ? 4 * i + g : units - 1;   // (past the last one: the query's columns are 0 there)
+            const uint32_t at = ((uint32_t)unit << (c.shift + 4)) + 16 * ((WHOLE ? 16 * (lane >> 2 & 3) : 0) + (lane & 3));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) k[t][i] = *reinterpret_cast<const u32x4*>(p + at + 64 * t);
+        }
     }
-}
+    __device__ __forceinline__ void load_values(const cache::Cache& c, int h, int key0, int kl, int lane)
+    {
+        const int64_t head = c.head_of(v_page < 0 ? 0 : v_page, h);
+        const int g = lane >> 4, in = c.page_tokens() - 1, place = WHOLE ? key0 & in : (key0 + 16 * g) & in, units = c.head_dim / cache::kUnit, left = kl - (key0 + 16 * g);
+        there = v_page < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+        const uint8_t* const p = c.v + head * c.page_bytes() + place * c.head_dim;
+        v_scale = cache::two_to(c.v_exps[head]);
+        const uint32_t at = 16 * ((WHOLE ? g * c.head_dim : 0) + (lane & 15));
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1));   // (columns past the last are not stored)
+    }
+    __device__ __forceinline__ void clear_values()   // those that are not there
+    {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int bytes = there - 4 * w;
+            const uint32_t keep = bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) v[i][w] &= keep;
+        }
+    }
+};
 
-template <typename T, int DP> __global__ void __launch_bounds__(256, 2) tokens_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts)
+template <typename T, int DP, int CT, bool WHOLE> __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2)) tokens_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts)
 {
+    using Step = Few<T, DP, WHOLE>;
+    constexpr int kChunks = Step::kChunks, kBlocks = Step::kBlocks, kStep = 4 * kTile;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int columns = a.q_tokens * a.group;
     const int hk = blockIdx.x % a.kv_heads, part = blockIdx.x / a.kv_heads % parts.count, b = blockIdx.x / a.kv_heads / parts.count;
-    const int ql = a.queries(b), kl = a.keys(b);
-    Columns at;
-    at.set(a, hk, 0, 0, columns, ql, kl, lane);
-    const Window window(a.left, a.right);
-    const BiasLds places(a);
-    int end = ql == 0 ? 0 : kl;   // (the last query sees all keys under the causal mask too)
     const int begin = part * parts.keys;
+    int key0 = begin + kTile * wave;
+    Step codes;
+    codes.find(c, b, key0, a.k_tokens, lane);
+    const int ql = a.queries(b), kl = a.keys(b);
+    int end = ql == 0 ? 0 : kl;   // (the last query sees all keys under the causal mask too)
     if (parts.count > 1) end = end < begin + parts.keys ? end : begin + parts.keys;
 
-    Running<T, DP> run;
-    run.clear();
+    // this lane's columns (those past the last are the last once more, and not its own)
+    int t[CT], p[CT], limit[CT], head[CT];
+    bool mine[CT];
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+        const int at = 16 * x + n < columns ? 16 * x + n : columns - 1;
+        t[x] = at / a.group;
+        head[x] = at % a.group;
+        mine[x] = 16 * x + n < columns && t[x] < ql;
+        p[x] = kl - ql + t[x];
+        limit[x] = a.causal ? (p[x] + 1 < kl ? p[x] + 1 : kl) : kl;
+    }
+    const int all_see = a.causal ? (kl - ql + 1 < kl ? kl - ql + 1 : kl) : kl;
+    float m[CT], l[CT];
+    f32x4 o[CT][kBlocks];
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+        m[x] = -ATT_INF;
+        l[x] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) o[x][i] = zero;
+    }
     if (begin < end) {
-        constexpr int kStep = 4 * kTile;
-        int key0 = begin + kTile * wave;
-        Codes<T, DP> codes;
-        codes.find(c, b, key0, key0 < end ? kl : 0, lane);
-        u32x4 qf[DP / 16];
-        load_query<T, DP>(qf, a, b, at, half);
         if (key0 < end) {
             codes.load_keys(c, hk, key0, lane);
             codes.load_values(c, hk, key0, kl, lane);
-            codes.find(c, b, key0 + kStep, key0 + kStep < end ? kl : 0, lane);
+            codes.find(c, b, key0 + kStep, a.k_tokens, lane);
         }
-        float bias_left = 0.f, bias_right = 0.f;
+        u32x4 qf[CT][2 * kChunks];
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            const T* const from = a.q.at<T>(b, hk * a.group + head[x]) + (int64_t)t[x] * a.q.token;
+#pragma unroll
+            for (int i = 0; i < 2 * kChunks; ++i) {
+                const int d = 64 * (i / 2) + 16 * g + 8 * (i % 2);
+                qf[x][i] = u32x4{0u, 0u, 0u, 0u};
+                if (mine[x] && d < a.head_dim) qf[x][i] = *reinterpret_cast<const u32x4*>(from + d);
+            }
+        }
+        const Window window(a.left, a.right);
+        const BiasLds places(a);
+        float bias_left[CT], bias_right[CT];
         if (a.table) {
-            bias_left = a.bias<T>(a.n_edges, at.h);
-            bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, at.h);
-            if (kl - ql - (end + kTile) < a.left) places.fill<T>(a, window, lds, hk, 0);   // (else all of this part's keys lie beyond the last edge)
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                bias_left[x] = a.bias<T>(a.n_edges, hk * a.group + head[x]);
+                bias_right[x] = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, hk * a.group + head[x]);
+            }
+            if (kl - ql - (end + kTile) < a.left) {   // (else all of this part's keys lie beyond the last edge)
+                places.fill<T>(a, window, lds, hk, 0);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        for (; key0 < end; key0 += kStep)
-            step<T, DP>(run, codes, qf, a, c, at, lds, places, window, bias_left, bias_right, b, hk, ql, kl, key0, key0 + kStep, key0 + 2 * kStep, end, lane);
+        for (; key0 < end; key0 += kStep) {
+            f32x4 s[CT][4];
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[x][i] = zero;
+#pragma unroll
+            for (int i = 0; i < 2 * kChunks; ++i)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const u32x4 row = cache::eight_from<T>(codes.k[u][i / 2][2 * (i % 2)], codes.k[u][i / 2][2 * (i % 2) + 1], codes.k_scale);
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) s[x][u] = mfma16(row, qf[x][i], s[x][u], T{});
+                }
+            const int there = codes.there, next = key0 + kStep;
+            const bool short_of = __any(there < 16);
+            if (short_of) codes.clear_values();
+            if (next < end) codes.load_keys(c, hk, next, lane);
+            const int r_lo = key0 - (kl - ql + a.q_tokens - 1), r_hi = key0 + kTile - 1 - (kl - ql);
+            const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
+            u32x4 w[CT][2];
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                float shift = 0.f;
+                bool fused = true;
+                if (a.table) {
+                    shift = place == kRight ? bias_right[x] : bias_left[x];
+                    if (place == kNear) {
+                        const uint8_t* const of = reinterpret_cast<const uint8_t*>(lds + places.biases) + (key0 - p[x] - window.first + 16 * g);
+                        const float* const bias = reinterpret_cast<const float*>(lds) + head[x];
+                        fused = false;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i / 4][i % 4] = __builtin_fmaf(s[x][i / 4][i % 4], a.scale, bias[of[i] * places.heads]);
+                    } else if (__any(!(__builtin_fabsf(shift) < kLarge))) {   // (lanes have biases of different heads)
+                        fused = false;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i / 4][i % 4] = __builtin_fmaf(s[x][i / 4][i % 4], a.scale, shift);
+                    }
+                }
+                if (short_of || key0 + kTile > all_see) {
+                    const int seen = limit[x] - (key0 + 16 * g), left = seen < there ? seen : there;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[x][i / 4][i % 4] = i < left ? s[x][i / 4][i % 4] : -ATT_INF;
+                }
+                float top = s[x][0][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = __builtin_fmaxf(top, s[x][i / 4][i % 4]);
+                top = max_of_rows(top);
+                if (fused) top = __builtin_fmaf(top, a.scale, shift);
+                if (__any(top > m[x] + kSlack)) {   // (from minus infinity: any score)
+                    const float now = __builtin_fmaxf(m[x], top), factor = now == -ATT_INF ? 1.f : exp2_of((m[x] - now) * kLog2e);
+                    m[x] = now;
+                    l[x] *= factor;
+#pragma unroll
+                    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[x][i][e] *= factor;
+                }
+                const float from = m[x] == -ATT_INF ? 0.f : m[x];   // (no key yet: every weight is exp(-infinity))
+                float sum = 0.f;
+                if (fused) {
+                    const float scale = a.scale * kLog2e, off = (shift - from) * kLog2e;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[x][i / 4][i % 4] = exp2_of(__builtin_fmaf(s[x][i / 4][i % 4], scale, off));
+                        sum += s[x][i / 4][i % 4];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[x][i / 4][i % 4] = exp2_of((s[x][i / 4][i % 4] - from) * kLog2e);
+                        sum += s[x][i / 4][i % 4];
+                    }
+                }
+                l[x] += sum;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    w[x][u] = u32x4{pair_of(s[x][2 * u][0], s[x][2 * u][1], T{}), pair_of(s[x][2 * u][2], s[x][2 * u][3], T{}), pair_of(s[x][2 * u + 1][0], s[x][2 * u + 1][1], T{}),
+                                    pair_of(s[x][2 * u + 1][2], s[x][2 * u + 1][3], T{})};
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) {
+                    const u32x4 row = cache::eight_from<T>(codes.v[i][2 * u], codes.v[i][2 * u + 1], codes.v_scale);
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) o[x][i] = mfma16(row, w[x][u], o[x][i], T{});
+                }
+            if (next < end) {
+                codes.load_values(c, hk, next, kl, lane);
+                codes.find(c, b, next + kStep, a.k_tokens, lane);
+            }
+        }
     }
-    meet<T, DP>(run, lds, a, out, lse, parts, b, hk, part, columns, at.mine);
+    const Meeting<DP> at(lds);
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+        const float sum = sum_of_rows(l[x]);
+        if (g == 0) at.stats[wave * 32 + 16 * x + n] = make_float2(m[x], mine[x] ? sum : 0.f);
+        if (16 * x + n < columns)
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) *reinterpret_cast<f32x4*>(at.sums + (wave * columns + 16 * x + n) * Meeting<DP>::kStride + 16 * i + 4 * g) = o[x][i];
+    }
+    __syncthreads();
+    at.template join<T>(a, out, lse, parts, b, hk, part, columns);
 }
+
+// ---- many columns: products of 32 x 32 x 16
+
+// 64 keys' codes on their way to a tile that four wavefronts share: a thread takes sixteen columns of a key, or tokens of a column, at a time, and parks them as operands' type: keys in rows of DP
+// columns, row 8 q + 4 h + j of a block of 32 being key 16 h + 4 q + j, so that a lane's sixteen scores are of sixteen neighbouring keys; values in rows of 64 tokens.  Rows past the sequence's end, or
+// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).
+template <typename T, int DP> struct Shared {
+    static constexpr int kEach = kTile * DP / 16 / 256, kKeyBytes = kTile * Tile<DP>::kRowBytes, kValueBytes = DP * Tile<kTile>::kRowBytes, kBytes = kKeyBytes + kValueBytes;
+    static_assert(kTile == 64 && kEach >= 0, "a wavefront's lanes are the keys of a tile");
+    static constexpr int kLoads = kEach > 0 ? kEach : 1;   // (32 columns: half of the threads have a chunk)
+    u32x4 k[kLoads], v[kLoads];
+    float k_scale, v_scale[kLoads];
+    int k_page, v_page[kLoads], there[kLoads];
+    __device__ __forceinline__ static int key_unit(int i) { return ((int)threadIdx.x >> 6) + 4 * i; }           // of DP / 16
+    __device__ __forceinline__ static int value_unit(int i) { return ((int)threadIdx.x + 256 * i) / DP; }       // of 4
+    __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most)   // most: the sequences' room
+    {
+        const int at = key0 + ((int)threadIdx.x & 63);
+        k_page = at < most ? c.page_of(b, at) : -1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int first = key0 + 16 * value_unit(i);
+            v_page[i] = value_unit(i) < 4 && first < most ? c.page_of(b, first) : -1;
+        }
+    }
+    __device__ __forceinline__ void load(const cache::Cache& c, int h, int key0, int kl)
+    {
+        const int in = c.page_tokens() - 1, units = c.head_dim / cache::kUnit;
+        const int64_t head = c.head_of(k_page < 0 ? 0 : k_page, h);
+        const uint8_t* const p = c.k + head * c.page_bytes() + (((key0 + ((int)threadIdx.x & 63)) & in) << 4);
+        k_scale = cache::two_to(c.k_exps[head]);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int unit = key_unit(i), first = key0 + 16 * value_unit(i), d = ((int)threadIdx.x + 256 * i) % DP, left = kl - first;
+            k[i] = u32x4{0u, 0u, 0u, 0u};   // (columns past the last: a query's are 0 there)
+            if (unit < units) k[i] = *reinterpret_cast<const u32x4*>(p + ((uint32_t)unit << (c.shift + 4)));
+            there[i] = v_page[i] < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+            const int64_t of = c.head_of(v_page[i] < 0 ? 0 : v_page[i], h);
+            v_scale[i] = cache::two_to(c.v_exps[of]);
+            v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + 16 * (d < c.head_dim ? d : c.head_dim - 1));   // (columns past the last are not stored)
+        }
+    }
+    __device__ __forceinline__ void park(char* tile, int* there_of)
+    {
+        const int key = (int)threadIdx.x & 63, row = (key & 32) | (key & 12) << 1 | (key >> 4 & 1) << 2 | (key & 3);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (kEach > 0 || key_unit(i) < DP / 16) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<u32x4*>(tile + Tile<DP>::at(row, 2 * key_unit(i) + u)) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
+            }
+            if (kEach > 0 || value_unit(i) < 4) {
+                if (there[i] < 16)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int bytes = there[i] - 4 * w;
+                        v[i][w] &= bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
+                    }
+                const int d = ((int)threadIdx.x + 256 * i) % DP;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<u32x4*>(tile + kKeyBytes + Tile<kTile>::at(d, 2 * value_unit(i) + u)) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale[i]);
+                if (d == 0) there_of[value_unit(i)] = there[i];
+            }
+        }
+    }
+};
 
 template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
 {
+    using Turn = Shared<T, DP>;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    int(*const there_of)[4] = reinterpret_cast<int(*)[4]>(lds + 2 * Turn::kBytes);   // by turn, of sixteen tokens
+    char* const bias_lds = lds + 2 * Turn::kBytes + 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     const int columns = a.q_tokens * a.group;
     const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, 1, (uint32_t)tiles * parts.count);
-    const int b = it.head / a.kv_heads, hk = it.head % a.kv_heads, part = it.tile % parts.count, first = it.tile / parts.count * 128 + 32 * wave;
+    const int b = it.head / a.kv_heads, hk = it.head % a.kv_heads, part = it.tile % parts.count, from = it.tile / parts.count * 128, first = from + 32 * wave;
+    const int begin = part * parts.keys;
+    Turn codes;
+    codes.find(c, b, begin, a.k_tokens);
     const int ql = a.queries(b), kl = a.keys(b);
     Columns at;
-    at.set(a, hk, first - 32 * wave, first < columns ? first : columns - 1, columns, ql, kl, lane);
+    at.set(a, hk, from, first < columns ? first : columns - 1, columns, ql, kl, lane);
     if (first >= columns) at.mine = false;
     const Window window(a.left, a.right);
     const BiasLds places(a);
-    // the keys that this wavefront's queries see, and of them this part's
-    int end = first >= columns || at.q_first >= ql ? 0 : a.causal ? kl - ql + at.q_last + 1 : kl;
-    end = end < kl ? end : kl;
-    const int begin = part * parts.keys;
+    // the keys that this wavefront's and this workgroup's queries see, and of them this part's
+    auto seen_by = [&](int last_column) {
+        int q = last_column / a.group;
+        q = q < ql ? q : ql - 1;
+        const int n = a.causal ? kl - ql + q + 1 : kl;
+        return n < kl ? n : kl;
+    };
+    const int last = from + 127 < columns ? from + 127 : columns - 1;
+    int end = from / a.group >= ql ? 0 : seen_by(last), seen = first >= columns || at.q_first >= ql ? 0 : seen_by(first + 31 < columns ? first + 31 : columns - 1);
     if (parts.count > 1) end = end < begin + parts.keys ? end : begin + parts.keys;
 
     float bias_left = 0.f, bias_right = 0.f;
     if (a.table) {
         bias_left = a.bias<T>(a.n_edges, at.h);
         bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, at.h);
-        places.fill<T>(a, window, lds, hk, first - 32 * wave);
-        __syncthreads();
     }
     Running<T, DP> run;
     run.clear();
     if (begin < end) {
-        Codes<T, DP> codes;
-        codes.find(c, b, begin, kl, lane);
-        u32x4 qf[DP / 16];
-        load_query<T, DP>(qf, a, b, at, half);
-        codes.load_keys(c, hk, begin, lane);
-        codes.load_values(c, hk, begin, kl, lane);
-        codes.find(c, b, begin + kTile, begin + kTile < end ? kl : 0, lane);
-        for (int key0 = begin; key0 < end; key0 += kTile)
-            step<T, DP>(run, codes, qf, a, c, at, lds, places, window, bias_left, bias_right, b, hk, ql, kl, key0, key0 + kTile, key0 + 2 * kTile, end, lane);
+        codes.load(c, hk, begin, kl);
+        codes.find(c, b, begin + kTile, a.k_tokens);
+        u32x4 qf[kSteps];
+        load_row<T, DP>(qf, a.q.at<T>(b, at.h) + (int64_t)at.t * a.q.token, at.mine, a.head_dim, half);
+        if (a.table) places.fill<T>(a, window, bias_lds, hk, from);
+        const int l32 = lane & 31, row_at = Tile<DP>::at(l32, half), value_at = Tile<kTile>::at(l32, 2 * half);
+        int turn = 0;
+        for (int key0 = begin; key0 < end; key0 += kTile) {
+            char* const tile = lds + turn * Turn::kBytes;
+            codes.park(tile, there_of[turn]);
+            if (key0 + kTile < end) {
+                codes.load(c, hk, key0 + kTile, kl);
+                codes.find(c, b, key0 + 2 * kTile, a.k_tokens);
+            }
+            __syncthreads();   // (what is parked is there, and the tile before is done with)
+            if (key0 < seen) {
+                floatx16 s[2] = {zero16(), zero16()};
+                auto key = [&](int x) { return *reinterpret_cast<const u32x4*>(tile + (row_at ^ ((x / 2) << 5)) + (x % 2) * 32 * Tile<DP>::kRowBytes); };
+                Operands<2 * kSteps, 4> keys;
+                keys.start(key);
+                keys.products(key, [&](int x, u32x4 w) { s[x % 2] = mfma(w, qf[x / 2], s[x % 2], T{}); });
+                // (product x: depth step x / kBlocks of 16 keys in the scores' order, block x % kBlocks of 32 columns)
+                auto value = [&](int x) {
+                    const int step = x / kBlocks, d = x % kBlocks;
+                    return *reinterpret_cast<const u32x4*>(tile + Turn::kKeyBytes + (value_at ^ ((4 * (step / 2) + step % 2) << 4)) + d * 32 * Tile<kTile>::kRowBytes);
+                };
+                Operands<4 * kBlocks, 4> values;
+                values.start(value);
+                const int there[2] = {there_of[turn][half], there_of[turn][2 + half]};
+                const bool short_of = __any(there[0] < 16 || there[1] < 16);
+                const int r_lo = key0 - (kl - ql + at.q_last), r_hi = key0 + kTile - 1 - (kl - ql + at.q_first);
+                const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
+                const float bias = place == kRight ? bias_right : bias_left;
+                bool fused = true;
+                if (place == kNear) {
+                    const uint8_t* const n = reinterpret_cast<const uint8_t*>(bias_lds + places.biases) + (key0 - at.p - window.first + 16 * half);
+                    const float* const of = reinterpret_cast<const float*>(bias_lds) + at.bias;
+                    fused = false;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, of[n[32 * x + i] * places.heads]);
+                } else if (__any(!(__builtin_fabsf(bias) < kLarge))) {   // (lanes have biases of different heads)
+                    fused = false;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, bias);
+                }
+                if (short_of || key0 + kTile > at.all_see)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int to = at.limit - (key0 + 32 * x + 16 * half), left = to < there[x] ? to : there[x];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i] = i < left ? s[x][i] : -ATT_INF;
+                    }
+                run.weigh(s, fused, a.scale, bias);
+                u32x4 weights{};
+                values.products(value, [&](int x, u32x4 w) {
+                    const int step = x / kBlocks, d = x % kBlocks;
+                    if (d == 0) weights = weights_of<T>(s[step / 2], step % 2);
+                    run.o[d] = mfma(w, weights, run.o[d], T{});
+                });
+            }
+            turn ^= 1;
+        }
     }
     if (first + (lane & 31) >= columns) return;
     const float l = sum_of_halves(run.l);
@@ -333,30 +538,37 @@ Plan plan_of(const pruner_attention* a)
     return p;
 }
 
+template <typename T, int DP, int CT, bool WHOLE> int run_tokens(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
+{
+    const size_t biases = (size_t)BiasLds(args).bytes(), last = Meeting<DP>::bytes(args.q_tokens * args.group);
+    hipLaunchKernelGGL((tokens_kernel<T, DP, CT, WHOLE>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > biases ? last : biases, st, args, c, out, lse, parts);
+    PRUNER_LAUNCH_CHECK();
+    return PRUNER_OK;
+}
 template <typename T, int DP> int run(const Args& args, const cache::Cache& c, const Plan& plan, const Heads& out, float* lse, void* workspace, hipStream_t st)
 {
-    static PerDeviceFlag ready;
-    int dev = current_device(nullptr);
-    if (dev < 0) return PRUNER_EHIP;
-    if (!ready.get(dev)) {
-        for (const void* fn : {reinterpret_cast<const void*>(&tokens_kernel<T, DP>), reinterpret_cast<const void*>(&chunk_kernel<T, DP>)})
-            if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
-        ready.mark(dev);
-    }
     Parts parts{nullptr, nullptr, plan.parts, plan.part_keys};
     if (plan.parts > 1) {
         parts.stats = static_cast<float2*>(workspace);
         parts.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up((size_t)plan.parts * plan.rows * 8, 256));
     }
-    const size_t biases = (size_t)BiasLds(args).bytes();
-    const int64_t key_heads = (int64_t)args.batch * args.kv_heads;
     if (plan.tokens) {
-        const size_t columns = (size_t)args.q_tokens * args.group, last = 4 * 32 * 8 + 4 * columns * (DP + 4) * 4;
-        hipLaunchKernelGGL((tokens_kernel<T, DP>), dim3((unsigned)(key_heads * plan.parts)), dim3(256), last > biases ? last : biases, st, args, c, out, lse, parts);
+        const bool narrow = args.q_tokens * args.group <= 16, whole = c.page_tokens() >= kTile;
+        const int rc = narrow ? (whole ? run_tokens<T, DP, 1, true>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 1, false>(args, c, plan, parts, out, lse, st))
+                              : (whole ? run_tokens<T, DP, 2, true>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 2, false>(args, c, plan, parts, out, lse, st));
+        if (rc) return rc;
     } else {
-        hipLaunchKernelGGL((chunk_kernel<T, DP>), dim3((unsigned)(key_heads * plan.tiles * plan.parts)), dim3(256), biases, st, args, c, out, lse, parts, plan.tiles);
+        static PerDeviceFlag ready;
+        const int dev = current_device(nullptr);
+        if (dev < 0) return PRUNER_EHIP;
+        if (!ready.get(dev)) {
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+            ready.mark(dev);
+        }
+        const size_t lds = 2 * (size_t)Shared<T, DP>::kBytes + 32 + BiasLds(args).bytes();
+        hipLaunchKernelGGL((chunk_kernel<T, DP>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.tiles * plan.parts)), dim3(256), lds, st, args, c, out, lse, parts, plan.tiles);
+        PRUNER_LAUNCH_CHECK();
     }
-    PRUNER_LAUNCH_CHECK();
     if (plan.parts > 1) {
         hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)((plan.rows * (DP / 4) + 255) / 256)), dim3(256), 0, st, args, out, lse, parts);
         PRUNER_LAUNCH_CHECK();
