@@ -28,7 +28,8 @@ struct Cache {
     __device__ __forceinline__ int page_of(int b, int at) const
     {
         const int64_t i = (int64_t)b * seq_pages + (at >> shift);
-        const int p = table ? table[i] : (int)i;
+        typedef const __attribute__((address_space(4))) int32_t* read_only;   // (read by the scalar unit where all lanes ask for the same)
+        const int p = table ? *((read_only)(uintptr_t)table + i) : (int)i;
         return (uint32_t)p < (uint32_t)pages ? p : -1;
     }
     __device__ __forceinline__ int64_t head_of(int page, int h) const { return (int64_t)page * kv_heads + h; }

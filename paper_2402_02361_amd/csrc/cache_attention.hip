@@ -314,73 +314,101 @@ template <typename T, int DP, int CT, bool WHOLE> __global__ void __launch_bound
 
 // 64 keys' codes on their way to a tile that four wavefronts share: a thread takes sixteen columns of a key, or tokens of a column, at a time, and parks them as operands' type: keys in rows of DP
 // columns, row 8 q + 4 h + j of a block of 32 being key 16 h + 4 q + j, so that a lane's sixteen scores are of sixteen neighbouring keys; values in rows of 64 tokens.  Rows past the sequence's end, or
-// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).
-template <typename T, int DP> struct Shared {
+// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).  WHOLE: the 64 keys lie in one page, whose place is the same for all.
+template <typename T, int DP, bool WHOLE> struct Shared {
     static constexpr int kEach = kTile * DP / 16 / 256, kKeyBytes = kTile * Tile<DP>::kRowBytes, kValueBytes = DP * Tile<kTile>::kRowBytes, kBytes = kKeyBytes + kValueBytes;
-    static_assert(kTile == 64 && kEach >= 0, "a wavefront's lanes are the keys of a tile");
+    static_assert(kTile == 64 && DP <= 128, "a wavefront's lanes are the keys of a tile; a thread's second chunk is four units of keys, two of values further");
     static constexpr int kLoads = kEach > 0 ? kEach : 1;   // (32 columns: half of the threads have a chunk)
     u32x4 k[kLoads], v[kLoads];
     float k_scale, v_scale[kLoads];
-    int k_page, v_page[kLoads], there[kLoads];
-    __device__ __forceinline__ static int key_unit(int i) { return ((int)threadIdx.x >> 6) + 4 * i; }           // of DP / 16
-    __device__ __forceinline__ static int value_unit(int i) { return ((int)threadIdx.x + 256 * i) / DP; }       // of 4
+    int k_page, v_page[kLoads];
+    int there[kLoads];               // tokens of a chunk of values (WHOLE: of the 64)
+    int unit, group, d, k_at, v_at;  // this thread's first chunks: unit of columns of a key, of tokens of column d; where they are parked
+    uint32_t k_from, v_from;         // WHOLE: where they lie behind the step's first key, or token
+    __device__ __forceinline__ void set(const cache::Cache& c)
+    {
+        const int key = (int)threadIdx.x & 63, row = (key & 32) | (key & 12) << 1 | (key >> 4 & 1) << 2 | (key & 3);
+        unit = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        group = (int)threadIdx.x / DP;
+        d = (int)threadIdx.x % DP;
+        k_at = Tile<DP>::at(row, 2 * unit & (Tile<DP>::kChunks - 1));
+        v_at = kKeyBytes + Tile<kTile>::at(d, 2 * group & 7);
+        k_from = ((uint32_t)unit << (c.shift + 4)) + 16u * (uint32_t)key;
+        v_from = 16u * (uint32_t)(group * c.head_dim + (d < c.head_dim ? d : c.head_dim - 1));   // (columns past the last are not stored)
+    }
+    __device__ __forceinline__ bool has_keys(int i) const { return kEach > 0 || unit + 4 * i < DP / 16; }
+    __device__ __forceinline__ bool has_values() const { return kEach > 0 || group < 4; }
     __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most)   // most: the sequences' room
     {
-        const int at = key0 + ((int)threadIdx.x & 63);
-        k_page = at < most ? c.page_of(b, at) : -1;
+        if constexpr (WHOLE) {
+            k_page = key0 < most ? c.page_of(b, key0) : -1;
+        } else {
+            const int at = key0 + ((int)threadIdx.x & 63);
+            k_page = at < most ? c.page_of(b, at) : -1;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int first = key0 + 16 * value_unit(i);
-            v_page[i] = value_unit(i) < 4 && first < most ? c.page_of(b, first) : -1;
+            for (int i = 0; i < kLoads; ++i) {
+                const int first = key0 + 16 * (group + 2 * i);
+                v_page[i] = has_values() && first < most ? c.page_of(b, first) : -1;
+            }
         }
     }
     __device__ __forceinline__ void load(const cache::Cache& c, int h, int key0, int kl)
     {
         const int in = c.page_tokens() - 1, units = c.head_dim / cache::kUnit;
         const int64_t head = c.head_of(k_page < 0 ? 0 : k_page, h);
-        const uint8_t* const p = c.k + head * c.page_bytes() + (((key0 + ((int)threadIdx.x & 63)) & in) << 4);
+        const uint8_t* const p = c.k + head * c.page_bytes() + (WHOLE ? 16 * (key0 & in) : 16 * ((key0 + ((int)threadIdx.x & 63)) & in));
         k_scale = cache::two_to(c.k_exps[head]);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int unit = key_unit(i), first = key0 + 16 * value_unit(i), d = ((int)threadIdx.x + 256 * i) % DP, left = kl - first;
             k[i] = u32x4{0u, 0u, 0u, 0u};   // (columns past the last: a query's are 0 there)
-            if (unit < units) k[i] = *reinterpret_cast<const u32x4*>(p + ((uint32_t)unit << (c.shift + 4)));
-            there[i] = v_page[i] < 0 || left < 0 ? 0 : left < 16 ? left : 16;
-            const int64_t of = c.head_of(v_page[i] < 0 ? 0 : v_page[i], h);
-            v_scale[i] = cache::two_to(c.v_exps[of]);
-            v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + 16 * (d < c.head_dim ? d : c.head_dim - 1));   // (columns past the last are not stored)
+            if (unit + 4 * i < units) k[i] = *reinterpret_cast<const u32x4*>(p + (WHOLE ? k_from : (uint32_t)unit << (c.shift + 4)) + ((4u * i) << (c.shift + 4)));
+        }
+        if constexpr (WHOLE) {
+            const uint8_t* const q = c.v + head * c.page_bytes() + (key0 & in) * c.head_dim;
+            there[0] = k_page < 0 ? 0 : kl - key0;
+            v_scale[0] = cache::two_to(c.v_exps[head]);
+            if (has_values())
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4*>(q + v_from + 32u * i * (uint32_t)c.head_dim);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int first = key0 + 16 * (group + 2 * i);
+                there[i] = v_page[i] < 0 ? 0 : kl - first;
+                const int64_t of = c.head_of(v_page[i] < 0 ? 0 : v_page[i], h);
+                v_scale[i] = cache::two_to(c.v_exps[of]);
+                v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + (v_from - 16u * (uint32_t)(group * c.head_dim)));
+            }
         }
     }
     __device__ __forceinline__ void park(char* tile, int* there_of)
     {
-        const int key = (int)threadIdx.x & 63, row = (key & 32) | (key & 12) << 1 | (key >> 4 & 1) << 2 | (key & 3);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            if (kEach > 0 || key_unit(i) < DP / 16) {
+            if (has_keys(i))
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    *reinterpret_cast<u32x4*>(tile + Tile<DP>::at(row, 2 * key_unit(i) + u)) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
-            }
-            if (kEach > 0 || value_unit(i) < 4) {
-                if (there[i] < 16)
+                for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4*>(tile + (k_at ^ (128 * i + 16 * u))) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
+            if (has_values()) {
+                if (WHOLE ? there[0] < kTile : there[i] < 16) {
+                    const int left = WHOLE ? there[0] - 16 * (group + 2 * i) : there[i];
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const int bytes = there[i] - 4 * w;
+                        const int bytes = left - 4 * w;
                         v[i][w] &= bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
                     }
-                const int d = ((int)threadIdx.x + 256 * i) % DP;
+                }
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
-                    *reinterpret_cast<u32x4*>(tile + kKeyBytes + Tile<kTile>::at(d, 2 * value_unit(i) + u)) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale[i]);
-                if (d == 0) there_of[value_unit(i)] = there[i];
+                    *reinterpret_cast<u32x4*>(tile + (v_at ^ (64 * i + 16 * u))) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale[WHOLE ? 0 : i]);
+                if (!WHOLE && d == 0) there_of[group + 2 * i] = there[i];
             }
         }
     }
 };
 
-template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
+template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256, 2) chunk_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
 {
-    using Turn = Shared<T, DP>;
+    using Turn = Shared<T, DP, WHOLE>;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int(*const there_of)[4] = reinterpret_cast<int(*)[4]>(lds + 2 * Turn::kBytes);   // by turn, of sixteen tokens
@@ -391,6 +419,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_ke
     const int b = it.head / a.kv_heads, hk = it.head % a.kv_heads, part = it.tile % parts.count, from = it.tile / parts.count * 128, first = from + 32 * wave;
     const int begin = part * parts.keys;
     Turn codes;
+    codes.set(c);
     codes.find(c, b, begin, a.k_tokens);
     const int ql = a.queries(b), kl = a.keys(b);
     Columns at;
@@ -424,18 +453,32 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_ke
         if (a.table) places.fill<T>(a, window, bias_lds, hk, from);
         const int l32 = lane & 31, row_at = Tile<DP>::at(l32, half), value_at = Tile<kTile>::at(l32, 2 * half);
         int turn = 0;
+        codes.park(lds, there_of[0]);
+        int there_now = codes.there[0];
+        if (begin + kTile < end) {
+            codes.load(c, hk, begin + kTile, kl);
+            codes.find(c, b, begin + 2 * kTile, a.k_tokens);
+        }
         for (int key0 = begin; key0 < end; key0 += kTile) {
+            __syncthreads();   // (what was parked is there, and the tile before is done with)
             char* const tile = lds + turn * Turn::kBytes;
-            codes.park(tile, there_of[turn]);
-            if (key0 + kTile < end) {
-                codes.load(c, hk, key0 + kTile, kl);
-                codes.find(c, b, key0 + 2 * kTile, a.k_tokens);
-            }
-            __syncthreads();   // (what is parked is there, and the tile before is done with)
+            const int there_here = there_now;
+            auto next = [&] {
+                if (key0 + kTile < end) {
+                    codes.park(lds + (turn ^ 1) * Turn::kBytes, there_of[turn ^ 1]);
+                    there_now = codes.there[0];
+                    if (key0 + 2 * kTile < end) {
+                        codes.load(c, hk, key0 + 2 * kTile, kl);
+                        codes.find(c, b, key0 + 3 * kTile, a.k_tokens);
+                    }
+                }
+            };
+            if (key0 >= seen) next();
             if (key0 < seen) {
                 floatx16 s[2] = {zero16(), zero16()};
                 auto key = [&](int x) { return *reinterpret_cast<const u32x4*>(tile + (row_at ^ ((x / 2) << 5)) + (x % 2) * 32 * Tile<DP>::kRowBytes); };
                 Operands<2 * kSteps, 4> keys;
+                __builtin_amdgcn_s_setprio(0);
                 keys.start(key);
                 keys.products(key, [&](int x, u32x4 w) { s[x % 2] = mfma(w, qf[x / 2], s[x % 2], T{}); });
                 // (product x: depth step x / kBlocks of 16 keys in the scores' order, block x % kBlocks of 32 columns)
@@ -444,9 +487,11 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_ke
                     return *reinterpret_cast<const u32x4*>(tile + Turn::kKeyBytes + (value_at ^ ((4 * (step / 2) + step % 2) << 4)) + d * 32 * Tile<kTile>::kRowBytes);
                 };
                 Operands<4 * kBlocks, 4> values;
+                __builtin_amdgcn_s_setprio(1);
+                next();
                 values.start(value);
-                const int there[2] = {there_of[turn][half], there_of[turn][2 + half]};
-                const bool short_of = __any(there[0] < 16 || there[1] < 16);
+                const int there[2] = {WHOLE ? there_here - 16 * half : there_of[turn][half], WHOLE ? there_here - 32 - 16 * half : there_of[turn][2 + half]};
+                const bool short_of = WHOLE ? there_here < kTile : __any(there[0] < 16 || there[1] < 16);
                 const int r_lo = key0 - (kl - ql + at.q_last), r_hi = key0 + kTile - 1 - (kl - ql + at.q_first);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
@@ -474,6 +519,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_ke
                         for (int i = 0; i < 16; ++i) s[x][i] = i < left ? s[x][i] : -ATT_INF;
                     }
                 run.weigh(s, fused, a.scale, bias);
+                __builtin_amdgcn_s_setprio(0);
                 u32x4 weights{};
                 values.products(value, [&](int x, u32x4 w) {
                     const int step = x / kBlocks, d = x % kBlocks;
@@ -545,6 +591,20 @@ template <typename T, int DP, int CT, bool WHOLE> int run_tokens(const Args& arg
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
+template <typename T, int DP, bool WHOLE> int run_chunk(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
+{
+    static PerDeviceFlag ready;
+    const int dev = current_device(nullptr);
+    if (dev < 0) return PRUNER_EHIP;
+    if (!ready.get(dev)) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_kernel<T, DP, WHOLE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+        ready.mark(dev);
+    }
+    const size_t lds = 2 * (size_t)Shared<T, DP, WHOLE>::kBytes + 32 + BiasLds(args).bytes();
+    hipLaunchKernelGGL((chunk_kernel<T, DP, WHOLE>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.tiles * plan.parts)), dim3(256), lds, st, args, c, out, lse, parts, plan.tiles);
+    PRUNER_LAUNCH_CHECK();
+    return PRUNER_OK;
+}
 template <typename T, int DP> int run(const Args& args, const cache::Cache& c, const Plan& plan, const Heads& out, float* lse, void* workspace, hipStream_t st)
 {
     Parts parts{nullptr, nullptr, plan.parts, plan.part_keys};
@@ -558,16 +618,8 @@ template <typename T, int DP> int run(const Args& args, const cache::Cache& c, c
                               : (whole ? run_tokens<T, DP, 2, true>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 2, false>(args, c, plan, parts, out, lse, st));
         if (rc) return rc;
     } else {
-        static PerDeviceFlag ready;
-        const int dev = current_device(nullptr);
-        if (dev < 0) return PRUNER_EHIP;
-        if (!ready.get(dev)) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
-            ready.mark(dev);
-        }
-        const size_t lds = 2 * (size_t)Shared<T, DP>::kBytes + 32 + BiasLds(args).bytes();
-        hipLaunchKernelGGL((chunk_kernel<T, DP>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.tiles * plan.parts)), dim3(256), lds, st, args, c, out, lse, parts, plan.tiles);
-        PRUNER_LAUNCH_CHECK();
+        const int rc = c.page_tokens() >= kTile ? run_chunk<T, DP, true>(args, c, plan, parts, out, lse, st) : run_chunk<T, DP, false>(args, c, plan, parts, out, lse, st);
+        if (rc) return rc;
     }
     if (plan.parts > 1) {
         hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)((plan.rows * (DP / 4) + 255) / 256)), dim3(256), 0, st, args, out, lse, parts);
