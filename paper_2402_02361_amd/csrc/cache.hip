@@ -15,11 +15,19 @@ struct Rows {
     char* p;
     int64_t batch, token, head;   // elements
 };
+// i / n for i < 4096 and n = 16 k <= 128, or i < 4096 and n <= 8: by a multiplication with the quotient of 2^19, which is off by less than i / 2^19.
+struct Over {
+    uint32_t by, n;
+    __host__ __device__ explicit Over(int n) : by((1u << 19) / (uint32_t)n + 1u), n((uint32_t)n) {}
+    __device__ __forceinline__ int quotient(int i) const { return (int)((uint32_t)i * by >> 19); }
+};
+
 struct Call {
     Cache c;
     Rows k, v;
     const int32_t *q_len, *k_len;
     int32_t batch, tokens, slots;   // slots: pages of a sequence that a call can touch
+    Over units, columns;            // of a head
 };
 
 typedef u32x4 Loose __attribute__((aligned(2)));
@@ -29,29 +37,28 @@ __device__ __forceinline__ f32x2 pair_to(uint32_t w, _Float16) { return __builti
 __device__ __forceinline__ uint32_t pair_of(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2)); }
 __device__ __forceinline__ uint32_t pair_of(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2)); }
 
-// Sixteen neighbouring values of a row, anywhere in memory.
-template <typename T> __device__ __forceinline__ void load16(float (&x)[16], const T* p)
-{
-    if constexpr (sizeof(T) == 4) {
+// Sixteen neighbouring values of a row, anywhere in memory, as they lie there.
+template <typename T> struct Sixteen {
+    static constexpr int kWords = sizeof(T);
+    u32x4 w[kWords];
+    __device__ __forceinline__ void load(const T* p)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4 w = *reinterpret_cast<const LooseF*>(p + 4 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * i + j] = __uint_as_float(w[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4 w = *reinterpret_cast<const Loose*>(p + 8 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x2 t = pair_to(w[j], T{});
-                x[8 * i + 2 * j] = t[0];
-                x[8 * i + 2 * j + 1] = t[1];
-            }
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 4)
+                w[i] = *reinterpret_cast<const LooseF*>(p + 4 * i);
+            else
+                w[i] = *reinterpret_cast<const Loose*>(p + 8 * i);
         }
     }
-}
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(w[i / 4][i % 4]);
+        else
+            return pair_to(w[i / 8][i / 2 % 4], T{})[i % 2];
+    }
+};
 template <typename T> __device__ __forceinline__ void store16(T* p, const float (&x)[16])
 {
     if constexpr (sizeof(T) == 4) {
@@ -130,18 +137,39 @@ template <typename T> __global__ void __launch_bounds__(256) append_kernel(Call 
     uint8_t* const codes = (values ? c.v : c.k) + head * c.page_bytes();
     uint8_t* const exps = (values ? c.v_exps : c.k_exps) + head;
     const Rows& from = values ? a.v : a.k;
-    const int units = c.head_dim / kUnit, rows = hi - lo;
+    const int units = c.head_dim / kUnit, rows = hi - lo, chunks = rows * units;
     const T* const x = reinterpret_cast<const T*>(from.p) + b * from.batch + h * from.head + (int64_t)(first + lo - begin) * from.token;
 
+    // the first kHeld chunks of a thread stay in its registers until the exponent is known, others are read again
+    constexpr int kHeld = 4;
+    Sixteen<T> held[kHeld];
+    auto place_of = [&](int i, int& row, int& unit) {
+        row = a.units.quotient(i);
+        unit = i - row * units;
+        return x + (int64_t)row * from.token + unit * kUnit;
+    };
     uint32_t top = 0u;
-    for (int i = threadIdx.x; i < rows * units; i += 256) {
-        float t[16];
-        load16(t, x + (int64_t)(i / units) * from.token + (i % units) * kUnit);
+    auto count = [&](const Sixteen<T>& t) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const uint32_t bits = finite_bits(t[j]);
+            const uint32_t bits = finite_bits(t.at(j));
             top = top > bits ? top : bits;
         }
+    };
+#pragma unroll
+    for (int n = 0; n < kHeld; ++n) {
+        const int i = threadIdx.x + 256 * n;
+        int row, unit;
+        if (i < chunks) held[n].load(place_of(i, row, unit));
+    }
+#pragma unroll
+    for (int n = 0; n < kHeld; ++n)
+        if ((int)threadIdx.x + 256 * n < chunks) count(held[n]);
+    for (int i = threadIdx.x + 256 * kHeld; i < chunks; i += 256) {
+        Sixteen<T> t;
+        int row, unit;
+        t.load(place_of(i, row, unit));
+        count(t);
     }
     const uint32_t was = *exps < 254u ? *exps : 254u;
     top = wave_inclusive_max(top);
@@ -157,12 +185,10 @@ template <typename T> __global__ void __launch_bounds__(256) append_kernel(Call 
     const float down = __uint_as_float((254u - byte) << 23), older = two_to(was + 127u > byte ? (int)(was + 127u - byte) : 1);
 
     const int stride = c.head_dim + kPad;
-    for (int i = threadIdx.x; i < rows * units; i += 256) {
-        const int row = i / units, unit = i % units;
+    auto put = [&](const Sixteen<T>& from16, int row, int unit) {
         float t[16];
-        load16(t, x + (int64_t)row * from.token + unit * kUnit);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) t[j] *= down;
+        for (int j = 0; j < 16; ++j) t[j] = from16.at(j) * down;
         const u32x4 w = codes_of(t);
         if (values) {
 #pragma unroll
@@ -170,11 +196,25 @@ template <typename T> __global__ void __launch_bounds__(256) append_kernel(Call 
         } else {
             *reinterpret_cast<u32x4*>(codes + c.key_at(lo + row, unit * kUnit)) = w;
         }
+    };
+#pragma unroll
+    for (int n = 0; n < kHeld; ++n) {
+        const int i = threadIdx.x + 256 * n;
+        int row, unit;
+        place_of(i, row, unit);
+        if (i < chunks) put(held[n], row, unit);
+    }
+    for (int i = threadIdx.x + 256 * kHeld; i < chunks; i += 256) {
+        Sixteen<T> t;
+        int row, unit;
+        t.load(place_of(i, row, unit));
+        put(t, row, unit);
     }
     if (!values) {
         if (again)
             for (int i = threadIdx.x; i < lo * units; i += 256) {
-                u32x4* const p = reinterpret_cast<u32x4*>(codes + c.key_at(i / units, i % units * kUnit));
+                const int row = a.units.quotient(i);
+                u32x4* const p = reinterpret_cast<u32x4*>(codes + c.key_at(row, (i - row * units) * kUnit));
                 float t[16];
                 values_of(t, *p, older);
                 *p = codes_of(t);
@@ -185,7 +225,7 @@ template <typename T> __global__ void __launch_bounds__(256) append_kernel(Call 
     // sixteen tokens of a column: new ones, older ones (rounded again, or as they are), and what lies behind, as it is
     const int unit0 = again ? 0 : lo / 16, unit1 = (hi + 15) / 16;
     for (int i = threadIdx.x; i < (unit1 - unit0) * c.head_dim; i += 256) {
-        const int d = i % c.head_dim, place0 = (unit0 + i / c.head_dim) * 16;
+        const int over = a.columns.quotient(i), d = i - over * c.head_dim, place0 = (unit0 + over) * 16;
         u32x4* const p = reinterpret_cast<u32x4*>(codes + c.value_at(place0, d));
         u32x4 w = {0u, 0u, 0u, 0u};
         if (place0 < lo || place0 + 16 > hi) {
@@ -231,7 +271,7 @@ template <typename T> __global__ void __launch_bounds__(256) restore_kernel(Call
     const int units = c.head_dim / kUnit, stride = c.head_dim + kPad;
     if (values) {
         for (int i = threadIdx.x; i < (there + 15) / 16 * c.head_dim; i += 256) {
-            const int d = i % c.head_dim, place0 = i / c.head_dim * 16;
+            const int over = a.columns.quotient(i), d = i - over * c.head_dim, place0 = over * 16;
             const u32x4 w = *reinterpret_cast<const u32x4*>(codes + c.value_at(place0, d));
 #pragma unroll
             for (int j = 0; j < 16; ++j) turned[(place0 + j) * stride + d] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
@@ -241,7 +281,7 @@ template <typename T> __global__ void __launch_bounds__(256) restore_kernel(Call
     const Rows& to = values ? a.v : a.k;
     T* const out = reinterpret_cast<T*>(to.p) + b * to.batch + h * to.head + (int64_t)first * to.token;
     for (int i = threadIdx.x; i < rows * units; i += 256) {
-        const int row = i / units, unit = i % units;
+        const int row = a.units.quotient(i), unit = i - row * units;
         float t[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) t[j] = 0.f;
@@ -305,7 +345,7 @@ extern "C" int pruner_cache_append(const pruner_cache* c, int32_t dtype, int32_t
     const int rc = cache::check(c, dtype, batch, tokens, q_len, k_len, k, v, slots);
     if (rc) return rc;
     if (batch == 0 || tokens == 0 || c->pages == 0 || c->seq_pages == 0) return PRUNER_OK;
-    const cache::Call call{cache::cache_of(c), cache::rows_of(k), cache::rows_of(v), q_len, k_len, batch, tokens, (int32_t)slots};
+    const cache::Call call{cache::cache_of(c), cache::rows_of(k), cache::rows_of(v), q_len, k_len, batch, tokens, (int32_t)slots, cache::Over(c->head_dim / cache::kUnit), cache::Over(c->head_dim)};
     const dim3 grid((unsigned)(2 * slots * batch * c->kv_heads));
     const size_t lds = (size_t)(tokens < c->page_tokens ? tokens : c->page_tokens) * (c->head_dim + cache::kPad);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -326,7 +366,7 @@ extern "C" int pruner_cache_restore(const pruner_cache* c, int32_t dtype, int32_
     if (rc) return rc;
     if (tokens > (int64_t)c->seq_pages * c->page_tokens) return PRUNER_EINVAL;
     if (batch == 0 || tokens == 0) return PRUNER_OK;
-    const cache::Call call{cache::cache_of(c), cache::rows_of(k), cache::rows_of(v), nullptr, k_len, batch, tokens, (int32_t)slots};
+    const cache::Call call{cache::cache_of(c), cache::rows_of(k), cache::rows_of(v), nullptr, k_len, batch, tokens, (int32_t)slots, cache::Over(c->head_dim / cache::kUnit), cache::Over(c->head_dim)};
     const dim3 grid((unsigned)(2 * slots * batch * c->kv_heads));
     const size_t lds = (size_t)c->page_tokens * (c->head_dim + cache::kPad);
     hipStream_t st = static_cast<hipStream_t>(stream);

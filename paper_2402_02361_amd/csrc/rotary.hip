@@ -65,7 +65,7 @@ template <typename T> struct Vec {
 
 template <typename T, bool SIDE_BY_SIDE> __global__ void __launch_bounds__(256) turn_kernel(Call a, int rows_each)
 {
-    constexpr int kN = Vec<T>::kN;   // pairs of a unit
+    constexpr int kN = Vec<T>::kN, kPairs = SIDE_BY_SIDE ? kN / 2 : kN;   // pairs of a unit: of one sixteen bytes, or of two
     const int all = a.units + a.rest_units, unit = (int)threadIdx.x % all, mine = (int)threadIdx.x / all;
     const int64_t row = (int64_t)blockIdx.x * rows_each + mine;
     if (mine >= rows_each || row >= (int64_t)a.batch * a.tokens) return;
@@ -78,14 +78,16 @@ template <typename T, bool SIDE_BY_SIDE> __global__ void __launch_bounds__(256) 
     T* y = reinterpret_cast<T*>(to.p) + b * to.batch + t * to.token + first * to.head;
     if (unit >= a.units) {   // columns that do not turn
         const int d = 2 * a.pairs + (unit - a.units) * kN, n = a.head_dim - d < kN ? a.head_dim - d : kN;
-        for (int h = first; h < last; ++h, x += from.head, y += to.head) {
-            if (n == kN) {
+        if (n == kN) {
+#pragma unroll 4
+            for (int h = first; h < last; ++h, x += from.head, y += to.head) {
                 Vec<T> v;
                 v.load(x + d);
                 v.store(y + d);
-            } else {
-                for (int i = 0; i < n; ++i) y[d + i] = x[d + i];
             }
+        } else {
+            for (int h = first; h < last; ++h, x += from.head, y += to.head)
+                for (int i = 0; i < n; ++i) y[d + i] = x[d + i];
         }
         return;
     }
@@ -94,44 +96,45 @@ template <typename T, bool SIDE_BY_SIDE> __global__ void __launch_bounds__(256) 
         p = a.positions[row];
     else
         p = t + (a.k_len ? a.k_len[b] - (a.q_len ? a.q_len[b] : a.tokens) : 0);
-    const int pair0 = unit * kN, n = a.pairs - pair0 < kN ? a.pairs - pair0 : kN;
-    float s[kN], c[kN];
+    const int pair0 = unit * kPairs, n = a.pairs - pair0 < kPairs ? a.pairs - pair0 : kPairs;
+    float s[kPairs], c[kPairs];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
+    for (int i = 0; i < kPairs; ++i) {
         angle_of(a.turn[pair0 + i < a.pairs ? pair0 + i : a.pairs - 1], p, s[i], c[i]);
         s[i] *= a.back ? -a.amplitude : a.amplitude;
         c[i] *= a.amplitude;
     }
-    if (n == kN) {
-        const int at0 = SIDE_BY_SIDE ? 2 * pair0 : pair0, at1 = SIDE_BY_SIDE ? 2 * pair0 + kN : a.pairs + pair0;
+    if (n == kPairs) {
 #pragma unroll 4
         for (int h = first; h < last; ++h, x += from.head, y += to.head) {
-            Vec<T> u, v;
-            u.load(x + at0);
-            v.load(x + at1);
+            if constexpr (SIDE_BY_SIDE) {
+                Vec<T> u;
+                u.load(x + 2 * pair0);
 #pragma unroll
-            for (int i = 0; i < kN; ++i) {
-                if constexpr (SIDE_BY_SIDE) {
-                    if (i % 2) continue;
-                    const float p0 = (float)u.w[i], q0 = (float)u.w[i + 1], p1 = (float)v.w[i], q1 = (float)v.w[i + 1];
-                    const int j = i / 2, k = kN / 2 + i / 2;
-                    u.w[i] = (T)__builtin_fmaf(p0, c[j], -(q0 * s[j]));
-                    u.w[i + 1] = (T)__builtin_fmaf(q0, c[j], p0 * s[j]);
-                    v.w[i] = (T)__builtin_fmaf(p1, c[k], -(q1 * s[k]));
-                    v.w[i + 1] = (T)__builtin_fmaf(q1, c[k], p1 * s[k]);
-                } else {
+                for (int i = 0; i < kPairs; ++i) {
+                    const float p0 = (float)u.w[2 * i], q0 = (float)u.w[2 * i + 1];
+                    u.w[2 * i] = (T)__builtin_fmaf(p0, c[i], -(q0 * s[i]));
+                    u.w[2 * i + 1] = (T)__builtin_fmaf(q0, c[i], p0 * s[i]);
+                }
+                u.store(y + 2 * pair0);
+            } else {
+                Vec<T> u, v;
+                u.load(x + pair0);
+                v.load(x + a.pairs + pair0);
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
                     const float p0 = (float)u.w[i], q0 = (float)v.w[i];
                     u.w[i] = (T)__builtin_fmaf(p0, c[i], -(q0 * s[i]));
                     v.w[i] = (T)__builtin_fmaf(q0, c[i], p0 * s[i]);
                 }
+                u.store(y + pair0);
+                v.store(y + a.pairs + pair0);
             }
-            u.store(y + at0);
-            v.store(y + at1);
         }
     } else {
         for (int h = first; h < last; ++h, x += from.head, y += to.head)
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
+            for (int i = 0; i < kPairs; ++i)
                 if (i < n) {
                     const int at0 = SIDE_BY_SIDE ? 2 * (pair0 + i) : pair0 + i, at1 = SIDE_BY_SIDE ? at0 + 1 : a.pairs + at0;
                     const float p0 = (float)x[at0], q0 = (float)x[at1];
@@ -150,7 +153,8 @@ constexpr int64_t kThreads = 1 << 18;   // that fill the device
 template <typename T> int launch(Call& a, bool side_by_side, bool in_place, hipStream_t st)
 {
     constexpr int kN = Vec<T>::kN;
-    a.units = (a.pairs + kN - 1) / kN;
+    const int pairs = side_by_side ? kN / 2 : kN;
+    a.units = (a.pairs + pairs - 1) / pairs;
     a.rest_units = in_place ? 0 : (a.rest + kN - 1) / kN;
     const int all = a.units + a.rest_units, rows_each = 256 / all;
     const int64_t rows = (int64_t)a.batch * a.tokens, threads = rows * all, blocks = (rows + rows_each - 1) / rows_each;
@@ -181,10 +185,7 @@ int turn(const pruner_rotation* r, const pruner_heads* q, const pruner_heads* k,
     a.pairs = r->rotary_dim / 2;
     for (int i = 0; i < a.pairs; ++i) {
         if (!(fabs(r->freqs[i]) <= PRUNER_MAX_ROTARY_FREQUENCY)) return PRUNER_EINVAL;
-        long double turns = (long double)r->freqs[i] * 0.159154943091895335768883763372514362L;   // 1 / (2 pi)
-        turns -= floorl(turns);
-        const long double bits = roundl(turns * 18446744073709551616.0L);
-        a.turn[i] = bits >= 18446744073709551616.0L ? 0ull : (uint64_t)bits;
+        a.turn[i] = (uint64_t)(__int128)((long double)r->freqs[i] * 2935890503282001226.496L);   // 2^64 / (2 pi), to the 64 bits of a long double; whole turns are the bits above
     }
     if (r->batch == 0 || r->tokens == 0 || r->q_heads + r->kv_heads == 0) return PRUNER_OK;
     if (r->q_heads > 0 && (!rows_ok(q, r->dtype) || !rows_ok(q_out, r->dtype))) return PRUNER_EINVAL;
