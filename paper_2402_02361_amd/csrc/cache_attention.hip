@@ -547,6 +547,52 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
     if (lse && half == 0) lse[row] = at.mine ? lse_of(run.m, l) : -ATT_INF;
 }
 
+// ---- the parts of a key axis that was cut
+
+// A row's DP columns, four to a thread, by `groups` threads that take every so many parts and meet in LDS: few rows of many parts would leave one thread to go through all of them in turn (8 rows of
+// 118 parts: 95 us a call where ...).
+template <typename T, int DP> __global__ void __launch_bounds__(256) join_groups_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int groups)
+{
+    constexpr int kFours = DP / 4;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[256];
+    __shared__ float2 stats[256];
+    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens;
+    const int four = threadIdx.x % kFours, group = threadIdx.x / kFours % groups, each = 256 / kFours / groups;
+    const int64_t row = (int64_t)blockIdx.x * each + threadIdx.x / kFours / groups;
+    float m = -ATT_INF, total = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (row < rows)
+#pragma unroll 4
+        for (int n = group; n < parts.count; n += groups) {
+            const float2 st = parts.stats[n * rows + row];
+            const f32x4 x = *reinterpret_cast<const f32x4*>(parts.sums + (n * rows + row) * DP + 4 * four);
+            const bool any = st.y != 0.f;   // (a part that no key reached counts for nothing, whatever it left)
+            const float now = any ? __builtin_fmaxf(m, st.x) : m, keep = m == -ATT_INF ? 0.f : exp2_of((m - now) * kLog2e), f = any ? exp2_of((st.x - now) * kLog2e) : 0.f;
+            m = now;
+            total = __builtin_fmaf(f, any ? st.y : 0.f, total * keep);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, any ? x[e] : 0.f, o[e] * keep);
+        }
+    sums[threadIdx.x] = o;
+    stats[threadIdx.x] = make_float2(m, total);
+    __syncthreads();
+    if (group != 0 || row >= rows) return;
+    for (int n = 1; n < groups; ++n) {
+        const float2 st = stats[threadIdx.x + n * kFours];
+        const f32x4 x = sums[threadIdx.x + n * kFours];
+        if (st.y == 0.f) continue;
+        const float now = __builtin_fmaxf(m, st.x), keep = m == -ATT_INF ? 0.f : exp2_of((m - now) * kLog2e), f = exp2_of((st.x - now) * kLog2e);
+        m = now;
+        total = __builtin_fmaf(f, st.y, total * keep);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, x[e], o[e] * keep);
+    }
+    const float f = total != 0.f ? 1.f / total : 0.f;
+    const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads, d = 4 * four;
+    if (d < a.head_dim) *reinterpret_cast<u32x2*>(out.at<T>(b, h) + (int64_t)i * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
+    if (lse && d == 0) lse[row] = lse_of(m, total);
+}
+
 // Which kernel, and into how many parts the keys are cut.
 struct Plan {
     bool tokens;
@@ -622,7 +668,10 @@ template <typename T, int DP> int run(const Args& args, const cache::Cache& c, c
         if (rc) return rc;
     }
     if (plan.parts > 1) {
-        hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)((plan.rows * (DP / 4) + 255) / 256)), dim3(256), 0, st, args, out, lse, parts);
+        int groups = 1;
+        while (groups < plan.parts && groups < 256 / (DP / 4)) groups *= 2;
+        const int64_t each = 256 / (DP / 4) / groups;
+        hipLaunchKernelGGL((join_groups_kernel<T, DP>), dim3((unsigned)((plan.rows + each - 1) / each)), dim3(256), 0, st, args, out, lse, parts, groups);
         PRUNER_LAUNCH_CHECK();
     }
     return PRUNER_OK;

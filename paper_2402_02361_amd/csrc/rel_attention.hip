@@ -197,6 +197,16 @@ __global__ void __launch_bounds__(256, (DP == 128 ? 2 : 3)) tile_kernel(Args a, 
     if (lse && half == 0) lse[row] = i < ql ? lse_of(run.m, l) : -ATT_INF;
 }
 
+// LDS of rows_kernel before the tiles: the biases of the group's heads, and the bucket of every r that a tile which is not wholly at one end can ask for.
+struct RowsLds {
+    int n_buckets, biases, buckets;   // bytes
+    __host__ __device__ explicit RowsLds(const Args& a)
+        : n_buckets(a.table ? (a.n_edges + 1) * (a.two_sided ? 2 : 1) : 0), biases((n_buckets * a.group * 4 + 15) & ~15),
+          buckets(a.table ? (Window(a.left, a.right).size + 15) & ~15 : 0)
+    {
+    }
+};
+
 // Query t of head hk * group + g is column t * group + g.
 template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts)
 {
@@ -286,6 +296,37 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) rows_ker
         }
     }
     meet<T, DP>(run, lds, a, out, lse, parts, b, hk, part, columns, mine);
+}
+
+// Four neighbouring values of a row per thread.
+template <typename T, int DP> __global__ void __launch_bounds__(256) join_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts)
+{
+    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_tokens, item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = item / (DP / 4);
+    const int d = 4 * (int)(item % (DP / 4));
+    if (row >= rows) return;
+    float m = -ATT_INF, total = 0.f;
+#pragma unroll 8
+    for (int n = 0; n < parts.count; ++n) {
+        const float2 st = parts.stats[n * rows + row];
+        m = __builtin_fmaxf(m, st.y != 0.f ? st.x : -ATT_INF);
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int n = 0; n < parts.count; ++n) {
+        const float2 st = parts.stats[n * rows + row];
+        const f32x4 x = *reinterpret_cast<const f32x4*>(parts.sums + (n * rows + row) * DP + d);
+        const bool any = st.y != 0.f;   // (a part that no key reached counts for nothing, whatever it left)
+        const float f = any ? exp2_of((st.x - m) * kLog2e) : 0.f;
+        total = __builtin_fmaf(f, st.y, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, any ? x[e] : 0.f, o[e]);
+    }
+    const float f = total != 0.f ? 1.f / total : 0.f;
+    const int i = (int)(row % a.q_tokens), bh = (int)(row / a.q_tokens), b = bh / a.q_heads, h = bh % a.q_heads;
+    if (d < a.head_dim)
+        *reinterpret_cast<u32x2*>(out.at<T>(b, h) + (int64_t)i * out.token + d) = u32x2{pair_of(o[0] * f, o[1] * f, T{}), pair_of(o[2] * f, o[3] * f, T{})};
+    if (lse && d == 0) lse[row] = lse_of(m, total);
 }
 
 // Which kernel, and into how many parts the keys are cut.
