@@ -75,7 +75,8 @@ template <typename T, int GROUP, int RT, int CT> struct Block {
             for (int u = 0; u < kGroups; ++u) s[t][u] = *reinterpret_cast<const u32x2*>(a.scales + ((at * 4 + g) * kGroups + u) * 4);
         }
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c) {
+            if (!x_row[c]) continue;   // (columns past the last: what they give is not stored)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int at = kBlock * block + 32 * j + 8 * g;
@@ -88,6 +89,7 @@ template <typename T, int GROUP, int RT, int CT> struct Block {
                         if (at + i < a.dim) x[c][j][i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, x_row[c][at + i]) << (16 * (i % 2));
                 }
             }
+        }
     }
     __device__ __forceinline__ void add(f32x4 (&acc)[RT][CT]) const
     {
@@ -125,7 +127,7 @@ template <typename T, int GROUP, int RT, int CT> struct Block {
     }
 };
 
-template <typename T, int GROUP, int RT, int CT> __global__ void __launch_bounds__(1024) linear_kernel(Call a)
+template <typename T, int GROUP, int RT, int CT> __global__ void __launch_bounds__(RT == 1 && CT == 1 ? 1024 : 512) linear_kernel(Call a)
 {
     extern __shared__ __attribute__((aligned(16))) float sums[];   // [wavefront][RT * CT][64][4]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
@@ -134,21 +136,28 @@ template <typename T, int GROUP, int RT, int CT> __global__ void __launch_bounds
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const int row = row0 + 16 * c + (lane & 15);
-        x_row[c] = reinterpret_cast<const T*>(a.x) + (int64_t)(row < a.rows ? row : a.rows - 1) * a.x_pitch;   // (what a column past the last gives is not stored)
+        x_row[c] = row < a.rows ? reinterpret_cast<const T*>(a.x) + (int64_t)row * a.x_pitch : nullptr;
     }
     f32x4 acc[RT][CT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Block<T, GROUP, RT, CT> now, next;
-    int block = wave;
-    if (block < a.blocks) now.load(a, x_row, tile0, tiles, block, lane);
-    while (block < a.blocks) {
-        if (block + waves < a.blocks) next.load(a, x_row, tile0, tiles, block + waves, lane);
-        now.add(acc);
-        block += waves;
-        now = next;
+    Block<T, GROUP, RT, CT> on_way[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) on_way[n].x[c][j] = u32x4{0u, 0u, 0u, 0u};
+    if (wave < a.blocks) on_way[0].load(a, x_row, tile0, tiles, wave, lane);
+    for (int block = wave; block < a.blocks;) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            if (block + waves < a.blocks) on_way[n ^ 1].load(a, x_row, tile0, tiles, block + waves, lane);
+            if (block < a.blocks) on_way[n].add(acc);
+            block += waves;
+        }
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -259,10 +268,16 @@ template <typename T, int GROUP, int RT, int CT> int launch(const Call& a, int w
 }
 template <typename T, int GROUP> int route(const Call& a, hipStream_t st)
 {
-    const int tiles = (a.n_out + kOutputs - 1) / kOutputs;
-    const int waves = a.blocks < 8 ? a.blocks : 8;
-    if (a.rows > 16) return launch<T, GROUP, 2, 2>(a, waves, st);
-    return tiles >= 1024 ? launch<T, GROUP, 2, 1>(a, waves, st) : launch<T, GROUP, 1, 1>(a, waves, st);
+    // Output tiles of a wavefront: the more, the less often x is read, and the fewer workgroups there are.  (us a call of up to 16 rows, one tile and two, by 8 and 16 wavefronts: 32768 x 8192 41
+    // and 49, 32 and 38; 8192 x 8192 12.2 and 13.3, 10.8 and 10.6; 4096 x 16384 14 and 11, 17 and 15.  More rows, two tiles and four: 32 over 8192 x 8192 21 and 24, 100 over 4096 x 4096 22 and
+    // 16, 64 over 16384 x 4096 42 and 29, 17 over 2000 x 3000 10.6 and 12.7.)
+    const int tiles = (a.n_out + kOutputs - 1) / kOutputs, eight = a.blocks < 8 ? a.blocks : 8;
+    if (a.rows > 16) {
+        if constexpr (GROUP > 32)   // (the scales of four tiles in groups of 32 do not fit the registers)
+            if ((int64_t)((tiles + 3) / 4) * ((a.rows + 31) / 32) >= 256) return launch<T, GROUP, 4, 2>(a, eight, st);
+        return launch<T, GROUP, 2, 2>(a, eight, st);
+    }
+    return tiles >= 512 ? launch<T, GROUP, 2, 1>(a, eight, st) : launch<T, GROUP, 1, 1>(a, a.blocks < 16 ? a.blocks : 16, st);
 }
 template <typename T> int by_group(const Call& a, int group, hipStream_t st) { return group == 32 ? route<T, 32>(a, st) : group == 64 ? route<T, 64>(a, st) : route<T, 128>(a, st); }
 
