@@ -14,6 +14,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
+constexpr int64_t kCached = 256 << 20;   // bytes: the last cache
 constexpr int kUnit = 16;            // columns of a key, tokens of values, that lie side by side
 constexpr uint32_t kNotANumber = 0x7Fu;   // e4m3's
 constexpr uint32_t kLargestFraction = 0x600000u;   // of 448 = 1.75 x 2^8

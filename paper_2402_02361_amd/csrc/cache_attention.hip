@@ -80,7 +80,7 @@ __device__ __forceinline__ float sum_of_rows(float v)
 
 // 64 keys' codes: keys in four operands of 16 rows, row 4 u + j of operand t being key 16 u + 4 t + j, so that lane (n = lane & 15, g = lane >> 4) of the results has column n's scores of the sixteen
 // keys 16 g + 4 t + j; of values it has the sixteen of those keys.  WHOLE: the 64 keys lie in one page, whose place all lanes share.
-template <typename T, int DP, bool WHOLE> struct Few {
+template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
     static constexpr int kChunks = (DP + 63) / 64, kBlocks = DP / 16;
     u32x4 k[4][kChunks], v[kBlocks];
     float k_scale, v_scale;
@@ -105,8 +105,13 @@ template <typename T, int DP, bool WHOLE> struct Few {
         for (int i = 0; i < kChunks; ++i) {
             const int unit = 4 * i + g < units ? 4 * i + g : units - 1;   // (past the last one: the query's columns are 0 there)
             const uint32_t at = ((uint32_t)unit << (c.shift + 4)) + 16 * ((WHOLE ? 16 * (lane >> 2 & 3) : 0) + (lane & 3));
+            if constexpr (ONCE) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) k[t][i] = *reinterpret_cast<const u32x4*>(p + at + 64 * t);
+                for (int t = 0; t < 4; ++t) k[t][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + at + 64 * t));
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) k[t][i] = *reinterpret_cast<const u32x4*>(p + at + 64 * t);
+            }
         }
     }
     __device__ __forceinline__ void load_values(const cache::Cache& c, int h, int key0, int kl, int lane)
@@ -117,8 +122,14 @@ template <typename T, int DP, bool WHOLE> struct Few {
         const uint8_t* const p = c.v + head * c.page_bytes() + place * c.head_dim;
         v_scale = cache::two_to(c.v_exps[head]);
         const uint32_t at = 16 * ((WHOLE ? g * c.head_dim : 0) + (lane & 15));
+        // (columns past the last are not stored)
+        if constexpr (ONCE) {
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1));   // (columns past the last are not stored)
+            for (int i = 0; i < kBlocks; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1));
+        }
     }
     __device__ __forceinline__ void clear_values()   // those that are not there
     {
@@ -132,9 +143,12 @@ template <typename T, int DP, bool WHOLE> struct Few {
     }
 };
 
-template <typename T, int DP, int CT, bool WHOLE> __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2)) tokens_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts)
+// ONCE: the caches hold more than stays cached from one call to the next, and are read past it (us a call with and without: 32 caches of 32768, 8 heads of 128, 348 and 379, of up to 32768 201 and 208;
+// 8 of up to 20000 51 and 52; 16 of up to 5003, 4 heads of 80, 26 and 24).
+template <typename T, int DP, int CT, bool WHOLE, bool ONCE>
+__global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2)) tokens_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts)
 {
-    using Step = Few<T, DP, WHOLE>;
+    using Step = Few<T, DP, WHOLE, ONCE>;
     constexpr int kChunks = Step::kChunks, kBlocks = Step::kBlocks, kStep = 4 * kTile;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -630,10 +644,12 @@ Plan plan_of(const pruner_attention* a)
     return p;
 }
 
-template <typename T, int DP, int CT, bool WHOLE> int run_tokens(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
+template <typename T, int DP, int CT> int run_tokens(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
 {
     const size_t biases = (size_t)BiasLds(args).bytes(), last = Meeting<DP>::bytes(args.q_tokens * args.group);
-    hipLaunchKernelGGL((tokens_kernel<T, DP, CT, WHOLE>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > biases ? last : biases, st, args, c, out, lse, parts);
+    const bool once = 2 * (int64_t)args.batch * args.kv_heads * args.k_tokens * args.head_dim > cache::kCached;
+    void (*const kernel)(Args, cache::Cache, Heads, float*, Parts) = c.page_tokens() < kTile ? tokens_kernel<T, DP, CT, false, false> : once ? tokens_kernel<T, DP, CT, true, true> : tokens_kernel<T, DP, CT, true, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.parts)), dim3(256), last > biases ? last : biases, st, args, c, out, lse, parts);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
@@ -659,9 +675,7 @@ template <typename T, int DP> int run(const Args& args, const cache::Cache& c, c
         parts.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up((size_t)plan.parts * plan.rows * 8, 256));
     }
     if (plan.tokens) {
-        const bool narrow = args.q_tokens * args.group <= 16, whole = c.page_tokens() >= kTile;
-        const int rc = narrow ? (whole ? run_tokens<T, DP, 1, true>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 1, false>(args, c, plan, parts, out, lse, st))
-                              : (whole ? run_tokens<T, DP, 2, true>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 2, false>(args, c, plan, parts, out, lse, st));
+        const int rc = args.q_tokens * args.group <= 16 ? run_tokens<T, DP, 1>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 2>(args, c, plan, parts, out, lse, st);
         if (rc) return rc;
     } else {
         const int rc = c.page_tokens() >= kTile ? run_chunk<T, DP, true>(args, c, plan, parts, out, lse, st) : run_chunk<T, DP, false>(args, c, plan, parts, out, lse, st);

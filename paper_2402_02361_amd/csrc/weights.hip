@@ -24,6 +24,7 @@ typedef u32x4 Loose __attribute__((aligned(2)));
 
 constexpr int kOutputs = 16, kBlock = 128, kBlockWords = kOutputs * kBlock / 8;
 constexpr int kZero = 8;   // the code of 0
+constexpr int64_t kCached = 96 << 20;   // bytes of codes (us a call read past the caches and not: 32768 x 8192 30.1 and 31.8, 16384 x 4096 13.2 and 12.7, 8192 x 8192 11.5 and 10.7)
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, __bf16)
 {
@@ -60,7 +61,7 @@ struct Call {
 };
 
 // A wavefront's operands of one block of inputs.
-template <typename T, int GROUP, int RT, int CT> struct Block {
+template <typename T, int GROUP, int RT, int CT, bool ONCE> struct Block {
     static constexpr int kGroups = kBlock / GROUP;
     u32x4 w[RT], x[CT][4];
     u32x2 s[RT][kGroups];   // four bfloat16 each
@@ -70,7 +71,11 @@ template <typename T, int GROUP, int RT, int CT> struct Block {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const int64_t at = (int64_t)(tile0 + t < tiles ? tile0 + t : tiles - 1) * a.blocks + block;
-            w[t] = *reinterpret_cast<const u32x4*>(a.codes + at * kBlockWords + 4 * lane);
+            const u32x4* const p = reinterpret_cast<const u32x4*>(a.codes + at * kBlockWords + 4 * lane);
+            if constexpr (ONCE)
+                w[t] = __builtin_nontemporal_load(p);
+            else
+                w[t] = *p;
 #pragma unroll
             for (int u = 0; u < kGroups; ++u) s[t][u] = *reinterpret_cast<const u32x2*>(a.scales + ((at * 4 + g) * kGroups + u) * 4);
         }
@@ -127,7 +132,8 @@ template <typename T, int GROUP, int RT, int CT> struct Block {
     }
 };
 
-template <typename T, int GROUP, int RT, int CT> __global__ void __launch_bounds__(RT == 1 && CT == 1 ? 1024 : 512) linear_kernel(Call a)
+// ONCE: the weights are more than stays cached from one call to the next, and are read past it.
+template <typename T, int GROUP, int RT, int CT, bool ONCE> __global__ void __launch_bounds__(RT == 1 && CT == 1 ? 1024 : 512) linear_kernel(Call a)
 {
     extern __shared__ __attribute__((aligned(16))) float sums[];   // [wavefront][RT * CT][64][4]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
@@ -143,7 +149,7 @@ template <typename T, int GROUP, int RT, int CT> __global__ void __launch_bounds
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Block<T, GROUP, RT, CT> on_way[2];
+    Block<T, GROUP, RT, CT, ONCE> on_way[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -252,17 +258,17 @@ bool weights_ok(const pruner_weights* w)
 int blocks_of(const pruner_weights* w) { return (w->dim + kBlock - 1) / kBlock; }
 size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 
-template <typename T, int GROUP, int RT, int CT> int launch(const Call& a, int waves, hipStream_t st)
+template <typename T, int GROUP, int RT, int CT, bool ONCE = false> int launch(const Call& a, int waves, hipStream_t st)
 {
     static PerDeviceFlag ready;
     const int dev = current_device(nullptr);
     if (dev < 0) return PRUNER_EHIP;
     if (!ready.get(dev)) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_kernel<T, GROUP, RT, CT>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_kernel<T, GROUP, RT, CT, ONCE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
         ready.mark(dev);
     }
     const dim3 grid((unsigned)((a.n_out + kOutputs * RT - 1) / (kOutputs * RT)), (unsigned)((a.rows + 16 * CT - 1) / (16 * CT)));
-    hipLaunchKernelGGL((linear_kernel<T, GROUP, RT, CT>), grid, dim3(64 * waves), (size_t)waves * RT * CT * 1024, st, a);
+    hipLaunchKernelGGL((linear_kernel<T, GROUP, RT, CT, ONCE>), grid, dim3(64 * waves), (size_t)waves * RT * CT * 1024, st, a);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
@@ -277,7 +283,8 @@ template <typename T, int GROUP> int route(const Call& a, hipStream_t st)
             if ((int64_t)((tiles + 3) / 4) * ((a.rows + 31) / 32) >= 256) return launch<T, GROUP, 4, 2>(a, eight, st);
         return launch<T, GROUP, 2, 2>(a, eight, st);
     }
-    return tiles >= 512 ? launch<T, GROUP, 2, 1>(a, eight, st) : launch<T, GROUP, 1, 1>(a, a.blocks < 16 ? a.blocks : 16, st);
+    if (tiles >= 512) return (int64_t)a.n_out * a.dim / 2 > kCached ? launch<T, GROUP, 2, 1, true>(a, eight, st) : launch<T, GROUP, 2, 1>(a, eight, st);
+    return launch<T, GROUP, 1, 1>(a, a.blocks < 16 ? a.blocks : 16, st);
 }
 template <typename T> int by_group(const Call& a, int group, hipStream_t st) { return group == 32 ? route<T, 32>(a, st) : group == 64 ? route<T, 64>(a, st) : route<T, 128>(a, st); }
 
