@@ -3,7 +3,8 @@
 // Angles are exact at any position: a frequency is held as turns per position in 64 bits of fraction, so that the product with the position wraps at whole
 // turns as the angle does; the quadrant is its two highest bits, and what is left, at most an eighth of a turn, goes to binary32 and the series of sine and cosine
 // (x^9 / 9!, x^10 / 10!; the next terms are below 2e-9).
-// A thread takes pairs of one token for several heads in turn, and forms their sines and cosines once.  Bound: memory.
+// A workgroup takes a few tokens: it forms their sines and cosines once, in LDS, and goes through the columns of all their heads as they lie in memory, sixteen bytes (with pairs half
+// of the columns apart, twice sixteen) to a thread.  Bound: memory.
 #include "common.h"
 
 #include <math.h>
@@ -24,7 +25,8 @@ struct Call {
     int32_t heads[2];
     const int32_t *positions, *q_len, *k_len;
     int32_t batch, tokens, head_dim, pairs, rest;   // rest: columns behind the pairs that are copied
-    int32_t units, rest_units, each;                // of a head; heads that a thread takes
+    int32_t units, all_units;   // of a head: those that turn, and with those that are copied
+    int32_t rows_each;          // tokens of a workgroup
     float amplitude;
     int32_t back;
     uint64_t turn[PRUNER_MAX_ROTARY_DIM / 2];       // 2^-64 turns per position
@@ -66,89 +68,137 @@ template <typename T> struct Vec {
         else
             w = *reinterpret_cast<const Loose*>(p);
     }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Loose*>(p) = w; }
+    template <bool ONCE> __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (ONCE)
+            __builtin_nontemporal_store(w, reinterpret_cast<Loose*>(p));
+        else
+            *reinterpret_cast<Loose*>(p) = w;
+    }
 };
 
-// ONCE: inputs are more than the caches keep, and are not to take the outputs' place there (us a call with and without: 168 MB of bfloat16 in, 59 and 71, 126 MB 46 and 46, 42 MB 19 and 17;
-// writes that are not kept either: 70).
-template <typename T, bool SIDE_BY_SIDE, bool ONCE> __global__ void __launch_bounds__(256) turn_kernel(Call a, int rows_each)
+struct RowAt {
+    int64_t x[2], y[2];   // elements: where a token's queries and keys begin
+};
+
+// ONCE: inputs and outputs are more than the caches are good for.
+template <typename T, bool SIDE_BY_SIDE, bool ONCE> __global__ void __launch_bounds__(256) turn_kernel(Call a)
 {
-    constexpr int kN = Vec<T>::kN, kPairs = SIDE_BY_SIDE ? kN / 2 : kN;   // pairs of a unit: of one sixteen bytes, or of two
-    const int all = a.units + a.rest_units, unit = (int)threadIdx.x % all, mine = (int)threadIdx.x / all;
-    const int64_t row = (int64_t)blockIdx.x * rows_each + mine;
-    if (mine >= rows_each || row >= (int64_t)a.batch * a.tokens) return;
-    const int b = (int)(row / a.tokens), t = (int)(row % a.tokens);
-    const int groups = (a.heads[0] + a.each - 1) / a.each, which = (int)blockIdx.y >= groups ? 1 : 0;
-    const int first = ((int)blockIdx.y - (which ? groups : 0)) * a.each, last = first + a.each < a.heads[which] ? first + a.each : a.heads[which];
-    const Rows& from = a.x[which];
-    const Rows& to = a.y[which];
-    const T* x = reinterpret_cast<const T*>(from.p) + b * from.batch + t * from.token + first * from.head;
-    T* y = reinterpret_cast<T*>(to.p) + b * to.batch + t * to.token + first * to.head;
-    if (unit >= a.units) {   // columns that do not turn
-        const int d = 2 * a.pairs + (unit - a.units) * kN, n = a.head_dim - d < kN ? a.head_dim - d : kN;
-        if (n == kN) {
-#pragma unroll 4
-            for (int h = first; h < last; ++h, x += from.head, y += to.head) {
-                Vec<T> v;
-                v.template load<ONCE>(x + d);
-                v.store(y + d);
-            }
-        } else {
-            for (int h = first; h < last; ++h, x += from.head, y += to.head)
-                for (int i = 0; i < n; ++i) y[d + i] = x[d + i];
-        }
-        return;
-    }
-    int p;
-    if (a.positions)
-        p = a.positions[row];
-    else
-        p = t + (a.k_len ? a.k_len[b] - (a.q_len ? a.q_len[b] : a.tokens) : 0);
-    const int pair0 = unit * kPairs, n = a.pairs - pair0 < kPairs ? a.pairs - pair0 : kPairs;
-    float s[kPairs], c[kPairs];
+    constexpr int kN = Vec<T>::kN, kPairs = SIDE_BY_SIDE ? kN / 2 : kN, kAtOnce = 4;   // pairs of a unit; units that a thread asks for before it works on them
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    RowAt* const rows_at = reinterpret_cast<RowAt*>(lds);
+    f32x2* const angles = reinterpret_cast<f32x2*>(lds + a.rows_each * sizeof(RowAt));   // [token][pair] sine and cosine
+    const int64_t all_rows = (int64_t)a.batch * a.tokens, row0 = (int64_t)blockIdx.x * a.rows_each;
+    const int rows = all_rows - row0 < a.rows_each ? (int)(all_rows - row0) : a.rows_each;
+    for (int i = threadIdx.x; i < rows * a.pairs; i += 256) {
+        const int row = i / a.pairs, pair = i - row * a.pairs, b = (int)((row0 + row) / a.tokens), t = (int)((row0 + row) - (int64_t)b * a.tokens);
+        const int p = a.positions ? a.positions[row0 + row] : (int)((uint32_t)t + (a.k_len ? (uint32_t)a.k_len[b] - (uint32_t)(a.q_len ? a.q_len[b] : a.tokens) : 0u));
+        float s, c;
+        angle_of(a.turn[pair], p, s, c);
+        angles[i] = f32x2{(a.back ? -s : s) * a.amplitude, c * a.amplitude};
+        if (pair == 0)
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-        angle_of(a.turn[pair0 + i < a.pairs ? pair0 + i : a.pairs - 1], p, s[i], c[i]);
-        s[i] *= a.back ? -a.amplitude : a.amplitude;
-        c[i] *= a.amplitude;
+            for (int w = 0; w < 2; ++w) {
+                rows_at[row].x[w] = b * a.x[w].batch + t * a.x[w].token;
+                rows_at[row].y[w] = b * a.y[w].batch + t * a.y[w].token;
+            }
     }
-    if (n == kPairs) {
-#pragma unroll 4
-        for (int h = first; h < last; ++h, x += from.head, y += to.head) {
-            if constexpr (SIDE_BY_SIDE) {
-                Vec<T> u;
-                u.template load<ONCE>(x + 2 * pair0);
+    __syncthreads();
+    // (unit, head, token) of this thread's first item, and how far the next one is
+    const int heads = a.heads[0] + a.heads[1];
+    int unit = (int)threadIdx.x % a.all_units, head = (int)threadIdx.x / a.all_units % heads, row = (int)threadIdx.x / a.all_units / heads;
+    const int unit_step = 256 % a.all_units, head_step = 256 / a.all_units % heads, row_step = 256 / a.all_units / heads;
+    while (row < rows) {
+        Vec<T> u[kAtOnce], v[kAtOnce];
+        T* to[kAtOnce];
+        const f32x2* by[kAtOnce];
+        int pairs[kAtOnce];   // pairs of the unit; 0: none, below 0: columns that are copied
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            const int which = head >= a.heads[0] ? 1 : 0, h = head - (which ? a.heads[0] : 0), first = unit * kPairs;
+            const bool turns = unit < a.units;
+            const int d = !turns ? 2 * a.pairs + (unit - a.units) * kN : SIDE_BY_SIDE ? 2 * first : first;
+            pairs[n] = 0;
+            if (row < rows) {
+                const T* const x = reinterpret_cast<const T*>(which ? a.x[1].p : a.x[0].p) + rows_at[row].x[which] + h * (which ? a.x[1].head : a.x[0].head) + d;
+                to[n] = reinterpret_cast<T*>(which ? a.y[1].p : a.y[0].p) + rows_at[row].y[which] + h * (which ? a.y[1].head : a.y[0].head) + d;
+                by[n] = angles + row * a.pairs + first;
+                if (turns) {
+                    pairs[n] = a.pairs - first < kPairs ? a.pairs - first : kPairs;
+                    if (pairs[n] == kPairs) {
+                        u[n].template load<ONCE>(x);
+                        if constexpr (!SIDE_BY_SIDE) v[n].template load<ONCE>(x + a.pairs);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i)
+                            if (i < pairs[n]) {
+                                if constexpr (SIDE_BY_SIDE) {
+                                    u[n].w[2 * i] = x[2 * i];
+                                    u[n].w[2 * i + 1] = x[2 * i + 1];
+                                } else {
+                                    u[n].w[i] = x[i];
+                                    v[n].w[i] = x[a.pairs + i];
+                                }
+                            }
+                    }
+                } else {
+                    pairs[n] = a.head_dim - d < kN ? d - a.head_dim : -kN;
+                    if (pairs[n] == -kN) {
+                        u[n].template load<ONCE>(x);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kN; ++i)
+                            if (i < -pairs[n]) u[n].w[i] = x[i];
+                    }
+                }
+            }
+            unit += unit_step;
+            const int carry = unit >= a.all_units ? 1 : 0;
+            unit -= carry ? a.all_units : 0;
+            head += head_step + carry;
+            const int over = head >= heads ? 1 : 0;
+            head -= over ? heads : 0;
+            row += row_step + over;
+        }
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            if (pairs[n] > 0)
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) {
-                    const float p0 = (float)u.w[2 * i], q0 = (float)u.w[2 * i + 1];
-                    u.w[2 * i] = (T)__builtin_fmaf(p0, c[i], -(q0 * s[i]));
-                    u.w[2 * i + 1] = (T)__builtin_fmaf(q0, c[i], p0 * s[i]);
+                    const f32x2 sc = by[n][i < pairs[n] ? i : 0];
+                    if constexpr (SIDE_BY_SIDE) {
+                        const float p = (float)u[n].w[2 * i], q = (float)u[n].w[2 * i + 1];
+                        u[n].w[2 * i] = (T)__builtin_fmaf(p, sc[1], -(q * sc[0]));
+                        u[n].w[2 * i + 1] = (T)__builtin_fmaf(q, sc[1], p * sc[0]);
+                    } else {
+                        const float p = (float)u[n].w[i], q = (float)v[n].w[i];
+                        u[n].w[i] = (T)__builtin_fmaf(p, sc[1], -(q * sc[0]));
+                        v[n].w[i] = (T)__builtin_fmaf(q, sc[1], p * sc[0]);
+                    }
                 }
-                u.store(y + 2 * pair0);
-            } else {
-                Vec<T> u, v;
-                u.template load<ONCE>(x + pair0);
-                v.template load<ONCE>(x + a.pairs + pair0);
+            if (pairs[n] == kPairs) {
+                u[n].template store<ONCE>(to[n]);
+                if constexpr (!SIDE_BY_SIDE) v[n].template store<ONCE>(to[n] + a.pairs);
+            } else if (pairs[n] == -kN) {
+                u[n].template store<ONCE>(to[n]);
+            } else if (pairs[n] > 0) {
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const float p0 = (float)u.w[i], q0 = (float)v.w[i];
-                    u.w[i] = (T)__builtin_fmaf(p0, c[i], -(q0 * s[i]));
-                    v.w[i] = (T)__builtin_fmaf(q0, c[i], p0 * s[i]);
-                }
-                u.store(y + pair0);
-                v.store(y + a.pairs + pair0);
+                for (int i = 0; i < kPairs; ++i)
+                    if (i < pairs[n]) {
+                        if constexpr (SIDE_BY_SIDE) {
+                            to[n][2 * i] = u[n].w[2 * i];
+                            to[n][2 * i + 1] = u[n].w[2 * i + 1];
+                        } else {
+                            to[n][i] = u[n].w[i];
+                            to[n][a.pairs + i] = v[n].w[i];
+                        }
+                    }
+            } else if (pairs[n] < 0) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i)
+                    if (i < -pairs[n]) to[n][i] = u[n].w[i];
             }
         }
-    } else {
-        for (int h = first; h < last; ++h, x += from.head, y += to.head)
-#pragma unroll
-            for (int i = 0; i < kPairs; ++i)
-                if (i < n) {
-                    const int at0 = SIDE_BY_SIDE ? 2 * (pair0 + i) : pair0 + i, at1 = SIDE_BY_SIDE ? at0 + 1 : a.pairs + at0;
-                    const float p0 = (float)x[at0], q0 = (float)x[at1];
-                    y[at0] = (T)__builtin_fmaf(p0, c[i], -(q0 * s[i]));
-                    y[at1] = (T)__builtin_fmaf(q0, c[i], p0 * s[i]);
-                }
     }
 }
 
@@ -156,28 +206,25 @@ size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 bool rows_ok(const pruner_heads* h, int32_t dtype) { return h && h->p && aligned(h->p, size_of(dtype)) && h->batch >= 0 && h->token >= 0 && h->head >= 0; }
 Rows rows_of(const pruner_heads* h) { return Rows{static_cast<char*>(h->p), h->batch, h->token, h->head}; }
 
-constexpr int64_t kThreads = 1 << 18;   // that fill the device
-constexpr int64_t kCached = 128 << 20;   // bytes of input: half of the last cache
+// Bytes of input from which on accesses go past the caches: rows of whole lines, others.  (us a call past them and not, outputs kept: 168 MB of bfloat16 in, heads of 128, 64 and 70, 126 MB 48 and 53, 42 MB
+// 21 and 24; binary32, heads of 128, 336 MB 112 and 125, of 100, 54 MB 32 and 30; with loads alone past them 168 MB 67.)
+constexpr int64_t kCachedLines = 32 << 20, kCachedParts = 128 << 20;
+// Units of a workgroup, about.  (1024, 2048 and 4096, us a call: 168 MB in 64, 69, 75; 54 MB in heads of 100 30, 30, 32.)
+constexpr int kItems = 1024;
 
 template <typename T> int launch(Call& a, bool side_by_side, bool in_place, hipStream_t st)
 {
     constexpr int kN = Vec<T>::kN;
-    const int pairs = side_by_side ? kN / 2 : kN;
+    const int pairs = side_by_side ? kN / 2 : kN, heads = a.heads[0] + a.heads[1];
     a.units = (a.pairs + pairs - 1) / pairs;
-    a.rest_units = in_place ? 0 : (a.rest + kN - 1) / kN;
-    const int all = a.units + a.rest_units, rows_each = 256 / all;
-    const int64_t rows = (int64_t)a.batch * a.tokens, threads = rows * all, blocks = (rows + rows_each - 1) / rows_each;
+    a.all_units = a.units + (in_place ? 0 : (a.rest + kN - 1) / kN);
+    const int64_t rows = (int64_t)a.batch * a.tokens, items = (int64_t)a.all_units * heads;
+    a.rows_each = items >= kItems ? 1 : (int)(kItems / items < 16 ? kItems / items : 16);
+    const int64_t blocks = (rows + a.rows_each - 1) / a.rows_each;
     if (blocks >= (1 << 24)) return PRUNER_EINVAL;   // (a launch is below 2^24 workgroups of 256 threads)
-    const int heads = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
-    int64_t each = threads * (a.heads[0] + a.heads[1]) / kThreads;
-    each = each < 1 ? 1 : each > 8 ? 8 : each;
-    while ((a.heads[0] + a.heads[1]) / each > 60000) each *= 2;   // (a launch has at most 65535 workgroups in its second axis)
-    a.each = (int)(each < heads ? each : heads);
-    const int groups = (a.heads[0] + a.each - 1) / a.each + (a.heads[1] + a.each - 1) / a.each;
-    const dim3 grid((unsigned)blocks, (unsigned)groups);
-    const bool once = rows * (a.heads[0] + a.heads[1]) * a.head_dim * (int64_t)sizeof(T) > kCached;
-    void (*const kernel)(Call, int) = side_by_side ? (once ? turn_kernel<T, true, true> : turn_kernel<T, true, false>) : once ? turn_kernel<T, false, true> : turn_kernel<T, false, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, rows_each);
+    const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > (a.head_dim * sizeof(T) % 128 ? kCachedParts : kCachedLines);
+    void (*const kernel)(Call) = side_by_side ? (once ? turn_kernel<T, true, true> : turn_kernel<T, true, false>) : once ? turn_kernel<T, false, true> : turn_kernel<T, false, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), (size_t)a.rows_each * (sizeof(RowAt) + (size_t)a.pairs * 8), st, a);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
