@@ -544,7 +544,7 @@ int pruner_rotary_grad(const pruner_rotation* r, const pruner_heads* dq_out, con
  *   q_len  device int32 [batch] or NULL: tokens for all (values outside 0..tokens are clamped);  k_len  device int32 [batch] or NULL: q_len (sequences begin)
  * pruner_cache_restore reads tokens 0 .. k_len[b] - 1 back (k_len NULL: tokens for all; clamped to 0..tokens); rows from there on are zeros.  Values are exact
  * within the type's range.  tokens up to seq_pages x page_tokens.
- * No workspace.  2 x batch x kv_heads x (pages that a call's tokens can touch) below 2^24.  Errors: PRUNER_EINVAL.
+ * No workspace.  batch x kv_heads x (pages that a call's tokens can touch) below 2^24.  Errors: PRUNER_EINVAL.
  *
  * pruner_cache_attention is pruner_rel_attention over a cache: the same formulas, masks, biases, types and limits (head_dim a multiple of 16; a->kv_heads and
  * a->head_dim are the cache's; a->k_tokens at most seq_pages x page_tokens), q, o and lse as there.  Tokens of a page that is not there are not seen; a NaN among the codes of
