@@ -2,7 +2,8 @@
 
 The cost model's dataflow branch reads the data-movement blocks of a schedule in their order.  Here a small model of that kind (an
 embedding, one attention block with a learned relative position bias, one feed-forward block, a pooled score) is trained to rank
-candidates, its Siamese copy follows by momentum, and a sequence is scored as it grows, token by token against a cache:
+candidates, its Siamese copy follows by momentum, and a sequence is scored as it grows, token by token against a cache, in 16 bits or in what a served
+model keeps (weights in 4 bits, keys and values in 8):
 
     python examples/flow_block.py [--steps 60] [--candidates 512]
 
@@ -114,6 +115,22 @@ class FlowModel:
             out.append(P.rel_attention(q.view(1, 1, self.heads, self.head_dim), cache[0], cache[1], past, self.edges, q_len=one, k_len=one * (t + 1), causal=True).view(1, -1))
         return torch.cat(out)
 
+    def grow_small(self, flows):
+        """As grow, for several candidates side by side [candidates, blocks, 23], with what a served model keeps: weights in 4 bits, and keys and values in 8 bits in pages of one pool."""
+        w, p = self.weight, self.p
+        batch, tokens, _ = flows.shape
+        embed, qkv = P.weights_pack(w("embed")), P.weights_pack(w("qkv"))
+        past = w("table")[: len(self.edges) + 1].contiguous()
+        cache = P.new_cache(batch * -(-tokens // 16), self.heads, self.head_dim, -(-tokens // 16), page_tokens=16)
+        one, out = torch.ones(batch, dtype=torch.int32, device="cuda"), []
+        for t in range(tokens):
+            x = P.weights_linear(flows[:, t].to(self.dtype), embed)
+            _, y, _ = P.gated_norm(x, None, None, p["pre1"])
+            q, k, v = P.weights_linear(y, qkv).view(batch, 1, 3, self.heads, self.head_dim).unbind(2)
+            P.cache_append(cache, k, v, k_len=one * (t + 1))
+            out.append(P.cache_attention(q, cache, past, self.edges, k_len=one * (t + 1)).view(batch, 1, -1))
+        return torch.cat(out, 1)
+
 
 def rank_loss(score, latency, group):
     """Pairs of one task's candidates: the faster one is to score higher; the mean of log(1 + exp(-(difference))) and its gradient."""
@@ -165,6 +182,9 @@ def main():
     print(f"siamese weights follow at a distance of {(siamese - model.phi).norm().item():.3f}")
     grown = model.grow(synthetic(1, 8, 1)[0][0])
     print(f"one candidate's blocks as they arrive: {grown.shape[0]} outputs of {grown.shape[1]}")
+    flows = synthetic(16, 8, 1)[0]
+    small = model.grow_small(flows)
+    print(f"the same from weights in 4 bits and a cache in 8, {flows.shape[0]} candidates at once: off by {((small[0] - model.grow(flows[0])).norm() / model.grow(flows[0]).norm()).item():.2f} of themselves")
 
 
 if __name__ == "__main__":

@@ -564,7 +564,7 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
 // ---- the parts of a key axis that was cut
 
 // A row's DP columns, four to a thread, by `groups` threads that take every so many parts and meet in LDS: few rows of many parts would leave one thread to go through all of them in turn (8 rows of
-// 118 parts: 95 us a call where ...).
+// 118 parts: 54 us a call where this takes 18).
 template <typename T, int DP> __global__ void __launch_bounds__(256) join_groups_kernel(Args a, Heads out, float* __restrict__ lse, Parts parts, int groups)
 {
     constexpr int kFours = DP / 4;
@@ -646,6 +646,15 @@ Plan plan_of(const pruner_attention* a)
 
 template <typename T, int DP, int CT> int run_tokens(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
 {
+    static PerDeviceFlag ready;
+    const int dev = current_device(nullptr);
+    if (dev < 0) return PRUNER_EHIP;
+    if (!ready.get(dev)) {
+        for (const void* fn : {reinterpret_cast<const void*>(&tokens_kernel<T, DP, CT, false, false>), reinterpret_cast<const void*>(&tokens_kernel<T, DP, CT, true, false>),
+                               reinterpret_cast<const void*>(&tokens_kernel<T, DP, CT, true, true>)})
+            if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+        ready.mark(dev);
+    }
     const size_t biases = (size_t)BiasLds(args).bytes(), last = Meeting<DP>::bytes(args.q_tokens * args.group);
     const bool once = 2 * (int64_t)args.batch * args.kv_heads * args.k_tokens * args.head_dim > cache::kCached;
     void (*const kernel)(Args, cache::Cache, Heads, float*, Parts) = c.page_tokens() < kTile ? tokens_kernel<T, DP, CT, false, false> : once ? tokens_kernel<T, DP, CT, true, true> : tokens_kernel<T, DP, CT, true, false>;

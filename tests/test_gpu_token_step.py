@@ -1,5 +1,8 @@
 """The operators of a token step together, as a served model uses them: against the definitions in 64 bits, with what each step rounds; captured and replayed; what calls on a given stream
 allocate; the kernels that only large calls reach."""
+import os
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -7,6 +10,8 @@ import torch
 import block_reference as block
 import paper_2402_02361_amd as P
 import token_reference as ref
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
 
 pytestmark = pytest.mark.gpu
 BF, HALF, F32 = torch.bfloat16, torch.float16, torch.float32
@@ -129,6 +134,21 @@ def test_on_a_given_stream():
     junk = [torch.full((1 << b,), float("nan"), device="cuda") for b in range(22, 6, -1) for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(got, want) and all(j.isnan().all() for j in junk)
+
+
+def test_the_example_of_a_sequence_that_grows():
+    """With weights that 4 bits hold exactly, what is left between the example's two ways are roundings of keys and values to 8 bits: half a step, 2^-4, of a value and of a score's terms."""
+    from flow_block import FlowModel, synthetic
+    model = FlowModel(seed=7)
+    for name in ("embed", "qkv"):
+        packed = P.weights_pack(model.weight(name))
+        model.p[name].copy_(P.weights_restore(packed, BF))
+        # (restored values round to bfloat16, so packing them again may differ by that: 2^-8 of a weight)
+    flows = synthetic(5, 8, 8)[0]
+    small = model.grow_small(flows)
+    for i in range(5):
+        want = model.grow(flows[i]).float()
+        assert (small[i].float() - want).abs().max() <= 0.25 * want.abs().max() and (small[i].float() - want).norm() <= 0.1 * want.norm()
 
 
 # ---- kernels that only large calls reach

@@ -99,6 +99,16 @@ def test_many_outputs_inputs_and_rows(dtype, rows, n_out, dim, group):
     _check(dtype, rows, n_out, dim, group, bias=True, seed=1)
 
 
+def test_inputs_below_the_smallest_normal_number():
+    """binary16 below 2^-14, and sums of them that are normal: nothing is taken for 0."""
+    rng = np.random.default_rng(9)
+    packed = P.weights_pack(torch.from_numpy(rng.standard_normal((64, 256)) * 300).float().cuda())
+    x = torch.from_numpy(rng.integers(-1000, 1000, (3, 256)) * 2.0 ** -24).half().cuda()
+    dense = ref.cpu(P.weights_restore(packed, F32))
+    want, size = ref.cpu(x) @ dense.T, np.abs(ref.cpu(x)) @ np.abs(dense).T
+    assert (np.abs(ref.cpu(P.weights_linear(x, packed)) - want) <= 1.01 * ref.UNIT[HALF] * np.abs(want) + 256 * 2 * ref.F32 * size + ref.TINY[HALF]).all()
+
+
 def test_rows_are_each_for_itself():
     """The same bits whatever the other rows are, up to the rows that a workgroup takes: one row of sixteen, a NaN among the others."""
     x, packed, y = _check(BF, 16, 100, 600, 64, seed=2)
