@@ -812,15 +812,25 @@ def rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, trained=None, low=1
     return f * (kept + (1.0 - kept) / factor)
 
 
+def _dense_heads(t, tokens, heads, head_dim):
+    """A contiguous tensor [batch, tokens, heads, head_dim] as a pruner_heads."""
+    return _PACK_HEADS.pack(t.data_ptr(), tokens * heads * head_dim, heads * head_dim, head_dim)
+
+
 def _rotary(name, q, k, freqs, positions, q_len, k_len, interleaved, amplitude, out, stream):
     import torch
     lib = load_library()
     batch, tokens, q_heads, head_dim = q.shape
-    assert q.is_cuda, "q"
-    assert k is None or (k.is_cuda and k.dtype == q.dtype and k.dim() == 4 and k.shape[:2] == q.shape[:2] and k.shape[3] == head_dim), "k"
+    dtype, kv_heads, in_k, out_k = q.dtype, 0, None, None
+    in_q = _heads(q, "q")
+    if k is not None:
+        k_batch, k_rows, kv_heads, k_dim = k.shape
+        assert k.dtype == dtype and k_batch == batch and k_rows == tokens and k_dim == head_dim, "k"
+        in_k = _heads(k, "k")
     if not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
         freqs = np.ascontiguousarray(freqs, dtype=np.float64)
-    assert freqs.ndim == 1 and 2 <= 2 * len(freqs) <= head_dim, "freqs"
+    pairs = len(freqs)
+    assert freqs.ndim == 1 and 2 <= 2 * pairs <= head_dim, "freqs"
     if positions is not None:
         assert positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == (batch, tokens), "positions"
     if out is None:
@@ -828,13 +838,19 @@ def _rotary(name, q, k, freqs, positions, q_len, k_len, interleaved, amplitude, 
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k is not None else None
         _returned(stream, q_out, k_out)
+        out_q = _dense_heads(q_out, tokens, q_heads, head_dim)
+        if k is not None:
+            out_k = _dense_heads(k_out, tokens, kv_heads, head_dim)
     else:
         q_out, k_out = out
-        assert q_out.is_cuda and q_out.shape == q.shape and q_out.dtype == q.dtype, "out"
-        assert (k is None) == (k_out is None) and (k is None or (k_out.is_cuda and k_out.shape == k.shape and k_out.dtype == k.dtype)), "out"
-    r = _PACK_ROTATION.pack(_dtype(q.dtype), batch, tokens, q_heads, k.shape[2] if k is not None else 0, head_dim, 2 * len(freqs), _ROTARY_INTERLEAVED if interleaved else 0, amplitude,
+        assert q_out.shape == q.shape and q_out.dtype == dtype, "out"
+        assert (k is None) == (k_out is None) and (k is None or (k_out.shape == k.shape and k_out.dtype == dtype)), "out"
+        out_q = _heads(q_out, "out")
+        if k is not None:
+            out_k = _heads(k_out, "out")
+    r = _PACK_ROTATION.pack(_dtype(dtype), batch, tokens, q_heads, kv_heads, head_dim, 2 * pairs, _ROTARY_INTERLEAVED if interleaved else 0, amplitude,
                             freqs.__array_interface__["data"][0], positions.data_ptr() if positions is not None else 0, _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"))
-    rc = getattr(lib, name)(r, _heads(q, "q"), _heads(k, "k") if k is not None else None, _heads(q_out, "out"), _heads(k_out, "out") if k is not None else None, _stream_on(stream, q))
+    rc = getattr(lib, name)(r, in_q, in_k, out_q, out_k, _stream_on(stream, q))
     if rc:
         raise PrunerError(rc, name)
     return q_out, k_out
@@ -869,17 +885,19 @@ def _c_cache(cache, batch):
     """(the struct, kv_heads, head_dim, the tokens that a sequence has room for)"""
     import torch
     k, v, k_exps, v_exps, table = cache
+    uint8 = torch.uint8
     pages, kv_heads, units, page_tokens, unit = k.shape
     head_dim = 16 * units
-    assert k.is_cuda and k.dtype == torch.uint8 and k.is_contiguous() and unit == 16, "k_codes"
-    assert v.is_cuda and v.dtype == torch.uint8 and v.is_contiguous() and v.shape == (pages, kv_heads, page_tokens // 16, head_dim, 16), "v_codes"
-    for t, what in ((k_exps, "k_exps"), (v_exps, "v_exps")):
-        assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.shape == (pages, kv_heads), what
-    if isinstance(table, int):
-        at, seq_pages = 0, table
-    else:
-        assert table.is_cuda and table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2 and table.shape[0] == batch, "table"
-        at, seq_pages = table.data_ptr(), table.shape[1]
+    assert k.is_cuda and k.dtype == uint8 and k.is_contiguous() and unit == 16, "k_codes"
+    assert v.is_cuda and v.dtype == uint8 and v.is_contiguous() and v.shape == (pages, kv_heads, page_tokens // 16, head_dim, 16), "v_codes"
+    heads = (pages, kv_heads)
+    assert k_exps.is_cuda and k_exps.dtype == uint8 and k_exps.is_contiguous() and k_exps.shape == heads, "k_exps"
+    assert v_exps.is_cuda and v_exps.dtype == uint8 and v_exps.is_contiguous() and v_exps.shape == heads, "v_exps"
+    at, seq_pages = 0, table
+    if not isinstance(table, int):
+        rows, seq_pages = table.shape
+        assert table.is_cuda and table.dtype == torch.int32 and table.is_contiguous() and rows == batch, "table"
+        at = table.data_ptr()
     return (_PACK_CACHE.pack(k.data_ptr(), v.data_ptr(), k_exps.data_ptr(), v_exps.data_ptr(), at, pages, page_tokens, kv_heads, head_dim, seq_pages), kv_heads, head_dim,
             seq_pages * page_tokens)
 
@@ -888,9 +906,9 @@ def cache_append(cache, k, v, q_len=None, k_len=None, stream=None):
     """pruner_cache_append: row t of k and v (bfloat16, float16 or float32 CUDA [batch, tokens, kv_heads, head_dim], any strides with contiguous heads) becomes token k_len - q_len + t
     of its sequence, t < q_len.  q_len, k_len: int32 CUDA [batch]; q_len None: tokens, k_len None: q_len."""
     lib = load_library()
-    batch, tokens = k.shape[:2]
+    batch, tokens, k_heads, k_dim = k.shape
     c, kv_heads, head_dim, _ = _c_cache(cache, batch)
-    assert k.shape == (batch, tokens, kv_heads, head_dim) and v.shape == k.shape and v.dtype == k.dtype, "k, v"
+    assert k_heads == kv_heads and k_dim == head_dim and v.shape == k.shape and v.dtype == k.dtype, "k, v"
     rc = lib.pruner_cache_append(c, _dtype(k.dtype), batch, tokens, _heads(k, "k"), _heads(v, "v"), _lengths(q_len, batch, "q_len"), _lengths(k_len, batch, "k_len"), _stream_on(stream, k))
     if rc:
         raise PrunerError(rc, "pruner_cache_append")
@@ -906,7 +924,8 @@ def cache_restore(cache, tokens, k_len, dtype, stream=None):
         k = torch.empty((batch, tokens, kv_heads, head_dim), dtype=dtype, device=k_len.device)
         v = torch.empty_like(k)
     _returned(stream, k, v)
-    rc = lib.pruner_cache_restore(c, _dtype(dtype), batch, tokens, _lengths(k_len, batch, "k_len"), _heads(k, "k"), _heads(v, "v"), _stream_on(stream, k_len))
+    rc = lib.pruner_cache_restore(c, _dtype(dtype), batch, tokens, _lengths(k_len, batch, "k_len"), _dense_heads(k, tokens, kv_heads, head_dim), _dense_heads(v, tokens, kv_heads, head_dim),
+                                  _stream_on(stream, k_len))
     if rc:
         raise PrunerError(rc, "pruner_cache_restore")
     return k, v
@@ -920,17 +939,23 @@ def cache_attention(q, cache, table=None, edges=None, q_len=None, k_len=None, ca
     lib = load_library()
     batch, q_tokens, q_heads, head_dim = q.shape
     c, kv_heads, width, room = _c_cache(cache, batch)
-    assert q.is_cuda and head_dim == width, "q"
+    assert head_dim == width, "q"
+    in_q = _heads(q, "q")
     a, held_edges = _c_attention_of(q, room if k_tokens is None else k_tokens, kv_heads, table, edges, q_len, k_len, causal, scale)
     made_o = o is None
     with _made_on(stream):
         if made_o:
             o = torch.empty_like(q, memory_format=torch.contiguous_format)
         lse = torch.empty((batch, q_heads, q_tokens), dtype=torch.float32, device=q.device) if want_lse else None
-    _returned(stream, o if made_o else None, lse)
-    assert o.shape == q.shape and o.dtype == q.dtype, "o"
+    if made_o:
+        out_o = _dense_heads(o, q_tokens, q_heads, head_dim)
+        _returned(stream, o, lse)
+    else:
+        assert o.shape == q.shape and o.dtype == q.dtype, "o"
+        out_o = _heads(o, "o")
+        _returned(stream, lse)
     held, ws, size = _scratch(workspace, lib.pruner_cache_attention_workspace_bytes(a), q.device, stream)
-    rc = lib.pruner_cache_attention(a, c, _heads(q, "q"), _heads(o, "o"), _ptr(lse), ws, size, _stream_on(stream, q))
+    rc = lib.pruner_cache_attention(a, c, in_q, out_o, lse.data_ptr() if want_lse else None, ws, size, _stream_on(stream, q))
     if rc:
         raise PrunerError(rc, "pruner_cache_attention")
     return (o, lse) if want_lse else o
@@ -984,17 +1009,18 @@ def weights_restore(packed, dtype=None, w=None, stream=None):
 def weights_linear(x, packed, bias=None, y=None, stream=None):
     """pruner_weights_linear: y = x W^T + bias.  x: bfloat16 or float16 CUDA [rows, dim] (rows may be further apart), packed: PackedWeights, bias float32 [n_out] or None.
     Returns y [rows, n_out]."""
-    import torch
     lib = load_library()
     p, pitch = _rows_of(x, "x")
     rows, dim = x.shape
     assert dim == packed.dim, "x"
     if y is None:
         with _made_on(stream):
-            y = torch.empty((rows, packed.n_out), dtype=x.dtype, device=x.device)
+            y = x.new_empty((rows, packed.n_out))
         _returned(stream, y)
-    assert y.shape == (rows, packed.n_out) and y.dtype == x.dtype, "y"
-    py, y_pitch = _rows_of(y, "y")
+        py, y_pitch = y.data_ptr(), packed.n_out
+    else:
+        assert y.shape == (rows, packed.n_out) and y.dtype == x.dtype, "y"
+        py, y_pitch = _rows_of(y, "y")
     rc = lib.pruner_weights_linear(_c_weights(packed), p, _dtype(x.dtype), rows, pitch, _vector(bias, packed.n_out, "bias") if bias is not None else None, py, y_pitch, _stream_on(stream, x))
     if rc:
         raise PrunerError(rc, "pruner_weights_linear")
