@@ -206,9 +206,9 @@ size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 bool rows_ok(const pruner_heads* h, int32_t dtype) { return h && h->p && aligned(h->p, size_of(dtype)) && h->batch >= 0 && h->token >= 0 && h->head >= 0; }
 Rows rows_of(const pruner_heads* h) { return Rows{static_cast<char*>(h->p), h->batch, h->token, h->head}; }
 
-// Bytes of input from which on accesses go past the caches: rows of whole lines, others.  (us a call past them and not, outputs kept: 168 MB of bfloat16 in, heads of 128, 64 and 70, 126 MB 48 and 53, 42 MB
-// 21 and 24; binary32, heads of 128, 336 MB 112 and 125, of 100, 54 MB 32 and 30; with loads alone past them 168 MB 67.)
-constexpr int64_t kCachedLines = 32 << 20, kCachedParts = 128 << 20;
+// Bytes of input from which on accesses go past the caches: half of the last one.  (us a call past them and not: heads of 128 in bfloat16, 168 MB, 64 and 70; 42 MB 21 and 24 where results lie in new memory
+// each time, 20 and 17 where they find the last call's; heads of 100 in binary32, 54 MB, 32 and 30; with loads alone past them 168 MB 67.)
+constexpr int64_t kCached = 128 << 20;
 // Units of a workgroup, about.  (1024, 2048 and 4096, us a call: 168 MB in 64, 69, 75; 54 MB in heads of 100 30, 30, 32.)
 constexpr int kItems = 1024;
 
@@ -222,7 +222,7 @@ template <typename T> int launch(Call& a, bool side_by_side, bool in_place, hipS
     a.rows_each = items >= kItems ? 1 : (int)(kItems / items < 16 ? kItems / items : 16);
     const int64_t blocks = (rows + a.rows_each - 1) / a.rows_each;
     if (blocks >= (1 << 24)) return PRUNER_EINVAL;   // (a launch is below 2^24 workgroups of 256 threads)
-    const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > (a.head_dim * sizeof(T) % 128 ? kCachedParts : kCachedLines);
+    const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > kCached;
     void (*const kernel)(Call) = side_by_side ? (once ? turn_kernel<T, true, true> : turn_kernel<T, true, false>) : once ? turn_kernel<T, false, true> : turn_kernel<T, false, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), (size_t)a.rows_each * (sizeof(RowAt) + (size_t)a.pairs * 8), st, a);
     PRUNER_LAUNCH_CHECK();
