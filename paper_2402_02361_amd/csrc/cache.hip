@@ -369,9 +369,8 @@ template <typename T, bool ONCE> __global__ void __launch_bounds__(256) restore_
     }
 }
 
-// Bytes of results from which on they go past the caches: half of the last one.  (us a call with 50 MB of them, past the caches and not: 23 and 26 where they lie in new memory each time, 22 and 19 where
-// they find the last call's.)
-constexpr int64_t kResults = 128 << 20;
+// Bytes of results from which on they go past the caches: a quarter of the last one.  (us of an append and a restore, past them and not: 50 MB of results 22 and 18, 67 MB 44 and 47.)
+constexpr int64_t kResults = 64 << 20;
 size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 bool rows_ok(const pruner_heads* h, int32_t dtype) { return h && h->p && aligned(h->p, size_of(dtype)) && h->batch >= 0 && h->token >= 0 && h->head >= 0; }
 Rows rows_of(const pruner_heads* h) { return Rows{static_cast<char*>(h->p), h->batch, h->token, h->head}; }
