@@ -1,5 +1,5 @@
-// What kernels of attention that go over the keys once have in common: the running softmax of a query, its parts' sums where the key axis is cut (by
-// wavefronts, or by workgroups), and the one launch that joins the latter.
+// What kernels of attention that go over the keys once have in common: the running softmax of a query, and what its parts leave where the key axis is cut, by wavefronts that meet in LDS or by
+// workgroups whose parts a later launch joins.
 #pragma once
 #include "rel_attention.h"
 
@@ -71,7 +71,6 @@ template <typename T, int DP> struct Running {
 };
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -ATT_INF : __builtin_fmaf(__builtin_amdgcn_logf(l), kLn2, m); }   // (logf: base 2)
-
 
 // Where a workgroup's four wavefronts, each of which has seen keys of its own for the same columns (query t of head hk * group + g is column t * group + g), leave what they have: a column's
 // (maximum, sum), and its weighted sums in rows of DP + 4 floats, so that neighbouring rows lie in other banks.

@@ -1,11 +1,19 @@
 // Attention over keys and values held in 8 bits in pages: pruner_rel_attention's formulas with k^ = code 2^e, v^ = code 2^e.
 //
-// S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16, as where keys are of 16 bits.  Codes go from memory straight to the lanes whose operands they become: which
-// key a row of the first product's operand is, is ours to choose, and with row 8 q + 4 half + j being key 16 half + 4 q + j of 32, a lane's sixteen scores are of
-// sixteen neighbouring keys, the depth that its sixteen bytes of values have.  The page's powers of two go in with the conversion.
-// The columns of a wavefront are 32 pairs of a query and a head that share a key head: query t of the group's head g is column t * group + g.
-//   tokens_kernel   at most 32 columns: the four wavefronts of a workgroup take 64 keys each in turn, and meet at the end
-//   chunk_kernel    more: 32 columns each
+// A column is a pair of a query and a head, of those that share a key head: query t of the group's head g is column t * group + g.  S^T = K Q^T leaves a column's scores in a few lanes, whose softmax runs
+// with a maximum and a sum, and the weights are the next product's operand as they stand (O^T += V^T P^T).  Which key a row of the first product's operand is, is ours to choose: a lane's sixteen
+// scores are made to be of sixteen neighbouring keys, the depth that sixteen bytes of values have.  A page's powers of two go in with the conversion, which is exact (binary16: within its range); the weights
+// are rounded to the operands' type for the second product, which is the rate of the matrix cores' 16-bit forms, and their sum is of the unrounded ones.
+//
+//   tokens_kernel       at most 32 columns, on v_mfma_f32_16x16x32: the four wavefronts of a workgroup take 64 keys each in turn and meet in LDS at the end.  Codes go from memory straight to the lanes whose
+//                       operands they become, 64 bytes a lane ahead of the products for keys and values each.  Products of 32 x 32 x 16 held half as many wavefronts and took 315 us where this takes 200.
+//                       Bound by memory: one token against 32 caches of up to 32768, 32 heads of 128 sharing 8, 195 to 200 us, 5.3 to 5.5 TB/s (a large copy: 5.2 read and written together);
+//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of up to 500 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 22.6.
+//   chunk_kernel        more columns, on v_mfma_f32_32x32x16: 32 of them to a wavefront.  The four wavefronts share tiles of 64 keys and values in LDS, which hold operands: a code is converted once for
+//                       128 columns, and the next tile's are parked among this one's scores and softmax (700 us where this takes 530).  Bound by the matrix cores, the exponentials between their
+//                       products and the clock under both: 2048 tokens against 16384, 32 heads of 128 sharing 8, 530 to 560 us, 920 to 970 TFLOP/s; 64 tokens against 30000 62 us.
+//                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer.)
+//   join_groups_kernel  the parts of a key axis that was split over workgroups.
 #include "attention_softmax.h"
 #include "cache.h"
 
@@ -492,7 +500,6 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
                 floatx16 s[2] = {zero16(), zero16()};
                 auto key = [&](int x) { return *reinterpret_cast<const u32x4*>(tile + (row_at ^ ((x / 2) << 5)) + (x % 2) * 32 * Tile<DP>::kRowBytes); };
                 Operands<2 * kSteps, 4> keys;
-                __builtin_amdgcn_s_setprio(0);
                 keys.start(key);
                 keys.products(key, [&](int x, u32x4 w) { s[x % 2] = mfma(w, qf[x / 2], s[x % 2], T{}); });
                 // (product x: depth step x / kBlocks of 16 keys in the scores' order, block x % kBlocks of 32 columns)
@@ -501,7 +508,6 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
                     return *reinterpret_cast<const u32x4*>(tile + Turn::kKeyBytes + (value_at ^ ((4 * (step / 2) + step % 2) << 4)) + d * 32 * Tile<kTile>::kRowBytes);
                 };
                 Operands<4 * kBlocks, 4> values;
-                __builtin_amdgcn_s_setprio(1);
                 next();
                 values.start(value);
                 const int there[2] = {WHOLE ? there_here - 16 * half : there_of[turn][half], WHOLE ? there_here - 32 - 16 * half : there_of[turn][2 + half]};
@@ -533,7 +539,6 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
                         for (int i = 0; i < 16; ++i) s[x][i] = i < left ? s[x][i] : -ATT_INF;
                     }
                 run.weigh(s, fused, a.scale, bias);
-                __builtin_amdgcn_s_setprio(0);
                 u32x4 weights{};
                 values.products(value, [&](int x, u32x4 w) {
                     const int step = x / kBlocks, d = x % kBlocks;
