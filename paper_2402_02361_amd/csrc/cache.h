@@ -25,13 +25,19 @@ struct Cache {
     int32_t pages, shift, kv_heads, head_dim, seq_pages;   // shift: a page has 1 << shift tokens
     __host__ __device__ __forceinline__ int page_tokens() const { return 1 << shift; }
     __host__ __device__ __forceinline__ int page_bytes() const { return head_dim << shift; }   // of a head
-    // The page that holds token at (0 .. seq_pages * page_tokens - 1) of sequence b, or -1: there is none.
-    __device__ __forceinline__ int page_of(int b, int at) const
+    // The number that stands for token at (0 .. seq_pages * page_tokens - 1) of sequence b, as it is in the table, and whether it is a page: apart, so that who asks ahead does not wait for it there.
+    __device__ __forceinline__ int number_of(int b, int at) const
     {
         const int64_t i = (int64_t)b * seq_pages + (at >> shift);
         typedef const __attribute__((address_space(4))) int32_t* read_only;   // (read by the scalar unit where all lanes ask for the same)
-        const int p = table ? *((read_only)(uintptr_t)table + i) : (int)i;
-        return (uint32_t)p < (uint32_t)pages ? p : -1;
+        return table ? *((read_only)(uintptr_t)table + i) : (int)i;
+    }
+    __device__ __forceinline__ bool is_page(int number) const { return (uint32_t)number < (uint32_t)pages; }
+    // The page that holds it, or -1: there is none.
+    __device__ __forceinline__ int page_of(int b, int at) const
+    {
+        const int p = number_of(b, at);
+        return is_page(p) ? p : -1;
     }
     __device__ __forceinline__ int64_t head_of(int page, int h) const { return (int64_t)page * kv_heads + h; }
     // From the begin of a page's head: column d of the key at a place, column d of the value at a place.

@@ -12,7 +12,8 @@
 //   chunk_kernel        more columns, on v_mfma_f32_32x32x16: 32 of them to a wavefront.  The four wavefronts share tiles of 64 keys and values in LDS, which hold operands: a code is converted once for
 //                       128 columns, and the next tile's are parked among this one's scores and softmax (700 us where this takes 530).  Bound by the matrix cores, the exponentials between their
 //                       products and the clock under both: 2048 tokens against 16384, 32 heads of 128 sharing 8, 530 to 560 us, 920 to 970 TFLOP/s; 64 tokens against 30000 62 us.
-//                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer.)
+//                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer; 64 columns to a wavefront, with the next tile's
+//                       scores among this one's exponentials, 690 us: its values move between the two halves of the registers.)
 //   join_groups_kernel  the parts of a key axis that was split over workgroups.
 #include "attention_softmax.h"
 #include "cache.h"
@@ -91,24 +92,23 @@ __device__ __forceinline__ float sum_of_rows(float v)
 template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
     static constexpr int kChunks = (DP + 63) / 64, kBlocks = DP / 16;
     u32x4 k[4][kChunks], v[kBlocks];
-    float k_scale, v_scale;
-    int k_page, v_page, there;
+    int k_byte, v_byte, k_page, v_page, there;   // (exponents and pages as memory has them: what is asked for ahead is looked at when it is used.  16 sequences of up to 5003 in pages of 16, us a call, without and with: 24.9 and 23.7)
     __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most, int lane)   // most: the sequences' room (their lengths may still be on the way)
     {
         if constexpr (WHOLE) {
-            k_page = v_page = key0 < most ? c.page_of(b, key0) : -1;
+            k_page = v_page = key0 < most ? c.number_of(b, key0) : -1;
         } else {
             const int k_at = key0 + 16 * (lane >> 2 & 3), v_at = key0 + 16 * (lane >> 4);
-            k_page = k_at < most ? c.page_of(b, k_at) : -1;
-            v_page = v_at < most ? c.page_of(b, v_at) : -1;
+            k_page = k_at < most ? c.number_of(b, k_at) : -1;
+            v_page = v_at < most ? c.number_of(b, v_at) : -1;
         }
     }
     __device__ __forceinline__ void load_keys(const cache::Cache& c, int h, int key0, int lane)
     {
-        const int64_t head = c.head_of(k_page < 0 ? 0 : k_page, h);
+        const int64_t head = c.head_of(c.is_page(k_page) ? k_page : 0, h);
         const int g = lane >> 4, in = c.page_tokens() - 1, place = WHOLE ? key0 & in : (key0 + 16 * (lane >> 2 & 3)) & in, units = c.head_dim / cache::kUnit;
         const uint8_t* const p = c.k + head * c.page_bytes() + 16 * place;
-        k_scale = cache::two_to(c.k_exps[head]);
+        k_byte = c.k_exps[head];
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int unit = 4 * i + g < units ? 4 * i + g : units - 1;   // (past the last one: the query's columns are 0 there)
@@ -124,11 +124,11 @@ template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
     }
     __device__ __forceinline__ void load_values(const cache::Cache& c, int h, int key0, int kl, int lane)
     {
-        const int64_t head = c.head_of(v_page < 0 ? 0 : v_page, h);
+        const int64_t head = c.head_of(c.is_page(v_page) ? v_page : 0, h);
         const int g = lane >> 4, in = c.page_tokens() - 1, place = WHOLE ? key0 & in : (key0 + 16 * g) & in, units = c.head_dim / cache::kUnit, left = kl - (key0 + 16 * g);
-        there = v_page < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+        there = !c.is_page(v_page) || left < 0 ? 0 : left < 16 ? left : 16;
         const uint8_t* const p = c.v + head * c.page_bytes() + place * c.head_dim;
-        v_scale = cache::two_to(c.v_exps[head]);
+        v_byte = c.v_exps[head];
         const uint32_t at = 16 * ((WHOLE ? g * c.head_dim : 0) + (lane & 15));
         // (columns past the last are not stored)
         if constexpr (ONCE) {
@@ -226,6 +226,7 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
         }
         for (; key0 < end; key0 += kStep) {
             f32x4 s[CT][4];
+            const float k_scale = cache::two_to(codes.k_byte);
 #pragma unroll
             for (int x = 0; x < CT; ++x)
 #pragma unroll
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
             for (int i = 0; i < 2 * kChunks; ++i)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const u32x4 row = cache::eight_from<T>(codes.k[u][i / 2][2 * (i % 2)], codes.k[u][i / 2][2 * (i % 2) + 1], codes.k_scale);
+                    const u32x4 row = cache::eight_from<T>(codes.k[u][i / 2][2 * (i % 2)], codes.k[u][i / 2][2 * (i % 2) + 1], k_scale);
 #pragma unroll
                     for (int x = 0; x < CT; ++x) s[x][u] = mfma16(row, qf[x][i], s[x][u], T{});
                 }
@@ -304,11 +305,12 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
                     w[x][u] = u32x4{pair_of(s[x][2 * u][0], s[x][2 * u][1], T{}), pair_of(s[x][2 * u][2], s[x][2 * u][3], T{}), pair_of(s[x][2 * u + 1][0], s[x][2 * u + 1][1], T{}),
                                     pair_of(s[x][2 * u + 1][2], s[x][2 * u + 1][3], T{})};
             }
+            const float v_scale = cache::two_to(codes.v_byte);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < kBlocks; ++i) {
-                    const u32x4 row = cache::eight_from<T>(codes.v[i][2 * u], codes.v[i][2 * u + 1], codes.v_scale);
+                    const u32x4 row = cache::eight_from<T>(codes.v[i][2 * u], codes.v[i][2 * u + 1], v_scale);
 #pragma unroll
                     for (int x = 0; x < CT; ++x) o[x][i] = mfma16(row, w[x][u], o[x][i], T{});
                 }
@@ -342,8 +344,7 @@ template <typename T, int DP, bool WHOLE> struct Shared {
     static_assert(kTile == 64 && DP <= 128, "a wavefront's lanes are the keys of a tile; a thread's second chunk is four units of keys, two of values further");
     static constexpr int kLoads = kEach > 0 ? kEach : 1;   // (32 columns: half of the threads have a chunk)
     u32x4 k[kLoads], v[kLoads];
-    float k_scale, v_scale[kLoads];
-    int k_page, v_page[kLoads];
+    int k_byte, v_byte[kLoads], k_page, v_page[kLoads];   // (as in Few)
     int there[kLoads];               // tokens of a chunk of values (WHOLE: of the 64)
     int unit, group, d, k_at, v_at;  // this thread's first chunks: unit of columns of a key, of tokens of column d; where they are parked
     uint32_t k_from, v_from;         // WHOLE: where they lie behind the step's first key, or token
@@ -363,23 +364,23 @@ template <typename T, int DP, bool WHOLE> struct Shared {
     __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most)   // most: the sequences' room
     {
         if constexpr (WHOLE) {
-            k_page = key0 < most ? c.page_of(b, key0) : -1;
+            k_page = key0 < most ? c.number_of(b, key0) : -1;
         } else {
             const int at = key0 + ((int)threadIdx.x & 63);
-            k_page = at < most ? c.page_of(b, at) : -1;
+            k_page = at < most ? c.number_of(b, at) : -1;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int first = key0 + 16 * (group + 2 * i);
-                v_page[i] = has_values() && first < most ? c.page_of(b, first) : -1;
+                v_page[i] = has_values() && first < most ? c.number_of(b, first) : -1;
             }
         }
     }
     __device__ __forceinline__ void load(const cache::Cache& c, int h, int key0, int kl)
     {
         const int in = c.page_tokens() - 1, units = c.head_dim / cache::kUnit;
-        const int64_t head = c.head_of(k_page < 0 ? 0 : k_page, h);
+        const int64_t head = c.head_of(c.is_page(k_page) ? k_page : 0, h);
         const uint8_t* const p = c.k + head * c.page_bytes() + (WHOLE ? 16 * (key0 & in) : 16 * ((key0 + ((int)threadIdx.x & 63)) & in));
-        k_scale = cache::two_to(c.k_exps[head]);
+        k_byte = c.k_exps[head];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             k[i] = u32x4{0u, 0u, 0u, 0u};   // (columns past the last: a query's are 0 there)
@@ -387,8 +388,8 @@ template <typename T, int DP, bool WHOLE> struct Shared {
         }
         if constexpr (WHOLE) {
             const uint8_t* const q = c.v + head * c.page_bytes() + (key0 & in) * c.head_dim;
-            there[0] = k_page < 0 ? 0 : kl - key0;
-            v_scale[0] = cache::two_to(c.v_exps[head]);
+            there[0] = c.is_page(k_page) ? kl - key0 : 0;
+            v_byte[0] = c.v_exps[head];
             if (has_values())
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4*>(q + v_from + 32u * i * (uint32_t)c.head_dim);
@@ -396,17 +397,19 @@ template <typename T, int DP, bool WHOLE> struct Shared {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int first = key0 + 16 * (group + 2 * i);
-                there[i] = v_page[i] < 0 ? 0 : kl - first;
-                const int64_t of = c.head_of(v_page[i] < 0 ? 0 : v_page[i], h);
-                v_scale[i] = cache::two_to(c.v_exps[of]);
+                there[i] = c.is_page(v_page[i]) ? kl - first : 0;
+                const int64_t of = c.head_of(c.is_page(v_page[i]) ? v_page[i] : 0, h);
+                v_byte[i] = c.v_exps[of];
                 v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + (v_from - 16u * (uint32_t)(group * c.head_dim)));
             }
         }
     }
     __device__ __forceinline__ void park(char* tile, int* there_of)
     {
+        const float k_scale = cache::two_to(k_byte);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
+            const float v_scale = cache::two_to(v_byte[WHOLE ? 0 : i]);
             if (has_keys(i))
 #pragma unroll
                 for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4*>(tile + (k_at ^ (128 * i + 16 * u))) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
@@ -421,7 +424,7 @@ template <typename T, int DP, bool WHOLE> struct Shared {
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
-                    *reinterpret_cast<u32x4*>(tile + (v_at ^ (64 * i + 16 * u))) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale[WHOLE ? 0 : i]);
+                    *reinterpret_cast<u32x4*>(tile + (v_at ^ (64 * i + 16 * u))) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale);
                 if (!WHOLE && d == 0) there_of[group + 2 * i] = there[i];
             }
         }
