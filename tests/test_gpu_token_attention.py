@@ -6,6 +6,7 @@ import torch
 import block_reference as block
 import paper_2402_02361_amd as P
 import token_reference as ref
+from paper_2402_02361_amd import binding
 
 pytestmark = pytest.mark.gpu
 BF, HALF = torch.bfloat16, torch.float16
@@ -150,6 +151,24 @@ def test_large_groups_of_heads(q_heads, q_tokens):
 @pytest.mark.parametrize("q_tokens", [1, 100])
 def test_long_axes_in_parts(q_tokens):
     _check(BF, 2, q_tokens, 20000, 4, 2, 64, 64, 1, k_len=[20000, 513], seed=5)
+
+
+def _in_one_part(batch, q_tokens, k_tokens, heads, head_dim):
+    q = torch.empty(batch, q_tokens, heads, head_dim, dtype=BF, device="cuda")
+    a, _ = binding._c_attention_of(q, k_tokens, heads, None, None, None, None, True, 1.0)
+    return binding.load_library().pruner_cache_attention_workspace_bytes(a) == 0
+
+
+@pytest.mark.parametrize("page_tokens,dtype", [(64, BF), (256, HALF), (16, BF)])
+def test_long_axes_in_one_part(page_tokens, dtype):
+    """Many columns over more than 64 tiles of 64 keys, lengths that end about the 64th: what is known of 64 tiles at a time is asked for again."""
+    assert _in_one_part(8, 33, 4500, 64, 16)
+    _check(dtype, 8, 33, 4500, 64, 64, 16, page_tokens, sides=1, k_len=[4500, 4096, 4097, 4095, 4159, 4160, 64, 4224])
+
+
+def test_pages_that_are_not_there_on_a_long_axis():
+    assert _in_one_part(8, 33, 4500, 64, 16)
+    _check(BF, 8, 33, 4500, 64, 64, 16, 64, missing={(0, 0), (1, 63), (2, 64), (3, 66), (4, 65), (4, 67)})
 
 
 def test_no_edges_and_masks_through_the_table():
