@@ -151,6 +151,35 @@ def test_strides():
         assert all(torch.equal(x, y) for x, y in zip(cache[:4], want[:4]))
 
 
+@pytest.mark.parametrize("page_tokens", [16, 64])
+def test_sequences_that_share_a_full_page(page_tokens):
+    """The same as sequences with that page's tokens for themselves."""
+    rng = np.random.default_rng(17)
+    n, heads, d = page_tokens + 5, 2, 48
+    k, v = _new(rng, BF, 2, n, heads, d), _new(rng, BF, 2, n, heads, d)
+    k[1, :page_tokens], v[1, :page_tokens] = k[0, :page_tokens], v[0, :page_tokens]
+    shared, own = P.new_cache(4, heads, d, _ints([[2, 0], [2, 3]]), page_tokens), P.new_cache(4, heads, d, 2, page_tokens)
+    P.cache_append(own, k, v)
+    P.cache_append(shared, k[:, :page_tokens], v[:, :page_tokens], _ints([page_tokens, 0]), _ints([page_tokens, 0]))
+    P.cache_append(shared, k[:, page_tokens:], v[:, page_tokens:], None, _ints([n, n]))
+    lengths = _ints([n, n - 2])
+    for x, y in zip(P.cache_restore(shared, n, lengths, BF), P.cache_restore(own, n, lengths, BF)):
+        assert torch.equal(x, y)
+    for tokens in (1, 17, 40):   # (two rows to a key head, so few columns, and many)
+        q = _new(rng, BF, 2, tokens, 4, d)
+        assert torch.equal(P.cache_attention(q, shared, k_len=lengths), P.cache_attention(q, own, k_len=lengths))
+
+
+def test_the_end_of_binary16s_range():
+    """Values from 31/32 of 2^16 on round to 2^16, which binary16 does not have; what lies below rounds down to 15/16 of it."""
+    for x, want in ((65504.0, float("inf")), (63488.0, float("inf")), (63456.0, 61440.0)):
+        cache = P.new_cache(1, 1, 16, 1, 16)
+        t = torch.full((1, 1, 1, 16), x, dtype=HALF).cuda()
+        P.cache_append(cache, t, -t)
+        k, v = P.cache_restore(cache, 1, _ints([1]), HALF)
+        assert (k == want).all() and (v == -want).all()
+
+
 def test_pages_in_a_row_without_a_table():
     """A number of pages for a table: the same as the table that says so."""
     rng = np.random.default_rng(7)
