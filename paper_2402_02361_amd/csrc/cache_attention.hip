@@ -8,12 +8,12 @@
 //   tokens_kernel       at most 32 columns, on v_mfma_f32_16x16x32: the four wavefronts of a workgroup take 64 keys each in turn and meet in LDS at the end.  Codes go from memory straight to the lanes whose
 //                       operands they become, 64 bytes a lane ahead of the products for keys and values each.  Products of 32 x 32 x 16 held half as many wavefronts and took 315 us where this takes 200.
 //                       Bound by memory: one token against 32 caches of up to 32768, 32 heads of 128 sharing 8, 195 to 200 us, 5.3 to 5.5 TB/s (a large copy: 5.2 read and written together);
-//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of up to 500 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 21.4.
+//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of 300, 8 heads of 64, 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 21.4.
 //   codes_kernel        more columns, 32 to a wavefront, on v_mfma_f32_32x32x16, over pages of 64 tokens and more.  The four wavefronts share tiles of 64 keys and values in LDS, which are requested straight
 //                       to it as codes and converted by who reads them.  Bound by the matrix cores, the exponentials and conversions beside their products, and the clock under both: 2048 tokens against
 //                       16384, 32 heads of 128 sharing 8, 505 to 520 us, 990 to 1020 TFLOP/s; 2000 against 8000, 16 heads of 64 sharing 4, 127 us; 64 against 30000 58.
 //                       Converted tiles in LDS as below: 543, 138 and 61.  Codes in LDS without the next tile's scores among this one's weights 542 (three wavefronts to a SIMD, by scores of 32 keys, 557);
-//                       those with requests and pages asked for between the steps 545; a wavefront's registers moved about between steps were half of that.
+//                       with them, but a memory access for each tile's page, its requests all between the steps, and scores copied there from register to register, 545.
 //   chunk_kernel        the same over smaller pages: tiles in LDS hold operands, so that a code is converted once for 128 columns, and the next tile's are parked among this one's scores and softmax.
 //                       8 sequences of 100 tokens against up to 800 in pages of 16, 16 heads of 64 sharing 4, 27 us, by a workgroup's start and chain of tiles.
 //                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer; 64 columns to a wavefront a quarter longer.)
