@@ -46,6 +46,9 @@ struct Cache {
 };
 
 __device__ __forceinline__ float two_to(int byte) { return __uint_as_float((uint32_t)byte << 23); }   // 2^(byte - 127), byte 1..254
+// Of a page's values of which `there` are a sequence's tokens.  Of none: the page may be reserved and not yet written, or not there, and the byte anything; 255 is NaN to the scaled conversions whatever the
+// code is, and a weight of 0 does not take that away.
+__device__ __forceinline__ float two_to(int byte, int there) { return two_to(there > 0 ? byte : 127); }
 
 // Two codes (the low or the high half of a word) times a power of two, in the operands' type: exact but for binary16's range.
 template <bool HIGH> __device__ __forceinline__ uint32_t pair_from(uint32_t codes, float scale, __bf16)

@@ -142,7 +142,7 @@ template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
             for (int i = 0; i < kBlocks; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1));
         }
     }
-    __device__ __forceinline__ void clear_values()   // those that are not there
+    __device__ __forceinline__ void clear_values()   // those that are not there (their page's byte may be anything as well: see two_to)
     {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
                     w[x][u] = u32x4{pair_of(s[x][2 * u][0], s[x][2 * u][1], T{}), pair_of(s[x][2 * u][2], s[x][2 * u][3], T{}), pair_of(s[x][2 * u + 1][0], s[x][2 * u + 1][1], T{}),
                                     pair_of(s[x][2 * u + 1][2], s[x][2 * u + 1][3], T{})};
             }
-            const float v_scale = cache::two_to(codes.v_byte);
+            const float v_scale = cache::two_to(codes.v_byte, there);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -657,7 +657,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256, 2) codes_ke
 
 // 64 keys' codes on their way to a tile that four wavefronts share: a thread takes sixteen columns of a key, or tokens of a column, at a time, and parks them as operands' type: keys in rows of DP
 // columns, row 8 q + 4 h + j of a block of 32 being key 16 h + 4 q + j, so that a lane's sixteen scores are of sixteen neighbouring keys; values in rows of 64 tokens.  Rows past the sequence's end, or
-// whose page is not there, hold anything; of values they are cleared (their weight is 0, but anything may be a NaN).
+// whose page is not there, hold anything; of values they are cleared, and their page's byte is left out (their weight is 0, but anything may be a NaN).
 template <typename T, int DP> struct Shared {
     static constexpr int kEach = kTile * DP / 16 / 256, kKeyBytes = kTile * Tile<DP>::kRowBytes, kValueBytes = DP * Tile<kTile>::kRowBytes, kBytes = kKeyBytes + kValueBytes;
     static_assert(kTile == 64 && DP <= 128, "a wavefront's lanes are the keys of a tile; a thread's second chunk is four units of keys, two of values further");
@@ -714,7 +714,7 @@ template <typename T, int DP> struct Shared {
         const float k_scale = cache::two_to(k_byte);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const float v_scale = cache::two_to(v_byte[i]);
+            const float v_scale = cache::two_to(v_byte[i], there[i]);
             if (has_keys(i))
 #pragma unroll
                 for (int u = 0; u < 2; ++u) *reinterpret_cast<u32x4*>(tile + (k_at ^ (128 * i + 16 * u))) = cache::eight_from<T>(k[i][2 * u], k[i][2 * u + 1], k_scale);
