@@ -504,8 +504,8 @@ int pruner_rel_attention_grad(const pruner_attention* a, const pruner_heads* dou
  *   q, k, q_out, k_out  pruner_heads of any strides >= 0 (queries q_heads, keys kv_heads; a count of 0: none, its pointers are not read), head_dim contiguous, at their
  *                       type's size; an output may be its input (with the same strides), and overlaps it in no other way
  *   freqs               host double [rotary_dim / 2], |f| <= PRUNER_MAX_ROTARY_FREQUENCY
- *   positions           device int32 [batch][tokens], or NULL: token t of sequence b stands at k_len[b] - q_len[b] + t (k_len NULL: at t; q_len NULL: tokens).
- *                       Any value, negative ones too.
+ *   positions           device int32 [batch][tokens], or NULL: token t of sequence b stands at k_len[b] - q_len[b] + t (k_len NULL: at t; q_len NULL: tokens, values
+ *                       outside 0..tokens are clamped, as by the calls below).  Positions have any value, negative ones too.
  * Every one of the batch x tokens rows is turned.  head_dim 2..512, rotary_dim even, 2..min(head_dim, 256); batch x tokens below 2^30, heads up to 65535.
  * No workspace.  Errors: PRUNER_EINVAL.
  */

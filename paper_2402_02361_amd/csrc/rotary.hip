@@ -31,6 +31,12 @@ struct Call {
     float amplitude;
     int32_t back;
     uint64_t turn[PRUNER_MAX_ROTARY_DIM / 2];       // 2^-64 turns per position
+    __device__ __forceinline__ int queries(int b) const   // (as the cache and its attention take them)
+    {
+        if (!q_len) return tokens;
+        const int n = q_len[b];
+        return n < 0 ? 0 : n > tokens ? tokens : n;
+    }
 };
 
 // sin and cos of p times a pair's frequency.
@@ -93,7 +99,7 @@ template <typename T, bool SIDE_BY_SIDE, bool ONCE> __global__ void __launch_bou
     const int rows = all_rows - row0 < a.rows_each ? (int)(all_rows - row0) : a.rows_each;
     for (int i = threadIdx.x; i < rows * a.pairs; i += 256) {
         const int row = i / a.pairs, pair = i - row * a.pairs, b = (int)((row0 + row) / a.tokens), t = (int)((row0 + row) - (int64_t)b * a.tokens);
-        const int p = a.positions ? a.positions[row0 + row] : (int)((uint32_t)t + (a.k_len ? (uint32_t)a.k_len[b] - (uint32_t)(a.q_len ? a.q_len[b] : a.tokens) : 0u));
+        const int p = a.positions ? a.positions[row0 + row] : (int)((uint32_t)t + (a.k_len ? (uint32_t)a.k_len[b] - (uint32_t)a.queries(b) : 0u));
         float s, c;
         angle_of(a.turn[pair], p, s, c);
         angles[i] = f32x2{(a.back ? -s : s) * a.amplitude, c * a.amplitude};
