@@ -547,7 +547,8 @@ int pruner_rotary_grad(const pruner_rotation* r, const pruner_heads* dq_out, con
  * No workspace.  batch x kv_heads x (pages that a call's tokens can touch) below 2^24.  Errors: PRUNER_EINVAL.
  *
  * pruner_cache_attention is pruner_rel_attention over a cache: the same formulas, masks, biases, types and limits (head_dim a multiple of 16; a->kv_heads and
- * a->head_dim are the cache's; in binary16 what the cache holds lies within its range; a->k_tokens at most seq_pages x page_tokens), q, o and lse as there.  Tokens of a page that is not there are not seen; a NaN among the codes of
+ * a->head_dim are the cache's; in binary16 what the cache holds lies within its range; a->k_tokens at most seq_pages x page_tokens), q, o and lse as there; where q_tokens x q_heads / kv_heads is 32 or less, weights
+ * keep 2^-16 of themselves in the second product.  Tokens of a page that is not there are not seen; a NaN among the codes of
  * a sequence's tokens may reach every row of the sequence.  What lies behind a sequence's tokens does not matter.
  * workspace: pruner_cache_attention_workspace_bytes(a), which reads the sizes only.  Errors: PRUNER_EINVAL, PRUNER_EWORKSPACE.
  */

@@ -2,8 +2,9 @@
 //
 // A column is a pair of a query and a head, of those that share a key head: query t of the group's head g is column t * group + g.  S^T = K Q^T leaves a column's scores in a few lanes, whose softmax runs
 // with a maximum and a sum, and the weights are the next product's operand as they stand (O^T += V^T P^T).  Which key a row of the first product's operand is, is ours to choose: a lane's sixteen
-// scores are made to be of sixteen neighbouring keys, the depth that sixteen bytes of values have.  A page's powers of two go in with the conversion, which is exact (binary16: within its range); the weights
-// are rounded to the operands' type for the second product, which is the rate of the matrix cores' 16-bit forms, and their sum is of the unrounded ones.
+// scores are made to be of sixteen neighbouring keys, the depth that sixteen bytes of values have.  A page's powers of two go in with the conversion, which is exact (binary16: within its range).  The
+// second product is of 16-bit operands, the rate of the matrix cores; the weights' sum is of the unrounded ones.  Few columns have weights in two terms (bfloat16, off by 2^-16), for which there is room beside the
+// reading.  Of many columns they are rounded to the operands' type: two terms take 685 us where one takes 515 (2048 tokens against 16384, 32 heads of 128 sharing 8, one card).
 //
 //   tokens_kernel       at most 32 columns, on v_mfma_f32_16x16x32: the four wavefronts of a workgroup take 64 keys each in turn and meet in LDS at the end.  Codes go from memory straight to the lanes whose
 //                       operands they become, 64 bytes a lane ahead of the products for keys and values each.  Products of 32 x 32 x 16 held half as many wavefronts and took 315 us where this takes 200.
@@ -78,6 +79,20 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c, _Float16)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// Eight weights as sums of two bfloat16: the nearest one, and the nearest to what that leaves, so off by 2^-16 of the weight at most (2^-8 of 2^-8), however small it is.  One term would be off by 2^-8, one of
+// binary16 by 2^-11, and its smallest ones by all they are.
+struct TwoTerms {
+    u32x4 first, rest;
+    __device__ __forceinline__ void set(f32x4 a, f32x4 b)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = (i < 2 ? a : b)[2 * (i % 2)], y = (i < 2 ? a : b)[2 * (i % 2) + 1];
+            first[i] = pair_of(x, y, __bf16{});
+            rest[i] = pair_of(x - __uint_as_float(first[i] << 16), y - __uint_as_float(first[i] & 0xFFFF0000u), __bf16{});
+        }
+    }
+};
 // Of a lane and the three of the same column in the other rows of sixteen.
 __device__ __forceinline__ float max_of_rows(float v)
 {
@@ -93,7 +108,7 @@ __device__ __forceinline__ float sum_of_rows(float v)
 // 64 keys' codes: keys in four operands of 16 rows, row 4 u + j of operand t being key 16 u + 4 t + j, so that lane (n = lane & 15, g = lane >> 4) of the results has column n's scores of the sixteen
 // keys 16 g + 4 t + j; of values it has the sixteen of those keys.  WHOLE: the 64 keys lie in one page, whose place all lanes share.
 template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
-    static constexpr int kChunks = (DP + 63) / 64, kBlocks = DP / 16;
+    static constexpr int kChunks = (DP + 63) / 64, kBlocks = DP / 16, kSure = DP == 32 ? 1 : DP / 32 + 1;   // kSure: blocks of 16 columns that every head of this instance has; others may be past the last
     u32x4 k[4][kChunks], v[kBlocks];
     int k_byte, v_byte, k_page, v_page, there;   // (exponents and pages as memory has them: what is asked for ahead is looked at when it is used.  16 sequences of up to 5003 in pages of 16, us a call, without and with: 24.9 and 23.7)
     __device__ __forceinline__ void find(const cache::Cache& c, int b, int key0, int most, int lane)   // most: the sequences' room (their lengths may still be on the way)
@@ -133,14 +148,14 @@ template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
         const uint8_t* const p = c.v + head * c.page_bytes() + place * c.head_dim;
         v_byte = c.v_exps[head];
         const uint32_t at = 16 * ((WHOLE ? g * c.head_dim : 0) + (lane & 15));
-        // (columns past the last are not stored)
-        if constexpr (ONCE) {
 #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1)));
-        } else {
-#pragma unroll
-            for (int i = 0; i < kBlocks; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * (i < units ? i : units - 1));
-        }
+        for (int i = 0; i < kBlocks; ++i)
+            if (i < kSure || i < units) {
+                if constexpr (ONCE)
+                    v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + at + 256 * i));
+                else
+                    v[i] = *reinterpret_cast<const u32x4*>(p + at + 256 * i);
+            }
     }
     __device__ __forceinline__ void clear_values()   // those that are not there (their page's byte may be anything as well: see two_to)
     {
@@ -248,7 +263,6 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
             if (next < end) codes.load_keys(c, hk, next, lane);
             const int r_lo = key0 - (kl - ql + a.q_tokens - 1), r_hi = key0 + kTile - 1 - (kl - ql);
             const int place = a.table ? place_of(a, r_lo, r_hi) : kLeft;
-            u32x4 w[CT][2];
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 float shift = 0.f;
@@ -303,20 +317,21 @@ __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2))
                     }
                 }
                 l[x] += sum;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    w[x][u] = u32x4{pair_of(s[x][2 * u][0], s[x][2 * u][1], T{}), pair_of(s[x][2 * u][2], s[x][2 * u][3], T{}), pair_of(s[x][2 * u + 1][0], s[x][2 * u + 1][1], T{}),
-                                    pair_of(s[x][2 * u + 1][2], s[x][2 * u + 1][3], T{})};
             }
             const float v_scale = cache::two_to(codes.v_byte, there);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
+                TwoTerms w[CT];
 #pragma unroll
-                for (int i = 0; i < kBlocks; ++i) {
-                    const u32x4 row = cache::eight_from<T>(codes.v[i][2 * u], codes.v[i][2 * u + 1], v_scale);
+                for (int x = 0; x < CT; ++x) w[x].set(s[x][2 * u], s[x][2 * u + 1]);
 #pragma unroll
-                    for (int x = 0; x < CT; ++x) o[x][i] = mfma16(row, w[x][u], o[x][i], T{});
-                }
+                for (int i = 0; i < kBlocks; ++i)
+                    if (i < Step::kSure || 16 * i < a.head_dim) {
+                        const u32x4 row = cache::eight_from<__bf16>(codes.v[i][2 * u], codes.v[i][2 * u + 1], v_scale);
+#pragma unroll
+                        for (int x = 0; x < CT; ++x) o[x][i] = mfma16(row, w[x].rest, mfma16(row, w[x].first, o[x][i], __bf16{}), __bf16{});
+                    }
+            }
             if (next < end) {
                 codes.load_values(c, hk, next, kl, lane);
                 codes.find(c, b, next + kStep, a.k_tokens, lane);
@@ -884,7 +899,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) join_groups
     const int64_t row = (int64_t)blockIdx.x * each + threadIdx.x / kFours / groups;
     float m = -ATT_INF, total = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (row < rows)
+    if (row < rows && 4 * four < a.head_dim)
 #pragma unroll 4
         for (int n = group; n < parts.count; n += groups) {
             const float2 st = parts.stats[n * rows + row];
