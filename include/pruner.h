@@ -576,8 +576,8 @@ int pruner_cache_attention(const pruner_attention* a, const pruner_cache* c, con
  *   group   32, 64 or 128;  n_out and dim 1..2^24
  * pruner_weights_pack and pruner_weights_restore: w device [n_out][pitch] of any of the three types (restored values are rounded to it).
  * pruner_weights_linear: x device [rows][x_pitch], y device [rows][y_pitch], PRUNER_BF16 or PRUNER_F16; bias device float [n_out] or NULL; rows 0..PRUNER_MAX_LINEAR_ROWS (made for few: the
- * weights are read once for every 16 or 32).  Products with codes are exact and sums binary32, rounded once.  (bfloat16: sums are of x times 128 + code, less 136 times x: an
- * infinity in x gives a NaN, and so may values beyond 2^120.)
+ * weights are read once for every 16 or 32).  Products with codes are exact and sums binary32, rounded once.  (bfloat16: sums are of x times 128 + code, less 136 times x;
+ * where one is not finite, of x times code - 8.)
  * No workspace.  Errors: PRUNER_EINVAL (pointers; w, x, y at their type's size, bias 4 bytes; sizes, types, a pitch below the row).
  */
 #define PRUNER_MAX_LINEAR_ROWS (1 << 20)

@@ -51,6 +51,17 @@ __device__ __forceinline__ u32x4 operand(uint32_t w, _Float16)
     return r;
 }
 
+// Eight weights without their scale, code - 8, in bfloat16.
+__device__ __forceinline__ u32x4 weights_of(uint32_t w)
+{
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = pair_of((float)((int)(w >> (4 * i) & 15u) - kZero), (float)((int)(w >> (4 * i + 16) & 15u) - kZero), __bf16{});
+    return r;
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
+
 struct Call {
     const uint32_t* codes;
     const uint16_t* scales;
@@ -120,18 +131,76 @@ template <typename T, int GROUP, int RT, int CT, bool ONCE> struct Block {
 #pragma unroll
                     for (int c = 0; c < CT; ++c) sum[c] = mfma(o, x[c][u * kEach + e], e == 0 ? from[c] : sum[c], T{});
                 }
-                const f32x2 lo = pair_to(s[t][u][0]), hi = pair_to(s[t][u][1]);
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    acc[t][c][0] = __builtin_fmaf(lo[0], sum[c][0], acc[t][c][0]);
-                    acc[t][c][1] = __builtin_fmaf(lo[1], sum[c][1], acc[t][c][1]);
-                    acc[t][c][2] = __builtin_fmaf(hi[0], sum[c][2], acc[t][c][2]);
-                    acc[t][c][3] = __builtin_fmaf(hi[1], sum[c][3], acc[t][c][3]);
-                }
+                scaled(t, u, sum, acc[t]);
             }
         }
     }
+    __device__ __forceinline__ void scaled(int t, int u, const f32x4 (&sum)[CT], f32x4 (&acc)[CT]) const   // a group's sums, added up
+    {
+        const f32x2 lo = pair_to(s[t][u][0]), hi = pair_to(s[t][u][1]);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            acc[c][0] = __builtin_fmaf(lo[0], sum[c][0], acc[c][0]);
+            acc[c][1] = __builtin_fmaf(lo[1], sum[c][1], acc[c][1]);
+            acc[c][2] = __builtin_fmaf(hi[0], sum[c][2], acc[c][2]);
+            acc[c][3] = __builtin_fmaf(hi[1], sum[c][3], acc[c][3]);
+        }
+    }
 };
+
+// In bfloat16 the products above reach infinities of their own where x has one, or is so large that 143 of it are one: sums that came out not finite are made again, of x times 2^-16 and the weights without
+// their scale, which no finite x takes out of binary32's range before a group's sum is scaled.  (Others stay as they are, whatever other rows hold.)
+constexpr float kSmaller = 0x1p-16f;
+template <int GROUP, int RT, int CT, bool ONCE>
+__device__ __forceinline__ void again(const Call& a, const __bf16* const (&x_row)[CT], int tile0, int tiles, int wave, int waves, int lane, f32x4 (&acc)[RT][CT])
+{
+    using Turn = Block<__bf16, GROUP, RT, CT, ONCE>;
+    constexpr int kEach = GROUP / 32;
+    f32x4 made[RT][CT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) made[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int block = wave; block < a.blocks; block += waves) {
+        Turn now;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) now.x[c][j] = u32x4{0u, 0u, 0u, 0u};
+        now.load(a, x_row, tile0, tiles, block, lane);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 x = pair_to(now.x[c][j][i]);
+                    now.x[c][j][i] = pair_of(x[0] * kSmaller, x[1] * kSmaller, __bf16{});
+                }
+#pragma unroll
+        for (int u = 0; u < Turn::kGroups; ++u)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                f32x4 sum[CT];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) sum[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const u32x4 o = weights_of(now.w[t][u * kEach + e]);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) sum[c] = mfma(o, now.x[c][u * kEach + e], sum[c], __bf16{});
+                }
+                now.scaled(t, u, sum, made[t]);
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][c][e] = is_finite(acc[t][c][e]) ? acc[t][c][e] : made[t][c][e] * (1.f / kSmaller);
+}
 
 // ONCE: the weights are more than stays cached from one call to the next, and are read past it.
 template <typename T, int GROUP, int RT, int CT, bool ONCE> __global__ void __launch_bounds__(RT == 1 && CT == 1 ? 1024 : 512) linear_kernel(Call a)
@@ -165,6 +234,16 @@ template <typename T, int GROUP, int RT, int CT, bool ONCE> __global__ void __la
             if (block < a.blocks) on_way[n].add(acc);
             block += waves;
         }
+    }
+    if constexpr (__is_same(T, __bf16)) {
+        bool all = true;
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) all = all && is_finite(acc[t][c][e]);
+        if (!__all(all)) again<GROUP, RT, CT, ONCE>(a, x_row, tile0, tiles, wave, waves, lane, acc);
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t)
