@@ -213,9 +213,29 @@ size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 bool rows_ok(const pruner_heads* h, int32_t dtype) { return h && h->p && aligned(h->p, size_of(dtype)) && h->batch >= 0 && h->token >= 0 && h->head >= 0; }
 Rows rows_of(const pruner_heads* h) { return Rows{static_cast<char*>(h->p), h->batch, h->token, h->head}; }
 
-// Bytes of input from which on accesses go past the caches: half of the last one.  (us a call past them and not: heads of 128 in bfloat16, 168 MB, 64 and 70; 42 MB 21 and 24 where results lie in new memory
-// each time, 20 and 17 where they find the last call's; heads of 100 in binary32, 54 MB, 32 and 30; with loads alone past them 168 MB 67.)
+// Bytes of input from which on accesses go past the caches: half of the last one.  (us a call past them and not: heads of 128 in bfloat16, 42 MB 21 and 24 where results lie in new memory each time, 20 and 17
+// where they find the last call's; new memory, 63 MB 26 and 28, 105 MB 40 and 46, 127 MB 48 and 53, 168 MB 61 and 68, 246 MB 88 and 96; with loads alone past them 168 MB 67.)
 constexpr int64_t kCached = 128 << 20;
+// And only where an access leaves no parts of lines to others: past the caches those are not put together.  What is written lies in pieces: with pairs side by side and nothing copied a token's heads, else half
+// heads, or what turns of a head, and what is copied.  (168 MB, us a call past the caches and not.  Pairs half of the columns apart: bfloat16, heads of 128 61 and 68, 96 74 and 69, 80 75 and 69, 100 170 and 100;
+// binary32, heads of 96 64 and 68, 80 69 and 68, 100 122 and 77; bfloat16 in place in rows that begin 2 bytes behind a line 94 and 71.  Side by side: bfloat16, heads of 80 61 and 67, 100 104 and 79, 80 in place in
+// such rows 104 and 73, 128 of which 64 turn 64 and 74; binary32, heads of 100 60 and 67, of which 36 turn 101 and 81.)
+constexpr int64_t kLine = 64;
+bool whole(int64_t piece) { return piece % kLine == 0 && piece >= 2 * kLine; }   // bytes; (pieces of 64: 67.9 and 67.5, 67.1 and 69.0, 73.6 and 70.7)
+bool leaves_no_parts(const Call& a, bool side_by_side, bool in_place, int64_t size)
+{
+    const bool copied = a.rest > 0 && !in_place;
+    for (int w = 0; w < 2; ++w) {
+        if (a.heads[w] == 0) continue;
+        const Rows& y = a.y[w];
+        const int64_t row = (int64_t)a.heads[w] * a.head_dim;
+        const bool side_by_side_rows = side_by_side && a.rest == 0 && a.pairs * 2 * size % 16 == 0 && (a.heads[w] == 1 || y.head == a.head_dim) && (y.token == row || row * size >= 1024) && aligned(y.p, 16);
+        if (side_by_side_rows) continue;
+        if (!whole((side_by_side ? 2 : 1) * a.pairs * size) || (copied && !whole(a.rest * size))) return false;
+        if (!aligned(y.p, kLine) || y.batch * size % kLine || y.token * size % kLine || y.head * size % kLine) return false;
+    }
+    return true;
+}
 // Units of a workgroup, about.  (1024, 2048 and 4096, us a call: 168 MB in 64, 69, 75; 54 MB in heads of 100 30, 30, 32.)
 constexpr int kItems = 1024;
 
@@ -229,7 +249,7 @@ template <typename T> int launch(Call& a, bool side_by_side, bool in_place, hipS
     a.rows_each = items >= kItems ? 1 : (int)(kItems / items < 16 ? kItems / items : 16);
     const int64_t blocks = (rows + a.rows_each - 1) / a.rows_each;
     if (blocks >= (1 << 24)) return PRUNER_EINVAL;   // (a launch is below 2^24 workgroups of 256 threads)
-    const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > kCached;
+    const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > kCached && leaves_no_parts(a, side_by_side, in_place, sizeof(T));
     void (*const kernel)(Call) = side_by_side ? (once ? turn_kernel<T, true, true> : turn_kernel<T, true, false>) : once ? turn_kernel<T, false, true> : turn_kernel<T, false, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), (size_t)a.rows_each * (sizeof(RowAt) + (size_t)a.pairs * 8), st, a);
     PRUNER_LAUNCH_CHECK();
