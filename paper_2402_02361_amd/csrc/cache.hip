@@ -370,8 +370,17 @@ template <typename T, bool ONCE> __global__ void __launch_bounds__(256) restore_
     }
 }
 
-// Bytes of results from which on they go past the caches: a quarter of the last one.  (us of an append and a restore, past them and not: 50 MB of results 22 and 18, 67 MB 44 and 47.)
+// Bytes of results from which on they go past the caches: a quarter of the last one.  (us past them and not: an append and a restore of 50 MB that finds the last call's memory 22 and 18, of 67 MB 44 and 47; a restore to
+// new memory of 33 MB 13.8 and 15.5, 57 MB 23.7 and 25.7, 67 MB 25.4 and 28.4, 98 MB 37.6 and 39.6, 131 MB 49.3 and 49.4, 197 MB 67.1 and 69.5.)
 constexpr int64_t kResults = 64 << 20;
+// And only where an access leaves no parts of lines to others, which are not put together there: in 16 bits (in binary32 a thread's sixteen columns are a line, which four accesses write), of heads, or of a page's rows
+// where there is one head, that are lines.  (100 MB, us past the caches and not: bfloat16, 8 heads of 128 37 and 41, 112 63 and 50, 96 39 and 46, 80 73 and 53, 48 99 and 61, 32 28 and 56, one head of 80 35 and 40;
+// binary32, 8 heads of 128 114 and 44, of 64 98 and 43.)
+bool leaves_no_parts(const Rows& y, int64_t heads, int64_t head_dim)   // y: of 16 bits
+{
+    if (heads == 1 && y.token == head_dim) return aligned(y.p, 16);
+    return head_dim % 32 == 0 && aligned(y.p, 64) && y.batch % 32 == 0 && y.token % 32 == 0 && y.head % 32 == 0;
+}
 size_t size_of(int32_t dtype) { return dtype == PRUNER_F32 ? 4 : 2; }
 bool rows_ok(const pruner_heads* h, int32_t dtype) { return h && h->p && aligned(h->p, size_of(dtype)) && h->batch >= 0 && h->token >= 0 && h->head >= 0; }
 Rows rows_of(const pruner_heads* h) { return Rows{static_cast<char*>(h->p), h->batch, h->token, h->head}; }
@@ -443,10 +452,11 @@ extern "C" int pruner_cache_restore(const pruner_cache* c, int32_t dtype, int32_
     const dim3 grid((unsigned)(slots * batch * c->kv_heads));
     const size_t lds = (size_t)c->page_tokens * (c->head_dim + cache::kPad);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool once = 2 * (int64_t)batch * tokens * c->kv_heads * c->head_dim * (int64_t)cache::size_of(dtype) > cache::kResults;
+    const bool once = dtype != PRUNER_F32 && 2 * (int64_t)batch * tokens * c->kv_heads * c->head_dim * 2 > cache::kResults && cache::leaves_no_parts(call.k, c->kv_heads, c->head_dim) &&
+                      cache::leaves_no_parts(call.v, c->kv_heads, c->head_dim);
     void (*const kernel)(cache::Call) = dtype == PRUNER_BF16  ? (once ? cache::restore_kernel<__bf16, true> : cache::restore_kernel<__bf16, false>)
                                         : dtype == PRUNER_F16 ? (once ? cache::restore_kernel<_Float16, true> : cache::restore_kernel<_Float16, false>)
-                                                              : (once ? cache::restore_kernel<float, true> : cache::restore_kernel<float, false>);
+                                                              : cache::restore_kernel<float, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, call);
     PRUNER_LAUNCH_CHECK();
     return PRUNER_OK;

@@ -1,4 +1,4 @@
-"""cache_restore: without lengths, and of more than the caches are good for in the 16-bit types (in binary32: see the tests of a token step)."""
+"""cache_restore: without lengths, and of so many results in the 16-bit types that they go past the caches."""
 import numpy as np
 import pytest
 import torch
