@@ -28,6 +28,7 @@ struct Call {
     int32_t batch, tokens, head_dim, pairs, rest;   // rest: columns behind the pairs that are copied
     int32_t units, all_units;   // of a head: those that turn, and with those that are copied
     int32_t rows_each;          // tokens of a workgroup
+    int32_t first;              // workgroup, of those of a call, that a launch begins with
     float amplitude;
     int32_t back;
     uint64_t turn[PRUNER_MAX_ROTARY_DIM / 2];       // 2^-64 turns per position
@@ -95,7 +96,7 @@ template <typename T, bool SIDE_BY_SIDE, bool ONCE> __global__ void __launch_bou
     extern __shared__ __attribute__((aligned(16))) char lds[];
     RowAt* const rows_at = reinterpret_cast<RowAt*>(lds);
     f32x2* const angles = reinterpret_cast<f32x2*>(lds + a.rows_each * sizeof(RowAt));   // [token][pair] sine and cosine
-    const int64_t all_rows = (int64_t)a.batch * a.tokens, row0 = (int64_t)blockIdx.x * a.rows_each;
+    const int64_t all_rows = (int64_t)a.batch * a.tokens, row0 = ((int64_t)a.first + blockIdx.x) * a.rows_each;
     const int rows = all_rows - row0 < a.rows_each ? (int)(all_rows - row0) : a.rows_each;
     for (int i = threadIdx.x; i < rows * a.pairs; i += 256) {
         const int row = i / a.pairs, pair = i - row * a.pairs, b = (int)((row0 + row) / a.tokens), t = (int)((row0 + row) - (int64_t)b * a.tokens);
@@ -248,11 +249,14 @@ template <typename T> int launch(Call& a, bool side_by_side, bool in_place, hipS
     const int64_t rows = (int64_t)a.batch * a.tokens, items = (int64_t)a.all_units * heads;
     a.rows_each = items >= kItems ? 1 : (int)(kItems / items < 16 ? kItems / items : 16);
     const int64_t blocks = (rows + a.rows_each - 1) / a.rows_each;
-    if (blocks >= (1 << 24)) return PRUNER_EINVAL;   // (a launch is below 2^24 workgroups of 256 threads)
     const bool once = rows * heads * a.head_dim * (int64_t)sizeof(T) > kCached && leaves_no_parts(a, side_by_side, in_place, sizeof(T));
     void (*const kernel)(Call) = side_by_side ? (once ? turn_kernel<T, true, true> : turn_kernel<T, true, false>) : once ? turn_kernel<T, false, true> : turn_kernel<T, false, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), (size_t)a.rows_each * (sizeof(RowAt) + (size_t)a.pairs * 8), st, a);
-    PRUNER_LAUNCH_CHECK();
+    constexpr int64_t kLaunch = 1 << 23;   // (a launch is below 2^24 workgroups of 256 threads)
+    for (int64_t first = 0; first < blocks; first += kLaunch) {
+        a.first = (int32_t)first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks - first < kLaunch ? blocks - first : kLaunch)), dim3(256), (size_t)a.rows_each * (sizeof(RowAt) + (size_t)a.pairs * 8), st, a);
+        PRUNER_LAUNCH_CHECK();
+    }
     return PRUNER_OK;
 }
 
