@@ -4,8 +4,8 @@
 // older tokens have.  Codes of four significant bits only lose what falls below e4m3's smallest steps when they are divided by a power of two, so a page whose
 // exponent grows is rounded again without hurting what it can still hold.
 // A workgroup takes one page of one head, its keys and its values: nothing is shared with another, and one launch does a whole call.  Values lie with 16 tokens side by side and arrive
-// row by row, so they are turned over in LDS, four columns of four tokens at a time.  Bound: memory; 2 x 8191 tokens in bfloat16, 8 heads of 128, stored and read back 44 us a pair of calls, kernels of 19 and 23 us (5.3 and 4.4 TB/s); one token of each of 64
-// sequences stored and up to 190 read back 17.6 us, kernels of 5 and 13.
+// row by row, so they are turned over in LDS, four columns of four tokens at a time.  Bound: memory; 2 x 8191 tokens in binary16, 8 heads of 128, stored and read back 44 us a pair of calls, kernels of 19 and 23 us (5.2 and 4.4 TB/s), stored alone 24; one token of each
+// of 64 sequences stored and up to 190 read back 17.8 us, kernels of 5 and 14, stored alone 9.
 #include "cache.h"
 
 namespace pruner {

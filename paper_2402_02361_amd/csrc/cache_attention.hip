@@ -4,19 +4,23 @@
 // with a maximum and a sum, and the weights are the next product's operand as they stand (O^T += V^T P^T).  Which key a row of the first product's operand is, is ours to choose: a lane's sixteen
 // scores are made to be of sixteen neighbouring keys, the depth that sixteen bytes of values have.  A page's powers of two go in with the conversion, which is exact (binary16: within its range).  The
 // second product is of 16-bit operands, the rate of the matrix cores; the weights' sum is of the unrounded ones.  Few columns have weights in two terms (bfloat16, off by 2^-16), for which there is room beside the
-// reading.  Of many columns they are rounded to the operands' type: two terms take 685 us where one takes 515 (2048 tokens against 16384, 32 heads of 128 sharing 8, one card).
+// reading.  Of many columns they are rounded to the operands' type: two terms take 685 us where one takes 515 to 520, a second term in 8 bits, by products of 64 keys that take the codes as they are, 637 (2048 tokens
+// against 16384, 32 heads of 128 sharing 8, one card; the result is off by 2.4e-3 of itself, of which its own rounding makes 1.65e-3, in binary16 2.9e-4 and 2.1e-4; with either second term by its rounding alone).
 //
 //   tokens_kernel       at most 32 columns, on v_mfma_f32_16x16x32: the four wavefronts of a workgroup take 64 keys each in turn and meet in LDS at the end.  Codes go from memory straight to the lanes whose
 //                       operands they become, 64 bytes a lane ahead of the products for keys and values each.  Products of 32 x 32 x 16 held half as many wavefronts and took 315 us where this takes 200.
 //                       Bound by memory: one token against 32 caches of up to 32768, 32 heads of 128 sharing 8, 195 to 200 us, 5.3 to 5.5 TB/s (a large copy: 5.2 read and written together);
-//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of 300, 8 heads of 64, 11.6 us a call, with 5 queries each of 16 sequences of up to 5003 21.4.
+//                       short ones by a workgroup's chain of lengths, pages, codes: one token against a cache of 300, 8 heads of 64, 11.6 us a call, with 5 queries each of 16 sequences of up to 5003
+//                       in pages of 16, 16 heads of 80 sharing 4, 21.5 (heads of 64 20.6, of 128 26.4).
 //   codes_kernel        more columns, 32 to a wavefront, on v_mfma_f32_32x32x16, over pages of 64 tokens and more.  The four wavefronts share tiles of 64 keys and values in LDS, which are requested straight
 //                       to it as codes and converted by who reads them.  Bound by the matrix cores, the exponentials and conversions beside their products, and the clock under both: 2048 tokens against
-//                       16384, 32 heads of 128 sharing 8, 505 to 520 us, 990 to 1020 TFLOP/s; 2000 against 8000, 16 heads of 64 sharing 4, 127 us; 64 against 30000 58.
+//                       16384, 32 heads of 128 sharing 8, in hundreds of calls in a row 505 to 530 us, 970 to 1020 TFLOP/s (the first dozen after a pause 535 to 600); heads of 112, 96 and 80 511, 498 and 492, since the products
+//                       are those of 128 columns; 2000 against 8000, 16 heads of 64 sharing 4, 127 us; 64 against 30000 58.
 //                       Converted tiles in LDS as below: 543, 138 and 61.  Codes in LDS without the next tile's scores among this one's weights 542 (three wavefronts to a SIMD, by scores of 32 keys, 557);
 //                       with them, but a memory access for each tile's page, its requests all between the steps, and scores copied there from register to register, 545.
 //   chunk_kernel        the same over smaller pages: tiles in LDS hold operands, so that a code is converted once for 128 columns, and the next tile's are parked among this one's scores and softmax.
-//                       8 sequences of 100 tokens against up to 800 in pages of 16, 16 heads of 64 sharing 4, 27 us, by a workgroup's start and chain of tiles.
+//                       8 sequences of 100 tokens against up to 800 in pages of 16, 16 heads of 64 sharing 4, 27 us, by a workgroup's start and chain of tiles; 2048 tokens against 16384 in pages of 16 or 32, 32 heads of 128
+//                       sharing 8, 610 (516 over pages of 128), by LDS and the threads that convert and park.
 //                       (Wavefronts' priorities raised for products or for the softmax: 1 to 4 % longer; eight wavefronts that share a tile 4 % longer; 64 columns to a wavefront a quarter longer.)
 //   join_groups_kernel  the parts of a key axis that was split over workgroups.
 #include "attention_softmax.h"
@@ -170,7 +174,8 @@ template <typename T, int DP, bool WHOLE, bool ONCE> struct Few {
 };
 
 // ONCE: the caches hold more than stays cached from one call to the next, and are read past it (us a call with and without: 32 caches of 32768, 8 heads of 128, 348 and 379, of up to 32768 201 and 208;
-// 8 of up to 20000 51 and 52; 16 of up to 5003, 4 heads of 80, 26 and 24).
+// 8 of up to 20000 51 and 52; 16 of up to 5003, 4 heads of 80, 26 and 24; with other caches in each call 4 of 8000 20.2 and 21.3, 8 of 8000 31 and 34, of 12000 42 and 46, of 16000 52 and 58, of 20000 63 and 71;
+// heads of 32 to 112 as those of 128).
 template <typename T, int DP, int CT, bool WHOLE, bool ONCE>
 __global__ void __launch_bounds__(256, (CT == 1 && (WHOLE || DP < 128) ? 3 : 2)) tokens_kernel(Args a, cache::Cache c, Heads out, float* __restrict__ lse, Parts parts)
 {

@@ -5,8 +5,10 @@
 // bytes its eight depths of four products.  A group's depths are those of whole products, so a group's sum is a result of its own and is scaled in binary32 when it is added.
 // Codes become operands without a conversion: a code under the bits of 128 is the bfloat16 128 + code, and the products start from -136 times the sum of x (one more product,
 // shared by all outputs); in binary16 1024 + code, less 1032, which is exact.
+// (bfloat16 by conversions to code - 8, which costs no digits of binary32: 32768 x 8192 for one row 39.5 us where this takes 30.3; as 16 + code, from -24 times the sum, 30.9.)
 // The wavefronts of a workgroup take every so many blocks of 128 inputs and meet in LDS.  Bound: reading the weights, 32768 x 8192 for one row 29 us, 4.75 TB/s with the launch; where they are few, start and end, 1603 x 1100 8.4 us, 16384 x 4096 for 12 rows 11.6;
-// from 17 rows on x, which every 32 or 64 outputs read again: 32 rows over 8192 x 8192 20 us.
+// from 17 rows on x, which every 32 or 64 outputs read again: 32 rows over 8192 x 8192 21 us.  One row over 34 MB of codes takes 11 to 13 us (8192 x 8192, 4096 x 16384, 16384 x 4096; the bytes ask for 6.7): a workgroup's start
+// and end, 5 us, are not covered by the two blocks that a wavefront has on the way.
 #include "common.h"
 
 namespace pruner {
@@ -25,7 +27,7 @@ typedef u32x4 Loose __attribute__((aligned(2)));
 
 constexpr int kOutputs = 16, kBlock = 128, kBlockWords = kOutputs * kBlock / 8;
 constexpr int kZero = 8;   // the code of 0
-constexpr int64_t kCached = 96 << 20;   // bytes of codes (us a call read past the caches and not: 32768 x 8192 30.1 and 31.8, 16384 x 4096 13.2 and 12.7, 8192 x 8192 11.5 and 10.7)
+constexpr int64_t kCached = 96 << 20;   // bytes of codes (us a call read past the caches and not: 32768 x 8192 30.1 and 31.8, 16384 x 4096 13.2 and 12.7, 8192 x 8192 11.5 and 10.7; with other weights in each call 67 MB 17.3 and 18.1, 98 MB 23.6 and 24.6, 115 MB 29.4 and 30.7)
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, __bf16)
 {
@@ -268,6 +270,7 @@ template <typename T, int GROUP, int RT, int CT, bool ONCE> __global__ void __la
 }
 
 // ---- there and back: a thread takes 32 neighbouring inputs of an output; neighbouring threads those of the same block
+// (Once per set of weights, so written for clearness: 32768 x 8192 in bfloat16 packed in 630 us and restored in 2.1 ms, where the bytes ask for 134; single values, 32 apart between lanes, are the cause.)
 
 template <typename T> __device__ __forceinline__ float value_of(const T* p) { return (float)*p; }
 
