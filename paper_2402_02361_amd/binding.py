@@ -919,19 +919,20 @@ def cache_restore(cache, tokens, k_len, dtype, stream=None):
     all sequences have `tokens`; there are as many as the table has rows, or, where it is a number, as the pool has room for."""
     import torch
     lib = load_library()
+    codes, table = cache[0], cache[4]
     if k_len is not None:
         batch = k_len.numel()
-    elif isinstance(cache.table, int):
-        batch = cache.k_codes.shape[0] // cache.table if cache.table else 0
+    elif isinstance(table, int):
+        batch = codes.shape[0] // table if table else 0
     else:
-        batch = cache.table.shape[0]
+        batch = table.shape[0]
     c, kv_heads, head_dim, _ = _c_cache(cache, batch)
     with _made_on(stream):
-        k = torch.empty((batch, tokens, kv_heads, head_dim), dtype=dtype, device=cache.k_codes.device)
+        k = torch.empty((batch, tokens, kv_heads, head_dim), dtype=dtype, device=codes.device)
         v = torch.empty_like(k)
     _returned(stream, k, v)
     rc = lib.pruner_cache_restore(c, _dtype(dtype), batch, tokens, _lengths(k_len, batch, "k_len"), _dense_heads(k, tokens, kv_heads, head_dim), _dense_heads(v, tokens, kv_heads, head_dim),
-                                  _stream_on(stream, cache.k_codes))
+                                  _stream_on(stream, codes))
     if rc:
         raise PrunerError(rc, "pruner_cache_restore")
     return k, v

@@ -85,7 +85,7 @@ template <int DP> struct Meeting {
     {
         for (int item = threadIdx.x; item < columns * (DP / 4); item += 256) {
             const int c = item / (DP / 4), d = 4 * (item % (DP / 4));
-            if (d >= a.head_dim) continue;   // (who joins parts leaves these columns out)
+            if (d >= a.head_dim) continue;   // (whoever joins parts does not store these columns)
             float m = -ATT_INF;
 #pragma unroll
             for (int w = 0; w < 4; ++w) m = __builtin_fmaxf(m, stats[w * 32 + c].y != 0.f ? stats[w * 32 + c].x : -ATT_INF);

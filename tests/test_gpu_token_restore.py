@@ -48,3 +48,15 @@ def test_more_than_the_caches_are_good_for(dtype, page_tokens):
             for x, y in zip(part, whole):
                 assert torch.equal(x[0], y[b, first:first + tokens])
     assert not whole[0][1, 9001:].any() and whole[0][1, 9000].any() and not whole[1][1, 9001:].any() and whole[1][0, 16999].any()
+
+
+def test_a_cache_is_any_five():
+    """A plain tuple of the same."""
+    cache = P.new_cache(4, 2, 32, 2, 16)
+    k = torch.randn(2, 20, 2, 32, device="cuda", dtype=BF)
+    P.cache_append(tuple(cache), k, k)
+    n = caches._ints([20, 7])
+    for lengths in (n, None):
+        for a, b in zip(P.cache_restore(tuple(cache), 20, lengths, BF), P.cache_restore(cache, 20, lengths, BF)):
+            assert torch.equal(a, b)
+    assert torch.equal(P.cache_attention(k, tuple(cache), k_len=n), P.cache_attention(k, cache, k_len=n))
